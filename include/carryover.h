@@ -78,8 +78,10 @@ enum {
                                carry_len outside [0, 16 * ceil(block / 16)]        */
   CO_ERR_GROUP = 8,         /* device: a sequence's committed page ids differ from its
                                group's first sequence (attention backward)          */
-  CO_ERR_TOKEN = 9          /* device: a proposed token outside [0, vocab)
+  CO_ERR_TOKEN = 9,         /* device: a proposed token outside [0, vocab)
                                (carryover_verify_sample)                            */
+  CO_ERR_POOL = 10          /* device: the page pool has too few free pages, or a free
+                               count that it cannot have (carryover_assign_pages)   */
 };
 
 enum { CO_DTYPE_F32 = 0, CO_DTYPE_BF16 = 1 };
@@ -162,6 +164,29 @@ typedef struct co_route {
   int32_t* row_dst;           /* [num_seqs][block] >= 0: global committed slot page*16+t%16;
                                  -1-r: carry row r; INT32_MIN: not stored                   */
 } co_route;
+
+/*
+ * The committed cache in 8 bits (serving; next to the paper, whose caches hold
+ * the drafter's own type).  A page holds its 16 tokens of one layer and KV head
+ * as e4m3 codes (OCP 8-bit floating point, largest value 448), laid out as in
+ * k_cache and v_cache, with one scale byte b for its keys and one for its
+ * values: an entry is code * 2^(b - 127).  Only bytes that carryover_store_kv8
+ * writes are defined; the cache needs no initial contents.
+ */
+typedef struct co_kv8 {
+  void* k_pages;              /* [num_layers][num_pages][num_kv_heads][P][head_dim], 16-byte aligned */
+  void* v_pages;              /* [num_layers][num_pages][num_kv_heads][head_dim][P], 16-byte aligned */
+  uint8_t* k_scale;           /* [num_layers][num_pages][num_kv_heads]                              */
+  uint8_t* v_scale;
+} co_kv8;
+
+/* Who holds which page of the pool (carryover_assign_pages). */
+typedef struct co_page_pool {
+  int32_t* page_table;        /* [num_seqs][max_pages_per_seq]: a state's, written          */
+  int32_t* held;              /* [num_seqs] pages that each sequence holds                  */
+  int32_t* free_pages;        /* [num_pages] the free pages' ids, in entries 0 .. *free_count - 1 */
+  int32_t* free_count;        /* one int32                                                  */
+} co_page_pool;
 
 /*
  * Route (Algorithm 1 "Given"; greedy verification, Section 2
@@ -440,8 +465,126 @@ co_status carryover_import_kv(const co_dims* dims, int32_t seq, int32_t pos0, in
                               const void* k_rows, const void* v_rows, const co_state* state,
                               hipStream_t stream);
 
+/*
+ * Page tables from request lengths, on the device (the serving stack's part;
+ * the paper leaves paging to it).  Afterwards every sequence s holds exactly the
+ * pages of the positions it wants: need_s = ceil((want_len[s] + reserve) / 16)
+ * pages, or none where want_len[s] is 0 (a slot that no request uses, or whose
+ * request has ended).  Entries held[s] .. need_s - 1 of its table row are filled
+ * from the free list, or entries need_s .. held[s] - 1 go back to it and become
+ * -1; entries past both are left as they are.  With the released pages
+ * numbered 0 .. R - 1 and the entries to fill 0 .. T - 1, both in (sequence,
+ * logical page) order, entry k takes released page k, or where k >= R free page
+ * n = *free_count + R - 1 - k, and released page k >= T becomes free page n: a
+ * call that goes back to the lengths before undoes this one exactly.  Free
+ * entries from the new *free_count on keep what they held, unspecified.
+ * want_len int32 [num_seqs] (ctx_len of a state, with reserve = block, makes
+ * room for a round); reserve >= 0.  Only num_seqs, max_pages_per_seq and
+ * num_pages of dims are used (the rest must still be valid).  `ws`:
+ * carryover_workspace_bytes(dims, CO_WS_ASSIGN_PAGES) bytes, 256-byte aligned.
+ * Device errors, written to *status (first one wins): CO_ERR_LENGTH (a negative
+ * want_len, or held outside [0, max_pages_per_seq]), CO_ERR_CAPACITY (need_s >
+ * max_pages_per_seq); that sequence stays as it is.  CO_ERR_POOL: sequences are
+ * served in order, and from the first whose pages do not fit on, none gets any
+ * (sequences that release or keep pages still do); with *free_count outside
+ * [0, num_pages] nothing changes.  Calls on one pool must not overlap.
+ * Host: num_seqs * max_pages_per_seq and num_pages * 16 below 2^31
+ * (CO_ERR_UNSUPPORTED).
+ */
+co_status carryover_assign_pages(const co_dims* dims, const int32_t* want_len, int32_t reserve,
+                                 const co_page_pool* pool, int32_t* status, void* ws,
+                                 size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Positions and committed slots of rows packed behind each other (prompts of
+ * any lengths, or one row per sequence): row r belongs to the sequence s with
+ * row_start[s] <= r < row_start[s + 1]; row_pos[r] = pos0[s] + r - row_start[s]
+ * and row_dst[r] is that position's slot, as in co_route, for
+ * carryover_store_kv8, or for carryover_project_kv of one sequence with block =
+ * num_rows.  Rows before row_start[0] and from row_start[num_seqs] on (padding)
+ * get row_dst INT32_MIN and row_pos 0.  row_start int32 [num_seqs + 1], not
+ * decreasing; pos0 int32 [num_seqs] (a state's ctx_len; lengths are not
+ * changed); row_pos, row_dst int32 [num_rows].  Only num_seqs,
+ * max_pages_per_seq and num_pages of dims are used (the rest must still be
+ * valid).  Device errors, written to *status; the row then gets INT32_MIN and 0:
+ * CO_ERR_LENGTH (pos0 < 0, or a start that decreases), CO_ERR_CAPACITY (a
+ * position >= max_pages_per_seq * 16), CO_ERR_PAGE_RANGE (a page id outside
+ * [0, num_pages)).  Host: num_pages * 16 below 2^31 (CO_ERR_UNSUPPORTED).
+ */
+co_status carryover_slot_map(const co_dims* dims, int32_t num_rows, const int32_t* row_start,
+                             const int32_t* pos0, const int32_t* page_table, int32_t* row_pos,
+                             int32_t* row_dst, int32_t* status, hipStream_t stream);
+
+/*
+ * Rows of projected keys (rotated) and values into the 8-bit cache: row r of
+ * k_rows, v_rows [num_layers][num_rows][num_kv_heads][head_dim] (bf16, 16-byte
+ * aligned) goes to slot row_dst[r] % 16 of page row_dst[r] / 16, in every layer
+ * and head; rows with a negative row_dst (carry rows, INT32_MIN) are skipped.  The
+ * rows of one page must be next to each other, in consecutive slots (as
+ * carryover_route and carryover_slot_map give them), and no page may be named
+ * twice; otherwise the contents of that page are unspecified.  For the keys, and
+ * likewise for the values, of a page: let 2^e be the smallest power of two, at
+ * least 2^-126, with |x| <= 448 * 2^e for every finite entry x of its new rows.
+ *   slot 0 among the rows: the page starts afresh, its scale is 2^e and the
+ *     slots without a row become 0;
+ *   otherwise its scale becomes the larger of the old one and 2^e, and the other
+ *     slots keep their values, rounded again where the scale grew.
+ * Entries are rounded to the nearest code, ties to even; infinities and NaNs
+ * become NaN.  Supported: bf16.  Device errors, written to *status:
+ * CO_ERR_PAGE_RANGE (row_dst / 16 >= num_pages; the row is skipped).
+ * num_layers * num_kv_heads <= 65535 (CO_ERR_UNSUPPORTED otherwise).
+ */
+co_status carryover_store_kv8(const co_dims* dims, int32_t num_rows, const void* k_rows,
+                              const void* v_rows, const int32_t* row_dst, const co_kv8* cache,
+                              int32_t* status, hipStream_t stream);
+
+/*
+ * carryover_project_kv with the committed segment in the 8-bit cache: committed
+ * rows are projected to bf16 rows in the workspace and stored as
+ * carryover_store_kv8 stores them, carry rows replace the carry segment in bf16
+ * as ever.  state->k_cache and v_cache are not used and may be NULL.  Supported:
+ * bf16.  `ws`: carryover_workspace_bytes(dims, CO_WS_PROJECT_KV8) bytes, 256-byte
+ * aligned.  Other arguments and errors: those of the two calls.
+ */
+co_status carryover_project_kv8(const co_dims* dims, const co_weights* w, const void* hidden,
+                                const co_route* route, const co_state* state, const co_kv8* cache,
+                                void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * drafter_block_attention_ext with the committed segment in the 8-bit cache: the
+ * attention over [C;U], or [C;U;S] where k_self and v_self are given, with C's
+ * keys and values read as code * 2^(b - 127) (exact in the bf16 products) and U
+ * and S in bf16; block 1 is a single token's.  k_self, v_self, lse and
+ * carry_mass are optional (NULL).  state->k_cache and v_cache are not used and
+ * may be NULL.  Supported: bf16; the shapes of drafter_block_attention.
+ * `ws`: carryover_workspace_bytes(dims, CO_WS_ATTENTION_KV8) bytes, 256-byte
+ * aligned.  Arguments, flags (CO_ATTN_SHARED_PREFIX is ignored), results for
+ * empty key sets and errors as there.  drafter_carry_mass and
+ * drafter_self_merge serve its results too.
+ */
+co_status drafter_block_attention_kv8(const co_dims* dims, int32_t layer_begin,
+                                      int32_t layer_count, const void* q, const void* k_self,
+                                      const void* v_self, const co_state* state,
+                                      const co_kv8* cache, void* out, float* lse,
+                                      float* carry_mass, uint32_t flags, void* ws,
+                                      size_t ws_bytes, hipStream_t stream);
+
+/*
+ * carryover_round with the committed segment in the 8-bit cache: carryover_route,
+ * carryover_project_kv8, then drafter_block_attention_kv8 over [C;U] with every
+ * layer's queries.  Every host check of the three steps is made before the first
+ * launch.  `ws`: carryover_workspace_bytes(dims, CO_WS_ROUND_KV8) bytes,
+ * 256-byte aligned.  Other arguments and errors: those of the steps.
+ */
+co_status carryover_round_kv8(const co_dims* dims, const co_weights* w, const void* hidden,
+                              const int32_t* draft_tok, const int32_t* target_tok, const void* q,
+                              co_state* state, const co_kv8* cache, const co_route* scratch,
+                              void* out, float* lse, uint32_t flags, void* ws, size_t ws_bytes,
+                              hipStream_t stream);
+
 enum { CO_WS_PROJECT = 0, CO_WS_ATTENTION = 1, CO_WS_ROUND = 2, CO_WS_ATTENTION_BACKWARD = 3,
-       CO_WS_PROJECT_BACKWARD = 4 };
+       CO_WS_PROJECT_BACKWARD = 4, CO_WS_PROJECT_KV8 = 5, CO_WS_ATTENTION_KV8 = 6,
+       CO_WS_ROUND_KV8 = 7, CO_WS_ASSIGN_PAGES = 8 };
 
 /* Workspace bytes a call needs for these dims (0 on unsupported dims). */
 size_t carryover_workspace_bytes(const co_dims* dims, int32_t which);

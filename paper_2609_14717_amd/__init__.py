@@ -17,13 +17,14 @@ LIB_PATH = os.path.join(HERE, "libcarryover.so")
 
 CO_OK, CO_ERR_INVALID_ARG, CO_ERR_UNSUPPORTED, CO_ERR_WORKSPACE = 0, 1, 2, 3
 CO_ERR_CAPACITY, CO_ERR_PAGE_RANGE, CO_ERR_HIP, CO_ERR_LENGTH, CO_ERR_GROUP = 4, 5, 6, 7, 8
-CO_ERR_TOKEN = 9
+CO_ERR_TOKEN, CO_ERR_POOL = 9, 10
 CO_DTYPE_F32, CO_DTYPE_BF16 = 0, 1
 CO_BASELINE_MODE, CO_ROUTE_ACCEPT_ALL, CO_ROUTE_CARRY_ONLY, CO_Q_PREROTATED = 1, 2, 4, 8
 CO_ATTN_SHARED_PREFIX = 16
 CO_ROUTE_ACCEPT_BITS = 32
 CO_WS_PROJECT, CO_WS_ATTENTION, CO_WS_ROUND, CO_WS_ATTENTION_BACKWARD = 0, 1, 2, 3
 CO_WS_PROJECT_BACKWARD = 4
+CO_WS_PROJECT_KV8, CO_WS_ATTENTION_KV8, CO_WS_ROUND_KV8, CO_WS_ASSIGN_PAGES = 5, 6, 7, 8
 # launch-shape overrides (carryover_set_tuning)
 TUNING = {"gemm_wide_variant": 0, "gemm_no_wide": 1, "project_fused_min_rows": 2, "attn_wave": 3,
           "attn_workgroups": 4, "attn_round_tiles": 5, "attn_group_split_tiles": 6}
@@ -64,6 +65,16 @@ class co_state(ctypes.Structure):
 class co_route(ctypes.Structure):
     _fields_ = [("accept_len", ctypes.c_void_p), ("row_pos", ctypes.c_void_p),
                 ("row_dst", ctypes.c_void_p)]
+
+
+class co_kv8(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class co_page_pool(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("held", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p)]
 
 
 _lib = None
@@ -107,6 +118,18 @@ def lib():
                                     _v, _P(co_state), _v],
             "carryover_verify_sample": [_P(co_dims), ctypes.c_int32, _v, _v, _v, _v, _v, _v, _v,
                                         _v, _v],
+            "carryover_assign_pages": [_P(co_dims), _v, ctypes.c_int32, _P(co_page_pool), _v, _v,
+                                       ctypes.c_size_t, _v],
+            "carryover_slot_map": [_P(co_dims), ctypes.c_int32, _v, _v, _v, _v, _v, _v, _v],
+            "carryover_store_kv8": [_P(co_dims), ctypes.c_int32, _v, _v, _v, _P(co_kv8), _v, _v],
+            "carryover_project_kv8": [_P(co_dims), _P(co_weights), _v, _P(co_route), _P(co_state),
+                                      _P(co_kv8), _v, ctypes.c_size_t, _v],
+            "drafter_block_attention_kv8": [_P(co_dims), ctypes.c_int32, ctypes.c_int32, _v, _v,
+                                            _v, _P(co_state), _P(co_kv8), _v, _v, _v,
+                                            ctypes.c_uint32, _v, ctypes.c_size_t, _v],
+            "carryover_round_kv8": [_P(co_dims), _P(co_weights), _v, _v, _v, _v, _P(co_state),
+                                    _P(co_kv8), _P(co_route), _v, _v, ctypes.c_uint32, _v,
+                                    ctypes.c_size_t, _v],
             "carryover_set_tuning": [ctypes.c_int32, ctypes.c_int64],
             "carryover_round_noalloc": [_P(co_dims), _P(co_weights), _v, _v, _v, _v,
                                         _P(co_state), _P(co_route), _v, _v, ctypes.c_uint32, _v],
@@ -129,6 +152,8 @@ EXPORTED = ("carryover_route", "carryover_project_kv", "drafter_block_attention"
             "carryover_round", "carryover_fold_e", "drafter_carry_mass", "drafter_self_merge",
             "drafter_block_attention_backward", "carryover_project_kv_backward",
             "carryover_import_kv", "carryover_verify_sample", "carryover_set_tuning",
+            "carryover_assign_pages", "carryover_slot_map", "carryover_store_kv8",
+            "carryover_project_kv8", "drafter_block_attention_kv8", "carryover_round_kv8",
             "carryover_round_noalloc",
             "carryover_workspace_bytes", "carryover_read_status", "carryover_status_string")
 
@@ -185,24 +210,40 @@ def route(t):
     return co_route(_ptr(t["accept_len"]), _ptr(t["row_pos"]), _ptr(t["row_dst"]))
 
 
+def kv8(t):
+    """co_kv8 over a dict of tensors (see ``alloc_kv8``)."""
+    return co_kv8(_ptr(t["k_pages"]), _ptr(t["v_pages"]), _ptr(t["k_scale"]), _ptr(t["v_scale"]))
+
+
+def page_pool(t):
+    """co_page_pool over a dict of tensors (see ``alloc_page_pool``)."""
+    return co_page_pool(_ptr(t["page_table"]), _ptr(t["held"]), _ptr(t["free_pages"]),
+                        _ptr(t["free_count"]))
+
+
 def workspace_bytes(dims, which=CO_WS_ROUND) -> int:
     return lib().carryover_workspace_bytes(ctypes.byref(dims), which)
 
 
-def alloc_state(dims, page_table, device="cuda"):
-    """Zero-initialised device buffers for one drafter state (layouts of carryover.h)."""
+def alloc_state(dims, page_table, device="cuda", committed=True):
+    """Zero-initialised device buffers for one drafter state (layouts of carryover.h).
+    ``committed=False`` leaves k_cache and v_cache None, for a committed segment in an
+    8-bit cache (``alloc_kv8``)."""
     import torch
     dt = torch.bfloat16 if dims.dtype == CO_DTYPE_BF16 else torch.float32
     L, Hkv, hd, S = dims.num_layers, dims.num_kv_heads, dims.head_dim, dims.num_seqs
     CP = -(-dims.block // PAGE)
     pt = torch.as_tensor(page_table, dtype=torch.int32).to(device).contiguous()
     assert tuple(pt.shape) == (S, dims.max_pages_per_seq)
+    pages = dims.num_pages if committed else 0
+    cache = [torch.zeros((L, pages, Hkv) + at, dtype=dt, device=device) if committed else None
+             for at in ((PAGE, hd), (hd, PAGE))]
     return dict(
         ctx_len=torch.zeros(S, dtype=torch.int32, device=device),
         carry_len=torch.zeros(S, dtype=torch.int32, device=device),
         page_table=pt,
-        k_cache=torch.zeros((L, dims.num_pages, Hkv, PAGE, hd), dtype=dt, device=device),
-        v_cache=torch.zeros((L, dims.num_pages, Hkv, hd, PAGE), dtype=dt, device=device),
+        k_cache=cache[0],
+        v_cache=cache[1],
         k_carry=torch.zeros((L, S, CP, Hkv, PAGE, hd), dtype=dt, device=device),
         v_carry=torch.zeros((L, S, CP, Hkv, hd, PAGE), dtype=dt, device=device),
         status=torch.zeros(1, dtype=torch.int32, device=device),
@@ -214,6 +255,27 @@ def alloc_route(S, B, device="cuda"):
     return dict(accept_len=torch.zeros(S, dtype=torch.int32, device=device),
                 row_pos=torch.zeros((S, B), dtype=torch.int32, device=device),
                 row_dst=torch.zeros((S, B), dtype=torch.int32, device=device))
+
+
+def alloc_kv8(dims, device="cuda"):
+    """The committed cache in 8 bits: e4m3 codes and scale bytes, as uint8 (an entry is
+    ``code.view(torch.float8_e4m3fn) * 2 ** (scale - 127)``)."""
+    import torch
+    L, P, Hkv, hd = dims.num_layers, dims.num_pages, dims.num_kv_heads, dims.head_dim
+    new = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)  # noqa: E731
+    return dict(k_pages=new(L, P, Hkv, PAGE, hd), v_pages=new(L, P, Hkv, hd, PAGE),
+                k_scale=new(L, P, Hkv), v_scale=new(L, P, Hkv))
+
+
+def alloc_page_pool(dims, device="cuda"):
+    """A pool whose pages are all free, and a page table that holds none (-1)."""
+    import torch
+    S, P = dims.num_seqs, dims.num_pages
+    return dict(page_table=torch.full((S, dims.max_pages_per_seq), -1, dtype=torch.int32,
+                                      device=device),
+                held=torch.zeros(S, dtype=torch.int32, device=device),
+                free_pages=torch.arange(P, dtype=torch.int32, device=device),
+                free_count=torch.full((1,), P, dtype=torch.int32, device=device))
 
 
 # ---------------------------------------------------------------- entry points
@@ -298,6 +360,65 @@ def carryover_round(dims, w, hidden, draft_tok, target_tok, q, st, rt, out, lse,
                                  _ptr(draft_tok), _ptr(target_tok), _ptr(q), ctypes.byref(s),
                                  ctypes.byref(r), _ptr(out), _ptr(lse), flags, _ptr(ws), nb,
                                  _stream(stream)), "carryover_round")
+
+
+def carryover_assign_pages(dims, want_len, reserve, pool, status, ws, stream=None, ws_bytes=None):
+    """Pages of every sequence for want_len (+ reserve) positions: taken from the
+    pool's free list or given back to it, on the device."""
+    p = page_pool(pool)
+    nb = ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    _check(lib().carryover_assign_pages(ctypes.byref(dims), _ptr(want_len), reserve,
+                                        ctypes.byref(p), _ptr(status), _ptr(ws), nb,
+                                        _stream(stream)), "carryover_assign_pages")
+
+
+def carryover_slot_map(dims, num_rows, row_start, pos0, page_table, row_pos, row_dst, status,
+                       stream=None):
+    """Positions and committed slots of rows packed sequence behind sequence."""
+    _check(lib().carryover_slot_map(ctypes.byref(dims), num_rows, _ptr(row_start), _ptr(pos0),
+                                    _ptr(page_table), _ptr(row_pos), _ptr(row_dst), _ptr(status),
+                                    _stream(stream)), "carryover_slot_map")
+
+
+def carryover_store_kv8(dims, num_rows, k_rows, v_rows, row_dst, cache, status, stream=None):
+    """Rows [num_layers][num_rows][num_kv_heads][head_dim] (bf16) into their slots of the
+    8-bit cache."""
+    c = kv8(cache)
+    _check(lib().carryover_store_kv8(ctypes.byref(dims), num_rows, _ptr(k_rows), _ptr(v_rows),
+                                     _ptr(row_dst), ctypes.byref(c), _ptr(status),
+                                     _stream(stream)), "carryover_store_kv8")
+
+
+def carryover_project_kv8(dims, w, hidden, rt, st, cache, ws, stream=None, ws_bytes=None):
+    """carryover_project_kv with the committed rows into the 8-bit cache."""
+    s, r, c = state(st), route(rt), kv8(cache)
+    nb = ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    _check(lib().carryover_project_kv8(ctypes.byref(dims), ctypes.byref(w), _ptr(hidden),
+                                       ctypes.byref(r), ctypes.byref(s), ctypes.byref(c),
+                                       _ptr(ws), nb, _stream(stream)), "carryover_project_kv8")
+
+
+def drafter_block_attention_kv8(dims, layer_begin, layer_count, q, k_self, v_self, st, cache, out,
+                                lse, mass, flags, ws, stream=None, ws_bytes=None):
+    """drafter_block_attention_ext with the committed segment in the 8-bit cache."""
+    s, c = state(st), kv8(cache)
+    nb = ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    _check(lib().drafter_block_attention_kv8(ctypes.byref(dims), layer_begin, layer_count, _ptr(q),
+                                             _ptr(k_self), _ptr(v_self), ctypes.byref(s),
+                                             ctypes.byref(c), _ptr(out), _ptr(lse), _ptr(mass),
+                                             flags, _ptr(ws), nb, _stream(stream)),
+           "drafter_block_attention_kv8")
+
+
+def carryover_round_kv8(dims, w, hidden, draft_tok, target_tok, q, st, cache, rt, out, lse, flags,
+                        ws, stream=None, ws_bytes=None):
+    """carryover_round with the committed segment in the 8-bit cache."""
+    s, r, c = state(st), route(rt), kv8(cache)
+    nb = ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    _check(lib().carryover_round_kv8(ctypes.byref(dims), ctypes.byref(w), _ptr(hidden),
+                                     _ptr(draft_tok), _ptr(target_tok), _ptr(q), ctypes.byref(s),
+                                     ctypes.byref(c), ctypes.byref(r), _ptr(out), _ptr(lse), flags,
+                                     _ptr(ws), nb, _stream(stream)), "carryover_round_kv8")
 
 
 NOALLOC_SCRATCH_BYTES = 136 << 20

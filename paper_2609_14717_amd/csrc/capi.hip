@@ -124,10 +124,37 @@ KvDest make_dest(const co_dims* d, const co_route* rt, const co_state* st) {
   return e;
 }
 
+// A state whose committed segment lies elsewhere (in an 8-bit cache), or is not read.
+bool state_ok_kv8(const co_state* st) {
+  return st && st->ctx_len && st->carry_len && st->page_table && st->k_carry && st->v_carry &&
+         st->status && aligned(st->k_carry, 16) && aligned(st->v_carry, 16);
+}
+
 bool state_ok(const co_state* st) {
-  return st && st->ctx_len && st->carry_len && st->page_table && st->k_cache && st->v_cache &&
-         st->k_carry && st->v_carry && st->status && aligned(st->k_cache, 16) &&
-         aligned(st->v_cache, 16) && aligned(st->k_carry, 16) && aligned(st->v_carry, 16);
+  return state_ok_kv8(st) && st->k_cache && st->v_cache && aligned(st->k_cache, 16) &&
+         aligned(st->v_cache, 16);
+}
+
+bool cache_ok(const co_kv8* c) {
+  return c && c->k_pages && c->v_pages && c->k_scale && c->v_scale && aligned(c->k_pages, 16) &&
+         aligned(c->v_pages, 16);
+}
+
+// Shapes of the 8-bit cache's calls: dims are already checked.
+co_status check_kv8_dims(const co_dims* d) {
+  if (d->dtype != CO_DTYPE_BF16) return CO_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(d->num_layers) * d->num_kv_heads > 65535 ||
+      d->num_pages > INT32_MAX / kPage)
+    return CO_ERR_UNSUPPORTED;
+  return CO_OK;
+}
+
+// Projected rows of the committed segment on their way into the 8-bit cache: the
+// keys', then the values', behind the projection's own workspace.
+size_t rows_bytes(const co_dims* d) {
+  const size_t n = static_cast<size_t>(d->num_layers) * d->num_seqs * d->block * d->num_kv_heads *
+                   d->head_dim * 2;
+  return (n + 255) / 256 * 256;
 }
 
 bool route_ok(const co_route* rt) { return rt && rt->accept_len && rt->row_pos && rt->row_dst; }
@@ -139,6 +166,11 @@ ProjectPlan project_plan(const co_dims* d) {
 }
 
 AttnPlan attention_plan(const co_dims* d) {
+  return plan_attention(d->num_seqs, d->block, d->num_layers, d->num_q_heads, d->num_kv_heads,
+                        d->head_dim, d->max_pages_per_seq, d->num_pages, d->dtype, num_cus());
+}
+
+AttnPlan attention_kv8_plan(const co_dims* d) {
   return plan_attention(d->num_seqs, d->block, d->num_layers, d->num_q_heads, d->num_kv_heads,
                         d->head_dim, d->max_pages_per_seq, d->num_pages, d->dtype, num_cus());
 }
@@ -166,8 +198,9 @@ co_status validate_route(const co_dims* d, const int32_t* draft_tok, const int32
 
 co_status validate_project(const co_dims* d, const co_weights* w, const void* hidden,
                            const co_route* route, const co_state* st, const void* ws,
-                           size_t ws_bytes) {
-  if (!w || !w->w_f || !w->w_kv || !w->e_carry || !hidden || !route_ok(route) || !state_ok(st))
+                           size_t ws_bytes, bool kv8 = false) {
+  if (!w || !w->w_f || !w->w_kv || !w->e_carry || !hidden || !route_ok(route) ||
+      !(kv8 ? state_ok_kv8(st) : state_ok(st)))
     return CO_ERR_INVALID_ARG;
   if (!aligned(hidden, 16) || !aligned(w->w_f, 16) || !aligned(w->w_kv, 16) ||
       !aligned(w->e_carry, 16) || !aligned(w->f_e, 16) || !aligned(w->w_f_carry, 16) ||
@@ -175,7 +208,7 @@ co_status validate_project(const co_dims* d, const co_weights* w, const void* hi
     return CO_ERR_INVALID_ARG;
   if (w->z_norm && d->model_dim > kNormMaxCols) return CO_ERR_UNSUPPORTED;
   if (!ws || !aligned(ws, 256)) return CO_ERR_INVALID_ARG;
-  if (ws_bytes < project_plan(d).total) return CO_ERR_WORKSPACE;
+  if (ws_bytes < project_plan(d).total + (kv8 ? 2 * rows_bytes(d) : 0)) return CO_ERR_WORKSPACE;
   return CO_OK;
 }
 
@@ -249,10 +282,31 @@ co_status enqueue_project(const co_dims* dims, const co_weights* w, const void* 
                                    project_plan(dims), stream));
 }
 
+co_status validate_attention_kv8(const co_dims* d, int32_t layer_begin, int32_t layer_count,
+                                 const void* q, const void* k_self, const void* v_self,
+                                 const co_state* st, const co_kv8* cache, const void* out,
+                                 const float* lse, const float* mass, const void* ws,
+                                 size_t ws_bytes) {
+  co_status s = check_kv8_dims(d);
+  if (s != CO_OK) return s;
+  if (d->block * (d->num_q_heads / d->num_kv_heads) > 64 || !attention_kv8_plan(d).ok)
+    return CO_ERR_UNSUPPORTED;
+  if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > d->num_layers)
+    return CO_ERR_INVALID_ARG;
+  if (!q || !out || !state_ok_kv8(st) || !cache_ok(cache) || !aligned(q, 16) ||
+      !aligned(out, 16) || !aligned(lse, 4) || !aligned(mass, 4) ||
+      (k_self == nullptr) != (v_self == nullptr) || !aligned(k_self, 16) || !aligned(v_self, 16))
+    return CO_ERR_INVALID_ARG;
+  if (!ws || !aligned(ws, 256)) return CO_ERR_INVALID_ARG;
+  if (ws_bytes < attention_kv8_plan(d).bytes) return CO_ERR_WORKSPACE;
+  return CO_OK;
+}
+
 co_status do_attention(const co_dims* d, int32_t layer_begin, int32_t layer_count, const void* q,
                        const co_state* st, void* out, float* lse, uint32_t flags, void* ws,
                        hipStream_t stream, const void* k_self = nullptr,
-                       const void* v_self = nullptr, float* mass = nullptr) {
+                       const void* v_self = nullptr, float* mass = nullptr,
+                       const co_kv8* kv8 = nullptr) {
   AttnArgs a{};
   a.rec_sums = (k_self || mass) ? 4 : 2;
   a.k_self = k_self;
@@ -283,8 +337,41 @@ co_status do_attention(const co_dims* d, int32_t layer_begin, int32_t layer_coun
   a.lse = lse;
   a.status = st->status;
   a.ws = static_cast<float*>(ws);
+  if (kv8) {
+    a.k_cache = kv8->k_pages;
+    a.v_cache = kv8->v_pages;
+    a.k_scale = kv8->k_scale;
+    a.v_scale = kv8->v_scale;
+  }
   clear_stale_error();
-  return hip_status(launch_attention(a, attention_plan(d), layer_count, stream));
+  return hip_status(kv8 ? launch_attention_kv8(a, attention_kv8_plan(d), layer_count, stream)
+                        : launch_attention(a, attention_plan(d), layer_count, stream));
+}
+
+// Project, committed rows to plain rows behind the projection's workspace, then
+// into the 8-bit cache.
+co_status enqueue_project_kv8(ProjectArgs& pa, const ProjectPlan& plan, const co_dims* d,
+                              const co_kv8* cache, void* ws, hipStream_t stream) {
+  const size_t nb = rows_bytes(d);
+  pa.dst.k_rows = static_cast<char*>(ws) + plan.total;
+  pa.dst.v_rows = static_cast<char*>(ws) + plan.total + nb;
+  const hipError_t err = launch_project(pa, plan, stream);
+  if (err != hipSuccess) return hip_status(err);
+  StoreArgs a{};
+  a.M = pa.M;
+  a.L = d->num_layers;
+  a.Hkv = d->num_kv_heads;
+  a.hd = d->head_dim;
+  a.num_pages = d->num_pages;
+  a.k_rows = pa.dst.k_rows;
+  a.v_rows = pa.dst.v_rows;
+  a.row_dst = pa.dst.row_dst;
+  a.k_pages = cache->k_pages;
+  a.v_pages = cache->v_pages;
+  a.k_scale = cache->k_scale;
+  a.v_scale = cache->v_scale;
+  a.status = pa.dst.status;
+  return hip_status(launch_store_kv8(a, stream));
 }
 
 }  // namespace
@@ -305,6 +392,15 @@ size_t carryover_workspace_bytes(const co_dims* dims, int32_t which) {
                                      2 * dims->num_layers * dims->num_kv_heads * dims->head_dim,
                                      dims->head_dim, num_cus())
                  : 0;
+    case CO_WS_PROJECT_KV8:
+      return check_kv8_dims(dims) == CO_OK ? pw + 2 * rows_bytes(dims) : 0;
+    case CO_WS_ATTENTION_KV8:
+    case CO_WS_ROUND_KV8: {
+      if (check_kv8_dims(dims) != CO_OK || check_attention_dims(dims) != CO_OK) return 0;
+      const size_t kw = attention_kv8_plan(dims).bytes;
+      return which == CO_WS_ATTENTION_KV8 ? kw : pw + 2 * rows_bytes(dims) + kw;
+    }
+    case CO_WS_ASSIGN_PAGES: return assign_ws_bytes(dims->num_seqs);
     case CO_WS_ATTENTION_BACKWARD:
       return bwd_workspace_bytes(dims->num_seqs, dims->num_layers, dims->num_kv_heads,
                                  dims->head_dim, dims->num_pages, carry_pages(dims));
@@ -508,7 +604,7 @@ co_status drafter_carry_mass(const co_dims* dims, int32_t layer_begin, int32_t l
   if (dims->block > kMaxCarryRows) return CO_ERR_UNSUPPORTED;
   if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > dims->num_layers)
     return CO_ERR_INVALID_ARG;
-  if (!q || !lse || !mass || !state_ok(state) || !aligned(q, 16) || !aligned(lse, 4) ||
+  if (!q || !lse || !mass || !state_ok_kv8(state) || !aligned(q, 16) || !aligned(lse, 4) ||
       !aligned(mass, 4))
     return CO_ERR_INVALID_ARG;
   MassArgs a{};
@@ -542,7 +638,7 @@ co_status drafter_self_merge(const co_dims* dims, int32_t layer_begin, int32_t l
   if (dims->block > kMaxCarryRows) return CO_ERR_UNSUPPORTED;
   if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > dims->num_layers)
     return CO_ERR_INVALID_ARG;
-  if (!q || !k_self || !v_self || !out || !lse || !state_ok(state) || !aligned(q, 16) ||
+  if (!q || !k_self || !v_self || !out || !lse || !state_ok_kv8(state) || !aligned(q, 16) ||
       !aligned(k_self, 16) || !aligned(v_self, 16) || !aligned(out, 16) || !aligned(lse, 4))
     return CO_ERR_INVALID_ARG;
   SelfArgs a{};
@@ -641,6 +737,147 @@ co_status carryover_verify_sample(const co_dims* dims, int32_t vocab, const int3
   return hip_status(launch_verify(a, stream));
 }
 
+co_status carryover_assign_pages(const co_dims* dims, const int32_t* want_len, int32_t reserve,
+                                 const co_page_pool* pool, int32_t* status, void* ws,
+                                 size_t ws_bytes, hipStream_t stream) {
+  co_status s = check_dims(dims);
+  if (s != CO_OK) return s;
+  if (static_cast<int64_t>(dims->num_seqs) * dims->max_pages_per_seq > INT32_MAX ||
+      dims->num_pages > INT32_MAX / kPage)
+    return CO_ERR_UNSUPPORTED;
+  if (!want_len || reserve < 0 || !pool || !pool->page_table || !pool->held || !pool->free_pages ||
+      !pool->free_count || !status || !aligned(want_len, 4) || !aligned(pool->page_table, 4) ||
+      !aligned(pool->held, 4) || !aligned(pool->free_pages, 4) || !aligned(pool->free_count, 4) ||
+      !aligned(status, 4) || !ws || !aligned(ws, 256))
+    return CO_ERR_INVALID_ARG;
+  if (ws_bytes < assign_ws_bytes(dims->num_seqs)) return CO_ERR_WORKSPACE;
+  PagesArgs a{};
+  a.S = dims->num_seqs;
+  a.max_pages = dims->max_pages_per_seq;
+  a.num_pages = dims->num_pages;
+  a.reserve = reserve;
+  a.want = want_len;
+  a.table = pool->page_table;
+  a.held = pool->held;
+  a.free_pages = pool->free_pages;
+  a.free_count = pool->free_count;
+  a.status = status;
+  a.ws = static_cast<int32_t*>(ws);
+  clear_stale_error();
+  return hip_status(launch_assign_pages(a, stream));
+}
+
+co_status carryover_slot_map(const co_dims* dims, int32_t num_rows, const int32_t* row_start,
+                             const int32_t* pos0, const int32_t* page_table, int32_t* row_pos,
+                             int32_t* row_dst, int32_t* status, hipStream_t stream) {
+  co_status s = check_dims(dims);
+  if (s != CO_OK) return s;
+  if (dims->num_pages > INT32_MAX / kPage) return CO_ERR_UNSUPPORTED;
+  if (num_rows < 0 || !row_start || !pos0 || !page_table || !row_pos || !row_dst || !status ||
+      !aligned(row_start, 4) || !aligned(pos0, 4) || !aligned(page_table, 4) ||
+      !aligned(row_pos, 4) || !aligned(row_dst, 4) || !aligned(status, 4))
+    return CO_ERR_INVALID_ARG;
+  SlotMapArgs a{};
+  a.S = dims->num_seqs;
+  a.max_pages = dims->max_pages_per_seq;
+  a.num_pages = dims->num_pages;
+  a.num_rows = num_rows;
+  a.row_start = row_start;
+  a.pos0 = pos0;
+  a.table = page_table;
+  a.row_pos = row_pos;
+  a.row_dst = row_dst;
+  a.status = status;
+  clear_stale_error();
+  return hip_status(launch_slot_map(a, stream));
+}
+
+co_status carryover_store_kv8(const co_dims* dims, int32_t num_rows, const void* k_rows,
+                              const void* v_rows, const int32_t* row_dst, const co_kv8* cache,
+                              int32_t* status, hipStream_t stream) {
+  co_status s = check_dims(dims);
+  if (s != CO_OK) return s;
+  if ((s = check_kv8_dims(dims)) != CO_OK) return s;
+  if (num_rows < 0 || !k_rows || !v_rows || !row_dst || !cache_ok(cache) || !status ||
+      !aligned(k_rows, 16) || !aligned(v_rows, 16) || !aligned(row_dst, 4) || !aligned(status, 4))
+    return CO_ERR_INVALID_ARG;
+  StoreArgs a{};
+  a.M = num_rows;
+  a.L = dims->num_layers;
+  a.Hkv = dims->num_kv_heads;
+  a.hd = dims->head_dim;
+  a.num_pages = dims->num_pages;
+  a.k_rows = k_rows;
+  a.v_rows = v_rows;
+  a.row_dst = row_dst;
+  a.k_pages = cache->k_pages;
+  a.v_pages = cache->v_pages;
+  a.k_scale = cache->k_scale;
+  a.v_scale = cache->v_scale;
+  a.status = status;
+  clear_stale_error();
+  return hip_status(launch_store_kv8(a, stream));
+}
+
+co_status carryover_project_kv8(const co_dims* dims, const co_weights* w, const void* hidden,
+                                const co_route* route, const co_state* state, const co_kv8* cache,
+                                void* ws, size_t ws_bytes, hipStream_t stream) {
+  co_status s = check_dims(dims);
+  if (s != CO_OK) return s;
+  if ((s = check_kv8_dims(dims)) != CO_OK) return s;
+  if (!cache_ok(cache)) return CO_ERR_INVALID_ARG;
+  if ((s = validate_project(dims, w, hidden, route, state, ws, ws_bytes, true)) != CO_OK) return s;
+  ProjectArgs pa = project_args(dims, w, hidden, route, state, ws);
+  clear_stale_error();
+  return enqueue_project_kv8(pa, project_plan(dims), dims, cache, ws, stream);
+}
+
+co_status drafter_block_attention_kv8(const co_dims* dims, int32_t layer_begin,
+                                      int32_t layer_count, const void* q, const void* k_self,
+                                      const void* v_self, const co_state* state,
+                                      const co_kv8* cache, void* out, float* lse,
+                                      float* carry_mass, uint32_t flags, void* ws,
+                                      size_t ws_bytes, hipStream_t stream) {
+  co_status s = check_dims(dims);
+  if (s != CO_OK) return s;
+  if ((s = validate_attention_kv8(dims, layer_begin, layer_count, q, k_self, v_self, state, cache,
+                                  out, lse, carry_mass, ws, ws_bytes)) != CO_OK)
+    return s;
+  return do_attention(dims, layer_begin, layer_count, q, state, out, lse, flags, ws, stream, k_self,
+                      v_self, carry_mass, cache);
+}
+
+co_status carryover_round_kv8(const co_dims* dims, const co_weights* w, const void* hidden,
+                              const int32_t* draft_tok, const int32_t* target_tok, const void* q,
+                              co_state* state, const co_kv8* cache, const co_route* scratch,
+                              void* out, float* lse, uint32_t flags, void* ws, size_t ws_bytes,
+                              hipStream_t stream) {
+  co_status s = check_dims(dims);
+  if (s != CO_OK) return s;
+  if ((s = check_kv8_dims(dims)) != CO_OK) return s;
+  if ((s = validate_route(dims, draft_tok, target_tok, flags, state, scratch)) != CO_OK) return s;
+  if (!cache_ok(cache)) return CO_ERR_INVALID_ARG;
+  if ((s = validate_project(dims, w, hidden, scratch, state, ws, ws_bytes, true)) != CO_OK) return s;
+  const size_t pw = project_plan(dims).total + 2 * rows_bytes(dims);   // a multiple of 256
+  void* attn_ws = static_cast<char*>(ws) + pw;
+  if ((s = validate_attention_kv8(dims, 0, dims->num_layers, q, nullptr, nullptr, state, cache, out,
+                                  lse, nullptr, attn_ws, ws_bytes - pw)) != CO_OK)
+    return s;
+  // the route rides in the F product's launch where it can, as in carryover_round
+  ProjectArgs pa = project_args(dims, w, hidden, scratch, state, ws);
+  const ProjectPlan plan = project_plan(dims);
+  const RouteArgs ra = route_args(dims, draft_tok, target_tok, flags, state, scratch);
+  clear_stale_error();
+  if (route_foldable(pa, plan)) {
+    pa.route = &ra;
+  } else if ((s = hip_status(launch_route(ra, stream))) != CO_OK) {
+    return s;
+  }
+  if ((s = enqueue_project_kv8(pa, plan, dims, cache, ws, stream)) != CO_OK) return s;
+  return do_attention(dims, 0, dims->num_layers, q, state, out, lse, flags, attn_ws, stream, nullptr,
+                      nullptr, nullptr, cache);
+}
+
 co_status carryover_set_tuning(int32_t knob, int64_t value) {
   if (knob < 0 || knob >= CO_TUNE_COUNT) return CO_ERR_INVALID_ARG;
   g_tuning.v[knob] = value < 0 ? -1 : value;
@@ -681,6 +918,7 @@ const char* carryover_status_string(co_status status) {
     case CO_ERR_HIP: return "HIP runtime error";
     case CO_ERR_LENGTH: return "invalid sequence length";
     case CO_ERR_GROUP: return "page rows differ within a sequence group";
+    case CO_ERR_POOL: return "page pool exhausted or corrupt";
     case CO_ERR_TOKEN: return "proposed token outside the vocabulary";
     default: return "unknown status";
   }

@@ -37,6 +37,10 @@ struct KvDest {
   void* v_carry;
   int32_t* status;
   const float* knorm;   // per-head key RMS-norm gain [L][hd], or null
+  // Committed rows as plain rows [L][S * B][Hkv][hd] by window row, in place of their
+  // cache slots (the 8-bit cache takes them from there), or null:
+  void* k_rows;
+  void* v_rows;
 };
 
 struct ProjectArgs {
@@ -94,6 +98,9 @@ struct AttnArgs {
   const void* k_self;   // the block's own keys [layers][S][B][Hkv][hd], unrotated
   const void* v_self;   // and values
   float* mass;          // share of the attention over [C;U] on U, [layers][S][B][Hq]
+  // Scale bytes [L][num_pages][Hkv] of an 8-bit k_cache and v_cache
+  const uint8_t* k_scale;
+  const uint8_t* v_scale;
 };
 
 constexpr int kMaxAttnSeqs = 2048;   // sequences one bf16 attention launch can cover
@@ -201,10 +208,58 @@ struct VerifyArgs {
   int32_t* status;
 };
 
+// Page tables from request lengths (carryover_assign_pages).
+struct PagesArgs {
+  int S, max_pages, num_pages, reserve;
+  const int32_t* want;   // [S]
+  int32_t* table;        // [S][max_pages]
+  int32_t* held;         // [S]
+  int32_t* free_pages;   // [num_pages], a stack of
+  int32_t* free_count;   // this many
+  int32_t* status;
+  int32_t* ws;           // kAssignHdr + 4 S
+};
+
+constexpr int kAssignHdr = 4;             // released, taken, free + released
+constexpr int kAssignSeqs = 1024;         // one workgroup assigns up to so many sequences
+constexpr int kAssignPlaces = 65536;      // with so many table entries
+
+size_t assign_ws_bytes(int S);
+
+// Positions and slots of packed rows (carryover_slot_map).
+struct SlotMapArgs {
+  int S, max_pages, num_pages, num_rows;
+  const int32_t* row_start;   // [S + 1]
+  const int32_t* pos0;        // [S]
+  const int32_t* table;
+  int32_t* row_pos;
+  int32_t* row_dst;
+  int32_t* status;
+};
+
+// Rows into the 8-bit cache (carryover_store_kv8).
+struct StoreArgs {
+  int M, L, Hkv, hd, num_pages;
+  const void* k_rows;   // [L][M][Hkv][hd] bf16
+  const void* v_rows;
+  const int32_t* row_dst;
+  void* k_pages;
+  void* v_pages;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int32_t* status;
+};
+
 // Launch-shape override in force (-1: automatic); see carryover_set_tuning.
 int64_t tuning(int knob);
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t stream);
+hipError_t launch_assign_pages(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_slot_map(const SlotMapArgs& a, hipStream_t stream);
+hipError_t launch_store_kv8(const StoreArgs& a, hipStream_t stream);
+// a.k_cache and a.v_cache are the codes of the 8-bit cache
+hipError_t launch_attention_kv8(const AttnArgs& a, const AttnPlan& p, int layer_count,
+                                hipStream_t stream);
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream);
 hipError_t launch_self_merge(const SelfArgs& a, int layer_count, int dtype, hipStream_t stream);
 hipError_t launch_carry_mass(const MassArgs& a, int layer_count, int dtype, hipStream_t stream);

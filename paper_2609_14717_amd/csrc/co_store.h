@@ -50,14 +50,15 @@ __device__ __forceinline__ void k_norm(const KvDest& e, int seg, int i0, int lan
 // Where a row of segment (layer, head g) lives: element offsets of its dim 0
 // in the K page layout ([16][hd]) and of its token slot in the V page layout
 // ([hd][16]), and which buffers.  ok is false for a skipped row and for a
-// destination out of range (the status word then records it).
+// destination out of range (the status word then records it).  rows: a committed
+// row that goes to KvDest::k_rows, v_rows, whose dims are next to each other.
 struct KvRow {
   int64_t kbase, vbase;
-  bool carry, ok;
+  bool carry, ok, rows;
 };
 
 __device__ __forceinline__ KvRow kv_row(const KvDest& e, int row, int32_t dst, int layer, int g) {
-  KvRow r{0, 0, false, false};
+  KvRow r{0, 0, false, false, false};
   if (dst == kSkip) return r;
   const int hd = e.hd;
   int64_t pg;
@@ -67,6 +68,12 @@ __device__ __forceinline__ KvRow kv_row(const KvDest& e, int row, int32_t dst, i
     t = dst % kPage;
     if (page >= e.num_pages) {
       set_status(e.status, CO_ERR_PAGE_RANGE);
+      return r;
+    }
+    if (e.k_rows != nullptr) {
+      r.kbase = r.vbase =
+          ((static_cast<int64_t>(layer) * e.S * e.B + row) * e.Hkv + g) * static_cast<int64_t>(hd);
+      r.ok = r.rows = true;
       return r;
     }
     pg = (static_cast<int64_t>(layer) * e.num_pages + page) * e.Hkv + g;
@@ -101,7 +108,7 @@ __device__ inline void kv_store(const KvDest& e, int row, int32_t dst, int pos, 
   const KvRow r = kv_row(e, row, dst, layer, g);
   if (!r.ok) return;
   if (kind == 0) {
-    T* kptr = static_cast<T*>(r.carry ? e.k_carry : e.k_cache);
+    T* kptr = static_cast<T*>(r.carry ? e.k_carry : (r.rows ? e.k_rows : e.k_cache));
     if constexpr (sizeof(T) == 2 && NP == 4) {
       // the four dims of each half are contiguous (i0 is a multiple of 4 and
       // a row starts on a multiple of hd): one 8-byte store per half
@@ -128,11 +135,13 @@ __device__ inline void kv_store(const KvDest& e, int row, int32_t dst, int pos, 
       kptr[r.kbase + i0 + p + half] = to_elem<T>(hi[p] * c + lo[p] * s);
     }
   } else {
-    T* vptr = static_cast<T*>(r.carry ? e.v_carry : e.v_cache);
+    T* vptr = static_cast<T*>(r.carry ? e.v_carry : (r.rows ? e.v_rows : e.v_cache));
+    const int sh = r.rows ? 0 : 4;   // a row's dims are 1 or kPage apart
+    static_assert(kPage == 1 << 4, "page of 16 slots");
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      vptr[r.vbase + static_cast<int64_t>(i0 + p) * kPage] = to_elem<T>(lo[p]);
-      vptr[r.vbase + static_cast<int64_t>(i0 + p + half) * kPage] = to_elem<T>(hi[p]);
+      vptr[r.vbase + (static_cast<int64_t>(i0 + p) << sh)] = to_elem<T>(lo[p]);
+      vptr[r.vbase + (static_cast<int64_t>(i0 + p + half) << sh)] = to_elem<T>(hi[p]);
     }
   }
 }

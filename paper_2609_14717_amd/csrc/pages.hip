@@ -1,0 +1,253 @@
+// Page tables and slot maps from request lengths, on the device: the pages that
+// every sequence holds follow its length (carryover_assign_pages), and packed
+// rows get their positions and committed slots (carryover_slot_map).  Next to
+// the paper, which leaves the cache's paging to the serving stack.
+//
+// Pages change hands by number.  Released pages are numbered 0 .. R - 1 in
+// (sequence, logical page) order, places to fill 0 .. T - 1 likewise; place k
+// takes released page k, or (k >= R) entry free + R - 1 - k of the free list,
+// and released page k >= T goes to that entry.  Every page that moves is so
+// read and written by one thread, no entry is both read and written, and going
+// back to the lengths before restores table and list exactly.
+#include <algorithm>
+
+#include "co_kernels.h"
+
+namespace co {
+
+namespace {
+
+constexpr int kScanThreads = 1024;
+constexpr int kSlotThreads = 256, kSlotRows = 4;   // rows per thread of the slot map
+constexpr int kSlotSeqs = 4096;                    // sequences whose starts fit in LDS
+
+// What a sequence holds and needs; an error leaves it as it is.
+struct Need {
+  int held, need, err;
+};
+
+__device__ __forceinline__ Need seq_need(const PagesArgs& a, int s) {
+  const int h = a.held[s], w = a.want[s];
+  const int64_t n = w > 0 ? (static_cast<int64_t>(w) + a.reserve + kPage - 1) / kPage : 0;
+  if (h < 0 || h > a.max_pages) return {0, 0, CO_ERR_LENGTH};
+  if (w < 0) return {h, h, CO_ERR_LENGTH};
+  if (n > a.max_pages) return {h, h, CO_ERR_CAPACITY};
+  return {h, static_cast<int>(n), CO_OK};
+}
+
+// The moves of one call: sequence s moves its places [lo, hi), out of its row
+// (bit 31 of `to` set) or into it, the first one numbered `first`; `grow` is the
+// number of its first place to fill.
+struct Moves {
+  int *lo, *hi, *first, *grow;   // [S] each
+  int released, taken, have;     // R, T, free + R
+};
+
+// One workgroup: numbers every sequence's moves and writes the new holdings.
+// Thread t takes ceil(S / 1024) sequences in a row.  sh: 2 * 16 ints of LDS.
+__device__ void number_moves(const PagesArgs& a, Moves& m, int* sh) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int per = (a.S + kScanThreads - 1) / kScanThreads;
+  const int s0 = min(a.S, t * per), s1 = min(a.S, s0 + per);
+  const int c = a.free_count[0];   // read by every thread before it changes below
+  const bool ok = c >= 0 && c <= a.num_pages;
+  int back = 0, more = 0;
+  for (int s = s0; s < s1; ++s) {
+    const Need n = seq_need(a, s);
+    if (n.err != CO_OK) set_status(a.status, n.err);
+    back += max(0, n.held - n.need);
+    more += max(0, n.need - n.held);
+  }
+  int bi = back, mi = more;   // inclusive over the wavefront
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int b = __shfl_up(bi, o), g = __shfl_up(mi, o);
+    if (lane >= o) {
+      bi += b;
+      mi += g;
+    }
+  }
+  if (lane == 63) {
+    sh[wave] = bi;
+    sh[16 + wave] = mi;
+  }
+  __syncthreads();
+  int R = 0, bx = bi - back, mx = mi - more;   // bx, mx: before this thread's sequences
+#pragma unroll
+  for (int w = 0; w < kScanThreads / 64; ++w) {
+    const int b = sh[w], g = sh[16 + w];
+    R += b;
+    bx += w < wave ? b : 0;
+    mx += w < wave ? g : 0;
+  }
+  if (!ok && t == 0) set_status(a.status, CO_ERR_POOL);
+  const int have = ok ? c + R : 0;
+  int T = 0;
+  for (int s = s0; s < s1; ++s) {
+    const Need n = seq_need(a, s);
+    const int b = max(0, n.held - n.need), g = max(0, n.need - n.held);
+    const bool fits = mx + g <= have;   // in order: none after the first that does not fit
+    if (ok && g > 0 && !fits) set_status(a.status, CO_ERR_POOL);
+    const bool out = ok && b > 0, in = ok && g > 0 && fits;
+    m.lo[s] = out ? n.need : n.held;
+    m.hi[s] = in ? n.need : n.held;
+    m.first[s] = out ? static_cast<int>(0x80000000u | static_cast<uint32_t>(bx)) : mx;
+    m.grow[s] = mx;
+    if (out || in) a.held[s] = n.need;
+    if (in) T = mx + g;
+    bx += b;
+    mx += g;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) T = max(T, __shfl_xor(T, o));
+  __syncthreads();   // sh is read
+  if (lane == 0) sh[wave] = T;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kScanThreads / 64; ++w) T = max(T, sh[w]);
+  m.released = ok ? R : 0;
+  m.taken = T;
+  m.have = have;
+  if (ok && t == 0) a.free_count[0] = have - T;
+}
+
+// Place p of sequence s, in [lo, hi), changes hands.
+__device__ __forceinline__ void move_page(const PagesArgs& a, const Moves& m, int s, int p, int lo,
+                                          int first) {
+  const bool out = first < 0;
+  const int k = (first & 0x7FFFFFFF) + p - lo;
+  int32_t* at = a.table + static_cast<int64_t>(s) * a.max_pages + p;
+  if (!out) {
+    // (entries from R on: the rest come with a released page)
+    if (k >= m.released) *at = a.free_pages[m.have - 1 - k];
+    return;
+  }
+  const int32_t id = *at;
+  *at = -1;
+  if (k < m.taken) {   // to the place of the same number
+    int l = 0, r = a.S;   // the last sequence whose places start at or before k
+    while (r - l > 1) {
+      const int mid = (l + r) >> 1;
+      if (m.grow[mid] <= k) l = mid;
+      else r = mid;
+    }
+    a.table[static_cast<int64_t>(l) * a.max_pages + m.lo[l] + k - m.grow[l]] = id;
+  } else if (m.have - 1 - k < a.num_pages) {
+    a.free_pages[m.have - 1 - k] = id;
+  } else {
+    set_status(a.status, CO_ERR_POOL);   // more pages than the pool has
+  }
+}
+
+// Both steps in one workgroup: wavefront w moves the pages of sequences w, w + 16, ...
+__global__ __launch_bounds__(kScanThreads) void assign_pages_kernel(PagesArgs a) {
+  __shared__ int sh[32], lds[4 * kAssignSeqs];
+  Moves m{lds, lds + kAssignSeqs, lds + 2 * kAssignSeqs, lds + 3 * kAssignSeqs, 0, 0, 0};
+  number_moves(a, m, sh);
+  __syncthreads();
+  const int lane = threadIdx.x & 63;
+  for (int s = threadIdx.x >> 6; s < a.S; s += kScanThreads / 64) {
+    const int lo = m.lo[s], hi = m.hi[s], first = m.first[s];
+    for (int p = lo + lane; p < hi; p += 64) move_page(a, m, s, p, lo, first);
+  }
+}
+
+// Or in two launches, the moves by a thread per place of the table.
+__global__ __launch_bounds__(kScanThreads) void assign_scan_kernel(PagesArgs a) {
+  __shared__ int sh[32];
+  int* w = a.ws + kAssignHdr;
+  Moves m{w, w + a.S, w + 2 * a.S, w + 3 * a.S, 0, 0, 0};
+  number_moves(a, m, sh);
+  if (threadIdx.x == 0) {
+    a.ws[0] = m.released;
+    a.ws[1] = m.taken;
+    a.ws[2] = m.have;
+  }
+}
+
+__global__ __launch_bounds__(256) void assign_move_kernel(PagesArgs a) {
+  int* w = a.ws + kAssignHdr;
+  const Moves m{w, w + a.S, w + 2 * a.S, w + 3 * a.S, a.ws[0], a.ws[1], a.ws[2]};
+  const int s = blockIdx.x, p = blockIdx.y * 256 + threadIdx.x;
+  const int lo = m.lo[s];
+  if (p >= lo && p < m.hi[s]) move_page(a, m, s, p, lo, m.first[s]);
+}
+
+// Position and slot of packed rows: row r belongs to the last sequence that
+// starts at or before it.  A thread takes kSlotRows rows in a row: one search, then
+// steps over the sequences' ends.  LDS: the starts fit there.
+template <bool LDS>
+__global__ __launch_bounds__(kSlotThreads) void slot_map_kernel(SlotMapArgs a) {
+  __shared__ int32_t lds[LDS ? kSlotSeqs + 1 : 1];
+  const int32_t* start = a.row_start;
+  if constexpr (LDS) {
+    for (int i = threadIdx.x; i <= a.S; i += kSlotThreads) lds[i] = a.row_start[i];
+    __syncthreads();
+    start = lds;
+  }
+  const int64_t r0 = (static_cast<int64_t>(blockIdx.x) * kSlotThreads + threadIdx.x) * kSlotRows;
+  if (r0 >= a.num_rows) return;
+  int s = -1, end = a.S;   // start[s] <= r0 < start[end], with -1 and S + 1 as the ends
+  ++end;
+  while (end - s > 1) {
+    const int mid = (s + end) >> 1;
+    if (start[mid] <= r0) s = mid;
+    else end = mid;
+  }
+#pragma unroll
+  for (int i = 0; i < kSlotRows; ++i) {
+    const int64_t r = r0 + i;
+    if (r >= a.num_rows) return;
+    while (s < a.S && start[s + 1] <= r) ++s;
+    int32_t pos = 0, dst = kSkip;
+    if (s >= 0 && s < a.S) {   // (rows before the first sequence and behind the last have no slot)
+      const int32_t p0 = a.pos0[s];
+      const int64_t p = p0 + (r - start[s]);
+      if (p0 < 0 || r < start[s]) {
+        set_status(a.status, CO_ERR_LENGTH);
+      } else if (p >= static_cast<int64_t>(a.max_pages) * kPage) {
+        set_status(a.status, CO_ERR_CAPACITY);
+      } else {
+        const int32_t id = a.table[static_cast<int64_t>(s) * a.max_pages + p / kPage];
+        if (id < 0 || id >= a.num_pages) {
+          set_status(a.status, CO_ERR_PAGE_RANGE);
+        } else {
+          pos = static_cast<int32_t>(p);
+          dst = id * kPage + pos % kPage;
+        }
+      }
+    }
+    a.row_pos[r] = pos;
+    a.row_dst[r] = dst;
+  }
+}
+
+}  // namespace
+
+size_t assign_ws_bytes(int S) {
+  return (kAssignHdr + 4 * static_cast<size_t>(S)) * 4 + 255 & ~static_cast<size_t>(255);
+}
+
+hipError_t launch_assign_pages(const PagesArgs& a, hipStream_t stream) {
+  if (a.S == 0) return hipSuccess;
+  if (a.S <= kAssignSeqs && static_cast<int64_t>(a.S) * a.max_pages <= kAssignPlaces) {
+    hipLaunchKernelGGL(assign_pages_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(assign_scan_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL(assign_move_kernel, dim3(a.S, (a.max_pages + 255) / 256), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_slot_map(const SlotMapArgs& a, hipStream_t stream) {
+  if (a.num_rows == 0) return hipSuccess;
+  const int per = kSlotThreads * kSlotRows;
+  const dim3 grid((a.num_rows + per - 1) / per);
+  if (a.S <= kSlotSeqs) hipLaunchKernelGGL(slot_map_kernel<true>, grid, dim3(kSlotThreads), 0, stream, a);
+  else hipLaunchKernelGGL(slot_map_kernel<false>, grid, dim3(kSlotThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace co
