@@ -56,6 +56,31 @@ __device__ __forceinline__ void lds_dma16_opaque(const void* src, uint32_t lds_d
       : "memory");
 }
 
+// N such loads of consecutive KiB, source and LDS alike, from a uniform base and a
+// 32-bit offset per lane (no 64-bit address arithmetic per lane).  Five wait states
+// lie between the statement's start and the first load, as a base fresh from a
+// lane read needs.
+template <int N>
+__device__ __forceinline__ void lds_dma_kib_opaque(const void* base, uint32_t off, uint32_t lds_dst) {
+  static_assert(N == 1 || N == 2, "KiB per page");
+  uint32_t saved;
+  if constexpr (N == 1)
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 2\n\t"
+        "global_load_lds_dwordx4 %1, %3\n\ts_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(off), "s"(lds_dst), "s"(base)
+        : "memory");
+  else
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 2\n\t"
+        "global_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(off), "s"(lds_dst), "s"(base)
+        : "memory");
+}
+
 // s_waitcnt vmcnt(N) lgkmcnt(0), then a workgroup barrier, as one statement that
 // no memory access is moved across.
 template <int N>
@@ -83,12 +108,15 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
          (static_cast<uint32_t>(__builtin_bit_cast(uint16_t, b)) << 16);
 }
 
-// The same pair conversion as one v_cvt_pk_bf16_f32 with both sources (the
-// compiler otherwise converts one value at a time and merges the halves).
+// The same pair conversion as one v_cvt_pk_bf16_f32 with both sources (the scalar
+// conversions above are made one value at a time and merged).  Not as inline asm:
+// a matrix instruction must come two wait states after the vector instruction that
+// wrote its operand, which the compiler sees to only for instructions it knows.
 __device__ __forceinline__ uint32_t cvt_pk_bf16(float lo, float hi) {
-  uint32_t r;
-  asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(lo), "v"(hi));
-  return r;
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const f32x2 v = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
 // The value lane q of each group of four lanes holds, in all four (a DPP
