@@ -473,6 +473,13 @@ __device__ __forceinline__ int swz_key_page(int slot) {
   return HD == 64 ? slot >> 1 : slot;
 }
 __device__ __forceinline__ int swz_value(int dim) { return (dim >> 3) & 1; }
+//   Key rows of 8-bit codes are 128 or 64 bytes: two or four to the window.  The sixteen
+//   lanes read one chunk of eight slots (0-7 or 8-15) of both pages of a pair; value
+//   rows are 16 bytes, one behind the other.
+template <int HD>
+__device__ __forceinline__ constexpr int swz_key8(int slot, int page) {
+  return HD == 64 ? ((slot >> 2) & 1) | (page << 1) : ((slot >> 1) & 3) | (page << 2);
+}
 
 // The block's own rows (drafter_block_attention_ext) as 32-key tiles of a
 // (layer, KV head, sequence): rows t0 .. t0 + 31 of k_self / v_self
@@ -1601,7 +1608,16 @@ __global__ __launch_bounds__(256) void attn_bf16_combine_kernel(AttnArgs a, int 
 // is rounded by nothing, so a reference kept over several tiles costs accuracy:
 // one over each tile 2.6e-3 from 64 bits, over three or four 2.75e-3, with the
 // remainders 2.3e-3.
-template <int HD, int NQT, bool EXT = false, bool PLO = false>
+//
+// KV8: committed tiles come from the 8-bit cache, 64 keys of 4 pages to a tile of the
+// same bytes ([K pages 0-3][V pages 0-3], rows of codes with their 16-byte chunks
+// XOR-permuted by swz_key8).  Codes go to bf16 in registers, exactly, the scale with
+// them (v_cvt_scalef32_pk_bf16_fp8: two codes, times a power of two).  A 16-byte
+// read then holds two operands: 16 dims of a key for two products, 16 slots of a dim.
+// So the products over dims pair them in that order (`chunk`, for the queries and
+// the carry keys too), and S^T takes its rows from two pages in turn, four slots
+// each: lane l holds the 16 keys of page l / 32 of the pair, register r slot r.
+template <int HD, int NQT, bool EXT = false, bool PLO = false, bool KV8 = false>
 struct Tile32 {
   static constexpr int KK = HD / 16, MO = HD / 32;
   static constexpr int ROWB = HD * 2, CPR = ROWB / 16;
@@ -1616,6 +1632,13 @@ struct Tile32 {
   u16x8 qf[NQT][16 > KK ? KK : KK];
   uint32_t kf_off[KK], vf_off;
   int slot_base, half, r32;
+  static constexpr int PAGE8 = kPage * HD;      // a page's codes
+  uint32_t k8_off;     // of chunk 0 of a pair of pages, kf_off[0] of bf16 rows: the other
+                       // chunks' differ in bits that an XOR sets (fewer registers)
+  int k8_shift;        // of its scale byte
+
+  // 16-byte chunk of a bf16 row that product k takes in half h
+  static __device__ int chunk(int k, int h) { return KV8 ? 4 * (k >> 1) + 2 * h + (k & 1) : 2 * k + h; }
 
   __device__ void setup(int lane) {
     half = lane >> 5;
@@ -1624,11 +1647,16 @@ struct Tile32 {
     const int kslot = key & 15;
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
-      const int ch = 2 * k + half;
+      const int ch = chunk(k, half);
       kf_off[k] = (key >> 4) * PAGE_BYTES + kslot * ROWB + ((ch ^ swz_key_page<HD>(kslot)) << 4);
     }
     vf_off = 2 * PAGE_BYTES + r32 * 32 + ((half ^ swz_value(r32)) << 4);
     slot_base = 8 * half;
+    if constexpr (KV8) {
+      const int page = (r32 >> 2) & 1, slot = 4 * (r32 >> 3) + (r32 & 3);
+      k8_shift = 8 * page;
+      k8_off = page * PAGE8 + slot * HD + ((half ^ swz_key8<HD>(slot, page)) << 4);
+    }
 #pragma unroll
     for (int qt = 0; qt < NQT; ++qt) {
 #pragma unroll
@@ -1659,7 +1687,8 @@ struct Tile32 {
     const bool partial = n0 < kPage || n1 < kPage;
     u16x8 kf[KK], vf[MO][2];
 #pragma unroll
-    for (int k = 0; k < KK; ++k) kf[k] = *reinterpret_cast<const u16x8*>(tb + kf_off[k]);
+    for (int k = 0; k < KK; ++k)
+      kf[k] = *reinterpret_cast<const u16x8*>(tb + (KV8 ? kf_off[0] ^ (chunk(k, 0) << 4) : kf_off[k]));
 #pragma unroll
     for (int m = 0; m < MO; ++m)
 #pragma unroll
@@ -1770,6 +1799,128 @@ struct Tile32 {
           if constexpr (PLO) o[qt][m] = mfma32x32x16(vf[m][j], pl[qt][j], o[qt][m]);
           o[qt][m] = mfma32x32x16(vf[m][j], pk[qt][j], o[qt][m]);
         }
+  }
+
+  // Eight codes as a bf16 operand, times the power of two `scale`.
+  static __device__ __forceinline__ u16x8 widen(uint32_t a, uint32_t b, float scale) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+    const bf16x2 w0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false);
+    const bf16x2 w1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+    const bf16x2 w2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
+    const bf16x2 w3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+    const u32x4v w = {__builtin_bit_cast(uint32_t, w0), __builtin_bit_cast(uint32_t, w1),
+                      __builtin_bit_cast(uint32_t, w2), __builtin_bit_cast(uint32_t, w3)};
+    return __builtin_bit_cast(u16x8, w);
+  }
+
+  // one 64-key tile of codes at tb: n[p] valid keys in page p, its scale bytes in
+  // byte p of kw and vw.  As step, one rescale decision for the tile.
+  __device__ void step8(const unsigned char* tb, const int (&n)[4], uint32_t kw, uint32_t vw) {
+    static_assert(NQT == 1 && KV8, "one query tile");
+    typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+    const bool partial = min(min(n[0], n[1]), min(n[2], n[3])) < kPage;
+    f32x16 sc[2];
+    const float base = (m_run[0] == -INFINITY) ? 0.f : m_run[0];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float ks = __uint_as_float(((kw >> (16 * h + k8_shift)) & 0xFFu) << 23);
+      u32x4v kc[KK / 2];
+#pragma unroll
+      for (int m = 0; m < KK / 2; ++m)
+        kc[m] = *reinterpret_cast<const u32x4v*>(tb + (k8_off ^ (m << 5)) + 2 * h * PAGE8);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[h][r] = -base;
+#pragma unroll
+      for (int m = 0; m < KK / 2; ++m) {
+        sc[h] = mfma32x32x16(widen(kc[m][0], kc[m][1], ks), qf[0][2 * m], sc[h]);
+        sc[h] = mfma32x32x16(widen(kc[m][2], kc[m][3], ks), qf[0][2 * m + 1], sc[h]);
+      }
+      __builtin_amdgcn_sched_barrier(0);   // no operand of a later phase in registers yet
+    }
+    if (partial) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int nv = half ? n[2 * h + 1] : n[2 * h];
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (r >= nv) sc[h][r] = -INFINITY;
+      }
+    }
+    // (integer maxima, as in step)
+    int vi = __float_as_int(sc[0][0]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) vi = max(vi, __float_as_int(sc[h][r]));
+    const auto sw = __builtin_amdgcn_permlane32_swap(vi, vi, false, false);
+    const float rel = __int_as_float(max(static_cast<int>(sw[0]), static_cast<int>(sw[1])));
+    if (__any(rel > kRescale || m_run[0] == -INFINITY)) {
+      float v = sc[0][0];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v = fmaxf(v, sc[h][r]);
+      const auto s2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+      const float mx = fmaxf(__uint_as_float(s2[0]), __uint_as_float(s2[1])) + base;
+      const float m_new = mx > m_run[0] + kRescale ? mx : m_run[0];
+      const float alpha = (m_new == m_run[0]) ? 1.f : exp2f(m_run[0] - m_new);
+      l_run[0] *= alpha;
+      if constexpr (EXT) {
+        lu_run[0] *= alpha;
+        ls_run[0] *= alpha;
+      }
+#pragma unroll
+      for (int m = 0; m < MO; ++m) o[0][m] *= alpha;
+      m_run[0] = m_new;
+      const float shift = (m_new == -INFINITY) ? 0.f : m_new - base;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[h][r] -= shift;
+    }
+    values8(tb + (4 + half) * PAGE8 + r32 * kPage, sc[0], half ? n[1] : n[0], partial, vw >> (8 * half));
+    __builtin_amdgcn_sched_barrier(0);
+    values8(tb + (6 + half) * PAGE8 + r32 * kPage, sc[1], half ? n[3] : n[2], partial,
+            vw >> (16 + 8 * half));
+  }
+
+  // The weights and products of one page per half of the wavefront: nv valid keys of
+  // the values at vp, scale byte in the low bits of vb.
+  __device__ __forceinline__ void values8(const unsigned char* vp, const f32x16& sc, int nv,
+                                          bool partial, uint32_t vb) {
+    typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+    u32x4v vc[MO];
+#pragma unroll
+    for (int m = 0; m < MO; ++m) vc[m] = *reinterpret_cast<const u32x4v*>(vp + m * 32 * kPage);
+    float p[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(sc[r]);
+    const float p0 = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    const float p1 = ((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15]));
+    l_run[0] += p0 + p1;
+    u16x8 pk[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const u32x4v w4 = {cvt_pk_bf16(p[8 * j + 0], p[8 * j + 1]), cvt_pk_bf16(p[8 * j + 2], p[8 * j + 3]),
+                         cvt_pk_bf16(p[8 * j + 4], p[8 * j + 5]), cvt_pk_bf16(p[8 * j + 6], p[8 * j + 7])};
+      pk[j] = __builtin_bit_cast(u16x8, w4);
+    }
+    const float vs = __uint_as_float((vb & 0xFFu) << 23);
+    if (partial) {   // codes behind the last key may be NaN
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int c = min(max(nv - 4 * w, 0), 4);
+        const uint32_t keep = c == 4 ? ~0u : (1u << (8 * c)) - 1;
+#pragma unroll
+        for (int m = 0; m < MO; ++m) vc[m][w] &= keep;
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < MO; ++m) {
+      o[0][m] = mfma32x32x16(widen(vc[m][0], vc[m][1], vs), pk[0], o[0][m]);
+      o[0][m] = mfma32x32x16(widen(vc[m][2], vc[m][3], vs), pk[1], o[0][m]);
+    }
   }
 
   // query tile qt: normalised output rows (bf16) and LSE; rows >= nq skipped
@@ -2256,11 +2407,12 @@ constexpr int kSliceTiles = 4;   // tiles per slice of the even split below whic
 // before each sequence [S+1], total tiles, 1 for parts / 0 for the even split.
 constexpr int wave_hdr_ints(int S) { return (2 * (S + 1) + 2 + 63) / 64 * 64; }
 
-template <int HD, int NQT, bool EXT, bool PLO>
+template <int HD, int NQT, bool EXT, bool PLO, bool KV8 = false>
 __global__ __launch_bounds__(64 * stream_waves(NQT) * wg_streams(HD, NQT), 2)
 __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     AttnArgs a, int layer_count, int n_places, int n_slices, int hdr_floats, int rec_rows) {
-  using TT = Tile32<HD, 1, EXT, PLO>;
+  using TT = Tile32<HD, 1, EXT, PLO, KV8>;
+  constexpr int TP = KV8 ? 4 : 2;   // committed pages per tile
   constexpr int QW = stream_waves(NQT), NST = wg_streams(HD, NQT);
   constexpr int NQP = NQT * 32, NS = kWaveRing, NTHR = 64 * QW * NST;
   constexpr int PAGE_BYTES = TT::PAGE_BYTES, LPP = TT::LPP, TILE_BYTES = TT::TILE_BYTES;
@@ -2288,7 +2440,7 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     ctx = si.ok ? si.ctx : 0;
     carry = si.ok ? si.carry : 0;
     if (!si.ok && blockIdx.x == 0) set_status(a.status, CO_ERR_LENGTH);
-    const int n = ((ctx + kPage - 1) / kPage + 1) / 2 + ((carry + kPage - 1) / kPage + 1) / 2;
+    const int n = (ctx + TP * kPage - 1) / (TP * kPage) + ((carry + kPage - 1) / kPage + 1) / 2;
     return n + (EXT && a.k_self && si.ok ? 1 : 0);   // the block's own rows: the last tile
   };
   auto scan64 = [&](int v) {   // inclusive sum over the lanes
@@ -2408,6 +2560,17 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     k_off[q] = r * HD + (pch ^ swz_key_page<HD>(r)) * 8;
     v_off[q] = (byte ^ (swz_value(byte / 32) << 4)) / 2;
   }
+  // The same of an 8-bit page's codes (a page's second KiB: 1024 more; keys of the
+  // tile's pages 1 and 3: under another XOR key)
+  const unsigned char* kc8 = static_cast<const unsigned char*>(a.k_cache);
+  const unsigned char* vc8 = static_cast<const unsigned char*>(a.v_cache);
+  uint32_t k8_src = lane * 16, k8_odd = 0;
+  if (QW == 1 || qw == 0) {
+    const int r = lane * 16 / HD;
+    k8_src = r * HD + ((((lane * 16 % HD) / 16) ^ swz_key8<HD>(r, 0)) << 4);
+    k8_odd = swz_key8<HD>(0, 1) << 4;
+  }
+  static_assert(swz_key8<HD>(0, 0) == swz_key8<HD>(1024 / HD % kPage, 0), "one key for both KiB");
   unsigned char* my_ring = ring + stream * NS * TILE_BYTES;
   const uint32_t my_ring_lds = lds_addr(my_ring);
   const int64_t page_stride = static_cast<int64_t>(a.Hkv) * kPage * HD;
@@ -2497,22 +2660,58 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     locate(local, s, ts, te, ctx, carry);
     const int pe = min(t1, seg * T1 + te), j0 = local - ts, j1 = j0 + (pe - t);
     const int layer_local = seg / a.Hkv, g = seg % a.Hkv, layer = a.layer_begin + layer_local;
-    const int npc = (ctx + kPage - 1) / kPage, nct = (npc + 1) / 2;
+    const int npc = (ctx + kPage - 1) / kPage, nct = (npc + TP - 1) / TP;
     const int ncp = (carry + kPage - 1) / kPage;
     const int64_t head0 = (static_cast<int64_t>(layer) * a.num_pages * a.Hkv + g) * (kPage * HD);
     const int32_t* pt = a.page_table + static_cast<int64_t>(s) * a.max_pages;
     // tile j of the sequence: two committed pages, or two carry pages; of two
     // wavefronts the first loads the keys, the second the values
-    auto issue = [&](int j, int phys0, int phys1) {
+    auto issue = [&](int j, const int (&phys)[TP]) {
       const uint32_t dst = my_ring_lds + (j % NS) * TILE_BYTES;
+      if constexpr (KV8) {
+        if (j < nct) {   // four pages of codes
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            const int64_t o = head0 + phys[p] * page_stride;
+            const uint32_t at = dst + p * TT::PAGE8;
+            constexpr int NK = TT::PAGE8 / 1024;
+            if constexpr (QW == 1) {
+              lds_dma_kib_opaque<NK>(kc8 + o, p & 1 ? k8_src ^ k8_odd : k8_src, at);
+              lds_dma_kib_opaque<NK>(vc8 + o, lane * 16, at + 4 * TT::PAGE8);
+            } else {   // (k8_src, k8_odd: this wavefront's half's)
+              lds_dma_kib_opaque<NK>((qw == 0 ? kc8 : vc8) + o, p & 1 ? k8_src ^ k8_odd : k8_src,
+                                     at + (qw == 0 ? 0 : 4 * TT::PAGE8));
+            }
+          }
+          return;
+        }
+      }
       int64_t o0, o1;
       if (j < nct) {
-        o0 = head0 + phys0 * page_stride;
-        o1 = head0 + phys1 * page_stride;
+        o0 = head0 + phys[0] * page_stride;
+        o1 = head0 + phys[1] * page_stride;
       } else {
         const int cp0 = 2 * (j - nct), cp1 = min(cp0 + 1, ncp - 1);
         o0 = (((static_cast<int64_t>(layer) * a.S + s) * a.CP + cp0) * a.Hkv + g) * (kPage * HD);
         o1 = (((static_cast<int64_t>(layer) * a.S + s) * a.CP + cp1) * a.Hkv + g) * (kPage * HD);
+      }
+      if constexpr (KV8) {   // carry pages: their lanes' offsets are made anew (registers)
+        int l = lane;
+        asm volatile("" : "+v"(l));
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int q = 0; q < LPP; ++q) {
+            const int byte = q * 1024 + l * 16, r = byte / TT::ROWB;
+            const int64_t o = p ? o1 : o0;
+            if (QW == 1 || qw == 0)
+              lds_dma16_opaque(kk + o + r * HD + (((byte % TT::ROWB) / 16) ^ swz_key_page<HD>(r)) * 8,
+                               dst + p * PAGE_BYTES + q * 1024);
+            if (QW == 1 || qw == 1)
+              lds_dma16_opaque(vk + o + (byte ^ (swz_value(byte / 32) << 4)) / 2,
+                               dst + (2 + p) * PAGE_BYTES + q * 1024);
+          }
+        return;
       }
       if (QW == 1 || qw == 0) {
         const uint16_t* kb = j < nct ? kc : kk;
@@ -2528,23 +2727,39 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     auto keys = [&](int j, int h) {
       return j < nct ? keys_in(ctx, j, h) : keys_in(carry, j - nct, h);
     };
-    // committed page ids of tiles [c0, c0 + 64): lane l holds pages 2(c0 + l), 2(c0 + l) + 1;
-    // a rejected id reads page 0 with its keys masked
-    int id0 = 0, id1 = 0, c0 = -(1 << 30), bad = 0;   // no window fetched yet
+    // committed page ids of tiles [c0, c0 + 64): lane l holds those of tile c0 + l (the
+    // last one again past the end); a rejected id reads page 0 with its keys
+    // masked.  8 bits: and their scale bytes.
+    int id[TP] = {}, c0 = -(1 << 30), bad = 0;   // no window fetched yet
+    uint32_t ks_l = 0, vs_l = 0;
     auto fetch_ids = [&](int c) {
       c0 = c;
-      const int jt = c + lane, p = 2 * jt;
-      id0 = 0;
-      id1 = 0;
+      const int jt = c + lane, p = TP * jt;
+#pragma unroll
+      for (int i = 0; i < TP; ++i) id[i] = 0;
       bad = 0;
       if (jt < nct) {
-        const int x0 = pt[p];
-        const int x1 = p + 1 < npc ? pt[p + 1] : x0;
-        const bool b0 = x0 < 0 || x0 >= a.num_pages, b1 = x1 < 0 || x1 >= a.num_pages;
-        if (b0 || b1) set_status(a.status, CO_ERR_PAGE_RANGE);
-        id0 = b0 ? 0 : x0;
-        id1 = b1 ? 0 : x1;
-        bad = (b0 ? 1 : 0) | (b1 ? 2 : 0);
+#pragma unroll
+        for (int i = 0; i < TP; ++i) id[i] = pt[min(p + i, npc - 1)];
+#pragma unroll
+        for (int i = 0; i < TP; ++i)
+          if (id[i] < 0 || id[i] >= a.num_pages) {
+            bad |= 1 << i;
+            id[i] = 0;
+          }
+        if (bad) set_status(a.status, CO_ERR_PAGE_RANGE);
+      }
+      if constexpr (KV8) {
+        ks_l = vs_l = 0;
+        if (jt < nct) {
+          const int64_t sc0 = static_cast<int64_t>(layer) * a.num_pages * a.Hkv + g;
+#pragma unroll
+          for (int i = 0; i < TP; ++i) {
+            const int64_t at = sc0 + static_cast<int64_t>(id[i]) * a.Hkv;
+            ks_l |= static_cast<uint32_t>(a.k_scale[at]) << (8 * i);
+            vs_l |= static_cast<uint32_t>(a.v_scale[at]) << (8 * i);
+          }
+        }
       }
     };
     // The block's own rows are the segment's last tile (drafter_block_attention_ext):
@@ -2563,8 +2778,8 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
       }
     };
     static_assert(2 * 32 * HD * 2 / 1024 == TL * QW, "the own rows take as many loads as a tile");
-    auto issue_tile = [&](int j, int& rejected) {
-      int p0 = 0, p1 = 0;
+    auto issue_tile = [&](int j, int& rejected, uint32_t& ks, uint32_t& vs) {
+      int p[TP] = {};
       rejected = 0;
       if (EXT && j == own) {
         own_issue(0);
@@ -2572,11 +2787,15 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
       }
       if (j < nct) {   // j uniform
         if (j >= c0 + 64 || j < c0) fetch_ids(j);
-        p0 = __builtin_amdgcn_readlane(id0, j - c0);
-        p1 = __builtin_amdgcn_readlane(id1, j - c0);
+#pragma unroll
+        for (int i = 0; i < TP; ++i) p[i] = __builtin_amdgcn_readlane(id[i], j - c0);
         rejected = __builtin_amdgcn_readlane(bad, j - c0);
+        if constexpr (KV8) {
+          ks = __builtin_amdgcn_readlane(ks_l, j - c0);
+          vs = __builtin_amdgcn_readlane(vs_l, j - c0);
+        }
       }
-      issue(j, p0, p1);
+      issue(j, p);
     };
 
     // This wavefront's 32 query rows land raw in the part of the ring's last slot
@@ -2585,6 +2804,7 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     // XOR-permuted as key rows are), then read into the B fragments.  Rows past
     // nq repeat the last one; nothing of them is stored.
     int b[NS] = {};   // rejected pages of the tiles in the ring, b[0] the current one's
+    uint32_t ksb[NS] = {}, vsb[NS] = {};   // and their scale bytes
     if (j0 < nct) fetch_ids(j0);
     constexpr int ROWB = HD * 2, CPR = ROWB / 16, CPP = CPR / 2, QL = 32 * ROWB / 1024;
     const int row0 = 32 * qw;
@@ -2605,7 +2825,7 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     }
 #pragma unroll
     for (int i = 0; i < NS - 1; ++i)
-      if (j0 + i < j1) issue_tile(j0 + i, b[i]);
+      if (j0 + i < j1) issue_tile(j0 + i, b[i], ksb[i], vsb[i]);
     static_assert(NS == 2, "one tile ahead");
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(TL) : "memory");   // the queries are in
     // With G a multiple of 4 the four lanes of a quad hold rows of one position
@@ -2657,7 +2877,7 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
 #pragma unroll
     for (int k = 0; k < KK; ++k)
       T.qf[0][k] = (ln & 31) >= jobs * RJ ? u16x8{} : *reinterpret_cast<const u16x8*>(
-          qs + (ln & 31) * ROWB + (((2 * k + (ln >> 5)) ^ swz_key_page<HD>(ln & 15)) << 4));
+          qs + (ln & 31) * ROWB + ((TT::chunk(k, ln >> 5) ^ swz_key_page<HD>(ln & 15)) << 4));
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the second tile lands there
 
     for (int j = j0; j < min(j1, own); ++j) {
@@ -2665,19 +2885,38 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
       // wait for their halves of tile j first: the barrier publishes it and tells
       // that both are done with tile j - 1.
       const bool more = j + NS - 1 < j1;
-      if (QW == 1 && more) issue_tile(j + NS - 1, b[NS - 1]);
+      if (QW == 1 && more) issue_tile(j + NS - 1, b[NS - 1], ksb[NS - 1], vsb[NS - 1]);
       if (QW == 1 && more) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(TL) : "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       stream_barrier();
-      if (QW > 1 && more) issue_tile(j + NS - 1, b[NS - 1]);
-      const int n0 = (b[0] & 1) ? 0 : keys(j, 0), n1 = (b[0] & 2) ? 0 : keys(j, 1);
-      if (n0 + n1 > 0) {
-        const int kind = (EXT && j >= nct) ? 1 : 0;   // a tile is committed or carry
-        T.step(my_ring + (j % NS) * TILE_BYTES, n0, n1, kind, kind);
+      if (QW > 1 && more) issue_tile(j + NS - 1, b[NS - 1], ksb[NS - 1], vsb[NS - 1]);
+      bool done = false;
+      if constexpr (KV8) {
+        if (j < nct) {
+          int n[4];
+#pragma unroll
+          for (int p = 0; p < 4; ++p)
+            n[p] = ((b[0] >> p) & 1) ? 0 : min(kPage, max(0, ctx - (4 * j + p) * kPage));
+          if (n[0] + n[1] + n[2] + n[3] > 0) T.step8(my_ring + (j % NS) * TILE_BYTES, n, ksb[0], vsb[0]);
+          done = true;
+        }
+      }
+      if (!done) {
+        const int n0 = (b[0] & 1) ? 0 : keys(j, 0), n1 = (b[0] & 2) ? 0 : keys(j, 1);
+        if (n0 + n1 > 0) {
+          const int kind = (EXT && j >= nct) ? 1 : 0;   // a tile is committed or carry
+          T.step(my_ring + (j % NS) * TILE_BYTES, n0, n1, kind, kind);
+        }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // tile j is read
 #pragma unroll
-      for (int i = 0; i + 1 < NS; ++i) b[i] = b[i + 1];
+      for (int i = 0; i + 1 < NS; ++i) {
+        b[i] = b[i + 1];
+        if constexpr (KV8) {
+          ksb[i] = ksb[i + 1];
+          vsb[i] = vsb[i + 1];
+        }
+      }
     }
     stream_barrier();   // the other slot is free
     if constexpr (EXT) {
@@ -2882,18 +3121,31 @@ AttnPlan plan_attention(int S, int B, int L, int Hq, int Hkv, int hd, int max_pa
   return p;
 }
 
-hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int layer_count,
-                            hipStream_t stream) {
-  if (a.S == 0 || layer_count == 0) return hipSuccess;
-  const int nt = p.nq_pad / 16;
-  // merge grid: one workgroup per 256 (query row, dims) items of a segment,
-  // 16 dims per item with at least kCombineWideSegs segments, else 4; per 64
-  // items with up to kCombineGroupSegs
+// The merge of a launch's records: one workgroup per 256 (query row, dims) items
+// of a segment, 16 dims per item with at least kCombineWideSegs segments, else 4;
+// per 64 items with up to kCombineGroupSegs.
+static void launch_combine(const AttnArgs& a, int layer_count, int slices, int hdr, int rec_rows,
+                           int waves, hipStream_t stream) {
   const int64_t n_segs = static_cast<int64_t>(a.S) * layer_count * a.Hkv;
   const bool wide = n_segs >= kCombineWideSegs, grouped = n_segs <= kCombineGroupSegs;
   const int items = (a.B * (a.Hq / a.Hkv)) * (a.hd / (wide ? 16 : 4));
   const int wg_items = grouped ? 64 : 256;
   const dim3 mgrid(a.S, layer_count * a.Hkv, (items + wg_items - 1) / wg_items);
+  if (wide)
+    hipLaunchKernelGGL((attn_bf16_combine_kernel<16, 1>), mgrid, dim3(256), 0, stream, a, layer_count,
+                       slices, hdr, rec_rows, waves);
+  else if (grouped)
+    hipLaunchKernelGGL((attn_bf16_combine_kernel<4, 4>), mgrid, dim3(256), 0, stream, a, layer_count,
+                       slices, hdr, rec_rows, waves);
+  else
+    hipLaunchKernelGGL((attn_bf16_combine_kernel<4, 1>), mgrid, dim3(256), 0, stream, a, layer_count,
+                       slices, hdr, rec_rows, waves);
+}
+
+hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int layer_count,
+                            hipStream_t stream) {
+  if (a.S == 0 || layer_count == 0) return hipSuccess;
+  const int nt = p.nq_pad / 16;
   const int items_f32 = (a.B * (a.Hq / a.Hkv)) * (a.hd / 4);
   const dim3 fgrid(a.S, layer_count * a.Hkv, (items_f32 + 255) / 256);
   // the extras (self segment, carry mass): the same kernels' EXT instantiations
@@ -2901,15 +3153,7 @@ hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int layer_coun
   const bool ext = a.k_self != nullptr || a.mass != nullptr;
   const int n_wg = p.n_wg, hdr_floats = p.hdr_floats;
   auto combine = [&](int slices, int hdr, int rec_rows, int waves) {
-    if (wide)
-      hipLaunchKernelGGL((attn_bf16_combine_kernel<16, 1>), mgrid, dim3(256), 0, stream, a, layer_count,
-                         slices, hdr, rec_rows, waves);
-    else if (grouped)
-      hipLaunchKernelGGL((attn_bf16_combine_kernel<4, 4>), mgrid, dim3(256), 0, stream, a, layer_count,
-                         slices, hdr, rec_rows, waves);
-    else
-      hipLaunchKernelGGL((attn_bf16_combine_kernel<4, 1>), mgrid, dim3(256), 0, stream, a, layer_count,
-                         slices, hdr, rec_rows, waves);
+    launch_combine(a, layer_count, slices, hdr, rec_rows, waves, stream);
   };
   // grouped kernel: any query count with head_dim 64, up to 32 rows with 128
   const int nq = a.B * (a.Hq / a.Hkv);
@@ -3018,6 +3262,66 @@ hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int layer_coun
   if (err != hipSuccess || p.n_chunks <= 1) return err;
   hipLaunchKernelGGL(attn_chunk_merge_kernel<float>, fgrid, dim3(256), 0, stream, a, p.chunk_pages,
                      p.n_chunks, p.nq_pad);
+  return hipGetLastError();
+}
+
+// The committed segment in the 8-bit cache: every shape takes the streams path.
+AttnPlan plan_attention_kv8(int S, int B, int L, int Hq, int Hkv, int hd, int max_pages,
+                            int num_pages, int num_cus) {
+  AttnPlan p{};
+  const int nq = B * (Hq / Hkv), cp = (B + kPage - 1) / kPage;
+  p.nq_pad = (nq + 15) / 16 * 16;
+  const int wg_st = wg_streams(hd, p.nq_pad <= 32 ? 1 : 2), cus = std::max(1, num_cus);
+  const int64_t segs = static_cast<int64_t>(L) * Hkv * S;
+  const int64_t tiles = segs * ((max_pages + 3) / 4 + (cp + 1) / 2);
+  // slices of the even split and streams launched, as for the bf16 cache
+  const int64_t wg_override = tuning(CO_TUNE_ATTN_WORKGROUPS);
+  const bool forced = wg_override >= 1 && wg_override <= kMaxMergeSlices / kCuStreams;
+  int n_sl = static_cast<int>(forced ? wg_override : cus) * kCuStreams;
+  if (!forced) {
+    const int64_t by_tiles = (tiles / kSliceTiles + kCuStreams - 1) / kCuStreams * kCuStreams;
+    n_sl = static_cast<int>(std::max<int64_t>(kCuStreams, std::min<int64_t>(n_sl, by_tiles)));
+  }
+  n_sl = (n_sl + wg_st - 1) / wg_st * wg_st;   // whole workgroups
+  p.n_slices = n_sl;
+  p.n_places = wg_st == 4 && !forced ? std::min(cus * kCuStreams, wg_st * n_sl) : n_sl;
+  p.hdr_slices = wave_hdr_ints(S);
+  // tile indices, and page rows of cache and carry segment, are int32
+  p.ok = S <= kMaxAttnSeqs && tiles + segs < INT32_MAX &&
+         static_cast<int64_t>(L) * num_pages * Hkv < INT32_MAX &&
+         static_cast<int64_t>(L) * S * cp * Hkv < INT32_MAX && n_sl <= kMaxMergeSlices;
+  const size_t rec = static_cast<size_t>(p.nq_pad) * (hd + 4);
+  p.bytes = (p.hdr_slices + (static_cast<size_t>(n_sl) + static_cast<size_t>(segs)) * rec) * 4;
+  p.bytes = (p.bytes + 255) / 256 * 256;
+  return p;
+}
+
+hipError_t launch_attention_kv8(const AttnArgs& a, const AttnPlan& p, int layer_count,
+                                hipStream_t stream) {
+  if (a.S == 0 || layer_count == 0) return hipSuccess;
+  const bool ext = a.k_self != nullptr || a.mass != nullptr;
+  const int nqt = p.nq_pad <= 32 ? 1 : 2, nst = wg_streams(a.hd, nqt);
+  const dim3 grid(p.n_places / nst), block(64 * stream_waves(nqt) * nst);
+#define CO_KV8_LAUNCH(HD, NQT)                                                                     \
+  do {                                                                                             \
+    if (ext)                                                                                       \
+      hipLaunchKernelGGL((attn_wave_kernel<HD, NQT, true, false, true>), grid, block, 0, stream,   \
+                         a, layer_count, p.n_places, p.n_slices, p.hdr_slices, p.nq_pad);          \
+    else                                                                                           \
+      hipLaunchKernelGGL((attn_wave_kernel<HD, NQT, false, false, true>), grid, block, 0, stream,  \
+                         a, layer_count, p.n_places, p.n_slices, p.hdr_slices, p.nq_pad);          \
+  } while (0)
+  if (a.hd == 128) {
+    if (nqt == 1) CO_KV8_LAUNCH(128, 1);
+    else CO_KV8_LAUNCH(128, 2);
+  } else {
+    if (nqt == 1) CO_KV8_LAUNCH(64, 1);
+    else CO_KV8_LAUNCH(64, 2);
+  }
+#undef CO_KV8_LAUNCH
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  launch_combine(a, layer_count, p.n_slices, p.hdr_slices, p.nq_pad, nst, stream);
   return hipGetLastError();
 }
 

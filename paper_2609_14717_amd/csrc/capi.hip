@@ -171,8 +171,16 @@ AttnPlan attention_plan(const co_dims* d) {
 }
 
 AttnPlan attention_kv8_plan(const co_dims* d) {
-  return plan_attention(d->num_seqs, d->block, d->num_layers, d->num_q_heads, d->num_kv_heads,
-                        d->head_dim, d->max_pages_per_seq, d->num_pages, d->dtype, num_cus());
+  return plan_attention_kv8(d->num_seqs, d->block, d->num_layers, d->num_q_heads,
+                            d->num_kv_heads, d->head_dim, d->max_pages_per_seq, d->num_pages,
+                            num_cus());
+}
+
+co_status check_attention_kv8_dims(const co_dims* d) {
+  const co_status s = check_kv8_dims(d);
+  if (s != CO_OK) return s;
+  const int64_t nq = static_cast<int64_t>(d->block) * (d->num_q_heads / d->num_kv_heads);
+  return nq <= 64 && attention_kv8_plan(d).ok ? CO_OK : CO_ERR_UNSUPPORTED;
 }
 
 co_status hip_status(hipError_t e) { return e == hipSuccess ? CO_OK : CO_ERR_HIP; }
@@ -287,10 +295,8 @@ co_status validate_attention_kv8(const co_dims* d, int32_t layer_begin, int32_t 
                                  const co_state* st, const co_kv8* cache, const void* out,
                                  const float* lse, const float* mass, const void* ws,
                                  size_t ws_bytes) {
-  co_status s = check_kv8_dims(d);
+  co_status s = check_attention_kv8_dims(d);
   if (s != CO_OK) return s;
-  if (d->block * (d->num_q_heads / d->num_kv_heads) > 64 || !attention_kv8_plan(d).ok)
-    return CO_ERR_UNSUPPORTED;
   if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > d->num_layers)
     return CO_ERR_INVALID_ARG;
   if (!q || !out || !state_ok_kv8(st) || !cache_ok(cache) || !aligned(q, 16) ||
@@ -396,7 +402,7 @@ size_t carryover_workspace_bytes(const co_dims* dims, int32_t which) {
       return check_kv8_dims(dims) == CO_OK ? pw + 2 * rows_bytes(dims) : 0;
     case CO_WS_ATTENTION_KV8:
     case CO_WS_ROUND_KV8: {
-      if (check_kv8_dims(dims) != CO_OK || check_attention_dims(dims) != CO_OK) return 0;
+      if (check_attention_kv8_dims(dims) != CO_OK) return 0;
       const size_t kw = attention_kv8_plan(dims).bytes;
       return which == CO_WS_ATTENTION_KV8 ? kw : pw + 2 * rows_bytes(dims) + kw;
     }

@@ -121,6 +121,9 @@ struct AttnPlan {
 AttnPlan plan_attention(int S, int B, int L, int Hq, int Hkv, int hd, int max_pages, int num_pages,
                         int dtype, int num_cus);
 
+AttnPlan plan_attention_kv8(int S, int B, int L, int Hq, int Hkv, int hd, int max_pages,
+                            int num_pages, int num_cus);
+
 // Reverse mode of the bf16 attention (head_dim 64, up to 32 query rows per KV
 // head): `a` carries the forward's arguments with ws = the backward workspace.
 struct BwdArgs {
