@@ -1611,12 +1611,21 @@ __global__ __launch_bounds__(256) void attn_bf16_combine_kernel(AttnArgs a, int 
 //
 // KV8: committed tiles come from the 8-bit cache, 64 keys of 4 pages to a tile of the
 // same bytes ([K pages 0-3][V pages 0-3], rows of codes with their 16-byte chunks
-// XOR-permuted by swz_key8).  Codes go to bf16 in registers, exactly, the scale with
-// them (v_cvt_scalef32_pk_bf16_fp8: two codes, times a power of two).  A 16-byte
-// read then holds two operands: 16 dims of a key for two products, 16 slots of a dim.
-// So the products over dims pair them in that order (`chunk`, for the queries and
-// the carry keys too), and S^T takes its rows from two pages in turn, four slots
-// each: lane l holds the 16 keys of page l / 32 of the pair, register r slot r.
+// XOR-permuted by swz_key8).
+//   Scores: v_mfma_scale_f32_32x32x64_f8f6f4 takes the keys' codes as they are, with
+//   the page's scale byte as its own block scale (the same format).  A bf16 query,
+//   8 significant bits, is the sum of two codes of 4, the second under 2^-4 of the
+//   first's scale, one power of two per row (entries under 2^-14 of a row's
+//   largest keep 2^-22 of that instead of 8 bits); two such products at twice the
+//   bf16 rate.  Widening the keys to bf16 took 64 of the 540 vector instructions
+//   of a tile.
+//   Values: codes to bf16 in registers, exactly, the scale with them
+//   (v_cvt_scalef32_pk_bf16_fp8), against bf16 weights: a weight has no largest
+//   value in its row that 8 bits could be relative to.  A 16-byte read holds 16
+//   slots of a dim, the operands of two products.
+// S^T takes its rows from two pages in turn, four slots each: lane l holds the 16 keys
+// of page l / 32 of the pair, register r slot r.  Lane l holds of its query the dims
+// 32 (l / 32) .. + 31 of every 64 (`chunk`, for the carry keys' bf16 products too).
 template <int HD, int NQT, bool EXT = false, bool PLO = false, bool KV8 = false>
 struct Tile32 {
   static constexpr int KK = HD / 16, MO = HD / 32;
@@ -1629,16 +1638,22 @@ struct Tile32 {
   f32x16 o[NQT][MO];
   float m_run[NQT], l_run[NQT];   // l_run: this half-wavefront's keys (summed at the end)
   float lu_run[NQT], ls_run[NQT];
-  u16x8 qf[NQT][16 > KK ? KK : KK];
+  u16x8 qf[NQT][KV8 ? 1 : KK];
   uint32_t kf_off[KK], vf_off;
   int slot_base, half, r32;
+  typedef int i32x8 __attribute__((ext_vector_type(8)));
+  typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+  static constexpr int NG = HD / 64;            // groups of 64 dims
+  i32x8 qh[KV8 ? NG : 1], ql[KV8 ? NG : 1];     // the query's two codes of every dim
+  int q_scale;                                  // their scale bytes (byte 0, byte 1)
+  f32x16 nb;                                    // minus the running reference, sixteen times
   static constexpr int PAGE8 = kPage * HD;      // a page's codes
   uint32_t k8_off;     // of chunk 0 of a pair of pages, kf_off[0] of bf16 rows: the other
                        // chunks' differ in bits that an XOR sets (fewer registers)
   int k8_shift;        // of its scale byte
 
   // 16-byte chunk of a bf16 row that product k takes in half h
-  static __device__ int chunk(int k, int h) { return KV8 ? 4 * (k >> 1) + 2 * h + (k & 1) : 2 * k + h; }
+  static __device__ int chunk(int k, int h) { return KV8 ? 8 * (k >> 2) + 4 * h + (k & 3) : 2 * k + h; }
 
   __device__ void setup(int lane) {
     half = lane >> 5;
@@ -1655,7 +1670,9 @@ struct Tile32 {
     if constexpr (KV8) {
       const int page = (r32 >> 2) & 1, slot = 4 * (r32 >> 3) + (r32 & 3);
       k8_shift = 8 * page;
-      k8_off = page * PAGE8 + slot * HD + ((half ^ swz_key8<HD>(slot, page)) << 4);
+      k8_off = page * PAGE8 + slot * HD + (((2 * half) ^ swz_key8<HD>(slot, page)) << 4);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) nb[r] = 0.f;
     }
 #pragma unroll
     for (int qt = 0; qt < NQT; ++qt) {
@@ -1702,10 +1719,22 @@ struct Tile32 {
 #pragma unroll
       for (int r = 0; r < 16; ++r) sc[qt][r] = -base[qt];
     }
+    if constexpr (KV8) {   // both codes of the query, widened here: these tiles are few
+      int b = q_scale;
+      asm volatile("" : "+v"(b));   // (and not kept in registers over the walk)
+      const float sh = __uint_as_float(static_cast<uint32_t>(b & 0xFF) << 23);
 #pragma unroll
-    for (int k = 0; k < KK; ++k)
+      for (int k = 0; k < KK; ++k) {
+        const int w = 2 * (k & 3);
+        sc[0] = mfma32x32x16(kf[k], widen(qh[k >> 2][w], qh[k >> 2][w + 1], sh), sc[0]);
+        sc[0] = mfma32x32x16(kf[k], widen(ql[k >> 2][w], ql[k >> 2][w + 1], sh * 0.0625f), sc[0]);
+      }
+    } else {
 #pragma unroll
-      for (int qt = 0; qt < NQT; ++qt) sc[qt] = mfma32x32x16(kf[k], qf[qt][k], sc[qt]);
+      for (int k = 0; k < KK; ++k)
+#pragma unroll
+        for (int qt = 0; qt < NQT; ++qt) sc[qt] = mfma32x32x16(kf[k], qf[qt][k], sc[qt]);
+    }
     if (partial) {
 #pragma unroll
       for (int m = 0; m < MO; ++m)
@@ -1758,6 +1787,7 @@ struct Tile32 {
         const float shift = (m_new == -INFINITY) ? 0.f : m_new - base[qt];
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[qt][r] -= shift;
+        if constexpr (KV8) set_reference();
       }
     }
     u16x8 pk[NQT][2], pl[NQT][2];
@@ -1801,10 +1831,55 @@ struct Tile32 {
         }
   }
 
+  __device__ __forceinline__ void set_reference() {
+    const float x = m_run[0] == -INFINITY ? 0.f : -m_run[0];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) nb[r] = x;
+  }
+
+  // The query of this lane's row out of an LDS row of bf16 (16-byte chunks XOR-permuted
+  // by x16), as two codes per dim; `live` false: a row of padding.
+  __device__ __forceinline__ void set_query(const unsigned char* row, int x16, bool live) {
+    static_assert(!KV8 || NQT == 1, "one query tile");
+    u32x4v x[KK];
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top2 = {0, 0};
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      x[k] = *reinterpret_cast<const u32x4v*>(row + ((chunk(k, half) ^ x16) << 4));
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        top2 = __builtin_elementwise_max(top2, __builtin_bit_cast(u16x2, x[k][e] & 0x7FFF7FFFu));
+    }
+    uint32_t top = max(top2[0], top2[1]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    top = max(static_cast<uint32_t>(sw[0]), static_cast<uint32_t>(sw[1]));
+    // (byte 1: four less; a row with an infinity or a NaN gives NaN under any scale)
+    const int b = max(5, scale_byte_e4m3(min(top, 0x7F7Fu)));
+    q_scale = b | ((b - 4) << 8);
+    const float f = __uint_as_float(static_cast<uint32_t>(254 - b) << 23), f16 = 16.f * f;
+    const float back = __uint_as_float(static_cast<uint32_t>(b) << 23);
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int k = 0; k < KK; ++k)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {   // four dims
+        const float v0 = __uint_as_float(x[k][2 * w] << 16), v1 = __uint_as_float(x[k][2 * w] & 0xFFFF0000u);
+        const float v2 = __uint_as_float(x[k][2 * w + 1] << 16), v3 = __uint_as_float(x[k][2 * w + 1] & 0xFFFF0000u);
+        int hi = __builtin_amdgcn_cvt_pk_fp8_f32(v0 * f, v1 * f, 0, false);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(v2 * f, v3 * f, hi, true);
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, back, false);
+        const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, back, true);
+        int lo = __builtin_amdgcn_cvt_pk_fp8_f32((v0 - a[0]) * f16, (v1 - a[1]) * f16, 0, false);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32((v2 - c[0]) * f16, (v3 - c[1]) * f16, lo, true);
+        qh[k >> 2][2 * (k & 3) + w] = live ? hi : 0;
+        ql[k >> 2][2 * (k & 3) + w] = live ? lo : 0;
+      }
+  }
+
   // Eight codes as a bf16 operand, times the power of two `scale`.
   static __device__ __forceinline__ u16x8 widen(uint32_t a, uint32_t b, float scale) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
     const bf16x2 w0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false);
     const bf16x2 w1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
     const bf16x2 w2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
@@ -1818,25 +1893,32 @@ struct Tile32 {
   // byte p of kw and vw.  As step, one rescale decision for the tile.
   __device__ void step8(const unsigned char* tb, const int (&n)[4], uint32_t kw, uint32_t vw) {
     static_assert(NQT == 1 && KV8, "one query tile");
-    typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
     const bool partial = min(min(n[0], n[1]), min(n[2], n[3])) < kPage;
     f32x16 sc[2];
-    const float base = (m_run[0] == -INFINITY) ? 0.f : m_run[0];
+    const float base = -nb[0];
+    const int ks = static_cast<int>(kw >> k8_shift);   // bytes 0 and 2: this lane's pages'
+    i32x8 kc[2][NG];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float ks = __uint_as_float(((kw >> (16 * h + k8_shift)) & 0xFFu) << 23);
-      u32x4v kc[KK / 2];
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int m = 0; m < KK / 2; ++m)
-        kc[m] = *reinterpret_cast<const u32x4v*>(tb + (k8_off ^ (m << 5)) + 2 * h * PAGE8);
+      for (int m = 0; m < NG; ++m) {
+        const u32x4v a = *reinterpret_cast<const u32x4v*>(tb + (k8_off ^ (m << 6)) + 2 * h * PAGE8);
+        const u32x4v b = *reinterpret_cast<const u32x4v*>(tb + (k8_off ^ (m << 6) ^ 16) + 2 * h * PAGE8);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[h][r] = -base;
-#pragma unroll
-      for (int m = 0; m < KK / 2; ++m) {
-        sc[h] = mfma32x32x16(widen(kc[m][0], kc[m][1], ks), qf[0][2 * m], sc[h]);
-        sc[h] = mfma32x32x16(widen(kc[m][2], kc[m][3], ks), qf[0][2 * m + 1], sc[h]);
+        for (int w = 0; w < 4; ++w) {
+          kc[h][m][w] = a[w];
+          kc[h][m][4 + w] = b[w];
+        }
       }
-      __builtin_amdgcn_sched_barrier(0);   // no operand of a later phase in registers yet
+#pragma unroll
+    for (int m = 0; m < NG; ++m) {   // (the pairs' products in turn: no result waits for the one before)
+      sc[0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc[0][m], qh[m], m ? sc[0] : nb, 0, 0, 0, ks, 0, q_scale);
+      sc[1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc[1][m], qh[m], m ? sc[1] : nb, 0, 0, 2, ks, 0, q_scale);
+    }
+#pragma unroll
+    for (int m = 0; m < NG; ++m) {
+      sc[0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc[0][m], ql[m], sc[0], 0, 0, 0, ks, 1, q_scale);
+      sc[1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc[1][m], ql[m], sc[1], 0, 0, 2, ks, 1, q_scale);
     }
     if (partial) {
 #pragma unroll
@@ -1878,6 +1960,7 @@ struct Tile32 {
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[h][r] -= shift;
+      set_reference();
     }
     values8(tb + (4 + half) * PAGE8 + r32 * kPage, sc[0], half ? n[1] : n[0], partial, vw >> (8 * half));
     __builtin_amdgcn_sched_barrier(0);
@@ -1889,7 +1972,6 @@ struct Tile32 {
   // the values at vp, scale byte in the low bits of vb.
   __device__ __forceinline__ void values8(const unsigned char* vp, const f32x16& sc, int nv,
                                           bool partial, uint32_t vb) {
-    typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
     u32x4v vc[MO];
 #pragma unroll
     for (int m = 0; m < MO; ++m) vc[m] = *reinterpret_cast<const u32x4v*>(vp + m * 32 * kPage);
@@ -2874,49 +2956,55 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
       *reinterpret_cast<u32x4v*>(hi_p) = yp;
     }
     T.setup(lane);
+    if constexpr (KV8)
+      T.set_query(qs + (ln & 31) * ROWB, swz_key_page<HD>(ln & 15), (ln & 31) < jobs * RJ);
+    else
 #pragma unroll
     for (int k = 0; k < KK; ++k)
       T.qf[0][k] = (ln & 31) >= jobs * RJ ? u16x8{} : *reinterpret_cast<const u16x8*>(
           qs + (ln & 31) * ROWB + ((TT::chunk(k, ln >> 5) ^ swz_key_page<HD>(ln & 15)) << 4));
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the second tile lands there
 
-    for (int j = j0; j < min(j1, own); ++j) {
-      // A lone wavefront refills tile j - 1's slot, then waits for tile j; two
-      // wait for their halves of tile j first: the barrier publishes it and tells
-      // that both are done with tile j - 1.
+    // A lone wavefront refills tile j - 1's slot, then waits for tile j; two
+    // wait for their halves of tile j first: the barrier publishes it and tells
+    // that both are done with tile j - 1.
+    auto next_tile = [&](int j) {
       const bool more = j + NS - 1 < j1;
       if (QW == 1 && more) issue_tile(j + NS - 1, b[NS - 1], ksb[NS - 1], vsb[NS - 1]);
       if (QW == 1 && more) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(TL) : "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       stream_barrier();
       if (QW > 1 && more) issue_tile(j + NS - 1, b[NS - 1], ksb[NS - 1], vsb[NS - 1]);
-      bool done = false;
-      if constexpr (KV8) {
-        if (j < nct) {
-          int n[4];
-#pragma unroll
-          for (int p = 0; p < 4; ++p)
-            n[p] = ((b[0] >> p) & 1) ? 0 : min(kPage, max(0, ctx - (4 * j + p) * kPage));
-          if (n[0] + n[1] + n[2] + n[3] > 0) T.step8(my_ring + (j % NS) * TILE_BYTES, n, ksb[0], vsb[0]);
-          done = true;
-        }
-      }
-      if (!done) {
-        const int n0 = (b[0] & 1) ? 0 : keys(j, 0), n1 = (b[0] & 2) ? 0 : keys(j, 1);
-        if (n0 + n1 > 0) {
-          const int kind = (EXT && j >= nct) ? 1 : 0;   // a tile is committed or carry
-          T.step(my_ring + (j % NS) * TILE_BYTES, n0, n1, kind, kind);
-        }
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // tile j is read
+    };
+    auto tile_done = [&]() {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile is read
 #pragma unroll
       for (int i = 0; i + 1 < NS; ++i) {
         b[i] = b[i + 1];
-        if constexpr (KV8) {
-          ksb[i] = ksb[i + 1];
-          vsb[i] = vsb[i + 1];
-        }
+        ksb[i] = ksb[i + 1];
+        vsb[i] = vsb[i + 1];
       }
+    };
+    int j = j0;
+    if constexpr (KV8) {   // committed tiles; the carry tiles in a loop of their own (registers)
+      for (; j < min(j1, nct); ++j) {
+        next_tile(j);
+        int n[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+          n[p] = ((b[0] >> p) & 1) ? 0 : min(kPage, max(0, ctx - (4 * j + p) * kPage));
+        if (n[0] + n[1] + n[2] + n[3] > 0) T.step8(my_ring + (j % NS) * TILE_BYTES, n, ksb[0], vsb[0]);
+        tile_done();
+      }
+    }
+    for (; j < min(j1, own); ++j) {
+      next_tile(j);
+      const int n0 = (b[0] & 1) ? 0 : keys(j, 0), n1 = (b[0] & 2) ? 0 : keys(j, 1);
+      if (n0 + n1 > 0) {
+        const int kind = (EXT && j >= nct) ? 1 : 0;   // a tile is committed or carry
+        T.step(my_ring + (j % NS) * TILE_BYTES, n0, n1, kind, kind);
+      }
+      tile_done();
     }
     stream_barrier();   // the other slot is free
     if constexpr (EXT) {

@@ -131,6 +131,19 @@ __device__ __forceinline__ float quad_bcast(float v, int q) {
   }
 }
 
+// Larger of m and the finite magnitudes (bf16 bits without the sign) of a packed pair.
+__device__ __forceinline__ uint32_t finite_max_bf16(uint32_t m, uint32_t pair) {
+  const uint32_t lo = pair & 0x7FFFu, hi = (pair >> 16) & 0x7FFFu;
+  m = max(m, lo < 0x7F80u ? lo : 0u);
+  return max(m, hi < 0x7F80u ? hi : 0u);
+}
+
+// Scale byte of e4m3 codes whose largest entry is `top` (bf16 bits): the smallest
+// k >= -126 with 1.mmm * 2^e <= 1.75 * 2^(8 + k), plus 127.
+__device__ __forceinline__ int scale_byte_e4m3(uint32_t top) {
+  return max(1, static_cast<int>(top >> 7) - 8 + ((top & 0x7Fu) > 0x60u ? 1 : 0));
+}
+
 // Max over the four 16-lane rows holding the same column (lanes l, l^16, l^32, l^48),
 // with the gfx950 row-swap permutes instead of LDS permutes.
 __device__ __forceinline__ float max_across_rows(float v) {

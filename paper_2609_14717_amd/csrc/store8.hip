@@ -20,23 +20,10 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStoreWaves = 4;        // wavefronts per workgroup
 
-// Larger of the finite magnitudes (bf16 bits, sign off) of two packed pairs.
-__device__ __forceinline__ uint32_t finite_max(uint32_t m, uint32_t pair) {
-  const uint32_t lo = pair & 0x7FFFu, hi = (pair >> 16) & 0x7FFFu;
-  m = max(m, lo < 0x7F80u ? lo : 0u);
-  return max(m, hi < 0x7F80u ? hi : 0u);
-}
-
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), o)));
   return v;
-}
-
-// Scale byte of a largest entry (bf16 bits): the smallest k >= -126 with
-// 1.mmm * 2^e <= 1.75 * 2^(8 + k), plus 127.
-__device__ __forceinline__ int scale_byte(uint32_t top) {
-  return max(1, static_cast<int>(top >> 7) - 8 + ((top & 0x7Fu) > 0x60u ? 1 : 0));
 }
 
 // 2^-(b - 127), exactly.
@@ -84,8 +71,8 @@ __device__ void store_keys(const uint16_t* rows, int64_t row_stride, int t0, int
 #pragma unroll
   for (int i = 0; i < NI; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) top = finite_max(top, x[i][e]);
-  const int b = max(before, scale_byte(wave_max(top)));
+    for (int e = 0; e < 4; ++e) top = finite_max_bf16(top, x[i][e]);
+  const int b = max(before, scale_byte_e4m3(wave_max(top)));
   const float f = unscale(b);
   const bool finer = t0 > 0 && b > before;
   const float g = finer ? __uint_as_float(static_cast<uint32_t>(max(0, 127 + before - b)) << 23) : 0.f;
@@ -132,8 +119,8 @@ __device__ void store_values(const uint16_t* rows, int64_t row_stride, int t0, i
 #pragma unroll
   for (int d = 0; d < ND; ++d) old[d] = t0 > 0 ? to[d] : u32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int t = 0; t < kPage; ++t) top = finite_max(top, x[t]);
-  const int b = max(before, scale_byte(wave_max(top)));
+  for (int t = 0; t < kPage; ++t) top = finite_max_bf16(top, x[t]);
+  const int b = max(before, scale_byte_e4m3(wave_max(top)));
   const float f = unscale(b);
   const bool finer = t0 > 0 && b > before;
   const float g = finer ? __uint_as_float(static_cast<uint32_t>(max(0, 127 + before - b)) << 23) : 0.f;
