@@ -1613,11 +1613,11 @@ __global__ __launch_bounds__(256) void attn_bf16_combine_kernel(AttnArgs a, int 
 // same bytes ([K pages 0-3][V pages 0-3], rows of codes with their 16-byte chunks
 // XOR-permuted by swz_key8).
 //   Scores: v_mfma_scale_f32_32x32x64_f8f6f4 takes the keys' codes as they are, with
-//   the page's scale byte as its own block scale (the same format).  A bf16 query,
-//   8 significant bits, is the sum of two codes of 4, the second under 2^-4 of the
-//   first's scale, one power of two per row (entries under 2^-14 of a row's
-//   largest keep 2^-22 of that instead of 8 bits); two such products at twice the
-//   bf16 rate.  Widening the keys to bf16 took 64 of the 540 vector instructions
+//   the page's scale byte as its own block scale (the same format).  A query
+//   is the sum of two codes of 4 significant bits, the second under 2^-4 of the
+//   first's scale, one power of two per row: rounded to 8 bits, as in bf16 (entries
+//   under 2^-14 of a row's largest: to 2^-22 of that).  Two such products at twice
+//   the bf16 rate.  Widening the keys to bf16 took 64 of the 540 vector instructions
 //   of a tile.
 //   Values: codes to bf16 in registers, exactly, the scale with them
 //   (v_cvt_scalef32_pk_bf16_fp8), against bf16 weights: a weight has no largest
@@ -1837,44 +1837,80 @@ struct Tile32 {
     for (int r = 0; r < 16; ++r) nb[r] = x;
   }
 
-  // The query of this lane's row out of an LDS row of bf16 (16-byte chunks XOR-permuted
-  // by x16), as two codes per dim; `live` false: a row of padding.
-  __device__ __forceinline__ void set_query(const unsigned char* row, int x16, bool live) {
+  // This lane's query row, its bf16 dims in x (16 bytes per chunk), rotated at pos and
+  // scaled in fp32, as two codes per dim; `live` false: a row of padding.  The
+  // partner of a dim is in the lane's other group of 64 (head_dim 128) or in the
+  // other half's lane of the row (64).  quad: the four lanes of a quad are rows of one
+  // position, so each computes every fourth angle and takes the others from them.
+  __device__ __forceinline__ void set_query(const u32x4v (&x)[KK], int pos, bool rotate, bool quad,
+                                            const double* inv_rev, float qscale, bool live) {
     static_assert(!KV8 || NQT == 1, "one query tile");
-    u32x4v x[KK];
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    u16x2 top2 = {0, 0};
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    float v[8 * KK];
 #pragma unroll
-    for (int k = 0; k < KK; ++k) {
-      x[k] = *reinterpret_cast<const u32x4v*>(row + ((chunk(k, half) ^ x16) << 4));
+    for (int u = 0; u < 8; ++u) {   // dims 4 u .. + 3 of each group's 32
+      float cs[4], sn[4];
+      if (!rotate) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        top2 = __builtin_elementwise_max(top2, __builtin_bit_cast(u16x2, x[k][e] & 0x7FFF7FFFu));
+        for (int e = 0; e < 4; ++e) {
+          cs[e] = 1.f;
+          sn[e] = 0.f;
+        }
+      } else {
+        const int i0 = (HD == 128 ? 32 * half : 0) + 4 * u;
+        if (quad) {
+          float c, n;
+          rope_cos_sin_rev(pos, inv_rev[i0 + (r32 & 3)], &c, &n);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            cs[e] = quad_bcast(c, e);
+            sn[e] = quad_bcast(n, e);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) rope_cos_sin_rev(pos, inv_rev[i0 + e], &cs[e], &sn[e]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = u >> 1, w = 2 * (u & 1) + (e >> 1);   // chunk and word of the dim
+        const float q = qscale;
+        if constexpr (HD == 128) {
+          const uint32_t xw = x[c][w], yw = x[4 + c][w];
+          const float a = __uint_as_float(e & 1 ? xw & 0xFFFF0000u : xw << 16);
+          const float b = __uint_as_float(e & 1 ? yw & 0xFFFF0000u : yw << 16);
+          v[4 * u + e] = (a * cs[e] - b * sn[e]) * q;
+          v[32 + 4 * u + e] = (b * cs[e] + a * sn[e]) * q;
+        } else {
+          const auto sw = __builtin_amdgcn_permlane32_swap(x[c][w], x[c][w], false, false);
+          const float a = __uint_as_float(e & 1 ? sw[0] & 0xFFFF0000u : sw[0] << 16);
+          const float b = __uint_as_float(e & 1 ? sw[1] & 0xFFFF0000u : sw[1] << 16);
+          v[4 * u + e] = (half ? b * cs[e] + a * sn[e] : a * cs[e] - b * sn[e]) * q;
+        }
+      }
     }
-    uint32_t top = max(top2[0], top2[1]);
+    uint32_t top = 0;
+#pragma unroll
+    for (int d = 0; d < 8 * KK; ++d) top = max(top, __float_as_uint(v[d]) & 0x7FFFFFFFu);
     const auto sw = __builtin_amdgcn_permlane32_swap(top, top, false, false);
     top = max(static_cast<uint32_t>(sw[0]), static_cast<uint32_t>(sw[1]));
     // (byte 1: four less; a row with an infinity or a NaN gives NaN under any scale)
-    const int b = max(5, scale_byte_e4m3(min(top, 0x7F7Fu)));
+    const int b = max(5, scale_byte_e4m3(min(top, 0x7F7FFFFFu)));
     q_scale = b | ((b - 4) << 8);
     const float f = __uint_as_float(static_cast<uint32_t>(254 - b) << 23), f16 = 16.f * f;
     const float back = __uint_as_float(static_cast<uint32_t>(b) << 23);
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int k = 0; k < KK; ++k)
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {   // four dims
-        const float v0 = __uint_as_float(x[k][2 * w] << 16), v1 = __uint_as_float(x[k][2 * w] & 0xFFFF0000u);
-        const float v2 = __uint_as_float(x[k][2 * w + 1] << 16), v3 = __uint_as_float(x[k][2 * w + 1] & 0xFFFF0000u);
-        int hi = __builtin_amdgcn_cvt_pk_fp8_f32(v0 * f, v1 * f, 0, false);
-        hi = __builtin_amdgcn_cvt_pk_fp8_f32(v2 * f, v3 * f, hi, true);
-        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, back, false);
-        const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, back, true);
-        int lo = __builtin_amdgcn_cvt_pk_fp8_f32((v0 - a[0]) * f16, (v1 - a[1]) * f16, 0, false);
-        lo = __builtin_amdgcn_cvt_pk_fp8_f32((v2 - c[0]) * f16, (v3 - c[1]) * f16, lo, true);
-        qh[k >> 2][2 * (k & 3) + w] = live ? hi : 0;
-        ql[k >> 2][2 * (k & 3) + w] = live ? lo : 0;
-      }
+    for (int w = 0; w < 2 * KK; ++w) {   // four dims
+      const float *y = v + 4 * w;
+      int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * f, y[1] * f, 0, false);
+      hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * f, y[3] * f, hi, true);
+      const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, back, false);
+      const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, back, true);
+      int lo = __builtin_amdgcn_cvt_pk_fp8_f32((y[0] - a[0]) * f16, (y[1] - a[1]) * f16, 0, false);
+      lo = __builtin_amdgcn_cvt_pk_fp8_f32((y[2] - c[0]) * f16, (y[3] - c[1]) * f16, lo, true);
+      qh[w >> 3][w & 7] = live ? hi : 0;
+      ql[w >> 3][w & 7] = live ? lo : 0;
+    }
   }
 
   // Eight codes as a bf16 operand, times the power of two `scale`.
@@ -2559,11 +2595,19 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
                                              __builtin_amdgcn_rcpf(static_cast<float>(t))))
                    : 0;
     };
-    const int lo = max(t_min, (T1 + budget - 1) / budget);
-    const int hi = max(lo, budget > ne ? min(mx, (T1 + budget - ne - 1) / (budget - ne)) : mx);
+    int lo = max(t_min, (T1 + budget - 1) / budget);
+    int hi = max(lo, budget > ne ? min(mx, (T1 + budget - ne - 1) / (budget - ne)) : mx);
+    if constexpr (KV8) {   // (the sum over the lanes' sequences falls with t: bisect)
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (wave_sum(cut(n_l, mid)) <= budget) hi = mid;
+        else lo = mid + 1;
+      }
+    }
     const int step = (hi - lo + 62) / 63, t = lo + lane * step;
     int sum = 0;
-    for (int s = 0; s < S; ++s) sum += cut(__builtin_amdgcn_readlane(n_l, s), t);
+    if constexpr (KV8) sum = wave_sum(cut(n_l, t));
+    else for (int s = 0; s < S; ++s) sum += cut(__builtin_amdgcn_readlane(n_l, s), t);
     const uint64_t fits = __ballot(sum <= budget);
     if (fits) {
       const int best = lo + (__ffsll(static_cast<long long>(fits)) - 1) * step;
@@ -2715,6 +2759,58 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     }
   };
 
+  // This wavefront's 32 rows (row0 on) of a finished piece from its registers: 16 bytes of
+  // a record row or 8 of an output row per store.
+  auto emit_own = [&](TT& T, bool whole, int seg, int s, float* rec, int row0) {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    const int qn = row0 + (l & 31), h = l >> 5;
+    const float den = T.l_run[0] + __shfl_xor(T.l_run[0], 32);
+    float den_u = 0.f, den_s = 0.f;
+    if constexpr (EXT) {
+      den_u = T.lu_run[0] + __shfl_xor(T.lu_run[0], 32);
+      den_s = T.ls_run[0] + __shfl_xor(T.ls_run[0], 32);
+    }
+    if (qn >= nq) return;
+    if (whole) {
+      const float inv = den > 0.f ? 1.f / den : 0.f;
+      const int64_t row = out_row(a, seg / a.Hkv, s, seg % a.Hkv, qn, G);
+      uint16_t* o = static_cast<uint16_t*>(a.out) + row * HD + 4 * h;
+#pragma unroll
+      for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          u16x4 v;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[c] = f2bf(T.o[0][m][4 * r4 + c] * inv);
+          *reinterpret_cast<u16x4*>(o + 32 * m + 8 * r4) = v;
+        }
+      if (h == 0 && a.lse) a.lse[row] = den > 0.f ? (T.m_run[0] + log2f(den)) * kLn2 : -INFINITY;
+      if constexpr (EXT) {   // share of the attention over [C;U] on U
+        const float lcu = den - den_s;
+        if (h == 0 && a.mass) a.mass[row] = lcu > 0.f ? den_u / lcu : 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          f32x4 v;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[c] = T.o[0][m][4 * r4 + c];
+          *reinterpret_cast<f32x4*>(rec + qn * HD + 32 * m + 8 * r4 + 4 * h) = v;
+        }
+      if (h == 0) {
+        rec[rec_rows * HD + qn] = T.m_run[0];
+        rec[rec_rows * HD + rec_rows + qn] = den;
+        if constexpr (EXT) {
+          rec[rec_rows * HD + 2 * rec_rows + qn] = den_u;
+          rec[rec_rows * HD + 3 * rec_rows + qn] = den_s;
+        }
+      }
+    }
+  };
+
   // ---- this stream's slice [t0, t1) of the global tile order: one part of one
   // segment (none past the last), or an even share, walked piece by piece
   int t0 = 0, t1 = 0;
@@ -2725,12 +2821,15 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
       const int n_s = __builtin_amdgcn_readlane(n_l, ps), k_s = __builtin_amdgcn_readlane(k_l, ps);
       const int part = min(rem - __builtin_amdgcn_readlane(kpre_l, ps), k_s);   // k_s: a place left free
       const int first = pseg * T1 + __builtin_amdgcn_readlane(pre_l, ps);
-      t0 = first + static_cast<int>(static_cast<int64_t>(n_s) * part / k_s);
-      t1 = part < k_s ? first + static_cast<int>(static_cast<int64_t>(n_s) * (part + 1) / k_s) : t0;
+      // floor(n_s * part / k_s), in 32 bits
+      const unsigned q = static_cast<unsigned>(n_s) / k_s, r = n_s - q * k_s;
+      t0 = first + static_cast<int>(q * part + r * part / k_s);
+      t1 = part < k_s ? first + static_cast<int>(q * (part + 1) + r * (part + 1) / k_s) : t0;
     }
   } else if (w < n_slices) {
-    t0 = static_cast<int>(t_all * w / n_slices);
-    t1 = static_cast<int>(t_all * (w + 1) / n_slices);
+    const unsigned q = static_cast<unsigned>(t_all) / n_slices, r = static_cast<unsigned>(t_all) - q * n_slices;
+    t0 = static_cast<int>(q * w + r * w / n_slices);
+    t1 = static_cast<int>(q * (w + 1) + r * (w + 1) / n_slices);
   }
   t0 = __builtin_amdgcn_readfirstlane(t0);
   t1 = __builtin_amdgcn_readfirstlane(t1);
@@ -2813,7 +2912,6 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     // last one again past the end); a rejected id reads page 0 with its keys
     // masked.  8 bits: and their scale bytes.
     int id[TP] = {}, c0 = -(1 << 30), bad = 0;   // no window fetched yet
-    uint32_t ks_l = 0, vs_l = 0;
     auto fetch_ids = [&](int c) {
       c0 = c;
       const int jt = c + lane, p = TP * jt;
@@ -2831,17 +2929,26 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
           }
         if (bad) set_status(a.status, CO_ERR_PAGE_RANGE);
       }
-      if constexpr (KV8) {
-        ks_l = vs_l = 0;
-        if (jt < nct) {
-          const int64_t sc0 = static_cast<int64_t>(layer) * a.num_pages * a.Hkv + g;
+    };
+    // Their scale bytes, four to a word.  Loaded behind the loads of the window's first
+    // tile, so that they arrive with it, and packed where they are needed.
+    uint32_t ks_l = 0, vs_l = 0;
+    uint8_t ks_r[KV8 ? TP : 1], vs_r[KV8 ? TP : 1];
+    auto load_scales = [&]() {
+      const int64_t sc0 = static_cast<int64_t>(layer) * a.num_pages * a.Hkv + g;
 #pragma unroll
-          for (int i = 0; i < TP; ++i) {
-            const int64_t at = sc0 + static_cast<int64_t>(id[i]) * a.Hkv;
-            ks_l |= static_cast<uint32_t>(a.k_scale[at]) << (8 * i);
-            vs_l |= static_cast<uint32_t>(a.v_scale[at]) << (8 * i);
-          }
-        }
+      for (int i = 0; i < TP; ++i) {
+        const int64_t at = sc0 + static_cast<int64_t>(id[i]) * a.Hkv;   // (id 0 past the end)
+        ks_r[i] = a.k_scale[at];
+        vs_r[i] = a.v_scale[at];
+      }
+    };
+    auto pack_scales = [&]() {
+      ks_l = vs_l = 0;
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        ks_l |= static_cast<uint32_t>(ks_r[i]) << (8 * i);
+        vs_l |= static_cast<uint32_t>(vs_r[i]) << (8 * i);
       }
     };
     // The block's own rows are the segment's last tile (drafter_block_attention_ext):
@@ -2867,34 +2974,78 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
         own_issue(0);
         return;
       }
+      bool fresh = false;
       if (j < nct) {   // j uniform
-        if (j >= c0 + 64 || j < c0) fetch_ids(j);
+        if (j >= c0 + 64 || j < c0) {
+          fetch_ids(j);
+          fresh = true;
+        }
 #pragma unroll
         for (int i = 0; i < TP; ++i) p[i] = __builtin_amdgcn_readlane(id[i], j - c0);
         rejected = __builtin_amdgcn_readlane(bad, j - c0);
-        if constexpr (KV8) {
+      }
+      issue(j, p);
+      if constexpr (KV8) {
+        if (fresh) {
+          load_scales();
+          pack_scales();
+        }
+        if (j < nct) {
           ks = __builtin_amdgcn_readlane(ks_l, j - c0);
           vs = __builtin_amdgcn_readlane(vs_l, j - c0);
         }
       }
-      issue(j, p);
     };
 
+    int b[NS] = {};   // rejected pages of the tiles in the ring, b[0] the current one's
+    uint32_t ksb[NS] = {}, vsb[NS] = {};   // and their scale bytes
+    const int row0 = 32 * qw;
+    static_assert(NS == 2, "one tile ahead");
+    // opaque copy: lane arithmetic of the piece's ends would otherwise be kept
+    // in registers over the whole walk
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    // With G a multiple of 4 the four lanes of a quad hold rows of one position
+    // and the same dims.
+    const bool quad = (G & 3) == 0;
+    if constexpr (KV8) {
+      // The queries come straight into registers, beside the page ids; the first tile
+      // and its scale bytes travel while they are rotated.
+      const int qn = min(row0 + (ln & 31), nq - 1), qi = qn / G;
+      const uint16_t* src = Q + (out_row(a, layer_local, s, g, 0, G) +
+                                 static_cast<int64_t>(qi) * a.Hq + (qn - qi * G)) * HD;
+      typename TT::u32x4v x[KK];
+#pragma unroll
+      for (int k = 0; k < KK; ++k)
+        x[k] = *reinterpret_cast<const typename TT::u32x4v*>(src + TT::chunk(k, ln >> 5) * 8);
+      const bool codes = j0 < nct;
+      if (codes) {
+        fetch_ids(j0);
+        b[0] = __builtin_amdgcn_readlane(bad, 0);
+        int p[TP];
+#pragma unroll
+        for (int i = 0; i < TP; ++i) p[i] = __builtin_amdgcn_readlane(id[i], 0);
+        issue(j0, p);
+        load_scales();
+      } else {
+        issue_tile(j0, b[0], ksb[0], vsb[0]);
+      }
+      T.setup(lane);
+      T.set_query(x, ctx + qi, rotate_q, quad, inv_lds, qscale, row0 + (ln & 31) < nq);
+      if (codes) {
+        pack_scales();
+        ksb[0] = __builtin_amdgcn_readlane(ks_l, 0);
+        vsb[0] = __builtin_amdgcn_readlane(vs_l, 0);
+      }
+    } else {
     // This wavefront's 32 query rows land raw in the part of the ring's last slot
     // that its own loads of a later tile will take, with the first tiles' loads
     // behind them; they are rotated there at ctx + i and scaled (rows' chunks
     // XOR-permuted as key rows are), then read into the B fragments.  Rows past
     // nq repeat the last one; nothing of them is stored.
-    int b[NS] = {};   // rejected pages of the tiles in the ring, b[0] the current one's
-    uint32_t ksb[NS] = {}, vsb[NS] = {};   // and their scale bytes
     if (j0 < nct) fetch_ids(j0);
     constexpr int ROWB = HD * 2, CPR = ROWB / 16, CPP = CPR / 2, QL = 32 * ROWB / 1024;
-    const int row0 = 32 * qw;
     unsigned char* qs = my_ring + ((j0 + NS - 1) % NS) * TILE_BYTES + qw * (TILE_BYTES / QW);
-    // opaque copy: lane arithmetic of the piece's ends would otherwise be kept
-    // in registers over the whole walk
-    int ln = lane;
-    asm volatile("" : "+v"(ln));
     {
       const int64_t qrow0 = out_row(a, layer_local, s, g, 0, G) * HD;
 #pragma unroll
@@ -2905,15 +3056,10 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
         lds_dma16_opaque(Q + qrow0 + off, lds_addr(qs) + q * 1024);
       }
     }
-#pragma unroll
-    for (int i = 0; i < NS - 1; ++i)
-      if (j0 + i < j1) issue_tile(j0 + i, b[i], ksb[i], vsb[i]);
-    static_assert(NS == 2, "one tile ahead");
+    issue_tile(j0, b[0], ksb[0], vsb[0]);
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(TL) : "memory");   // the queries are in
-    // With G a multiple of 4 the four lanes of a quad hold rows of one position
-    // and the same dims: each computes two of a chunk's eight rotation angles and
-    // takes the rest from its neighbours.
-    const bool quad = (G & 3) == 0;
+    // (of a quad's rows each lane computes two of a chunk's eight rotation angles
+    // and takes the rest from its neighbours)
     constexpr int RJ = 64 / CPP;                           // rows of a job
     const int jobs = (min(nq - row0, 32) + RJ - 1) / RJ;   // none for rows of padding only
 #pragma unroll 1
@@ -2956,14 +3102,12 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
       *reinterpret_cast<u32x4v*>(hi_p) = yp;
     }
     T.setup(lane);
-    if constexpr (KV8)
-      T.set_query(qs + (ln & 31) * ROWB, swz_key_page<HD>(ln & 15), (ln & 31) < jobs * RJ);
-    else
 #pragma unroll
     for (int k = 0; k < KK; ++k)
       T.qf[0][k] = (ln & 31) >= jobs * RJ ? u16x8{} : *reinterpret_cast<const u16x8*>(
           qs + (ln & 31) * ROWB + ((TT::chunk(k, ln >> 5) ^ swz_key_page<HD>(ln & 15)) << 4));
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the second tile lands there
+    }
 
     // A lone wavefront refills tile j - 1's slot, then waits for tile j; two
     // wait for their halves of tile j first: the barrier publishes it and tells
@@ -3026,6 +3170,13 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
       }
     }
 
+    // A whole segment is normalised and written, a part leaves a record (each
+    // wavefront its own rows), or stays in LDS for the merge below.
+    const bool whole = j0 == 0 && j1 == te - ts;
+    if (KV8 && !(NST > 1 && parts && !whole)) {
+      // straight from registers: no other stream's partial is merged here
+      emit_own(T, whole, seg, s, slot_ptr(a, hdr_floats, w + static_cast<int64_t>(seg) * S + s, rec_rows), row0);
+    } else {
     // ---- the piece into the stream's drained ring (rows of HD floats, 16-byte
     // chunks XOR-permuted by the row)
     float* my_sums = sums + stream * NSUM * NQP;
@@ -3058,15 +3209,13 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wavefront's own writes
-    // A whole segment is normalised and written, a part leaves a record (each
-    // wavefront its own rows), or stays there for the merge below.
-    const bool whole = j0 == 0 && j1 == te - ts;
     if (NST > 1 && parts && !whole) {
       held = seg * S + s;
     } else {
       emit_rows(ln, 64, row0, min(nq, row0 + 32), whole, seg, s,
                 slot_ptr(a, hdr_floats, w + static_cast<int64_t>(seg) * S + s, rec_rows), stream, stream + 1);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the ring refills
+    }
     }
     stream_barrier();
     t = pe;

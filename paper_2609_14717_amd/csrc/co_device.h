@@ -138,10 +138,22 @@ __device__ __forceinline__ uint32_t finite_max_bf16(uint32_t m, uint32_t pair) {
   return max(m, hi < 0x7F80u ? hi : 0u);
 }
 
-// Scale byte of e4m3 codes whose largest entry is `top` (bf16 bits): the smallest
+// Scale byte of e4m3 codes whose largest entry is `top` (fp32 bits): the smallest
 // k >= -126 with 1.mmm * 2^e <= 1.75 * 2^(8 + k), plus 127.
 __device__ __forceinline__ int scale_byte_e4m3(uint32_t top) {
-  return max(1, static_cast<int>(top >> 7) - 8 + ((top & 0x7Fu) > 0x60u ? 1 : 0));
+  return max(1, static_cast<int>(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0));
+}
+
+// Sum over the wavefront, in every lane, without LDS permutes.
+__device__ __forceinline__ int wave_sum(int v) {
+  v += __builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, false);   // rotations within 16 lanes: by 8, 4, 2, 1
+  v += __builtin_amdgcn_mov_dpp(v, 0x124, 0xF, 0xF, false);
+  v += __builtin_amdgcn_mov_dpp(v, 0x122, 0xF, 0xF, false);
+  v += __builtin_amdgcn_mov_dpp(v, 0x121, 0xF, 0xF, false);
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = static_cast<int>(a[0]) + static_cast<int>(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return static_cast<int>(b[0]) + static_cast<int>(b[1]);
 }
 
 // Max over the four 16-lane rows holding the same column (lanes l, l^16, l^32, l^48),

@@ -72,7 +72,7 @@ __device__ void store_keys(const uint16_t* rows, int64_t row_stride, int t0, int
   for (int i = 0; i < NI; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) top = finite_max_bf16(top, x[i][e]);
-  const int b = max(before, scale_byte_e4m3(wave_max(top)));
+  const int b = max(before, scale_byte_e4m3(wave_max(top) << 16));
   const float f = unscale(b);
   const bool finer = t0 > 0 && b > before;
   const float g = finer ? __uint_as_float(static_cast<uint32_t>(max(0, 127 + before - b)) << 23) : 0.f;
@@ -120,7 +120,7 @@ __device__ void store_values(const uint16_t* rows, int64_t row_stride, int t0, i
   for (int d = 0; d < ND; ++d) old[d] = t0 > 0 ? to[d] : u32x4{0, 0, 0, 0};
 #pragma unroll
   for (int t = 0; t < kPage; ++t) top = finite_max_bf16(top, x[t]);
-  const int b = max(before, scale_byte_e4m3(wave_max(top)));
+  const int b = max(before, scale_byte_e4m3(wave_max(top) << 16));
   const float f = unscale(b);
   const bool finer = t0 > 0 && b > before;
   const float g = finer ? __uint_as_float(static_cast<uint32_t>(max(0, 127 + before - b)) << 23) : 0.f;

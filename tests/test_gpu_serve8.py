@@ -3,9 +3,9 @@ cache, attention over it, and the round of all of them) with the fp64 oracle.
 
 Whole numbers, codes and scale bytes are equal to the oracle's.  Attention is held to
 the rule of the other bf16 paths, 2e-2 of a head vector's largest entry and 2e-2 of a
-log-sum-exp or share: the queries are rounded to bf16 after their rotation (half a
-step, 2^-9 of the value: a logit of a few units moves by a few 2^-9) and the softmax
-weights and the output once each (2^-9 of their size); the codes are exact in bf16.
+log-sum-exp or share: the queries are rounded to two codes after their rotation (2^-9 of
+the value: a logit of a few units moves by a few 2^-9) and the softmax weights and the
+output to bf16 once each (half a step, 2^-8 of their size); the codes are exact in bf16.
 """
 import math
 import random
@@ -368,8 +368,8 @@ class Serve:
 
     def check(self, got, l0=0, seqs=None, hidden=(), rotated=False, rounded=False):
         """Against the oracle, every sequence or some; ``hidden``: (s, page) left out;
-        ``rounded``: the oracle takes the queries as the kernels hold them, in bf16
-        after rotation and scaling (see the test that asks for it)."""
+        ``rounded``: the oracle takes the queries as the kernels hold them, two codes
+        per dim after rotation and scaling (see the test that asks for it)."""
         out, z, m = (None if t is None else t.double().cpu().numpy() for t in got)
         orc, G = serve8.Cache8.read(self.cache), self.Hq // self.Hkv
         kc, vc = (self.st[k].double().cpu().numpy() for k in ("k_carry", "v_carry"))
@@ -401,8 +401,7 @@ class Serve:
                     qp = np.repeat(0 * pos if rotated else pos, G)
                     if rounded:
                         c = math.log2(math.e) / math.sqrt(self.hd)
-                        x = torch.tensor(oracle.rope(qs, qp, self.theta) * c).float().bfloat16()
-                        qs, qp = x.double().numpy() / c, 0 * qp
+                        qs, qp = two_codes(oracle.rope(qs, qp, self.theta) * c) / c, 0 * qp
                     o, lse = oracle.attend(qs, qp, ks, vs, self.theta)
                     go = out[i, s, :, h * G:(h + 1) * G].reshape(self.B * G, self.hd)
                     assert np.all(np.isfinite(go)), (s, layer, h)
@@ -420,6 +419,17 @@ class Serve:
         assert worst <= TOL, worst
         assert int(self.st["status"]) == (co.CO_ERR_PAGE_RANGE if hidden else 0)
         return worst
+
+
+def two_codes(rows):
+    """Rows as the sum of two e4m3 codes per entry: one under the row's scale, one for the
+    rest under a sixteenth of it."""
+    out = np.empty_like(rows)
+    for i, x in enumerate(rows):
+        unit = 2.0 ** (max(5, serve8.scale_byte(x)) - 127)
+        hi = serve8.VALUES[serve8.e4m3_code(x / unit)]
+        out[i] = (hi + serve8.VALUES[serve8.e4m3_code((x / unit - hi) * 16)] / 16) * unit
+    return out
 
 
 def spread(lo, hi, n, seed):
@@ -490,13 +500,13 @@ def test_attention_takes_rotated_queries():
 def test_attention_of_flat_and_peaked_softmaxes(hd, B, G, size):
     """Queries of nothing (all weights equal), and logits far from each other, which
     move the reference at every tile; keys small on some pages and large on others.
-    The rounding of the queries moves a logit by up to 2^-8 sum |q_d k_d| / sqrt(hd): at
-    queries of 6 that sum is near 128 * (6 * 0.8) * 0.6 / 11 = 33, a tenth of a unit of
-    the logit and so of a weight.  The oracle therefore takes the rounded queries,
-    which leaves the rounding of the weights and the output to the rule.  At queries
-    of 60 a query that rounds the other way (a tie, to the sine's last bit: one
-    step, 2^-7 of 200 or so, times a key of 3) would move a logit by half a unit:
-    only finite results are asked for."""
+    The rounding of the queries (the second code's half step: 2^-9 of an entry) moves a
+    logit by up to 2^-9 sum |q_d k_d| / sqrt(hd): at queries of 6 that sum is near
+    128 * (6 * 0.8) * 0.6 / 11 = 33, so 0.06 of the logit and of a weight.  The oracle
+    therefore takes the rounded queries, which leaves the rounding of the weights and
+    the output to the rule.  At queries of 60 a query that rounds the other way (a
+    tie, to the sine's last bit: one step, 2^-8 of 200 or so, times a key of 3) would
+    move a logit by a fifth of a unit: only finite results are asked for."""
     sv = Serve(2, B, 1, G, 1, hd, [700, 90], [B, 0], seed=8, size=size)
     got = sv.run()
     if size < 60:
