@@ -1853,7 +1853,7 @@ struct Tile32 {
       if (!rotate) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          cs[e] = 1.f;
+          cs[e] = qscale;
           sn[e] = 0.f;
         }
       } else {
@@ -1861,6 +1861,8 @@ struct Tile32 {
         if (quad) {
           float c, n;
           rope_cos_sin_rev(pos, inv_rev[i0 + (r32 & 3)], &c, &n);
+          c *= qscale;
+          n *= qscale;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             cs[e] = quad_bcast(c, e);
@@ -1868,48 +1870,55 @@ struct Tile32 {
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) rope_cos_sin_rev(pos, inv_rev[i0 + e], &cs[e], &sn[e]);
+          for (int e = 0; e < 4; ++e) {
+            rope_cos_sin_rev(pos, inv_rev[i0 + e], &cs[e], &sn[e]);
+            cs[e] *= qscale;
+            sn[e] *= qscale;
+          }
         }
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int c = u >> 1, w = 2 * (u & 1) + (e >> 1);   // chunk and word of the dim
-        const float q = qscale;
         if constexpr (HD == 128) {
           const uint32_t xw = x[c][w], yw = x[4 + c][w];
           const float a = __uint_as_float(e & 1 ? xw & 0xFFFF0000u : xw << 16);
           const float b = __uint_as_float(e & 1 ? yw & 0xFFFF0000u : yw << 16);
-          v[4 * u + e] = (a * cs[e] - b * sn[e]) * q;
-          v[32 + 4 * u + e] = (b * cs[e] + a * sn[e]) * q;
+          v[4 * u + e] = a * cs[e] - b * sn[e];
+          v[32 + 4 * u + e] = b * cs[e] + a * sn[e];
         } else {
           const auto sw = __builtin_amdgcn_permlane32_swap(x[c][w], x[c][w], false, false);
           const float a = __uint_as_float(e & 1 ? sw[0] & 0xFFFF0000u : sw[0] << 16);
           const float b = __uint_as_float(e & 1 ? sw[1] & 0xFFFF0000u : sw[1] << 16);
-          v[4 * u + e] = (half ? b * cs[e] + a * sn[e] : a * cs[e] - b * sn[e]) * q;
+          v[4 * u + e] = half ? b * cs[e] + a * sn[e] : a * cs[e] - b * sn[e];
         }
       }
     }
-    uint32_t top = 0;
+    float big = 0.f;
 #pragma unroll
-    for (int d = 0; d < 8 * KK; ++d) top = max(top, __float_as_uint(v[d]) & 0x7FFFFFFFu);
+    for (int d = 0; d < 8 * KK; ++d) big = fmaxf(big, fabsf(v[d]));
+    uint32_t top = __float_as_uint(big);
     const auto sw = __builtin_amdgcn_permlane32_swap(top, top, false, false);
     top = max(static_cast<uint32_t>(sw[0]), static_cast<uint32_t>(sw[1]));
     // (byte 1: four less; a row with an infinity or a NaN gives NaN under any scale)
     const int b = max(5, scale_byte_e4m3(min(top, 0x7F7FFFFFu)));
     q_scale = b | ((b - 4) << 8);
-    const float f = __uint_as_float(static_cast<uint32_t>(254 - b) << 23), f16 = 16.f * f;
-    const float back = __uint_as_float(static_cast<uint32_t>(b) << 23);
+    const float f = __uint_as_float(static_cast<uint32_t>(b) << 23);
+    const float f16 = __uint_as_float(static_cast<uint32_t>(b - 4) << 23);
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int w = 0; w < 2 * KK; ++w) {   // four dims
+    for (int w = 0; w < 2 * KK; ++w) {   // four dims (the conversions divide and multiply by the scale)
       const float *y = v + 4 * w;
-      int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * f, y[1] * f, 0, false);
-      hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * f, y[3] * f, hi, true);
-      const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, back, false);
-      const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, back, true);
-      int lo = __builtin_amdgcn_cvt_pk_fp8_f32((y[0] - a[0]) * f16, (y[1] - a[1]) * f16, 0, false);
-      lo = __builtin_amdgcn_cvt_pk_fp8_f32((y[2] - c[0]) * f16, (y[3] - c[1]) * f16, lo, true);
+      s16x2 h2 = {0, 0}, l2 = {0, 0};
+      h2 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(h2, y[0], y[1], f, false);
+      h2 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(h2, y[2], y[3], f, true);
+      const int hi = __builtin_bit_cast(int, h2);
+      const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, f, false);
+      const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, f, true);
+      l2 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l2, y[0] - a[0], y[1] - a[1], f16, false);
+      l2 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l2, y[2] - c[0], y[3] - c[1], f16, true);
       qh[w >> 3][w & 7] = live ? hi : 0;
-      ql[w >> 3][w & 7] = live ? lo : 0;
+      ql[w >> 3][w & 7] = live ? __builtin_bit_cast(int, l2) : 0;
     }
   }
 
@@ -2519,7 +2528,12 @@ __device__ __forceinline__ int wave_min_tiles(int hd, int nqt, bool own, int mos
   if (nqt == 1) return hd == 128 ? (most < 384 ? 1 : 2) : 4;
   return most <= 6 && !own ? 3 : 4;
 }
-constexpr int kSliceTiles = 4;   // tiles per slice of the even split below which fewer are cut
+// The same for tiles of 64 codes.
+__device__ __forceinline__ int wave_min_tiles8(int nqt, bool own, int most) {
+  return nqt == 1 ? (most < 192 ? 1 : 2) : 2;
+}
+constexpr int kSliceTiles = 4;    // tiles per slice of the even split below which fewer are cut
+constexpr int kSliceTiles8 = 2;   // of 64 codes
 
 // Header of the workspace (ints): tiles before each sequence [S+1], parts
 // before each sequence [S+1], total tiles, 1 for parts / 0 for the even split.
@@ -2561,15 +2575,6 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     const int n = (ctx + TP * kPage - 1) / (TP * kPage) + ((carry + kPage - 1) / kPage + 1) / 2;
     return n + (EXT && a.k_self && si.ok ? 1 : 0);   // the block's own rows: the last tile
   };
-  auto scan64 = [&](int v) {   // inclusive sum over the lanes
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int u = __shfl_up(v, off);
-      if (lane >= off) v += u;
-    }
-    return v;
-  };
-
   // ---- the split (the same in every wavefront, in registers): lane l holds
   // sequences l * per .. + per - 1, a single one (n_l tiles) where per is 1
   const int per = (S + 63) / 64;
@@ -2578,16 +2583,14 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     const int s = lane * per + i;
     if (s < S) n_l += seq_tiles(s, ctx_v, carry_v);
   }
-  const int inc_l = scan64(n_l), pre_l = inc_l - n_l;
+  const int inc_l = wave_scan(n_l), pre_l = inc_l - n_l;
   const int T1 = __builtin_amdgcn_readlane(inc_l, 63);
   int k_l = 0, kpre_l = 0, K1 = 0;
   bool parts = false;
   const int ne = __popcll(__ballot(n_l > 0)), budget = n_places / n_segs;   // parts per segment row
   if (S <= kWavePartSeqs && ne > 0 && budget >= ne) {
-    int mx = n_l;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) mx = max(mx, __shfl_xor(mx, off));
-    const int t_min = wave_min_tiles(HD, NQT, EXT && a.k_self, mx);
+    const int mx = wave_max(n_l);
+    const int t_min = KV8 ? wave_min_tiles8(NQT, EXT && a.k_self, mx) : wave_min_tiles(HD, NQT, EXT && a.k_self, mx);
     // lane c tries t = lo + c * step; ceil by a reciprocal (any count of at
     // least one part is a valid cut; every wavefront gets the same)
     auto cut = [&](int n, int t) {
@@ -2616,10 +2619,10 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
         parts = true;
         k_l = cut(n_l, best);
         // whole workgroups to a segment where there are enough: the fewest share one
-        int places = (k_l + NST - 1) / NST * NST, kin = scan64(places);
+        int places = (k_l + NST - 1) / NST * NST, kin = wave_scan(places);
         if (__builtin_amdgcn_readlane(kin, 63) > budget) {
           places = k_l;
-          kin = scan64(k_l);
+          kin = wave_scan(k_l);
         }
         kpre_l = kin - places;
         K1 = __builtin_amdgcn_readlane(kin, 63);
@@ -2659,7 +2662,7 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     }
     int n = 0, c = 0, u = 0;   // lane L's sequences, one per lane (at most 32)
     if (lane < per && L * per + lane < S) n = seq_tiles(L * per + lane, c, u);
-    const int end = __builtin_amdgcn_readlane(pre_l, L) + scan64(n), beg = end - n;
+    const int end = __builtin_amdgcn_readlane(pre_l, L) + wave_scan(n), beg = end - n;
     const int i = 63 - __builtin_clzll(__ballot(n > 0 && beg <= local));
     s = L * per + i;
     ts = __builtin_amdgcn_readlane(beg, i);
@@ -3516,7 +3519,7 @@ AttnPlan plan_attention_kv8(int S, int B, int L, int Hq, int Hkv, int hd, int ma
   const bool forced = wg_override >= 1 && wg_override <= kMaxMergeSlices / kCuStreams;
   int n_sl = static_cast<int>(forced ? wg_override : cus) * kCuStreams;
   if (!forced) {
-    const int64_t by_tiles = (tiles / kSliceTiles + kCuStreams - 1) / kCuStreams * kCuStreams;
+    const int64_t by_tiles = (tiles / kSliceTiles8 + kCuStreams - 1) / kCuStreams * kCuStreams;
     n_sl = static_cast<int>(std::max<int64_t>(kCuStreams, std::min<int64_t>(n_sl, by_tiles)));
   }
   n_sl = (n_sl + wg_st - 1) / wg_st * wg_st;   // whole workgroups

@@ -156,6 +156,30 @@ __device__ __forceinline__ int wave_sum(int v) {
   return static_cast<int>(b[0]) + static_cast<int>(b[1]);
 }
 
+// Maximum over the wavefront, in every lane (values from 0 on).
+__device__ __forceinline__ int wave_max(int v) {
+  v = max(v, __builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_mov_dpp(v, 0x124, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_mov_dpp(v, 0x122, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_mov_dpp(v, 0x121, 0xF, 0xF, false));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(static_cast<int>(a[0]), static_cast<int>(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(static_cast<int>(b[0]), static_cast<int>(b[1]));
+}
+
+// Inclusive sums over the lanes, without LDS permutes: shifts by 1, 2, 4, 8 within 16
+// lanes, then each row's last lane into the rows behind it.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+
 // Max over the four 16-lane rows holding the same column (lanes l, l^16, l^32, l^48),
 // with the gfx950 row-swap permutes instead of LDS permutes.
 __device__ __forceinline__ float max_across_rows(float v) {
