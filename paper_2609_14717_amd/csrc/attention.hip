@@ -1434,15 +1434,19 @@ __global__ __launch_bounds__(256) void attn_bf16_combine_kernel(AttnArgs a, int 
   // (the persistent kernel records T after the slice starts); or, in parts mode
   // of the per-wavefront kernel (waves > 0), the segment's parts follow the
   // launch's wavefronts, `waves` of them to a workgroup and its record
+  // (the streams' words without a branch: one round trip for the whole header)
+  const int at = waves > 0 ? a.S + 1 : 0;
+  const int w_k0 = hdr[at + (waves > 0 ? s : 0)], w_k1 = hdr[at + (waves > 0 ? s + 1 : 0)];
+  const int w_K1 = hdr[waves > 0 ? 2 * a.S + 1 : 0], w_parts = hdr[waves > 0 ? 2 * a.S + 3 : 0];
+  const int T1 = hdr[a.S], ts = hdr[s], te = hdr[s + 1];
   const int64_t T = hdr[waves > 0 ? 2 * a.S + 2 : a.S + 1 + n_wg];
-  const bool parts = waves > 0 && hdr[2 * a.S + 3] != 0;
+  const bool parts = waves > 0 && w_parts != 0;
   auto bnd = [&](int w) { return static_cast<int>(T * w / n_wg); };
-  const SeqInfo si = seq_info(a, s, 1);
-  if (!si.ok && seg == 0 && tid == 0 && blockIdx.z == 0) set_status(a.status, CO_ERR_LENGTH);
-  const int T1 = hdr[a.S], ts = hdr[s];
-  const int nts = hdr[s + 1] - ts;
+  const int nts = te - ts;
   uint16_t* out = static_cast<uint16_t*>(a.out);
-  if (nts == 0) {                      // no keys: O = 0, LSE = -inf
+  if (nts == 0) {                      // no keys (or lengths out of range): O = 0, LSE = -inf
+    if (seg == 0 && tid == 0 && blockIdx.z == 0 && !seq_info(a, s, 1).ok)
+      set_status(a.status, CO_ERR_LENGTH);
     for (int idx = tid + blockIdx.z * 256; idx < nq * hd; idx += 256 * gridDim.z)
       out[out_row(a, layer_local, s, g, idx / hd, G) * hd + idx % hd] = 0;
     if (a.lse && blockIdx.z == 0)
@@ -1463,8 +1467,8 @@ __global__ __launch_bounds__(256) void attn_bf16_combine_kernel(AttnArgs a, int 
   // resident per CU)
   int w_lo, w_hi;
   if (parts) {
-    const int K1 = hdr[2 * a.S + 1], k0 = seg * K1 + hdr[a.S + 1 + s];
-    const int k1 = seg * K1 + (s + 1 < a.S ? hdr[a.S + 2 + s] : K1);
+    // (the word behind the last sequence's parts is their total)
+    const int k0 = seg * w_K1 + w_k0, k1 = seg * w_K1 + w_k1;
     w_lo = k0 / waves;
     w_hi = (k1 - 1) / waves;
   } else {
