@@ -2515,7 +2515,9 @@ constexpr int kWavePartSeqs = 64;   // sequences (one per lane) up to which segm
 
 // Wavefronts per stream and streams per workgroup, by query tiles of 32 rows.
 constexpr int stream_waves(int nqt) { return nqt; }
-constexpr int wg_streams(int hd, int nqt) { return nqt == 2 ? 1 : (hd == 128 ? 4 : 8); }
+constexpr int wg_streams(int hd, int nqt, bool kv8 = false) {
+  return nqt == 2 ? 1 : (hd == 128 || kv8 ? 4 : 8);
+}
 
 // Tiles per part below which fewer are cut, by the most tiles of a segment.  A walk
 // of a few tiles is a chain of latencies, so parts that a workgroup's streams merge
@@ -2544,12 +2546,12 @@ constexpr int kSliceTiles8 = 2;   // of 64 codes
 constexpr int wave_hdr_ints(int S) { return (2 * (S + 1) + 2 + 63) / 64 * 64; }
 
 template <int HD, int NQT, bool EXT, bool PLO, bool KV8 = false>
-__global__ __launch_bounds__(64 * stream_waves(NQT) * wg_streams(HD, NQT), 2)
+__global__ __launch_bounds__(64 * stream_waves(NQT) * wg_streams(HD, NQT, KV8), 2)
 __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     AttnArgs a, int layer_count, int n_places, int n_slices, int hdr_floats, int rec_rows) {
   using TT = Tile32<HD, 1, EXT, PLO, KV8>;
   constexpr int TP = KV8 ? 4 : 2;   // committed pages per tile
-  constexpr int QW = stream_waves(NQT), NST = wg_streams(HD, NQT);
+  constexpr int QW = stream_waves(NQT), NST = wg_streams(HD, NQT, KV8);
   constexpr int NQP = NQT * 32, NS = kWaveRing, NTHR = 64 * QW * NST;
   constexpr int PAGE_BYTES = TT::PAGE_BYTES, LPP = TT::LPP, TILE_BYTES = TT::TILE_BYTES;
   constexpr int KK = TT::KK, NSUM = EXT ? 4 : 2, CH = HD / 4;   // CH: 16-byte chunks per output row
@@ -3515,7 +3517,7 @@ AttnPlan plan_attention_kv8(int S, int B, int L, int Hq, int Hkv, int hd, int ma
   AttnPlan p{};
   const int nq = B * (Hq / Hkv), cp = (B + kPage - 1) / kPage;
   p.nq_pad = (nq + 15) / 16 * 16;
-  const int wg_st = wg_streams(hd, p.nq_pad <= 32 ? 1 : 2), cus = std::max(1, num_cus);
+  const int wg_st = wg_streams(hd, p.nq_pad <= 32 ? 1 : 2, true), cus = std::max(1, num_cus);
   const int64_t segs = static_cast<int64_t>(L) * Hkv * S;
   const int64_t tiles = segs * ((max_pages + 3) / 4 + (cp + 1) / 2);
   // slices of the even split and streams launched, as for the bf16 cache
@@ -3544,7 +3546,7 @@ hipError_t launch_attention_kv8(const AttnArgs& a, const AttnPlan& p, int layer_
                                 hipStream_t stream) {
   if (a.S == 0 || layer_count == 0) return hipSuccess;
   const bool ext = a.k_self != nullptr || a.mass != nullptr;
-  const int nqt = p.nq_pad <= 32 ? 1 : 2, nst = wg_streams(a.hd, nqt);
+  const int nqt = p.nq_pad <= 32 ? 1 : 2, nst = wg_streams(a.hd, nqt, true);
   const dim3 grid(p.n_places / nst), block(64 * stream_waves(nqt) * nst);
 #define CO_KV8_LAUNCH(HD, NQT)                                                                     \
   do {                                                                                             \
