@@ -1740,6 +1740,7 @@ struct Tile32 {
         for (int qt = 0; qt < NQT; ++qt) sc[qt] = mfma32x32x16(kf[k], qf[qt][k], sc[qt]);
     }
     if (partial) {
+      if constexpr (KV8) asm volatile("");   // (as in step8)
 #pragma unroll
       for (int m = 0; m < MO; ++m)
 #pragma unroll
@@ -1970,6 +1971,7 @@ struct Tile32 {
       sc[1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc[1][m], ql[m], sc[1], 0, 0, 2, ks, 1, q_scale);
     }
     if (partial) {
+      asm volatile("");   // a branch, not a hundred selects in every tile
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int nv = half ? n[2 * h + 1] : n[2 * h];
@@ -2039,6 +2041,7 @@ struct Tile32 {
     }
     const float vs = __uint_as_float((vb & 0xFFu) << 23);
     if (partial) {   // codes behind the last key may be NaN
+      asm volatile("");
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const int c = min(max(nv - 4 * w, 0), 4);
