@@ -2571,7 +2571,12 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int stream = wave / QW, qw = wave % QW;
   const int S = a.S, G = a.Hq / a.Hkv, nq = a.B * G;
-  const int w = blockIdx.x * NST + stream, n_segs = layer_count * a.Hkv;
+  // Consecutive workgroups run on the eight XCDs in turn; those of one segment are put
+  // on one, whose L2 then holds the queries that they share (8 bits: a second and a
+  // third copy of them weighs twice as much beside the codes).
+  int wg = blockIdx.x;
+  if (KV8 && (gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
+  const int w = wg * NST + stream, n_segs = layer_count * a.Hkv;
   int* hdr = reinterpret_cast<int*>(a.ws);
   if (tid < HD / 2) inv_lds[tid] = a.rope_inv[tid] * kInv2Pi;
 
@@ -3242,10 +3247,10 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     while (v1 < NST && run_l[v1] == sigma) ++v1;
     if (sigma >= 0) {
       const int rs = sigma % S, rseg = sigma / S;
-      const int p0 = blockIdx.x * NST + v0 - (rseg * K1 + __shfl(kpre_l, rs));
+      const int p0 = wg * NST + v0 - (rseg * K1 + __shfl(kpre_l, rs));
       const bool whole = p0 == 0 && v1 - v0 == __shfl(k_l, rs);   // every part is here
       emit_rows(tid, NTHR, 0, nq, whole, rseg, rs,
-                slot_ptr(a, hdr_floats, blockIdx.x + static_cast<int64_t>(sigma), rec_rows), v0, v1);
+                slot_ptr(a, hdr_floats, wg + static_cast<int64_t>(sigma), rec_rows), v0, v1);
     }
     v0 = v1;
   }
