@@ -788,6 +788,7 @@ co_status carryover_slot_map(const co_dims* dims, int32_t num_rows, const int32_
   a.max_pages = dims->max_pages_per_seq;
   a.num_pages = dims->num_pages;
   a.num_rows = num_rows;
+  a.wide = aligned(row_pos, 16) && aligned(row_dst, 16);
   a.row_start = row_start;
   a.pos0 = pos0;
   a.table = page_table;

@@ -224,14 +224,20 @@ struct PagesArgs {
 };
 
 constexpr int kAssignHdr = 4;             // released, taken, free + released
-constexpr int kAssignSeqs = 1024;         // one workgroup assigns up to so many sequences
-constexpr int kAssignPlaces = 65536;      // with so many table entries
+// One workgroup assigns up to so many sequences with so many table entries.  The host
+// cannot see how many pages move: where few do (a decoding step) one launch is better, a
+// step that ends and admits half of the requests takes it longer (us, graph replays,
+// one launch against two): 16K entries 3.9 / 5.6 where few move, 9.5 / 6.2 where half do;
+// 66K entries 5.5 / 5.8 and 23.7 / 6.4.
+constexpr int kAssignSeqs = 1024;
+constexpr int kAssignPlaces = 32768;
 
 size_t assign_ws_bytes(int S);
 
 // Positions and slots of packed rows (carryover_slot_map).
 struct SlotMapArgs {
   int S, max_pages, num_pages, num_rows;
+  bool wide;                  // row_pos and row_dst aligned for 16-byte stores
   const int32_t* row_start;   // [S + 1]
   const int32_t* pos0;        // [S]
   const int32_t* table;

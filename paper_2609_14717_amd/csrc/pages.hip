@@ -165,11 +165,18 @@ __global__ __launch_bounds__(kScanThreads) void assign_scan_kernel(PagesArgs a) 
   }
 }
 
+template <bool LDS>   // the sequences' first places, which released pages search, fit there
 __global__ __launch_bounds__(256) void assign_move_kernel(PagesArgs a) {
+  __shared__ int grow[LDS ? kAssignSeqs : 1];
   int* w = a.ws + kAssignHdr;
-  const Moves m{w, w + a.S, w + 2 * a.S, w + 3 * a.S, a.ws[0], a.ws[1], a.ws[2]};
+  Moves m{w, w + a.S, w + 2 * a.S, w + 3 * a.S, a.ws[0], a.ws[1], a.ws[2]};
   const int s = blockIdx.x, p = blockIdx.y * 256 + threadIdx.x;
   const int lo = m.lo[s];
+  if constexpr (LDS) {
+    for (int i = threadIdx.x; i < a.S; i += 256) grow[i] = m.grow[i];
+    m.grow = grow;
+    __syncthreads();
+  }
   if (p >= lo && p < m.hi[s]) move_page(a, m, s, p, lo, m.first[s]);
 }
 
@@ -194,31 +201,43 @@ __global__ __launch_bounds__(kSlotThreads) void slot_map_kernel(SlotMapArgs a) {
     if (start[mid] <= r0) s = mid;
     else end = mid;
   }
+  int32_t pos[kSlotRows], dst[kSlotRows];
 #pragma unroll
   for (int i = 0; i < kSlotRows; ++i) {
     const int64_t r = r0 + i;
-    if (r >= a.num_rows) return;
+    pos[i] = 0;
+    dst[i] = kSkip;
+    if (r >= a.num_rows) continue;
     while (s < a.S && start[s + 1] <= r) ++s;
-    int32_t pos = 0, dst = kSkip;
-    if (s >= 0 && s < a.S) {   // (rows before the first sequence and behind the last have no slot)
-      const int32_t p0 = a.pos0[s];
-      const int64_t p = p0 + (r - start[s]);
-      if (p0 < 0 || r < start[s]) {
-        set_status(a.status, CO_ERR_LENGTH);
-      } else if (p >= static_cast<int64_t>(a.max_pages) * kPage) {
-        set_status(a.status, CO_ERR_CAPACITY);
+    if (s < 0 || s >= a.S) continue;   // (rows before the first sequence and behind the last)
+    const int32_t p0 = a.pos0[s];
+    const int64_t p = p0 + (r - start[s]);
+    if (p0 < 0 || r < start[s]) {
+      set_status(a.status, CO_ERR_LENGTH);
+    } else if (p >= static_cast<int64_t>(a.max_pages) * kPage) {
+      set_status(a.status, CO_ERR_CAPACITY);
+    } else {
+      const int32_t id = a.table[static_cast<int64_t>(s) * a.max_pages + p / kPage];
+      if (id < 0 || id >= a.num_pages) {
+        set_status(a.status, CO_ERR_PAGE_RANGE);
       } else {
-        const int32_t id = a.table[static_cast<int64_t>(s) * a.max_pages + p / kPage];
-        if (id < 0 || id >= a.num_pages) {
-          set_status(a.status, CO_ERR_PAGE_RANGE);
-        } else {
-          pos = static_cast<int32_t>(p);
-          dst = id * kPage + pos % kPage;
-        }
+        pos[i] = static_cast<int32_t>(p);
+        dst[i] = id * kPage + pos[i] % kPage;
       }
     }
-    a.row_pos[r] = pos;
-    a.row_dst[r] = dst;
+  }
+  typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+  static_assert(kSlotRows == 4, "one store");
+  if (a.wide && r0 + kSlotRows <= a.num_rows) {
+    *reinterpret_cast<i32x4*>(a.row_pos + r0) = i32x4{pos[0], pos[1], pos[2], pos[3]};
+    *reinterpret_cast<i32x4*>(a.row_dst + r0) = i32x4{dst[0], dst[1], dst[2], dst[3]};
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kSlotRows; ++i) {
+    if (r0 + i >= a.num_rows) return;
+    a.row_pos[r0 + i] = pos[i];
+    a.row_dst[r0 + i] = dst[i];
   }
 }
 
@@ -237,7 +256,9 @@ hipError_t launch_assign_pages(const PagesArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL(assign_scan_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL(assign_move_kernel, dim3(a.S, (a.max_pages + 255) / 256), dim3(256), 0, stream, a);
+  const dim3 grid(a.S, (a.max_pages + 255) / 256);
+  if (a.S <= kAssignSeqs) hipLaunchKernelGGL(assign_move_kernel<true>, grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL(assign_move_kernel<false>, grid, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

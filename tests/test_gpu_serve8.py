@@ -27,7 +27,7 @@ DEV = "cuda"
 
 
 def ints(x):
-    return torch.tensor(np.asarray(x), dtype=torch.int32, device=DEV)
+    return torch.tensor(np.array(x), dtype=torch.int32, device=DEV)
 
 
 def zero():
@@ -73,7 +73,7 @@ class Pool:
         np.testing.assert_array_equal(np_(self.t["free_pages"])[:len(self.free)], self.free)
 
 
-# the last three in two launches: more than 65536 entries, or more than 1024 sequences
+# the last three in two launches: more than 32768 entries, or more than 1024 sequences
 @pytest.mark.parametrize("S,max_pages", [(1, 1), (1, 300), (2, 5), (7, 3), (33, 65), (1024, 4),
                                          (1025, 3), (130, 520), (1, 70000)])
 def test_pages_follow_lengths(S, max_pages):
@@ -151,6 +151,20 @@ def test_slot_map(S, lo, hi, extra):
     np.testing.assert_array_equal(np_(pos)[:rows], wp)
     np.testing.assert_array_equal(np_(dst)[:rows], wd)
     assert int(pos[rows]) == int(dst[rows]) == 77                     # nothing past the last row
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_slot_map_into_unaligned_arrays(off):
+    d, status, rows = dims(3, 9, 27), zero(), 300
+    start, pos0, table = [0, 120, 121, 300], [0, 5, 11], np.arange(26, -1, -1).reshape(3, 9)
+    pos, dst = torch.full((2, rows + 8), 77, dtype=torch.int32, device=DEV)
+    dst = torch.cat([dst, dst])[:rows + 8]
+    co.carryover_slot_map(d, rows, ints(start), ints(pos0), ints(table), pos[off:], dst[off:], status)
+    wp, wd, st = serve8.slot_map(rows, start, pos0, table, 9, 27)
+    assert int(status) == st
+    np.testing.assert_array_equal(np_(pos)[off:off + rows], wp)
+    np.testing.assert_array_equal(np_(dst)[off:off + rows], wd)
+    assert np.all(np_(pos)[:off] == 77) and np.all(np_(dst)[off + rows:] == 77)
 
 
 @pytest.mark.parametrize("pos0,page,code", [(-1, 0, co.CO_ERR_LENGTH), (30, 0, co.CO_ERR_CAPACITY),
