@@ -488,8 +488,8 @@ co_status carryover_import_kv(const co_dims* dims, int32_t seq, int32_t pos0, in
  * served in order, and from the first whose pages do not fit on, none gets any
  * (sequences that release or keep pages still do); with *free_count outside
  * [0, num_pages] nothing changes.  Calls on one pool must not overlap.
- * Host: num_seqs * max_pages_per_seq and num_pages * 16 below 2^31
- * (CO_ERR_UNSUPPORTED).
+ * Host: num_seqs * max_pages_per_seq and num_pages * 16 below 2^31, num_seqs and
+ * max_pages_per_seq below 2^23 (CO_ERR_UNSUPPORTED).
  */
 co_status carryover_assign_pages(const co_dims* dims, const int32_t* want_len, int32_t reserve,
                                  const co_page_pool* pool, int32_t* status, void* ws,
@@ -532,7 +532,8 @@ co_status carryover_slot_map(const co_dims* dims, int32_t num_rows, const int32_
  * Entries are rounded to the nearest code, ties to even; infinities and NaNs
  * become NaN.  Supported: bf16.  Device errors, written to *status:
  * CO_ERR_PAGE_RANGE (row_dst / 16 >= num_pages; the row is skipped).
- * num_layers * num_kv_heads <= 65535 (CO_ERR_UNSUPPORTED otherwise).
+ * num_layers * num_kv_heads <= 65535, num_rows (in the calls below num_seqs * block)
+ * below 2^28 and num_pages * 16 below 2^31 (CO_ERR_UNSUPPORTED otherwise).
  */
 co_status carryover_store_kv8(const co_dims* dims, int32_t num_rows, const void* k_rows,
                               const void* v_rows, const int32_t* row_dst, const co_kv8* cache,

@@ -144,7 +144,8 @@ bool cache_ok(const co_kv8* c) {
 co_status check_kv8_dims(const co_dims* d) {
   if (d->dtype != CO_DTYPE_BF16) return CO_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(d->num_layers) * d->num_kv_heads > 65535 ||
-      d->num_pages > INT32_MAX / kPage)
+      d->num_pages > INT32_MAX / kPage ||
+      static_cast<int64_t>(d->num_seqs) * d->block >= kMaxStoreRows)
     return CO_ERR_UNSUPPORTED;
   return CO_OK;
 }
@@ -297,7 +298,7 @@ co_status validate_attention_kv8(const co_dims* d, int32_t layer_begin, int32_t 
                                  size_t ws_bytes) {
   co_status s = check_attention_kv8_dims(d);
   if (s != CO_OK) return s;
-  if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > d->num_layers)
+  if (layer_begin < 0 || layer_count < 0 || layer_count > d->num_layers - layer_begin)
     return CO_ERR_INVALID_ARG;
   if (!q || !out || !state_ok_kv8(st) || !cache_ok(cache) || !aligned(q, 16) ||
       !aligned(out, 16) || !aligned(lse, 4) || !aligned(mass, 4) ||
@@ -749,6 +750,7 @@ co_status carryover_assign_pages(const co_dims* dims, const int32_t* want_len, i
   co_status s = check_dims(dims);
   if (s != CO_OK) return s;
   if (static_cast<int64_t>(dims->num_seqs) * dims->max_pages_per_seq > INT32_MAX ||
+      dims->num_seqs >= kMaxAssign || dims->max_pages_per_seq >= kMaxAssign ||
       dims->num_pages > INT32_MAX / kPage)
     return CO_ERR_UNSUPPORTED;
   if (!want_len || reserve < 0 || !pool || !pool->page_table || !pool->held || !pool->free_pages ||
@@ -805,6 +807,7 @@ co_status carryover_store_kv8(const co_dims* dims, int32_t num_rows, const void*
   co_status s = check_dims(dims);
   if (s != CO_OK) return s;
   if ((s = check_kv8_dims(dims)) != CO_OK) return s;
+  if (num_rows >= kMaxStoreRows) return CO_ERR_UNSUPPORTED;
   if (num_rows < 0 || !k_rows || !v_rows || !row_dst || !cache_ok(cache) || !status ||
       !aligned(k_rows, 16) || !aligned(v_rows, 16) || !aligned(row_dst, 4) || !aligned(status, 4))
     return CO_ERR_INVALID_ARG;

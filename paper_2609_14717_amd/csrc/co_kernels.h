@@ -231,6 +231,7 @@ constexpr int kAssignHdr = 4;             // released, taken, free + released
 // 66K entries 5.5 / 5.8 and 23.7 / 6.4.
 constexpr int kAssignSeqs = 1024;
 constexpr int kAssignPlaces = 32768;
+constexpr int kMaxAssign = 1 << 23;       // sequences, and pages of one, that a grid can cover
 
 size_t assign_ws_bytes(int S);
 
@@ -245,6 +246,8 @@ struct SlotMapArgs {
   int32_t* row_dst;
   int32_t* status;
 };
+
+constexpr int kMaxStoreRows = 1 << 28;    // rows that the store's grid can cover
 
 // Rows into the 8-bit cache (carryover_store_kv8).
 struct StoreArgs {

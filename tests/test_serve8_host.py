@@ -146,8 +146,8 @@ def store(d, n=8, k=FAKE, v=FAKE, dst=FAKE, cache=None, status=FAKE):
 
 
 def attend(d, layers=1, q=FAKE, ks=None, vs=None, st=None, cache=None, out=FAKE, lse=None, mass=None,
-           ws=FAKE, nb=BIG):
-    return co.drafter_block_attention_kv8(d, 0, layers, q, ks, vs, st or _state(), cache or _cache(),
+           ws=FAKE, nb=BIG, l0=0):
+    return co.drafter_block_attention_kv8(d, l0, layers, q, ks, vs, st or _state(), cache or _cache(),
                                           out, lse, mass, 0, ws, stream=0, ws_bytes=nb)
 
 
@@ -250,6 +250,23 @@ def test_tables_beyond_32_bits_are_refused():
     assert _rc(assign, d) == co.CO_ERR_UNSUPPORTED
     d = _dims(L=8192, Hkv=8, Hq=8)
     assert _rc(store, d) == co.CO_ERR_UNSUPPORTED
+
+
+@needs_lib
+def test_sizes_beyond_a_launch_are_refused():
+    assert _rc(assign, _dims(S=1 << 23, B=1, max_pages_per_seq=1)) == co.CO_ERR_UNSUPPORTED
+    assert _rc(assign, _dims(S=1, max_pages_per_seq=1 << 23)) == co.CO_ERR_UNSUPPORTED
+    assert _rc(store, _dims(), n=1 << 28) == co.CO_ERR_UNSUPPORTED
+    d = _dims(S=1 << 24, B=16, L=1)
+    assert _rc(project, d) == _rc(round_, d) == co.CO_ERR_UNSUPPORTED
+    assert co.workspace_bytes(d, co.CO_WS_PROJECT_KV8) == 0
+
+
+@needs_lib
+def test_layer_ranges_that_pass_32_bits_are_refused():
+    big = 2 ** 31 - 1
+    for l0, n in ((1, big), (big, 1), (big, big)):
+        assert _rc(attend, _dims(), l0=l0, layers=n) == co.CO_ERR_INVALID_ARG
 
 
 @needs_lib
