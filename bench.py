@@ -843,13 +843,37 @@ def variant_costs(torch, co, sc, w, lib, step, rewind, chain, args, stream, atte
             torch, stream, n, lambda kv=kv, ms=ms: co.drafter_block_attention_ext(
                 sc.dims, 0, w.L, q_last, kv[0], kv[1], sc.st, out, lse, ms, 0, sc.ws))
     ext["plain_call_us"] = plain_s * 1e6
+    kv8 = serve8_costs(torch, co, w, stream, n) if w.dtype == "bf16" else None
     return {"carry_mass_call_us": mass_s * 1e6,
             "self_merge_call_us": self_s * 1e6,
             "attention_ext": ext,
             "separate_projector": {"rounds_per_s": args.steps / dt_sep,
                                    "vs_embedding": dt / dt_sep},
+            "kv8": kv8,
             "z_norm": {"rounds_per_s": args.steps / dt_norm, "vs_plain": dt / dt_norm},
             "k_norm": {"rounds_per_s": args.steps / dt_knorm, "vs_plain": dt / dt_knorm}}
+
+
+def serve8_costs(torch, co, w, stream, n):
+    """The workload served from the 8-bit committed cache: a round with its page
+    assignment, repeated from the same lengths, and the attention call alone."""
+    from synth.scenario import Scenario8
+    sc = Scenario8(w)
+    inputs = sc.round_inputs(0)
+    out, lse = sc.new_output()
+    ctx = sc.st["ctx_len"].clone()
+
+    def step():
+        sc.st["ctx_len"].copy_(ctx)
+        sc.round(inputs, out, lse)
+
+    step()
+    round_s = timed_calls(torch, stream, n, step)
+    att_s = timed_calls(torch, stream, n, lambda: co.drafter_block_attention_kv8(
+        sc.dims, 0, w.L, inputs[1], None, None, sc.st, sc.cache, out, lse, None, 0, sc.ws))
+    if co.carryover_read_status(sc.st):
+        raise RuntimeError("device status after the rounds on the 8-bit cache")
+    return {"round_us": round_s * 1e6, "attention_call_us": att_s * 1e6}
 
 
 class Scrub:

@@ -2538,13 +2538,11 @@ __device__ __forceinline__ int wave_min_tiles(int hd, int nqt, bool own, int mos
   if (nqt == 1) return hd == 128 ? (most < 384 ? 1 : 2) : 4;
   return most <= 6 && !own ? 3 : 4;
 }
-// The same for tiles of 64 codes: a call of 64 query rows over 2048 positions (8
-// segments of 32 tiles) takes 15.7 us in parts of two tiles, 19.0 of four.
-__device__ __forceinline__ int wave_min_tiles8(int nqt, int most) {
-  return nqt == 1 && most < 192 ? 1 : 2;
-}
-constexpr int kSliceTiles = 4;    // tiles per slice of the even split below which fewer are cut
-constexpr int kSliceTiles8 = 2;   // of 64 codes
+// The same for tiles of 64 codes, and the tiles per slice of the even split: a call of 64
+// query rows over 2048 positions (8 segments of 32 tiles) takes 15.7 us in parts of two
+// tiles, 15.7 of one, 19.0 of four; a single token's over 300 (5 tiles) 13.5, 13.9 of one.
+constexpr int kPartTiles8 = 2;
+constexpr int kSliceTiles = 4;   // tiles per slice of the even split below which fewer are cut
 
 // Header of the workspace (ints): tiles before each sequence [S+1], parts
 // before each sequence [S+1], total tiles, 1 for parts / 0 for the even split.
@@ -2606,7 +2604,7 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
   const int ne = __popcll(__ballot(n_l > 0)), budget = n_places / n_segs;   // parts per segment row
   if (S <= kWavePartSeqs && ne > 0 && budget >= ne) {
     const int mx = wave_max(n_l);
-    const int t_min = KV8 ? wave_min_tiles8(NQT, mx) : wave_min_tiles(HD, NQT, EXT && a.k_self, mx);
+    const int t_min = KV8 ? kPartTiles8 : wave_min_tiles(HD, NQT, EXT && a.k_self, mx);
     // lane c tries t = lo + c * step; ceil by a reciprocal (any count of at
     // least one part is a valid cut; every wavefront gets the same)
     auto cut = [&](int n, int t) {
@@ -3535,7 +3533,7 @@ AttnPlan plan_attention_kv8(int S, int B, int L, int Hq, int Hkv, int hd, int ma
   const bool forced = wg_override >= 1 && wg_override <= kMaxMergeSlices / kCuStreams;
   int n_sl = static_cast<int>(forced ? wg_override : cus) * kCuStreams;
   if (!forced) {
-    const int64_t by_tiles = (tiles / kSliceTiles8 + kCuStreams - 1) / kCuStreams * kCuStreams;
+    const int64_t by_tiles = (tiles / kPartTiles8 + kCuStreams - 1) / kCuStreams * kCuStreams;
     n_sl = static_cast<int>(std::max<int64_t>(kCuStreams, std::min<int64_t>(n_sl, by_tiles)));
   }
   n_sl = (n_sl + wg_st - 1) / wg_st * wg_st;   // whole workgroups

@@ -31,11 +31,12 @@ class Scenario:
                  z_norm: bool = False, k_norm: bool = False):
         import torch
         import paper_2609_14717_amd as co
-        self.w, self.device = w, device
+        self.w, self.device, self.torch, self.co = w, device, torch, co
+        self.ctx0 = wl.initial_ctx(w)
         self.pt = wl.page_table(w)
         self.dims = co.make_dims(w.S, w.B, w.Dcat, w.d, w.L, w.Hq, w.Hkv, w.hd,
                                  w.max_pages_per_seq, self.pt.size, w.dtype, w.theta)
-        self.st = co.alloc_state(self.dims, self.pt, device)
+        self.st = self.alloc_state()
         self.rt = co.alloc_route(w.S, w.B, device)
         self.wf = sdev.materialise(w, wl.spec_wf(w), device)
         self.wkv = sdev.materialise(w, wl.spec_wkv(w), device)
@@ -51,14 +52,18 @@ class Scenario:
             self.knorm = torch.tensor(np.float32(w.sigma_kv), device=device) * (1.0 + off)
         self.W, self.f_e = make_weights(co, self.dims, self.wf, self.wkv, self.e, fold_e,
                                         self.wfc, self.znorm, self.knorm)
-        self.ws = torch.zeros(max(co.workspace_bytes(self.dims, co.CO_WS_ROUND), 256),
+        self.ws = torch.zeros(max(co.workspace_bytes(self.dims, self.round_ws(co)), 256),
                               dtype=torch.uint8, device=device)
         self.ws_project = co.workspace_bytes(self.dims, co.CO_WS_PROJECT)
-        self.ctx0 = wl.initial_ctx(w)
-        self.torch = torch
-        self.co = co
         if build_context:
             self.build_context()
+
+    def alloc_state(self):
+        return self.co.alloc_state(self.dims, self.pt, self.device)
+
+    @staticmethod
+    def round_ws(co):
+        return co.CO_WS_ROUND
 
     @property
     def tdtype(self):
@@ -123,6 +128,84 @@ class Scenario:
         out = torch.empty((w.L, w.S, w.B, w.Hq, w.hd), dtype=self.tdtype, device=self.device)
         lse = torch.empty((w.L, w.S, w.B, w.Hq), dtype=torch.float32, device=self.device)
         return out, lse
+
+
+class Scenario8(Scenario):
+    """The workload served from the 8-bit committed cache: pages are assigned on the
+    device from the lengths (``carryover_assign_pages``, the pool's pages in the
+    workload's order), contexts go to their slots (``carryover_slot_map``,
+    ``carryover_store_kv8``), rounds are ``carryover_round_kv8``."""
+
+    def alloc_state(self):
+        co, torch, w, d = self.co, self.torch, self.w, self.dims
+        self.cache = co.alloc_kv8(d, self.device)
+        self.pool = co.alloc_page_pool(d, self.device)
+        # taken from the end: the workload's table, last page first
+        order = np.ascontiguousarray(self.pt.ravel()[::-1]).astype(np.int32)
+        self.pool["free_pages"].copy_(torch.from_numpy(order))
+        st = co.alloc_state(d, self.pt, self.device, committed=False)
+        self.pool["page_table"] = st["page_table"].fill_(-1)
+        self.ws_pages = torch.zeros(max(co.workspace_bytes(d, co.CO_WS_ASSIGN_PAGES), 256),
+                                    dtype=torch.uint8, device=self.device)
+        return st
+
+    @staticmethod
+    def round_ws(co):
+        return co.CO_WS_ROUND_KV8
+
+    def assign(self, want, reserve=0):
+        """Pages of every sequence for ``want`` (+ reserve) positions."""
+        self.co.carryover_assign_pages(self.dims, want, reserve, self.pool, self.st["status"],
+                                       self.ws_pages)
+
+    def build_context(self):
+        w, co, torch = self.w, self.co, self.torch
+        n = torch.from_numpy(self.ctx0.astype(np.int32)).to(self.device)
+        self.assign(n, w.B)
+        start = torch.zeros(w.S + 1, dtype=torch.int32, device=self.device)
+        start[1:] = n.cumsum(0)
+        rows = int(self.ctx0.sum())
+        if rows == 0:
+            return
+        rt = co.alloc_route(1, rows, self.device)
+        co.carryover_slot_map(self.dims, rows, start, self.st["ctx_len"], self.st["page_table"],
+                              rt["row_pos"], rt["row_dst"], self.st["status"])
+        if w.ctx_mode == "direct":
+            at = 0
+            for s in range(w.S):
+                m = int(self.ctx0[s])
+                k, v = (sdev.materialise(w, wl.spec_kv_direct(w, x, s, 0, m), self.device)
+                        .transpose(1, 2).contiguous() for x in "kv")
+                co.carryover_store_kv8(self.dims, m, k, v, rt["row_dst"][0, at:at + m], self.cache,
+                                       self.st["status"])
+                at += m
+        else:
+            h = torch.empty((rows, w.Dcat), dtype=self.tdtype, device=self.device)
+            at = 0
+            for s in range(w.S):
+                m = int(self.ctx0[s])
+                st_, shape, strides, base, sigma = wl.spec_hctx(w, s, 0, m)
+                sdev.fill(h[at:at + m], w.key(st_), shape, strides, base, sigma)
+                at += m
+            self.project_packed(h, rt)
+        self.st["ctx_len"].copy_(n)
+
+    def project_packed(self, hidden, rt):
+        """Project rows [n][Dcat], packed sequence behind sequence, to their slots."""
+        co, d = self.co, self.dims
+        pd = co.make_dims(1, hidden.shape[0], d.feat_dim, d.model_dim, d.num_layers, d.num_q_heads,
+                          d.num_kv_heads, d.head_dim, d.max_pages_per_seq, d.num_pages, d.dtype,
+                          d.rope_theta)
+        ws = self.torch.empty(max(co.workspace_bytes(pd, co.CO_WS_PROJECT_KV8), 256),
+                              dtype=self.torch.uint8, device=self.device)
+        co.carryover_project_kv8(pd, self.W, hidden, rt, self.st, self.cache, ws)
+
+    def round(self, inputs, out, lse, flags=0):
+        """One round: room for its block, then route, projection and attention."""
+        hidden, q, draft, target = inputs[:4]
+        self.assign(self.st["ctx_len"], self.w.B)
+        self.co.carryover_round_kv8(self.dims, self.W, hidden, draft, target, q, self.st, self.cache,
+                                    self.rt, out, lse, flags, self.ws)
 
 
 class TrainScenario:
