@@ -1623,9 +1623,14 @@ __global__ __launch_bounds__(256) void attn_bf16_combine_kernel(AttnArgs a, int 
 //   under 2^-14 of a row's largest: to 2^-22 of that).  Two such products at twice
 //   the bf16 rate.  Widening the keys to bf16 took 64 of the 540 vector instructions
 //   of a tile.
-//   Values: codes to bf16 in registers, exactly, the scale with them
-//   (v_cvt_scalef32_pk_bf16_fp8), against bf16 weights: a weight has no largest
-//   value in its row that 8 bits could be relative to.  A 16-byte read holds 16
+//   Values: codes to fp16 in registers (v_cvt_scalef32_pk_f16_fp8), exactly, against
+//   fp16 weights.  Weights of 11 bits in place of 8 leave the output's own rounding:
+//   1.8e-3 from 64 bits (bf16 weights 2.4e-3), at the same rate.  fp16's range is met
+//   by two references.  The values' is the largest scale byte seen (v_ref): codes
+//   enter as code * 2^(b - v_ref + 7), at most 57344, exact down to b = v_ref - 22,
+//   and o is in its units, times 2^-15 with the weights'.  The weights' is 2^7 below
+//   a maximum: weights reach 2^15 before it moves, and are normal down to 2^-14, 2^-21
+//   of that maximum's.  Both leave at the end of the codes (end_codes).  A 16-byte read holds 16
 //   slots of a dim, the operands of two products.
 // S^T takes its rows from two pages in turn, four slots each: lane l holds the 16 keys
 // of page l / 32 of the pair, register r slot r.  Lane l holds of its query the dims
@@ -1647,9 +1652,15 @@ struct Tile32 {
   int slot_base, half, r32;
   typedef int i32x8 __attribute__((ext_vector_type(8)));
   typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
   static constexpr int NG = HD / 64;            // groups of 64 dims
   i32x8 qh[KV8 ? NG : 1], ql[KV8 ? NG : 1];     // the query's two codes of every dim
   int q_scale;                                  // their scale bytes (byte 0, byte 1)
+  int v_ref;                                    // the values' reference: a scale byte, 0: none yet
+  static constexpr float kRescale8 = 15.f, kRefBelow = 7.f;   // of the weights' reference
+  static constexpr int kValueUp = 7;
   f32x16 nb;                                    // minus the running reference, sixteen times
   static constexpr int PAGE8 = kPage * HD;      // a page's codes
   uint32_t k8_off;     // of chunk 0 of a pair of pages, kf_off[0] of bf16 rows: the other
@@ -1675,6 +1686,7 @@ struct Tile32 {
       const int page = (r32 >> 2) & 1, slot = 4 * (r32 >> 3) + (r32 & 3);
       k8_shift = 8 * page;
       k8_off = page * PAGE8 + slot * HD + (((2 * half) ^ swz_key8<HD>(slot, page)) << 4);
+      v_ref = 0;
 #pragma unroll
       for (int r = 0; r < 16; ++r) nb[r] = 0.f;
     }
@@ -1792,7 +1804,6 @@ struct Tile32 {
         const float shift = (m_new == -INFINITY) ? 0.f : m_new - base[qt];
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[qt][r] -= shift;
-        if constexpr (KV8) set_reference();
       }
     }
     u16x8 pk[NQT][2], pl[NQT][2];
@@ -1850,7 +1861,6 @@ struct Tile32 {
   __device__ __forceinline__ void set_query(const u32x4v (&x)[KK], int pos, bool rotate, bool quad,
                                             const double* inv_rev, float qscale, bool live) {
     static_assert(!KV8 || NQT == 1, "one query tile");
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
     float v[8 * KK];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {   // dims 4 u .. + 3 of each group's 32
@@ -1927,6 +1937,31 @@ struct Tile32 {
     }
   }
 
+  // After the last tile of codes: o and l under the reference that step keeps.
+  __device__ __forceinline__ void end_codes() {
+    if (v_ref == 0) return;   // (no tile with a key)
+    constexpr int up = static_cast<int>(kRescale8);
+    const float f = __uint_as_float((127 - up) << 23);
+    m_run[0] += kRescale8;
+    l_run[0] *= f;
+    const int e = v_ref - 127 - kValueUp - up;
+#pragma unroll
+    for (int m = 0; m < MO; ++m)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[0][m][r] = __builtin_amdgcn_ldexpf(o[0][m][r], e);
+  }
+
+  // Eight codes as an fp16 operand, times the power of two `scale`.
+  static __device__ __forceinline__ f16x8 widen16(uint32_t a, uint32_t b, float scale) {
+    const f16x2 w0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, scale, false);
+    const f16x2 w1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, scale, true);
+    const f16x2 w2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, scale, false);
+    const f16x2 w3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, scale, true);
+    const u32x4v w = {__builtin_bit_cast(uint32_t, w0), __builtin_bit_cast(uint32_t, w1),
+                      __builtin_bit_cast(uint32_t, w2), __builtin_bit_cast(uint32_t, w3)};
+    return __builtin_bit_cast(f16x8, w);
+  }
+
   // Eight codes as a bf16 operand, times the power of two `scale`.
   static __device__ __forceinline__ u16x8 widen(uint32_t a, uint32_t b, float scale) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -1944,6 +1979,18 @@ struct Tile32 {
   __device__ void step8(const unsigned char* tb, const int (&n)[4], uint32_t kw, uint32_t vw) {
     static_assert(NQT == 1 && KV8, "one query tile");
     const bool partial = min(min(n[0], n[1]), min(n[2], n[3])) < kPage;
+    int top = 1;   // (the byte 0 under the reference 1)
+#pragma unroll
+    for (int p = 0; p < 4; ++p) top = max(top, n[p] > 0 ? static_cast<int>(vw >> (8 * p) & 0xFF) : 0);
+    if (top > v_ref) {
+      asm volatile("");   // (a branch)
+      if (v_ref != 0)
+#pragma unroll
+        for (int m = 0; m < MO; ++m)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[0][m][r] = __builtin_amdgcn_ldexpf(o[0][m][r], v_ref - top);
+      v_ref = top;
+    }
     f32x16 sc[2];
     const float base = -nb[0];
     const int ks = static_cast<int>(kw >> k8_shift);   // bytes 0 and 2: this lane's pages'
@@ -1988,7 +2035,7 @@ struct Tile32 {
       for (int r = 0; r < 16; ++r) vi = max(vi, __float_as_int(sc[h][r]));
     const auto sw = __builtin_amdgcn_permlane32_swap(vi, vi, false, false);
     const float rel = __int_as_float(max(static_cast<int>(sw[0]), static_cast<int>(sw[1])));
-    if (__any(rel > kRescale || m_run[0] == -INFINITY)) {
+    if (__any(rel > kRescale8 || m_run[0] == -INFINITY)) {
       float v = sc[0][0];
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -1996,13 +2043,9 @@ struct Tile32 {
         for (int r = 0; r < 16; ++r) v = fmaxf(v, sc[h][r]);
       const auto s2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
       const float mx = fmaxf(__uint_as_float(s2[0]), __uint_as_float(s2[1])) + base;
-      const float m_new = mx > m_run[0] + kRescale ? mx : m_run[0];
+      const float m_new = mx > m_run[0] + kRescale8 ? mx - kRefBelow : m_run[0];
       const float alpha = (m_new == m_run[0]) ? 1.f : exp2f(m_run[0] - m_new);
-      l_run[0] *= alpha;
-      if constexpr (EXT) {
-        lu_run[0] *= alpha;
-        ls_run[0] *= alpha;
-      }
+      l_run[0] *= alpha;   // (no carry or own row yet)
 #pragma unroll
       for (int m = 0; m < MO; ++m) o[0][m] *= alpha;
       m_run[0] = m_new;
@@ -2032,14 +2075,17 @@ struct Tile32 {
     const float p0 = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     const float p1 = ((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15]));
     l_run[0] += p0 + p1;
-    u16x8 pk[2];
+    f16x8 pk[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const u32x4v w4 = {cvt_pk_bf16(p[8 * j + 0], p[8 * j + 1]), cvt_pk_bf16(p[8 * j + 2], p[8 * j + 3]),
-                         cvt_pk_bf16(p[8 * j + 4], p[8 * j + 5]), cvt_pk_bf16(p[8 * j + 6], p[8 * j + 7])};
-      pk[j] = __builtin_bit_cast(u16x8, w4);
+      u32x4v w4;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        w4[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p[8 * j + 2 * k], p[8 * j + 2 * k + 1]}), f16x2));
+      pk[j] = __builtin_bit_cast(f16x8, w4);
     }
-    float vs = __uint_as_float((vb & 0xFFu) << 23);
+    // (so far below the reference that the exponent ends: under 2^-133 of the largest value)
+    float vs = __uint_as_float(static_cast<uint32_t>(max(0, static_cast<int>(vb & 0xFFu) - v_ref + 127 + kValueUp)) << 23);
     if (partial) {   // codes behind the last key may be NaN, and a page left out has any scale
       asm volatile("");
       if (nv <= 0) vs = 1.f;
@@ -2053,8 +2099,8 @@ struct Tile32 {
     }
 #pragma unroll
     for (int m = 0; m < MO; ++m) {
-      o[0][m] = mfma32x32x16(widen(vc[m][0], vc[m][1], vs), pk[0], o[0][m]);
-      o[0][m] = mfma32x32x16(widen(vc[m][2], vc[m][3], vs), pk[1], o[0][m]);
+      o[0][m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen16(vc[m][0], vc[m][1], vs), pk[0], o[0][m], 0, 0, 0);
+      o[0][m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen16(vc[m][2], vc[m][3], vs), pk[1], o[0][m], 0, 0, 0);
     }
   }
 
@@ -3157,6 +3203,7 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
         if (n[0] + n[1] + n[2] + n[3] > 0) T.step8(my_ring + (j % NS) * TILE_BYTES, n, ksb[0], vsb[0]);
         tile_done();
       }
+      if (j0 < nct) T.end_codes();
     }
     for (; j < min(j1, own); ++j) {
       next_tile(j);
@@ -3559,10 +3606,10 @@ hipError_t launch_attention_kv8(const AttnArgs& a, const AttnPlan& p, int layer_
 #define CO_KV8_LAUNCH(HD, NQT)                                                                     \
   do {                                                                                             \
     if (ext)                                                                                       \
-      hipLaunchKernelGGL((attn_wave_kernel<HD, NQT, true, false, true>), grid, block, 0, stream,   \
+      hipLaunchKernelGGL((attn_wave_kernel<HD, NQT, true, true, true>), grid, block, 0, stream,   \
                          a, layer_count, p.n_places, p.n_slices, p.hdr_slices, p.nq_pad);          \
     else                                                                                           \
-      hipLaunchKernelGGL((attn_wave_kernel<HD, NQT, false, false, true>), grid, block, 0, stream,  \
+      hipLaunchKernelGGL((attn_wave_kernel<HD, NQT, false, true, true>), grid, block, 0, stream,  \
                          a, layer_count, p.n_places, p.n_slices, p.hdr_slices, p.nq_pad);          \
   } while (0)
   if (a.hd == 128) {

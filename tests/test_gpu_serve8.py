@@ -526,6 +526,70 @@ def test_attention_of_flat_and_peaked_softmaxes(hd, B, G, size):
         assert torch.isfinite(got[0].float()).all() and torch.isfinite(got[1]).all()
 
 
+@pytest.mark.parametrize("hd,B,G", [(64, 1, 2), (64, 16, 4), (128, 1, 2), (128, 16, 4)])
+@pytest.mark.parametrize("bytes_", [(0, 40), (100, 150), (200, 240), "up", "down"])
+def test_attention_over_values_of_any_scale(bytes_, hd, B, G):
+    """Value pages whose scales differ from page to page: by up to 2^50, or by 2^3 a page
+    up or down (the largest, which the outputs show, first or last)."""
+    sv = Serve(3, B, 1, G, 1, hd, [700, 77, 16], [0, 0, 0], seed=12, size=0.3)
+    N = sv.d.num_pages
+    if isinstance(bytes_, tuple):
+        g = torch.Generator(device=DEV).manual_seed(12)
+        b = torch.randint(*bytes_, (N,), generator=g, device=DEV)
+    else:
+        b = torch.full((N,), 120, device=DEV)
+        row = torch.tensor([int(p) for p in sv.table[0] if p >= 0], device=DEV)
+        b[row] = 40 + 3 * torch.arange(len(row), device=DEV)
+        if bytes_ == "down":
+            b[row] = b[row].flip(0)
+    sv.cache["v_scale"][0, :, 0] = b.to(torch.uint8)
+    sv.check(sv.run())
+
+
+@pytest.mark.parametrize("hd,B,G", [(64, 1, 2), (128, 16, 4)])
+@pytest.mark.parametrize("below", [12, 22])
+def test_attention_reads_small_values_beside_large_ones(below, hd, B, G):
+    """The key that has all the weight has values 2^-below of another page's: subnormal
+    beside them, and still exact.  Its score is 128 (head_dim 64: 64 * 2^4 / 8) or 90.5
+    (128 * 2^3 / 11.3) and the others' 0, whose weights of 2^-130 leave nothing of 2^35
+    times as large values: each row is one value row, rounded once to bf16."""
+    sv = Serve(1, B, 1, G, 1, hd, [32], [0], seed=14)
+    sv.q.fill_(1.0)
+    a, b = (int(x) for x in sv.table[0, :2])
+    one = 0x38                                                     # e4m3 1.0
+    sv.cache["k_pages"][0, a], sv.cache["k_pages"][0, b] = 0, 0
+    sv.cache["k_pages"][0, b, 0, 5] = one
+    sv.cache["k_scale"][0, b, 0] = 127 + (4 if hd == 64 else 3)
+    sv.cache["v_scale"][0, a, 0], sv.cache["v_scale"][0, b, 0] = 140, 140 - below
+    out, _, _ = sv.run(flags=co.CO_Q_PREROTATED)
+    v = serve8.Cache8.read(sv.cache).context(sv.table, 0, 0, 0, 32)[1]
+    want = torch.from_numpy(v[16 + 5]).to(DEV).float()
+    assert torch.all((out[0, 0].float() - want).abs() <= want.abs() * 2 ** -8)
+
+
+@pytest.mark.parametrize("hd,B,G", [(64, 1, 8), (64, 16, 4), (128, 1, 8), (128, 16, 4)])
+def test_attention_is_as_exact_as_its_output_type(hd, B, G):
+    """Rounding an exact result to bf16 leaves 1.7e-3 (half a step is 2^-9 to 2^-8 of an
+    entry, evenly spread: 2^-8 / sqrt(12) of the entries' 1.0 .. 2.0 is 1.1e-3 to 2.3e-3);
+    queries of two codes 0.7e-3, fp16 weights 0.3e-3: 1.9e-3 together, and 2.1e-3 allowed
+    (bf16 weights would leave 2.4e-3)."""
+    sv = Serve(4, B, 1, G, 1, hd, [3000, 2000, 1000, 300], [0, 0, 0, 0], seed=13)
+    g = torch.Generator(device=DEV).manual_seed(13)
+    r = lambda *n: torch.randn(n, generator=g, device=DEV).bfloat16()  # noqa: E731
+    dst = [sv.table[s][t // PAGE] * PAGE + t % PAGE for s in range(4) for t in range(sv.ctx[s])]
+    co.carryover_store_kv8(sv.d, len(dst), r(1, len(dst), 1, hd), r(1, len(dst), 1, hd), ints(dst),
+                           sv.cache, sv.st["status"])
+    out, _, _ = sv.run()
+    orc, off, all_ = serve8.Cache8.read(sv.cache), 0.0, 0.0
+    for s, n in enumerate(sv.ctx):
+        k, v = orc.context(sv.table, s, 0, 0, n)
+        q = sv.q[0, s].double().cpu().numpy().reshape(B * G, hd)
+        o, _ = oracle.attend(q, np.repeat(n + np.arange(B), G), k, v, sv.theta)
+        d = out[0, s].double().cpu().numpy().reshape(B * G, hd) - o
+        off, all_ = off + np.sum(d * d), all_ + np.sum(o * o)
+    assert math.sqrt(off / all_) <= 2.1e-3, math.sqrt(off / all_)
+
+
 @pytest.mark.parametrize("hd,B,G", [(64, 1, 2), (128, 16, 4)])
 def test_attention_leaves_out_pages_out_of_range(hd, B, G):
     sv = Serve(3, B, 1, G, 1, hd, [200, 77, 64], [B, 0, 0], seed=9)
