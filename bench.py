@@ -80,12 +80,13 @@ def parse():
                          "'--only projection' or '--only prefill' and exit")
     ap.add_argument("--bench-json", metavar="FILE",
                     help="the JSON line the profiled bench command printed (for the summaries)")
-    ap.add_argument("--only", choices=("projection", "prefill", "backward"),
+    ap.add_argument("--only", choices=("projection", "prefill", "backward", "kv8"),
                     help="time only carryover_project_kv: the projection of a round's rows "
                          "('projection'), or the whole context as one call ('prefill'); or, "
                          "for the training-shaped workload, only the attention backward "
                          "('backward'); prints one JSON line (the run the MFMA counters are "
-                         "taken on)")
+                         "taken on); 'kv8': only the rounds on the 8-bit cache and their "
+                         "attention call")
     ap.add_argument("--command", default="", help="command recorded in a summary")
     return ap.parse_args()
 
@@ -210,7 +211,7 @@ def summarize_pmc(args):
         # the plain instantiations only: the EXT ones serve
         # drafter_block_attention_ext, timed separately
         rows = [v for k, v in table.items()
-                if k[1] == counter and name in k[0] and not is_ext(k[0])]
+                if k[1] == counter and name in k[0] and is_plain(k[0])]
         if not rows:
             raise SystemExit(f"no {counter} rows for {name}")
         tot, cnt = 0.0, 0
@@ -373,6 +374,11 @@ def is_ext(name):
     return bools[:1] == ["true"]
 
 
+def is_plain(name):
+    """Neither an EXT instantiation nor the 8-bit cache's (the third bool)."""
+    return not is_ext(name) and re.findall(r"\b(true|false)\b", name)[2:3] != ["true"]
+
+
 def summarize_stats(args):
     rows = []
     with open(args.summarize_stats) as fh:
@@ -389,21 +395,21 @@ def summarize_stats(args):
         short = n if len(n) <= 90 else n[:87] + "..."
         lines.append(f"{short:90s} {c:6d} {a:8.2f} {lo:8.2f} {hi:8.2f} {pct:6.2f}")
     # the plain instantiations (the EXT ones serve drafter_block_attention_ext)
-    att = [(k, r) for k in ATTN_KERNELS for r in rows if is_kernel(r[0], k) and not is_ext(r[0])]
-    if att:
+    att = [(k, r) for k in ATTN_KERNELS for r in rows if is_kernel(r[0], k) and is_plain(r[0])]
+    if att and not args.only:
         lines += ["", "drafter_block_attention, all dispatches = " + " + ".join(
             f"{k} {r[2]:.2f} us" for k, r in att) +
             f" = {sum(r[2] for _, r in att):.2f} us per launch (kernel time, no launch gaps)"]
     trace = os.path.join(os.path.dirname(args.summarize_stats),
                          os.path.basename(args.summarize_stats).replace("kernel_stats",
                                                                         "kernel_trace"))
-    if att and os.path.exists(trace):
+    if att and not args.only and os.path.exists(trace):
         first, count = attention_window(args)
         per = {}
         with open(trace) as fh:
             for r in csv.DictReader(fh):
                 for k, _ in att:
-                    if is_kernel(r["Kernel_Name"], k) and not is_ext(r["Kernel_Name"]):
+                    if is_kernel(r["Kernel_Name"], k) and is_plain(r["Kernel_Name"]):
                         per.setdefault(k, []).append(
                             (int(r["Dispatch_Id"]),
                              (int(r["End_Timestamp"]) - int(r["Start_Timestamp"])) / 1e3))
@@ -418,7 +424,8 @@ def summarize_stats(args):
                          " + ".join(f"{k} {t:.2f} us" for k, t in parts) +
                          f" = {sum(t for _, t in parts):.2f} us per launch")
     os.makedirs(PROFILES, exist_ok=True)
-    out = os.path.join(PROFILES, f"kernel_stats_{args.workload}.txt")
+    part = f"_{args.only}" if args.only else ""
+    out = os.path.join(PROFILES, f"kernel_stats_{args.workload}{part}.txt")
     with open(out, "w") as fh:
         fh.write("\n".join(lines) + "\n")
     print("\n".join(lines))
@@ -589,8 +596,15 @@ def main():
     total = args.warmup + args.steps
     w = w.replace(rounds=max(w.rounds, total))
     torch.cuda.set_device(0)
-    sc = Scenario(w)
     stream = torch.cuda.current_stream()
+    if args.only == "kv8":
+        if w.dtype != "bf16":
+            raise SystemExit(f"{w.name}: the 8-bit cache is of bf16 drafters")
+        res = serve8_costs(torch, co, w, stream, args.steps)
+        res.update(only=args.only, calls=args.steps, warm=TIMED_WARM, config={"workload": w.name})
+        print(json.dumps(res), flush=True)
+        return
+    sc = Scenario(w)
     if args.only:
         return only_projection(args, torch, co, sc, w, stream)
 

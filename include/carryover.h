@@ -555,9 +555,9 @@ co_status carryover_project_kv8(const co_dims* dims, const co_weights* w, const 
  * drafter_block_attention_ext with the committed segment in the 8-bit cache: the
  * attention over [C;U], or [C;U;S] where k_self and v_self are given, with C's
  * keys and values read as code * 2^(b - 127) and U and S in bf16; block 1 is a
- * single token's.  Values enter the products exactly, but for entries below 2^-31 of
+ * single token's.  Values enter the products exactly, but for entries below 2^-35 of
  * the largest that their page scales allow in the sequence and head (448 * 2^e), which
- * are off by up to 2^-41 of it.  k_self, v_self, lse and
+ * are off by up to 2^-40 of it.  k_self, v_self, lse and
  * carry_mass are optional (NULL).  state->k_cache and v_cache are not used and
  * may be NULL.  Supported: bf16; the shapes of drafter_block_attention.
  * `ws`: carryover_workspace_bytes(dims, CO_WS_ATTENTION_KV8) bytes, 256-byte

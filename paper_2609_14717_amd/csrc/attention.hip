@@ -88,6 +88,7 @@ __device__ __forceinline__ int64_t out_row(const AttnArgs& a, int layer_local, i
 constexpr int kMaxMergeChunks = 64;
 constexpr int kMaxMergeSlices = 4096;   // workgroups of one persistent launch
 constexpr int kCombineWideSegs = 128;   // segments from which the merge takes 16 dims per thread
+constexpr int kCombineWideDims = 8192;  // of at least this many dims each
 constexpr int kCombineGroupSegs = 48;   // and up to which four wavefronts share an item's records
 constexpr int kAttnWaves64 = 8, kAttnWaves128 = 4;             // wavefronts per workgroup
 constexpr int kAttnRoundTiles64 = 64, kAttnRoundTiles128 = 128; // tiles per wavefront per round
@@ -1632,6 +1633,11 @@ __global__ __launch_bounds__(256) void attn_bf16_combine_kernel(AttnArgs a, int 
 //   a maximum: weights reach 2^15 before it moves, and are normal down to 2^-14, 2^-21
 //   of that maximum's.  Both leave at the end of the codes (end_codes).  A 16-byte read holds 16
 //   slots of a dim, the operands of two products.
+//   Measured, calls with 64 query rows per KV head and 8 heads of 128: 16 sequences of
+//   16K-32K positions in 5 layers 792 us, 5.1 TB/s of codes (the loads alone 746, the
+//   arithmetic alone 491); 32 of 512-8192 85 us, of which the merge of 8 MB to 33 MB of
+//   records 11; one of 2048 16 us.  Bound by the loads, 2 KiB or 1 KiB of a page at a
+//   time, and in short calls by the chain of lengths, page ids and first tiles.
 // S^T takes its rows from two pages in turn, four slots each: lane l holds the 16 keys
 // of page l / 32 of the pair, register r slot r.  Lane l holds of its query the dims
 // 32 (l / 32) .. + 31 of every 64 (`chunk`, for the carry keys' bf16 products too).
@@ -3423,12 +3429,16 @@ AttnPlan plan_attention(int S, int B, int L, int Hq, int Hkv, int hd, int max_pa
 }
 
 // The merge of a launch's records: one workgroup per 256 (query row, dims) items
-// of a segment, 16 dims per item with at least kCombineWideSegs segments, else 4;
-// per 64 items with up to kCombineGroupSegs.
+// of a segment, 16 dims per item with at least kCombineWideSegs segments of at least
+// kCombineWideDims dims (two workgroups), else 4; per 64 items with up to
+// kCombineGroupSegs.  A whole call on the 8-bit cache, 4 dims against 16: 512 segments of
+// 4 x 64 dims 44.0 us against 46.2, 256 of 16 x 64 43.2 / 43.8, of 64 x 64 53.0 / 53.7,
+// of 64 x 128 86.1 / 85.7, 640 of 64 x 128 810 / 804.
 static void launch_combine(const AttnArgs& a, int layer_count, int slices, int hdr, int rec_rows,
                            int waves, hipStream_t stream) {
   const int64_t n_segs = static_cast<int64_t>(a.S) * layer_count * a.Hkv;
-  const bool wide = n_segs >= kCombineWideSegs, grouped = n_segs <= kCombineGroupSegs;
+  const bool wide = n_segs >= kCombineWideSegs && a.B * (a.Hq / a.Hkv) * a.hd >= kCombineWideDims;
+  const bool grouped = n_segs <= kCombineGroupSegs;
   const int items = (a.B * (a.Hq / a.Hkv)) * (a.hd / (wide ? 16 : 4));
   const int wg_items = grouped ? 64 : 256;
   const dim3 mgrid(a.S, layer_count * a.Hkv, (items + wg_items - 1) / wg_items);
