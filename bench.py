@@ -275,14 +275,15 @@ def load_bench_json(path):
     return json.loads(lines[-1])
 
 
-MFMA_GAP_NS = 50_000_000   # the pause bench.py --only leaves before the calls it times
+MFMA_GAP_NS = 300_000_000   # less than the pause bench.py --only leaves before the calls it times
+# (a profiler's own pause between two sets of calls took 91 ms)
 
 
 def summarize_mfma(args):
     """MFMA counters of the projection call (or of the attention backward)
     from a rocprofv3 --pmc run (with --kernel-trace) of ``bench.py --only
     ...``: the call's kernel dispatches after the last pause of more than
-    50 ms are the warm-up and timed calls (``bench.py --only`` pauses before
+    0.3 s are the warm-up and timed calls (``bench.py --only`` pauses before
     them), all of the same shape.  Per call: the MFMA busy share of the SIMD cycles (rocprofv3's
     MfmaUtil, time-weighted over the dispatches), counted bf16 MFMA flops
     (SQ_INSTS_VALU_MFMA_MOPS_BF16 x 512) against the algorithmic flops, and
@@ -928,10 +929,10 @@ def only_projection(args, torch, co, sc, w, stream):
 
 
 def pause(torch):
-    """A pause of 0.1 s on an idle GPU: marks the start of the calls a counter
+    """A pause of 0.5 s on an idle GPU: marks the start of the calls a counter
     pass summarises."""
     torch.cuda.synchronize()
-    time.sleep(0.1)
+    time.sleep(0.5)
 
 
 def prefill_point(torch, co, sc, w, calls=20, pause_first=False):
