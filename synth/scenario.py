@@ -200,10 +200,11 @@ class Scenario8(Scenario):
                               dtype=self.torch.uint8, device=self.device)
         co.carryover_project_kv8(pd, self.W, hidden, rt, self.st, self.cache, ws)
 
-    def round(self, inputs, out, lse, flags=0):
+    def round(self, inputs, out, lse, flags=0, assign=True):
         """One round: room for its block, then route, projection and attention."""
         hidden, q, draft, target = inputs[:4]
-        self.assign(self.st["ctx_len"], self.w.B)
+        if assign:
+            self.assign(self.st["ctx_len"], self.w.B)
         self.co.carryover_round_kv8(self.dims, self.W, hidden, draft, target, q, self.st, self.cache,
                                     self.rt, out, lse, flags, self.ws)
 
