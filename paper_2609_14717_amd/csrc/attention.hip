@@ -1859,61 +1859,68 @@ struct Tile32 {
     for (int r = 0; r < 16; ++r) nb[r] = x;
   }
 
-  // This lane's query row, its bf16 dims in x (16 bytes per chunk), rotated at pos and
-  // scaled in fp32, as two codes per dim; `live` false: a row of padding.  The
+  // This lane's query row, its bf16 dims in x (16 bytes per chunk), rotated and scaled
+  // in fp32, as two codes per dim; `live` false: a row of padding.  The
   // partner of a dim is in the lane's other group of 64 (head_dim 128) or in the
-  // other half's lane of the row (64).  quad: the four lanes of a quad are rows of one
-  // position, so each computes every fourth angle and takes the others from them.
-  __device__ __forceinline__ void set_query(const u32x4v (&x)[KK], int pos, bool rotate, bool quad,
-                                            const double* inv_rev, float qscale, bool live) {
+  // other half's lane of the row (64).  The wavefront's rows lie at the P positions
+  // pos0 .., this lane's at pos0 + p_row: every lane computes angles of some position
+  // and all take theirs from LDS (`tab`, this wavefront's half of a tile), in two passes
+  // of half the angles.  Few evaluations in a loop of few instructions: rows of one
+  // position share them, and code that runs once is bound by its fetches.
+  __device__ __forceinline__ void set_query(const u32x4v (&x)[KK], unsigned char* tab, int p_row, int P,
+                                            int pos0, bool rotate, const double* inv_rev,
+                                            float qscale, bool live) {
     static_assert(!KV8 || NQT == 1, "one query tile");
+    constexpr int A = HD / 4, LP = 64 / A, CX = A / 2 - 1;   // angles of a pass, positions at once
+    const int lane = 32 * half + r32, al = lane % A;
     float v[8 * KK];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {   // dims 4 u .. + 3 of each group's 32
-      float cs[4], sn[4];
-      if (!rotate) {
+    for (int h = 0; h < 2; ++h) {
+      // dims 16 h .. + 15 of each half's 32 (head_dim 128), or of both halves' 32 (64)
+      const double inv = inv_rev[16 * h + (HD == 128 ? (al & 15) + 2 * (al & 16) : al)];
+#pragma unroll 1
+      for (int p = lane / A; p < P; p += LP) {
+        f32x2 t = {1.f, 0.f};
+        if (rotate) {
+          float c, n;
+          rope_cos_sin_rev(pos0 + p, inv, &c, &n);
+          t = f32x2{c, n};
+        }
+        // (16-byte chunks XOR-permuted by the position)
+        *reinterpret_cast<f32x2*>(tab + p * (A * 8) + (((al >> 1) ^ (p & CX)) << 4) + (al & 1) * 8) = t * qscale;
+      }
+      asm volatile("" ::: "memory");   // (a wavefront's LDS accesses are in order)
+#pragma unroll
+      for (int u = 4 * h; u < 4 * h + 4; ++u) {   // dims 4 u .. + 3 of each group's 32
+        float cs[4], sn[4];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const int ch = (HD == 128 ? 8 * half : 0) + 2 * (u - 4 * h) + q;
+          const f32x4 t = *reinterpret_cast<const f32x4*>(tab + p_row * (A * 8) + ((ch ^ (p_row & CX)) << 4));
+          cs[2 * q] = t[0];
+          sn[2 * q] = t[1];
+          cs[2 * q + 1] = t[2];
+          sn[2 * q + 1] = t[3];
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          cs[e] = qscale;
-          sn[e] = 0.f;
-        }
-      } else {
-        const int i0 = (HD == 128 ? 32 * half : 0) + 4 * u;
-        if (quad) {
-          float c, n;
-          rope_cos_sin_rev(pos, inv_rev[i0 + (r32 & 3)], &c, &n);
-          c *= qscale;
-          n *= qscale;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            cs[e] = quad_bcast(c, e);
-            sn[e] = quad_bcast(n, e);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            rope_cos_sin_rev(pos, inv_rev[i0 + e], &cs[e], &sn[e]);
-            cs[e] *= qscale;
-            sn[e] *= qscale;
+          const int c = u >> 1, w = 2 * (u & 1) + (e >> 1);   // chunk and word of the dim
+          if constexpr (HD == 128) {
+            const uint32_t xw = x[c][w], yw = x[4 + c][w];
+            const float a = __uint_as_float(e & 1 ? xw & 0xFFFF0000u : xw << 16);
+            const float b = __uint_as_float(e & 1 ? yw & 0xFFFF0000u : yw << 16);
+            v[4 * u + e] = a * cs[e] - b * sn[e];
+            v[32 + 4 * u + e] = b * cs[e] + a * sn[e];
+          } else {
+            const auto sw = __builtin_amdgcn_permlane32_swap(x[c][w], x[c][w], false, false);
+            const float a = __uint_as_float(e & 1 ? sw[0] & 0xFFFF0000u : sw[0] << 16);
+            const float b = __uint_as_float(e & 1 ? sw[1] & 0xFFFF0000u : sw[1] << 16);
+            v[4 * u + e] = half ? b * cs[e] + a * sn[e] : a * cs[e] - b * sn[e];
           }
         }
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int c = u >> 1, w = 2 * (u & 1) + (e >> 1);   // chunk and word of the dim
-        if constexpr (HD == 128) {
-          const uint32_t xw = x[c][w], yw = x[4 + c][w];
-          const float a = __uint_as_float(e & 1 ? xw & 0xFFFF0000u : xw << 16);
-          const float b = __uint_as_float(e & 1 ? yw & 0xFFFF0000u : yw << 16);
-          v[4 * u + e] = a * cs[e] - b * sn[e];
-          v[32 + 4 * u + e] = b * cs[e] + a * sn[e];
-        } else {
-          const auto sw = __builtin_amdgcn_permlane32_swap(x[c][w], x[c][w], false, false);
-          const float a = __uint_as_float(e & 1 ? sw[0] & 0xFFFF0000u : sw[0] << 16);
-          const float b = __uint_as_float(e & 1 ? sw[1] & 0xFFFF0000u : sw[1] << 16);
-          v[4 * u + e] = half ? b * cs[e] + a * sn[e] : a * cs[e] - b * sn[e];
-        }
-      }
+      if (h == 0) asm volatile("" ::: "memory");
+      else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next tile lands there
     }
     float big = 0.f;
 #pragma unroll
@@ -3074,9 +3081,6 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     // in registers over the whole walk
     int ln = lane;
     asm volatile("" : "+v"(ln));
-    // With G a multiple of 4 the four lanes of a quad hold rows of one position
-    // and the same dims.
-    const bool quad = (G & 3) == 0;
     if constexpr (KV8) {
       // The queries come straight into registers, beside the page ids; the first tile
       // and its scale bytes travel while they are rotated.
@@ -3100,7 +3104,9 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
         issue_tile(j0, b[0], ksb[0], vsb[0]);
       }
       T.setup(lane);
-      T.set_query(x, ctx + qi, rotate_q, quad, inv_lds, qscale, row0 + (ln & 31) < nq);
+      const int p0 = row0 / G, p1 = min(row0 + 31, nq - 1) / G;   // positions of these rows
+      T.set_query(x, my_ring + ((j0 + 1) % NS) * TILE_BYTES + qw * (TILE_BYTES / QW), qi - p0, p1 - p0 + 1,
+                  ctx + p0, rotate_q, inv_lds, qscale, row0 + (ln & 31) < nq);
       if (codes) {
         pack_scales();
         ksb[0] = __builtin_amdgcn_readlane(ks_l, 0);
@@ -3127,8 +3133,10 @@ __attribute__((amdgpu_num_vgpr(256))) void attn_wave_kernel(
     }
     issue_tile(j0, b[0], ksb[0], vsb[0]);
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(TL) : "memory");   // the queries are in
-    // (of a quad's rows each lane computes two of a chunk's eight rotation angles
-    // and takes the rest from its neighbours)
+    // With G a multiple of 4 the four lanes of a quad hold rows of one position
+    // and the same dims: each computes two of a chunk's eight rotation angles
+    // and takes the rest from its neighbours.
+    const bool quad = (G & 3) == 0;
     constexpr int RJ = 64 / CPP;                           // rows of a job
     const int jobs = (min(nq - row0, 32) + RJ - 1) / RJ;   // none for rows of padding only
 #pragma unroll 1
