@@ -1635,7 +1635,7 @@ __global__ __launch_bounds__(256) void attn_bf16_combine_kernel(AttnArgs a, int 
 //   slots of a dim, the operands of two products.
 //   Measured, calls with 64 query rows per KV head and 8 heads of 128: 16 sequences of
 //   16K-32K positions in 5 layers 792 us, 5.1 TB/s of codes (the loads alone 746, the
-//   arithmetic alone 491); 32 of 512-8192 85 us, of which the merge of 8 MB to 33 MB of
+//   arithmetic alone 491); 32 of 512-8192 85 us, of which the merge of 33 MB of
 //   records 11; one of 2048 16 us.  Bound by the loads, 2 KiB or 1 KiB of a page at a
 //   time, and in short calls by the chain of lengths, page ids and first tiles.
 // S^T takes its rows from two pages in turn, four slots each: lane l holds the 16 keys

@@ -19,7 +19,7 @@ import paper_2609_14717_amd as co  # noqa: E402
 from helpers import gather_carry, head_err  # noqa: E402
 from oracle import PAGE, SKIP, serve8  # noqa: E402
 from synth.scenario import Scenario, Scenario8  # noqa: E402
-from test_gpu_serve8 import TOL, check_cache, ints, np_, space, zero  # noqa: E402
+from test_gpu_serve8 import TOL, check_cache, ints, np_, space  # noqa: E402
 
 BASE = wl.RAGGED32.replace(S=5, L=2, Dcat=256, d=128, ctx_lo=20, ctx_hi=400, rounds=6,
                            accept=("geom", 0.25))
