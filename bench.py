@@ -249,8 +249,8 @@ def summarize_pmc(args):
              f"copy WRITE_SIZE KiB: {cw:.1f}  (factor {w_fac:.4f})"]
     tot = 0.0
     for kn in ATTN_KERNELS:
-        if not any(k[1] == "FETCH_SIZE" and kn in k[0] for k in fetch):
-            continue                            # a kernel this workload does not launch
+        if not any(k[1] == "FETCH_SIZE" and kn in k[0] and is_plain(k[0]) for k in fetch):
+            continue                            # a kernel this workload's attention does not launch
         kf, nf = one(fetch, "FETCH_SIZE", kn, win)
         kw, nw = one(write, "WRITE_SIZE", kn, win)
         b = kf * 1024.0 * f_fac + kw * 1024.0 * w_fac
