@@ -227,8 +227,8 @@ constexpr int kAssignHdr = 4;             // released, taken, free + released
 // One workgroup assigns up to so many sequences with so many table entries.  The host
 // cannot see how many pages move: where few do (a decoding step) one launch is better, a
 // step that ends and admits half of the requests takes it longer (us, graph replays,
-// one launch against two): 16K entries 3.9 / 5.6 where few move, 9.5 / 6.2 where half do;
-// 66K entries 5.5 / 5.8 and 23.7 / 6.4.
+// one launch against two): 16K entries 4.1 / 5.6 where few move, 9.5 / 6.2 where half do;
+// 32K entries 4.1 / 5.7 and 17.7 / 6.5; 66K entries 5.5 / 5.8 and 23.7 / 6.4.
 constexpr int kAssignSeqs = 1024;
 constexpr int kAssignPlaces = 32768;
 constexpr int kMaxAssign = 1 << 23;       // sequences, and pages of one, that a grid can cover

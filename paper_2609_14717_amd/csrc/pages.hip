@@ -139,16 +139,24 @@ __device__ __forceinline__ void move_page(const PagesArgs& a, const Moves& m, in
   }
 }
 
-// Both steps in one workgroup: wavefront w moves the pages of sequences w, w + 16, ...
+// Both steps in one workgroup: a power of two of threads to each sequence, so many that all
+// sequences have theirs in up to kTurns turns.  A turn and a thread's move are chains of loads: fewer
+// turns suit steps where few pages move, more threads per sequence those where whole
+// requests do.  Two turns against four (us, graph replays): 64 sequences of 512-8000
+// positions in a decoding step 4.1 / 4.5, all changed 17.7 / 13.7; 634 of 50-178, all changed, 8.7 / 7.9
+// (a wavefront per sequence, 40 turns: 24).
+constexpr int kTurns = 2;
+
 __global__ __launch_bounds__(kScanThreads) void assign_pages_kernel(PagesArgs a) {
   __shared__ int sh[32], lds[4 * kAssignSeqs];
   Moves m{lds, lds + kAssignSeqs, lds + 2 * kAssignSeqs, lds + 3 * kAssignSeqs, 0, 0, 0};
   number_moves(a, m, sh);
   __syncthreads();
-  const int lane = threadIdx.x & 63;
-  for (int s = threadIdx.x >> 6; s < a.S; s += kScanThreads / 64) {
+  const int w = min(31 - __clz(kScanThreads), 31 - __clz(kTurns * kScanThreads / a.S));   // S: 1 .. kAssignSeqs
+  static_assert(kAssignSeqs <= kScanThreads, "a thread at least");
+  for (int s = threadIdx.x >> w; s < a.S; s += kScanThreads >> w) {
     const int lo = m.lo[s], hi = m.hi[s], first = m.first[s];
-    for (int p = lo + lane; p < hi; p += 64) move_page(a, m, s, p, lo, first);
+    for (int p = lo + (threadIdx.x & ((1 << w) - 1)); p < hi; p += 1 << w) move_page(a, m, s, p, lo, first);
   }
 }
 
