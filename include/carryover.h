@@ -607,7 +607,7 @@ co_status carryover_read_status(const co_state* state, int32_t* host_out, hipStr
  *   CO_TUNE_ATTN_WAVE               bf16 attention by streams (1: one or two wavefronts
  *                                   walk a slice of the keys) or by the persistent
  *                                   kernel (0)
- *   CO_TUNE_ATTN_WORKGROUPS         bf16 attention workgroups (or slices)
+ *   CO_TUNE_ATTN_WORKGROUPS         bf16 and 8-bit attention workgroups (or slices)
  *   CO_TUNE_ATTN_ROUND_TILES        tiles per wavefront per round, persistent
  *                                   attention kernel
  *   CO_TUNE_ATTN_GROUP_SPLIT_TILES  committed tiles per share, grouped-prefix
