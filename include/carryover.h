@@ -507,9 +507,9 @@ co_status carryover_assign_pages(const co_dims* dims, const int32_t* want_len, i
  * changed); row_pos, row_dst int32 [num_rows].  Only num_seqs,
  * max_pages_per_seq and num_pages of dims are used (the rest must still be
  * valid).  Device errors, written to *status; the row then gets INT32_MIN and 0:
- * CO_ERR_LENGTH (pos0 < 0, or a start that decreases), CO_ERR_CAPACITY (a
- * position >= max_pages_per_seq * 16), CO_ERR_PAGE_RANGE (a page id outside
- * [0, num_pages)).  Host: num_pages * 16 below 2^31 (CO_ERR_UNSUPPORTED).
+ * CO_ERR_LENGTH (pos0 < 0), CO_ERR_CAPACITY (a position >= max_pages_per_seq *
+ * 16), CO_ERR_PAGE_RANGE (a page id outside [0, num_pages)).  With a start that
+ * decreases (CO_ERR_LENGTH) every row gets them.  Host: num_pages * 16 below 2^31 (CO_ERR_UNSUPPORTED).
  */
 co_status carryover_slot_map(const co_dims* dims, int32_t num_rows, const int32_t* row_start,
                              const int32_t* pos0, const int32_t* page_table, int32_t* row_pos,

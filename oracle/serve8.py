@@ -158,6 +158,8 @@ def assign_pages(want, reserve, table, held, free, max_pages, num_pages):
 def slot_map(num_rows, row_start, pos0, table, max_pages, num_pages):
     """(row_pos, row_dst, status) of packed rows."""
     pos, dst, status = np.zeros(num_rows, np.int32), np.full(num_rows, SKIP, np.int32), OK
+    if any(int(a) > int(b) for a, b in zip(row_start, row_start[1:])):
+        return pos, dst, ERR_LENGTH      # which row is whose is not defined
     for s in range(len(pos0)):
         for r in range(int(row_start[s]), min(num_rows, int(row_start[s + 1]))):
             p = int(pos0[s]) + r - int(row_start[s])

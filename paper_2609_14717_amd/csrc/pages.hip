@@ -190,14 +190,30 @@ __global__ __launch_bounds__(256) void assign_move_kernel(PagesArgs a) {
 
 // Position and slot of packed rows: row r belongs to the last sequence that
 // starts at or before it.  A thread takes kSlotRows rows in a row: one search, then
-// steps over the sequences' ends.  LDS: the starts fit there.
+// steps over the sequences' ends.  LDS: the starts fit there, and every workgroup
+// sees whether one decreases: no row gets a slot then, for which row is whose is not
+// defined (beyond, slot_starts_kernel looks afterwards).
 template <bool LDS>
 __global__ __launch_bounds__(kSlotThreads) void slot_map_kernel(SlotMapArgs a) {
   __shared__ int32_t lds[LDS ? kSlotSeqs + 1 : 1];
   const int32_t* start = a.row_start;
+  bool bad = false;
   if constexpr (LDS) {
-    for (int i = threadIdx.x; i <= a.S; i += kSlotThreads) lds[i] = a.row_start[i];
+    __shared__ int down[kSlotThreads / 64];   // a word per wavefront: one barrier for all
+    const int lane = threadIdx.x & 63;
+    bool mine = false;
+#pragma unroll 4
+    for (int i = threadIdx.x; i <= a.S; i += kSlotThreads) {
+      const int32_t v = a.row_start[i], before = a.row_start[max(i - 1, 0)];
+      lds[i] = v;
+      mine |= before > v;
+    }
+    const bool any = __any(mine);
+    if (lane == 0) down[threadIdx.x >> 6] = any;
     __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kSlotThreads / 64; ++w) bad |= down[w] != 0;
+    if (bad && threadIdx.x == 0) set_status(a.status, CO_ERR_LENGTH);
     start = lds;
   }
   const int64_t r0 = (static_cast<int64_t>(blockIdx.x) * kSlotThreads + threadIdx.x) * kSlotRows;
@@ -215,12 +231,12 @@ __global__ __launch_bounds__(kSlotThreads) void slot_map_kernel(SlotMapArgs a) {
     const int64_t r = r0 + i;
     pos[i] = 0;
     dst[i] = kSkip;
-    if (r >= a.num_rows) continue;
+    if (bad || r >= a.num_rows) continue;
     while (s < a.S && start[s + 1] <= r) ++s;
     if (s < 0 || s >= a.S) continue;   // (rows before the first sequence and behind the last)
     const int32_t p0 = a.pos0[s];
     const int64_t p = p0 + (r - start[s]);
-    if (p0 < 0 || r < start[s]) {
+    if (p0 < 0) {
       set_status(a.status, CO_ERR_LENGTH);
     } else if (p >= static_cast<int64_t>(a.max_pages) * kPage) {
       set_status(a.status, CO_ERR_CAPACITY);
@@ -249,6 +265,21 @@ __global__ __launch_bounds__(kSlotThreads) void slot_map_kernel(SlotMapArgs a) {
   }
 }
 
+// Starts that do not fit in LDS, behind the map: a thread per start looks for one that
+// decreases.  The workgroup of the first such start takes every row's slot back.
+__global__ __launch_bounds__(kSlotThreads) void slot_starts_kernel(SlotMapArgs a) {
+  const int i0 = blockIdx.x * kSlotThreads, i = i0 + threadIdx.x;   // S: at most 2^30
+  auto falls = [&](int k) { return a.row_start[k] > a.row_start[k + 1]; };
+  if (!__syncthreads_or(i < a.S && falls(i) ? 1 : 0)) return;
+  if (threadIdx.x == 0) set_status(a.status, CO_ERR_LENGTH);
+  for (int k0 = 0; k0 < i0; k0 += kSlotThreads)
+    if (__syncthreads_or(falls(k0 + static_cast<int>(threadIdx.x)) ? 1 : 0)) return;
+  for (int64_t r = threadIdx.x; r < a.num_rows; r += kSlotThreads) {
+    a.row_pos[r] = 0;
+    a.row_dst[r] = kSkip;
+  }
+}
+
 }  // namespace
 
 size_t assign_ws_bytes(int S) {
@@ -274,8 +305,15 @@ hipError_t launch_slot_map(const SlotMapArgs& a, hipStream_t stream) {
   if (a.num_rows == 0) return hipSuccess;
   const int per = kSlotThreads * kSlotRows;
   const dim3 grid((a.num_rows + per - 1) / per);
-  if (a.S <= kSlotSeqs) hipLaunchKernelGGL(slot_map_kernel<true>, grid, dim3(kSlotThreads), 0, stream, a);
-  else hipLaunchKernelGGL(slot_map_kernel<false>, grid, dim3(kSlotThreads), 0, stream, a);
+  if (a.S <= kSlotSeqs) {
+    hipLaunchKernelGGL(slot_map_kernel<true>, grid, dim3(kSlotThreads), 0, stream, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(slot_map_kernel<false>, grid, dim3(kSlotThreads), 0, stream, a);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  const unsigned blocks = (static_cast<unsigned>(a.S) + kSlotThreads - 1) / kSlotThreads;
+  hipLaunchKernelGGL(slot_starts_kernel, dim3(blocks), dim3(kSlotThreads), 0, stream, a);
   return hipGetLastError();
 }
 

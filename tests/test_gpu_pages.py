@@ -1,0 +1,57 @@
+"""GPU: page tables and slot maps where their inputs are at the edge of what the entry
+points take, against the oracle (whole numbers, equal)."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import paper_2609_14717_amd as co  # noqa: E402
+from oracle import serve8  # noqa: E402
+from test_gpu_serve8 import dims, ints, np_, zero  # noqa: E402
+
+
+def map_slots(start, pos0, table, rows, num_pages):
+    """row_pos, row_dst (one entry more than the rows) and the status of one call."""
+    d, status = dims(len(pos0), np.shape(table)[1], num_pages), zero()
+    pos, dst = torch.full((2, rows + 1), 77, dtype=torch.int32, device="cuda")
+    co.carryover_slot_map(d, rows, ints(start), ints(pos0), ints(table), pos, dst, status)
+    assert int(pos[rows]) == int(dst[rows]) == 77
+    return np_(pos)[:rows], np_(dst)[:rows], int(status)
+
+
+# sequences on both sides of what fits in LDS; the start that falls at any place of a group
+# of four rows, of a workgroup's threads, and the last one
+FALLS = [(S, at) for S in (2, 37, 4096, 4097, 9000)
+         for at in sorted({1, 2, 3, 6, 255, 256, 257, 4095, S}) if at <= S]
+
+
+@pytest.mark.parametrize("S,at", FALLS)
+@pytest.mark.parametrize("by", [1, 40])
+def test_starts_that_decrease_give_no_row_a_slot(S, at, by):
+    lengths = np.random.RandomState(S).randint(0, 4, S)
+    lengths[at - 1] = 3
+    start = np.concatenate([[0], np.cumsum(lengths)])
+    table = np.arange(S * 4).reshape(S, 4)
+    pos0 = np.arange(S) % 5
+    rows = int(start[-1])
+    want = serve8.slot_map(rows, start, pos0, table, 4, S * 4)
+    got = map_slots(start, pos0, table, rows, S * 4)
+    assert got[2] == want[2] == 0
+    np.testing.assert_array_equal(got[1], want[1])
+    start[at:] -= lengths[at - 1] + by                       # the sequence's end, before its start
+    start += max(0, -int(start.min()))
+    got = map_slots(start, pos0, table, rows, S * 4)
+    want = serve8.slot_map(rows, start, pos0, table, 4, S * 4)
+    assert got[2] == want[2] == co.CO_ERR_LENGTH
+    np.testing.assert_array_equal(got[0], want[0])
+    np.testing.assert_array_equal(got[1], want[1])
+
+
+def test_starts_that_decrease_more_than_once():
+    start = list(range(0, 6000)) + [5, 900, 7] + list(range(9000, 12000))
+    S = len(start) - 1
+    pos, dst, st = map_slots(start, [0] * S, np.zeros((S, 600), int), 9000, 1)
+    assert st == co.CO_ERR_LENGTH
+    assert np.all(pos == 0) and np.all(dst == serve8.SKIP)

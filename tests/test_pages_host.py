@@ -1,0 +1,12 @@
+"""Page tables and slot maps without a GPU: pins of the oracle's answers to inputs that the
+entry points report."""
+from oracle import SKIP, serve8
+
+
+def test_starts_that_decrease_give_no_row_a_slot():
+    table = [[0, 1], [2, 3], [4, 5]]
+    for start in ([0, 6, 2, 8], [3, 0, 4, 8], [0, 4, 8, 7]):
+        pos, dst, st = serve8.slot_map(8, start, [0, 0, 0], table, 2, 6)
+        assert st == serve8.ERR_LENGTH
+        assert pos.tolist() == [0] * 8 and dst.tolist() == [SKIP] * 8
+    assert serve8.slot_map(8, [0, 4, 4, 8], [0, 0, 0], table, 2, 6)[2] == serve8.OK
