@@ -304,7 +304,7 @@ hipError_t launch_assign_pages(const PagesArgs& a, hipStream_t stream) {
 hipError_t launch_slot_map(const SlotMapArgs& a, hipStream_t stream) {
   if (a.num_rows == 0) return hipSuccess;
   const int per = kSlotThreads * kSlotRows;
-  const dim3 grid((a.num_rows + per - 1) / per);
+  const dim3 grid((static_cast<unsigned>(a.num_rows) + per - 1) / per);   // (past 2^31 - per rows too)
   if (a.S <= kSlotSeqs) {
     hipLaunchKernelGGL(slot_map_kernel<true>, grid, dim3(kSlotThreads), 0, stream, a);
     return hipGetLastError();

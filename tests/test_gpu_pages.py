@@ -55,3 +55,21 @@ def test_starts_that_decrease_more_than_once():
     pos, dst, st = map_slots(start, [0] * S, np.zeros((S, 600), int), 9000, 1)
     assert st == co.CO_ERR_LENGTH
     assert np.all(pos == 0) and np.all(dst == serve8.SKIP)
+
+
+def test_as_many_rows_as_an_int_counts():
+    """The row count's last workgroup lies past 2^31 rows; all but a few rows are padding."""
+    rows = 2 ** 31 - 1
+    d, status = dims(2, 2, 4), zero()
+    pos, dst = (torch.full((rows + 1,), 77, dtype=torch.int32, device="cuda") for _ in range(2))
+    start = [rows - 30, rows - 25, rows - 1]
+    co.carryover_slot_map(d, rows, ints(start), ints([3, 0]), ints([[3, 1], [0, 2]]), pos, dst, status)
+    wp, wd, st = serve8.slot_map(40, [10, 15, 39], [3, 0], [[3, 1], [0, 2]], 2, 4)   # the last forty
+    assert int(status) == st == 0
+    np.testing.assert_array_equal(np_(pos[-41:-1]), wp)
+    np.testing.assert_array_equal(np_(dst[-41:-1]), wd)
+    assert int(pos[-1]) == int(dst[-1]) == 77
+    for a in range(0, rows - 40, 1 << 28):
+        part = slice(a, min(a + (1 << 28), rows - 40))
+        assert int(pos[part].count_nonzero()) == 0
+        assert int((dst[part] != serve8.SKIP).count_nonzero()) == 0
