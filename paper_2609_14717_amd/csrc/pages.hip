@@ -190,7 +190,7 @@ __global__ __launch_bounds__(256) void assign_move_kernel(PagesArgs a) {
 
 // Position and slot of packed rows: row r belongs to the last sequence that
 // starts at or before it.  A thread takes kSlotRows rows in a row: one search, then
-// steps over the sequences' ends.  LDS: the starts fit there, and every workgroup
+// on over the sequences' ends.  LDS: the starts fit there, and every workgroup
 // sees whether one decreases: no row gets a slot then, for which row is whose is not
 // defined (beyond, slot_starts_kernel looks afterwards).
 template <bool LDS>
@@ -232,7 +232,18 @@ __global__ __launch_bounds__(kSlotThreads) void slot_map_kernel(SlotMapArgs a) {
     pos[i] = 0;
     dst[i] = kSkip;
     if (bad || r >= a.num_rows) continue;
-    while (s < a.S && start[s + 1] <= r) ++s;
+    // on to the row's sequence by steps that double, then bisected: a run of n
+    // sequences without rows (free slots of a server) costs 2 log n reads
+    int next = min(s + 1, a.S + 1);
+    for (int step = 2; next <= a.S && start[next] <= r; step *= 2) {
+      s = next;
+      next = min(s + step, a.S + 1);
+    }
+    while (next - s > 1) {
+      const int mid = (s + next) >> 1;
+      if (start[mid] <= r) s = mid;
+      else next = mid;
+    }
     if (s < 0 || s >= a.S) continue;   // (rows before the first sequence and behind the last)
     const int32_t p0 = a.pos0[s];
     const int64_t p = p0 + (r - start[s]);

@@ -73,3 +73,44 @@ def test_as_many_rows_as_an_int_counts():
         part = slice(a, min(a + (1 << 28), rows - 40))
         assert int(pos[part].count_nonzero()) == 0
         assert int((dst[part] != serve8.SKIP).count_nonzero()) == 0
+
+
+# free slots of a server: runs of sequences without rows, in front, between and behind, where
+# a thread's four rows begin on either side of the run
+@pytest.mark.parametrize("idle", [1, 2, 3, 5, 8, 100, 2000, 4060, 6000])
+@pytest.mark.parametrize("rows_of", [1, 2, 3, 4, 5])
+def test_rows_on_both_sides_of_idle_sequences(idle, rows_of):
+    r = np.random.RandomState(idle * 8 + rows_of)
+    some = lambda: [rows_of] * 7  # noqa: E731
+    lengths = [0] * 3 + some() + [0] * idle + some() + [0, 0] + some() + [0] * (idle // 3)
+    S = len(lengths)
+    start, pos0 = np.concatenate([[0], np.cumsum(lengths)]) + 1, r.randint(0, 60, S)
+    table = r.permutation(S * 5).reshape(S, 5)
+    rows = int(start[-1]) + 6
+    want = serve8.slot_map(rows, start, pos0, table, 5, S * 5)
+    got = map_slots(start, pos0, table, rows, S * 5)
+    assert got[2] == want[2] == 0
+    np.testing.assert_array_equal(got[0], want[0])
+    np.testing.assert_array_equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("idle", [4000, 1 << 20])
+def test_idle_sequences_are_not_walked(idle):
+    """A walk of one sequence after the other is a chain of that many reads: 0.1 s for a
+    million, 0.2 ms for 4000; the search takes a few microseconds, of which ten times as
+    many are allowed."""
+    start = ints(np.concatenate([[0, 3, 3 + 3], np.full(idle, 6), [9, 12]]))
+    S = len(start) - 1
+    d, status = dims(S, 1, 1), zero()
+    pos, dst = torch.full((2, 12), 77, dtype=torch.int32, device="cuda")
+    table, pos0 = torch.zeros((S, 1), dtype=torch.int32, device="cuda"), torch.zeros_like(start)
+    times = []
+    for _ in range(20):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        co.carryover_slot_map(d, 12, start, pos0, table, pos, dst, status)
+        b.record()
+        b.synchronize()
+        times.append(a.elapsed_time(b) * 1e3)
+    assert np_(pos).tolist() == [0, 1, 2] * 4 and int(status) == 0
+    assert min(times) < 100, times
