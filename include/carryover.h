@@ -81,7 +81,8 @@ enum {
   CO_ERR_TOKEN = 9,         /* device: a proposed token outside [0, vocab)
                                (carryover_verify_sample)                            */
   CO_ERR_POOL = 10          /* device: the page pool has too few free pages, or a free
-                               count that it cannot have (carryover_assign_pages)   */
+                               count or holdings that it cannot have
+                               (carryover_assign_pages)                             */
 };
 
 enum { CO_DTYPE_F32 = 0, CO_DTYPE_BF16 = 1 };
@@ -486,8 +487,9 @@ co_status carryover_import_kv(const co_dims* dims, int32_t seq, int32_t pos0, in
  * want_len, or held outside [0, max_pages_per_seq]), CO_ERR_CAPACITY (need_s >
  * max_pages_per_seq); that sequence stays as it is.  CO_ERR_POOL: sequences are
  * served in order, and from the first whose pages do not fit on, none gets any
- * (sequences that release or keep pages still do); with *free_count outside
- * [0, num_pages] nothing changes.  Calls on one pool must not overlap.
+ * (sequences that release or keep pages still do); with a negative *free_count, or
+ * where *free_count and the released pages are more than num_pages together (holdings
+ * that the pool cannot have), nothing changes.  Calls on one pool must not overlap.
  * Host: num_seqs * max_pages_per_seq and num_pages * 16 below 2^31, num_seqs and
  * max_pages_per_seq below 2^23 (CO_ERR_UNSUPPORTED).
  */

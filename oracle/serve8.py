@@ -134,6 +134,8 @@ def assign_pages(want, reserve, table, held, free, max_pages, num_pages):
         need.append(held[s] if err else n)
     released = [(s, p) for s in range(len(need)) for p in range(need[s], held[s])]
     room = len(free) + len(released)
+    if room > num_pages:                 # holdings that the pool cannot have
+        return table, held, free, status or ERR_POOL
     places, asked = [], 0
     for s in range(len(need)):
         grow = max(0, need[s] - held[s])

@@ -50,7 +50,6 @@ __device__ void number_moves(const PagesArgs& a, Moves& m, int* sh) {
   const int per = (a.S + kScanThreads - 1) / kScanThreads;
   const int s0 = min(a.S, t * per), s1 = min(a.S, s0 + per);
   const int c = a.free_count[0];   // read by every thread before it changes below
-  const bool ok = c >= 0 && c <= a.num_pages;
   int back = 0, more = 0;
   for (int s = s0; s < s1; ++s) {
     const Need n = seq_need(a, s);
@@ -80,6 +79,8 @@ __device__ void number_moves(const PagesArgs& a, Moves& m, int* sh) {
     bx += w < wave ? b : 0;
     mx += w < wave ? g : 0;
   }
+  // free + released, in 64 bits: more than the pool's pages cannot be true, and nothing changes
+  const bool ok = c >= 0 && static_cast<int64_t>(c) + R <= a.num_pages;
   if (!ok && t == 0) set_status(a.status, CO_ERR_POOL);
   const int have = ok ? c + R : 0;
   int T = 0;
@@ -132,10 +133,8 @@ __device__ __forceinline__ void move_page(const PagesArgs& a, const Moves& m, in
       else r = mid;
     }
     a.table[static_cast<int64_t>(l) * a.max_pages + m.lo[l] + k - m.grow[l]] = id;
-  } else if (m.have - 1 - k < a.num_pages) {
-    a.free_pages[m.have - 1 - k] = id;
   } else {
-    set_status(a.status, CO_ERR_POOL);   // more pages than the pool has
+    a.free_pages[m.have - 1 - k] = id;   // (have: at most num_pages)
   }
 }
 

@@ -9,7 +9,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2609_14717_amd as co  # noqa: E402
 from oracle import serve8  # noqa: E402
-from test_gpu_serve8 import dims, ints, np_, zero  # noqa: E402
+from test_gpu_serve8 import Pool, dims, ints, np_, space, zero  # noqa: E402
 
 
 def map_slots(start, pos0, table, rows, num_pages):
@@ -114,3 +114,39 @@ def test_idle_sequences_are_not_walked(idle):
         times.append(a.elapsed_time(b) * 1e3)
     assert np_(pos).tolist() == [0, 1, 2] * 4 and int(status) == 0
     assert min(times) < 100, times
+
+
+# ------------------------------------------------------------- the page pool
+
+# in one launch and in two
+SIZES = pytest.mark.parametrize("max_pages", [8, 11000], ids=["one launch", "two"])
+
+
+@SIZES
+@pytest.mark.parametrize("want", [[0] * 6, [0, 30, 0, 5, 50, 0]])
+def test_holdings_that_the_pool_cannot_have_change_nothing(want, max_pages):
+    """More free and released pages than the pool has: before, the call took the holdings
+    away and left a free count that every later call refuses."""
+    p = Pool(6, max_pages, 20, 1)
+    p.assign([20, 30, 40, 0, 50, 60])
+    p.t["free_count"].fill_(20)                    # every page, and the held ones again
+    before = {k: v.clone() for k, v in p.t.items()}
+    p.status.zero_()
+    co.carryover_assign_pages(p.d, ints(want), 0, p.t, p.status, p.ws)
+    assert int(p.status) == co.CO_ERR_POOL
+    assert all(torch.equal(p.t[k], before[k]) for k in before)
+    p.t["free_count"].fill_(len(p.free))           # the count that it has: the pool serves on
+    p.assign(want)
+    p.assign([20, 30, 40, 0, 50, 60])
+
+
+def test_free_and_released_pages_past_32_bits():
+    S, P = 1024, 2 ** 21 - 1
+    d, status = dims(S, P, 2 ** 27 - 1), zero()
+    pool = dict(page_table=torch.full((S, P), 5, dtype=torch.int32, device="cuda"), held=ints([P] * S),
+                free_pages=torch.full((2 ** 27 - 1,), 6, dtype=torch.int32, device="cuda"),
+                free_count=ints([2 ** 27 - 1]))
+    co.carryover_assign_pages(d, ints([0] * S), 0, pool, status, space(d, co.CO_WS_ASSIGN_PAGES))
+    assert int(status) == co.CO_ERR_POOL
+    assert int(pool["free_count"]) == 2 ** 27 - 1 and int(pool["held"].min()) == P
+    assert int(pool["page_table"].min()) == 5 and int(pool["free_pages"].min()) == 6

@@ -1,5 +1,7 @@
 """Page tables and slot maps without a GPU: pins of the oracle's answers to inputs that the
 entry points report."""
+import numpy as np
+
 from oracle import SKIP, serve8
 
 
@@ -10,3 +12,12 @@ def test_starts_that_decrease_give_no_row_a_slot():
         assert st == serve8.ERR_LENGTH
         assert pos.tolist() == [0] * 8 and dst.tolist() == [SKIP] * 8
     assert serve8.slot_map(8, [0, 4, 4, 8], [0, 0, 0], table, 2, 6)[2] == serve8.OK
+
+
+def test_holdings_that_the_pool_cannot_have_change_nothing():
+    table = np.array([[0, 1], [2, 3]])
+    t, held, free, st = serve8.assign_pages([0, 16], 0, table, [2, 2], [4, 5, 6], 2, 5)
+    assert st == serve8.ERR_POOL and held == [2, 2] and free == [4, 5, 6]
+    np.testing.assert_array_equal(t, table)
+    t, held, free, st = serve8.assign_pages([0, 16], 0, table, [2, 2], [4, 5], 2, 5)
+    assert st == serve8.OK and held == [0, 1] and free == [4, 5, 3, 1, 0]
