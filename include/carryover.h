@@ -489,7 +489,9 @@ co_status carryover_import_kv(const co_dims* dims, int32_t seq, int32_t pos0, in
  * served in order, and from the first whose pages do not fit on, none gets any
  * (sequences that release or keep pages still do); with a negative *free_count, or
  * where *free_count and the released pages are more than num_pages together (holdings
- * that the pool cannot have), nothing changes.  Calls on one pool must not overlap.
+ * that the pool cannot have), nothing changes.  CO_ERR_PAGE_RANGE: an id outside
+ * [0, num_pages) among the entries that changed hands; it moved as the others did.
+ * Calls on one pool must not overlap.
  * Host: num_seqs * max_pages_per_seq and num_pages * 16 below 2^31, num_seqs and
  * max_pages_per_seq below 2^23 (CO_ERR_UNSUPPORTED).
  */

@@ -154,6 +154,9 @@ def assign_pages(want, reserve, table, held, free, max_pages, num_pages):
         free = free[:len(free) - (len(places) - len(pages))]
     else:
         free = free + pages[len(places):][::-1]
+    moved = pages + [int(table[s][p]) for s, p in places]
+    if any(not 0 <= x < num_pages for x in moved):
+        status = status or ERR_PAGE_RANGE
     return table, need, free, status
 
 

@@ -112,16 +112,20 @@ __device__ void number_moves(const PagesArgs& a, Moves& m, int* sh) {
   if (ok && t == 0) a.free_count[0] = have - T;
 }
 
-// Place p of sequence s, in [lo, hi), changes hands.
-__device__ __forceinline__ void move_page(const PagesArgs& a, const Moves& m, int s, int p, int lo,
+// Place p of sequence s, in [lo, hi), changes hands.  An id that is no page's moves as
+// the others do, so that going back undoes it too.  Returns the id (0: none moved here):
+// a thread reports the largest of its ids once, which costs one instruction a move.
+__device__ __forceinline__ uint32_t move_page(const PagesArgs& a, const Moves& m, int s, int p, int lo,
                                           int first) {
   const bool out = first < 0;
   const int k = (first & 0x7FFFFFFF) + p - lo;
   int32_t* at = a.table + static_cast<int64_t>(s) * a.max_pages + p;
   if (!out) {
     // (entries from R on: the rest come with a released page)
-    if (k >= m.released) *at = a.free_pages[m.have - 1 - k];
-    return;
+    if (k < m.released) return 0;
+    const int32_t id = a.free_pages[m.have - 1 - k];
+    *at = id;
+    return id;
   }
   const int32_t id = *at;
   *at = -1;
@@ -136,6 +140,11 @@ __device__ __forceinline__ void move_page(const PagesArgs& a, const Moves& m, in
   } else {
     a.free_pages[m.have - 1 - k] = id;   // (have: at most num_pages)
   }
+  return id;
+}
+
+__device__ __forceinline__ void report_ids(const PagesArgs& a, uint32_t largest) {
+  if (largest >= static_cast<uint32_t>(a.num_pages)) set_status(a.status, CO_ERR_PAGE_RANGE);
 }
 
 // Both steps in one workgroup: a power of two of threads to each sequence, so many that all
@@ -153,10 +162,12 @@ __global__ __launch_bounds__(kScanThreads) void assign_pages_kernel(PagesArgs a)
   __syncthreads();
   const int w = min(31 - __clz(kScanThreads), 31 - __clz(kTurns * kScanThreads / a.S));   // S: 1 .. kAssignSeqs
   static_assert(kAssignSeqs <= kScanThreads, "a thread at least");
+  uint32_t ids = 0;
   for (int s = threadIdx.x >> w; s < a.S; s += kScanThreads >> w) {
     const int lo = m.lo[s], hi = m.hi[s], first = m.first[s];
-    for (int p = lo + (threadIdx.x & ((1 << w) - 1)); p < hi; p += 1 << w) move_page(a, m, s, p, lo, first);
+    for (int p = lo + (threadIdx.x & ((1 << w) - 1)); p < hi; p += 1 << w) ids = max(ids, move_page(a, m, s, p, lo, first));
   }
+  report_ids(a, ids);
 }
 
 // Or in two launches, the moves by a thread per place of the table.
@@ -184,7 +195,7 @@ __global__ __launch_bounds__(256) void assign_move_kernel(PagesArgs a) {
     m.grow = grow;
     __syncthreads();
   }
-  if (p >= lo && p < m.hi[s]) move_page(a, m, s, p, lo, m.first[s]);
+  if (p >= lo && p < m.hi[s]) report_ids(a, move_page(a, m, s, p, lo, m.first[s]));
 }
 
 // Position and slot of packed rows: row r belongs to the last sequence that

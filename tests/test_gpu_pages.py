@@ -150,3 +150,30 @@ def test_free_and_released_pages_past_32_bits():
     assert int(status) == co.CO_ERR_POOL
     assert int(pool["free_count"]) == 2 ** 27 - 1 and int(pool["held"].min()) == P
     assert int(pool["page_table"].min()) == 5 and int(pool["free_pages"].min()) == 6
+
+
+@SIZES
+@pytest.mark.parametrize("bad", [-1, 60, 2 ** 31 - 1, -2 ** 31])
+def test_ids_of_no_page_are_reported_where_they_move(bad, max_pages):
+    """In an entry that a sequence gives back (to another one, and to the free list), and
+    in one that the free list gives."""
+    full, some = [100, 90, 0, 60, 0, 0], [10, 90, 33, 60, 0, 70]
+    for seq, place, then in ((0, 6, some), (0, 6, [0] * 6), (3, 1, [100, 90, 0, 0, 0, 0])):
+        p = Pool(6, max_pages, 60, 1)
+        p.assign(full)
+        assert int(p.status) == 0
+        p.table[seq][place] = bad
+        p.t["page_table"].copy_(ints(p.table))
+        p.assign(then)                                     # compares table, list and status
+        assert int(p.status) == co.CO_ERR_PAGE_RANGE
+        p.assign(full)                                     # and back again, exactly
+        assert int(p.status) == co.CO_ERR_PAGE_RANGE and int(p.table[seq][place]) == bad
+        p.assign([100, 90, 0, 60, 0, 0])                   # nothing moves: nothing to report
+        assert int(p.status) == 0
+    p = Pool(6, max_pages, 60, 1)
+    p.free[-3] = bad
+    p.t["free_pages"].copy_(ints(p.free))
+    p.assign([1, 1, 0, 0, 0, 0])
+    assert int(p.status) == 0
+    p.assign([1, 1, 1, 0, 0, 0])
+    assert int(p.status) == co.CO_ERR_PAGE_RANGE

@@ -21,3 +21,14 @@ def test_holdings_that_the_pool_cannot_have_change_nothing():
     np.testing.assert_array_equal(t, table)
     t, held, free, st = serve8.assign_pages([0, 16], 0, table, [2, 2], [4, 5], 2, 5)
     assert st == serve8.OK and held == [0, 1] and free == [4, 5, 3, 1, 0]
+
+
+def test_ids_of_no_page_are_reported_where_they_move():
+    table = np.array([[0, -1], [2, 3]])
+    t, held, free, st = serve8.assign_pages([1, 0], 0, table, [2, 2], [4, 9], 2, 6)
+    assert st == serve8.ERR_PAGE_RANGE and held == [1, 0] and free == [4, 9, 3, 2, -1]
+    t, held, free, st = serve8.assign_pages([17, 32], 0, t, held, free, 2, 6)
+    assert st == serve8.ERR_PAGE_RANGE and held == [2, 2] and free == [4, 9]
+    np.testing.assert_array_equal(t, table)
+    t, held, free, st = serve8.assign_pages([1, 32], 0, [[0, 1], [2, 3]], [2, 2], [4, 9], 2, 6)
+    assert st == serve8.OK                        # the free list's 9 stays where it is
