@@ -144,10 +144,15 @@ bool cache_ok(const co_kv8* c) {
 co_status check_kv8_dims(const co_dims* d) {
   if (d->dtype != CO_DTYPE_BF16) return CO_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(d->num_layers) * d->num_kv_heads > 65535 ||
-      d->num_pages > INT32_MAX / kPage ||
-      static_cast<int64_t>(d->num_seqs) * d->block >= kMaxStoreRows)
+      d->num_pages > INT32_MAX / kPage)
     return CO_ERR_UNSUPPORTED;
   return CO_OK;
+}
+
+// And of those that store a window's rows.
+co_status check_project_kv8_dims(const co_dims* d) {
+  if (static_cast<int64_t>(d->num_seqs) * d->block >= kMaxStoreRows) return CO_ERR_UNSUPPORTED;
+  return check_kv8_dims(d);
 }
 
 // Projected rows of the committed segment on their way into the 8-bit cache: the
@@ -181,7 +186,8 @@ co_status check_attention_kv8_dims(const co_dims* d) {
   const co_status s = check_kv8_dims(d);
   if (s != CO_OK) return s;
   const int64_t nq = static_cast<int64_t>(d->block) * (d->num_q_heads / d->num_kv_heads);
-  return nq <= 64 && attention_kv8_plan(d).ok ? CO_OK : CO_ERR_UNSUPPORTED;
+  return nq <= 64 && d->num_seqs <= kMaxAttnSeqs && attention_kv8_plan(d).ok ? CO_OK
+                                                                             : CO_ERR_UNSUPPORTED;
 }
 
 co_status hip_status(hipError_t e) { return e == hipSuccess ? CO_OK : CO_ERR_HIP; }
@@ -400,7 +406,7 @@ size_t carryover_workspace_bytes(const co_dims* dims, int32_t which) {
                                      dims->head_dim, num_cus())
                  : 0;
     case CO_WS_PROJECT_KV8:
-      return check_kv8_dims(dims) == CO_OK ? pw + 2 * rows_bytes(dims) : 0;
+      return check_project_kv8_dims(dims) == CO_OK ? pw + 2 * rows_bytes(dims) : 0;
     case CO_WS_ATTENTION_KV8:
     case CO_WS_ROUND_KV8: {
       if (check_attention_kv8_dims(dims) != CO_OK) return 0;
@@ -834,7 +840,7 @@ co_status carryover_project_kv8(const co_dims* dims, const co_weights* w, const 
                                 void* ws, size_t ws_bytes, hipStream_t stream) {
   co_status s = check_dims(dims);
   if (s != CO_OK) return s;
-  if ((s = check_kv8_dims(dims)) != CO_OK) return s;
+  if ((s = check_project_kv8_dims(dims)) != CO_OK) return s;
   if (!cache_ok(cache)) return CO_ERR_INVALID_ARG;
   if ((s = validate_project(dims, w, hidden, route, state, ws, ws_bytes, true)) != CO_OK) return s;
   ProjectArgs pa = project_args(dims, w, hidden, route, state, ws);
@@ -864,7 +870,7 @@ co_status carryover_round_kv8(const co_dims* dims, const co_weights* w, const vo
                               hipStream_t stream) {
   co_status s = check_dims(dims);
   if (s != CO_OK) return s;
-  if ((s = check_kv8_dims(dims)) != CO_OK) return s;
+  if ((s = check_project_kv8_dims(dims)) != CO_OK) return s;
   if ((s = validate_route(dims, draft_tok, target_tok, flags, state, scratch)) != CO_OK) return s;
   if (!cache_ok(cache)) return CO_ERR_INVALID_ARG;
   if ((s = validate_project(dims, w, hidden, scratch, state, ws, ws_bytes, true)) != CO_OK) return s;
