@@ -16,4 +16,4 @@ def test_a_store_is_bounded_by_its_own_rows():
         assert _rc(project, d) == _rc(round_, d) == _rc(attend, d) == co.CO_ERR_UNSUPPORTED
         for which in (co.CO_WS_PROJECT_KV8, co.CO_WS_ATTENTION_KV8, co.CO_WS_ROUND_KV8):
             assert co.workspace_bytes(d, which) == 0
-    assert _rc(store, _dims(S=1 << 30, B=1), n=0) == co.CO_OK
+    assert _rc(store, _dims(S=(1 << 30) - 1, B=1), n=0) == co.CO_OK    # every call's bound
