@@ -93,6 +93,10 @@ co_status check_attention_dims(const co_dims* d) {
   return attention_plan(d).ok ? CO_OK : CO_ERR_UNSUPPORTED;
 }
 
+bool layers_ok(const co_dims* d, int32_t begin, int32_t count) {   // (their sum may pass 32 bits)
+  return begin >= 0 && count >= 0 && count <= d->num_layers - begin;
+}
+
 size_t elem_bytes(const co_dims* d) { return d->dtype == CO_DTYPE_BF16 ? 2 : 4; }
 
 int carry_pages(const co_dims* d) { return (d->block + kPage - 1) / kPage; }
@@ -232,7 +236,7 @@ co_status validate_attention(const co_dims* d, int32_t layer_begin, int32_t laye
                              const void* ws, size_t ws_bytes) {
   co_status s = check_attention_dims(d);
   if (s != CO_OK) return s;
-  if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > d->num_layers)
+  if (!layers_ok(d, layer_begin, layer_count))
     return CO_ERR_INVALID_ARG;
   if (!q || !out || !state_ok(st) || !aligned(q, 16) || !aligned(out, 16) ||
       (lse && !aligned(lse, 4)))
@@ -304,7 +308,7 @@ co_status validate_attention_kv8(const co_dims* d, int32_t layer_begin, int32_t 
                                  size_t ws_bytes) {
   co_status s = check_attention_kv8_dims(d);
   if (s != CO_OK) return s;
-  if (layer_begin < 0 || layer_count < 0 || layer_count > d->num_layers - layer_begin)
+  if (!layers_ok(d, layer_begin, layer_count))
     return CO_ERR_INVALID_ARG;
   if (!q || !out || !state_ok_kv8(st) || !cache_ok(cache) || !aligned(q, 16) ||
       !aligned(out, 16) || !aligned(lse, 4) || !aligned(mass, 4) ||
@@ -508,8 +512,7 @@ co_status drafter_block_attention_backward(
   if (dims->dtype != CO_DTYPE_BF16 || dims->head_dim != 64 ||
       dims->block * (dims->num_q_heads / dims->num_kv_heads) > 32)
     return CO_ERR_UNSUPPORTED;
-  if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > dims->num_layers ||
-      seqs_per_group < 1)
+  if (!layers_ok(dims, layer_begin, layer_count) || seqs_per_group < 1)
     return CO_ERR_INVALID_ARG;
   if (!q || !out || !lse || !d_out || !d_q || !d_k_cache || !d_v_cache || !d_k_carry ||
       !d_v_carry || !state_ok(state) || !aligned(q, 16) || !aligned(out, 16) ||
@@ -615,7 +618,7 @@ co_status drafter_carry_mass(const co_dims* dims, int32_t layer_begin, int32_t l
   if (s != CO_OK) return s;
   if ((s = check_attention_dims(dims)) != CO_OK) return s;
   if (dims->block > kMaxCarryRows) return CO_ERR_UNSUPPORTED;
-  if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > dims->num_layers)
+  if (!layers_ok(dims, layer_begin, layer_count))
     return CO_ERR_INVALID_ARG;
   if (!q || !lse || !mass || !state_ok_kv8(state) || !aligned(q, 16) || !aligned(lse, 4) ||
       !aligned(mass, 4))
@@ -649,7 +652,7 @@ co_status drafter_self_merge(const co_dims* dims, int32_t layer_begin, int32_t l
   if (s != CO_OK) return s;
   if ((s = check_attention_dims(dims)) != CO_OK) return s;
   if (dims->block > kMaxCarryRows) return CO_ERR_UNSUPPORTED;
-  if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > dims->num_layers)
+  if (!layers_ok(dims, layer_begin, layer_count))
     return CO_ERR_INVALID_ARG;
   if (!q || !k_self || !v_self || !out || !lse || !state_ok_kv8(state) || !aligned(q, 16) ||
       !aligned(k_self, 16) || !aligned(v_self, 16) || !aligned(out, 16) || !aligned(lse, 4))

@@ -3,7 +3,7 @@ take (no compute call runs here: no GPU is needed)."""
 import pytest
 
 import paper_2609_14717_amd as co
-from test_serve8_host import _dims, _rc, attend, needs_lib, project, round_, store
+from test_serve8_host import BIG, FAKE, _dims, _rc, _state, attend, needs_lib, project, round_, store
 
 
 @needs_lib
@@ -17,3 +17,28 @@ def test_a_store_is_bounded_by_its_own_rows():
         for which in (co.CO_WS_PROJECT_KV8, co.CO_WS_ATTENTION_KV8, co.CO_WS_ROUND_KV8):
             assert co.workspace_bytes(d, which) == 0
     assert _rc(store, _dims(S=(1 << 30) - 1, B=1), n=0) == co.CO_OK    # every call's bound
+
+
+FULL = dict(_state(), k_cache=FAKE, v_cache=FAKE)
+LAYERS = {
+    "attention": lambda d, l0, n: co.drafter_block_attention(
+        d, l0, n, FAKE, FULL, FAKE, None, 0, FAKE, stream=0, ws_bytes=BIG),
+    "ext": lambda d, l0, n: co.drafter_block_attention_ext(
+        d, l0, n, FAKE, FAKE, FAKE, FULL, FAKE, None, None, 0, FAKE, stream=0, ws_bytes=BIG),
+    "kv8": lambda d, l0, n: attend(d, l0=l0, layers=n),
+    "backward": lambda d, l0, n: co.drafter_block_attention_backward(
+        d, l0, n, FAKE, FULL, FAKE, FAKE, FAKE, 1, *[FAKE] * 5, FAKE, stream=0, ws_bytes=BIG),
+    "mass": lambda d, l0, n: co.drafter_carry_mass(d, l0, n, FAKE, _state(), FAKE, FAKE, stream=0),
+    "merge": lambda d, l0, n: co.drafter_self_merge(
+        d, l0, n, FAKE, FAKE, FAKE, _state(), FAKE, FAKE, stream=0),
+}
+
+
+@needs_lib
+@pytest.mark.parametrize("call", LAYERS.values(), ids=LAYERS)
+def test_layer_ranges_past_32_bits_are_refused_by_every_call(call):
+    big, d = 2 ** 31 - 1, _dims(L=3)
+    for l0, n in ((0, 4), (3, 1), (1, big), (big, 1), (big, big), (big - 1, 3), (-1, 1), (0, -1)):
+        assert _rc(call, d, l0, n) == co.CO_ERR_INVALID_ARG, (l0, n)
+    for l0 in range(4):
+        assert _rc(call, _dims(L=3, S=0), l0, 3 - l0) == co.CO_OK
