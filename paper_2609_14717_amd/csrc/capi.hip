@@ -87,9 +87,13 @@ co_status check_dims(const co_dims* d) {
 
 AttnPlan attention_plan(const co_dims* d);
 
+// Query rows per KV head.
+int64_t query_rows(const co_dims* d) {
+  return static_cast<int64_t>(d->block) * (d->num_q_heads / d->num_kv_heads);
+}
+
 co_status check_attention_dims(const co_dims* d) {
-  const int nq = d->block * (d->num_q_heads / d->num_kv_heads);
-  if (nq > 64) return CO_ERR_UNSUPPORTED;
+  if (query_rows(d) > 64) return CO_ERR_UNSUPPORTED;
   return attention_plan(d).ok ? CO_OK : CO_ERR_UNSUPPORTED;
 }
 
@@ -189,8 +193,7 @@ AttnPlan attention_kv8_plan(const co_dims* d) {
 co_status check_attention_kv8_dims(const co_dims* d) {
   const co_status s = check_kv8_dims(d);
   if (s != CO_OK) return s;
-  const int64_t nq = static_cast<int64_t>(d->block) * (d->num_q_heads / d->num_kv_heads);
-  return nq <= 64 && d->num_seqs <= kMaxAttnSeqs && attention_kv8_plan(d).ok ? CO_OK
+  return query_rows(d) <= 64 && d->num_seqs <= kMaxAttnSeqs && attention_kv8_plan(d).ok ? CO_OK
                                                                              : CO_ERR_UNSUPPORTED;
 }
 
@@ -509,8 +512,7 @@ co_status drafter_block_attention_backward(
     float* d_v_carry, uint32_t flags, void* ws, size_t ws_bytes, hipStream_t stream) {
   co_status s = check_dims(dims);
   if (s != CO_OK) return s;
-  if (dims->dtype != CO_DTYPE_BF16 || dims->head_dim != 64 ||
-      dims->block * (dims->num_q_heads / dims->num_kv_heads) > 32)
+  if (dims->dtype != CO_DTYPE_BF16 || dims->head_dim != 64 || query_rows(dims) > 32)
     return CO_ERR_UNSUPPORTED;
   if (!layers_ok(dims, layer_begin, layer_count) || seqs_per_group < 1)
     return CO_ERR_INVALID_ARG;

@@ -42,3 +42,15 @@ def test_layer_ranges_past_32_bits_are_refused_by_every_call(call):
         assert _rc(call, d, l0, n) == co.CO_ERR_INVALID_ARG, (l0, n)
     for l0 in range(4):
         assert _rc(call, _dims(L=3, S=0), l0, 3 - l0) == co.CO_OK
+
+
+@needs_lib
+@pytest.mark.parametrize("call", LAYERS.values(), ids=LAYERS)
+@pytest.mark.parametrize("S", [0, 1])
+def test_query_rows_past_32_bits_are_refused(call, S):
+    """block * heads of a group = 2^32 and 2^32 + 17: neither no row nor 17."""
+    for B, G in ((1 << 29, 8), (1 << 28, 16), (613566759, 7)):
+        d = _dims(S=S, B=B, Hq=G, Hkv=1)
+        assert _rc(call, d, 0, 1) == co.CO_ERR_UNSUPPORTED, (B, G)
+        for which in (co.CO_WS_ATTENTION, co.CO_WS_ROUND, co.CO_WS_ATTENTION_KV8, co.CO_WS_ROUND_KV8):
+            assert co.workspace_bytes(d, which) == 0
