@@ -61,7 +61,8 @@ __device__ __forceinline__ bool z_row_selected(int z_rows, int32_t dst) {
 
 // ------------------------------------------------------------ bf16 MFMA GEMM
 
-template <int BM, int BN, int WM, int WN, int NSTAGE, bool HAS_E>
+// PLAIN: K/V mode with committed rows to KvDest::k_rows, v_rows (here and below).
+template <int BM, int BN, int WM, int WN, int NSTAGE, bool HAS_E, bool PLAIN = false>
 __global__ __launch_bounds__(256) void gemm_bf16_kernel(GemmArgs g) {
   constexpr int BK = 128;                 // K elements per stage
   constexpr int ROWB = BK * 2;            // bytes per staged row
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(256) void gemm_bf16_kernel(GemmArgs g) {
       }
       // the hd/8 lanes of a head segment are consecutive and take the same branches
       k_norm<4>(g.kv, gc0 / hd, i0, q_per_seg, lo, hi);
-      kv_store<uint16_t, 4>(g.kv, gr, dst_lds[row], pos_lds[row], gc0 / hd, i0, lo, hi, inv_tab);
+      kv_store<uint16_t, 4, PLAIN>(g.kv, gr, dst_lds[row], pos_lds[row], gc0 / hd, i0, lo, hi, inv_tab);
     }
   }
 }
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(256) void gemm_bf16_kernel(GemmArgs g) {
 // main loop carries no E at all.  Workgroup ids are renumbered so that each
 // XCD (ids congruent mod 8) works on consecutive tiles, which share the same
 // A panel and K range.
-template <int TMW, int TNW, int BK, int NS, bool HAS_E, int WGN>
+template <int TMW, int TNW, int BK, int NS, bool HAS_E, int WGN, bool PLAIN = false>
 __global__ __launch_bounds__(128 * WGN, 1) void gemm_wide_kernel(GemmArgs g, int tiles_m, int tiles_n) {
   constexpr int NW = 2 * WGN, NT = 64 * NW;        // wavefronts, threads
   constexpr int ROWB = 2 * BK;                     // bytes per staged row
@@ -627,7 +628,7 @@ __global__ __launch_bounds__(128 * WGN, 1) void gemm_wide_kernel(GemmArgs g, int
           hi[pp] = sc[rl * LDC + seg_local * hd + hd / 2 + i0 + pp];
         }
         k_norm<4>(g.kv, gc0 / hd, i0, q_per_seg, lo, hi);   // hd/8 consecutive lanes per segment
-        kv_store<uint16_t, 4>(g.kv, gr, dst_lds[row], pos_lds[row], gc0 / hd, i0, lo, hi, inv_tab);
+        kv_store<uint16_t, 4, PLAIN>(g.kv, gr, dst_lds[row], pos_lds[row], gc0 / hd, i0, lo, hi, inv_tab);
       }
     }
     __syncthreads();
@@ -816,6 +817,7 @@ constexpr int kFusedD = 256;                 // d and n_kv of the fused path
 constexpr int kFusedBM = 128;                // rows per workgroup
 constexpr int kFusedZLD = kFusedD * 2 + 16;  // bytes per Z row in LDS (padded against conflicts)
 
+template <bool PLAIN>
 __global__ __launch_bounds__(256, 1) void proj_fused_kernel(ProjectArgs a) {
   // F stages are 64 deep (3 in the ring), K/V stages 32 deep (4 in the ring
   // behind the resident Z rows)
@@ -1048,7 +1050,7 @@ __global__ __launch_bounds__(256, 1) void proj_fused_kernel(ProjectArgs a) {
         lo[j] = acc[0][tm][4 * q + j];
         hi[j] = acc[1][tm][4 * q + j];
       }
-      kv_store<uint16_t, 4>(a.dst, row, rdst[tm], rpos[tm], wave, 8 * q + i_base, lo, hi, inv_tab);
+      kv_store<uint16_t, 4, PLAIN>(a.dst, row, rdst[tm], rpos[tm], wave, 8 * q + i_base, lo, hi, inv_tab);
     }
   }
 }
@@ -1174,7 +1176,7 @@ __global__ __launch_bounds__(256) void epi_z_kernel(const float* part, int split
   for (int q = 0; q < 4; ++q) z[i + q] = to_elem<T>(v[q]);
 }
 
-template <typename T>
+template <typename T, bool PLAIN = false>
 __global__ __launch_bounds__(256) void epi_kv_kernel(const float* part, int splits, int M, int N,
                                                      KvDest e) {
   __shared__ double inv_tab[64];
@@ -1194,7 +1196,7 @@ __global__ __launch_bounds__(256) void epi_kv_kernel(const float* part, int spli
     hi += part[static_cast<int64_t>(s) * M * N + c_lo + half];
   }
   k_norm<1>(e, seg, p, half, &lo, &hi);   // a segment's hd/2 pairs: consecutive, aligned lanes
-  kv_store<T, 1>(e, row, e.row_dst[row], e.row_pos[row], seg, p, &lo, &hi, inv_tab);
+  kv_store<T, 1, PLAIN>(e, row, e.row_dst[row], e.row_pos[row], seg, p, &lo, &hi, inv_tab);
 }
 
 // Tile variants (BM x BN, waves WM x WN, ring depth):
@@ -1205,15 +1207,15 @@ __global__ __launch_bounds__(256) void epi_kv_kernel(const float* part, int spli
 constexpr int kTileBM[4] = {16, 16, 64, 128};
 constexpr int kTileBN[4] = {64, 128, 128, 128};
 
-template <bool HAS_E>
+template <bool HAS_E, bool PLAIN = false>
 hipError_t launch_gemm_bf16_t(const GemmArgs& g, int tile, int splits, hipStream_t stream) {
   const dim3 grid((g.N + kTileBN[tile] - 1) / kTileBN[tile],
                   (g.M + kTileBM[tile] - 1) / kTileBM[tile] + g.route_blocks, splits);
   switch (tile) {
-    case 0: hipLaunchKernelGGL((gemm_bf16_kernel<16, 64, 1, 4, 4, HAS_E>), grid, dim3(256), 0, stream, g); break;
-    case 1: hipLaunchKernelGGL((gemm_bf16_kernel<16, 128, 1, 4, 3, HAS_E>), grid, dim3(256), 0, stream, g); break;
-    case 2: hipLaunchKernelGGL((gemm_bf16_kernel<64, 128, 2, 2, 2, HAS_E>), grid, dim3(256), 0, stream, g); break;
-    default: hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 2, 2, 2, HAS_E>), grid, dim3(256), 0, stream, g); break;
+    case 0: hipLaunchKernelGGL((gemm_bf16_kernel<16, 64, 1, 4, 4, HAS_E, PLAIN>), grid, dim3(256), 0, stream, g); break;
+    case 1: hipLaunchKernelGGL((gemm_bf16_kernel<16, 128, 1, 4, 3, HAS_E, PLAIN>), grid, dim3(256), 0, stream, g); break;
+    case 2: hipLaunchKernelGGL((gemm_bf16_kernel<64, 128, 2, 2, 2, HAS_E, PLAIN>), grid, dim3(256), 0, stream, g); break;
+    default: hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 2, 2, 2, HAS_E, PLAIN>), grid, dim3(256), 0, stream, g); break;
   }
   return hipGetLastError();
 }
@@ -1229,7 +1231,7 @@ constexpr int kWide = 4, kWideVariants = 7;
 constexpr int kWideBM[kWideVariants] = {256, 256, 128, 256, 256, 128, 128};
 constexpr int kWideBN[kWideVariants] = {256, 128, 256, 256, 128, 256, 128};
 
-template <bool HAS_E>
+template <bool HAS_E, bool PLAIN = false>
 hipError_t launch_gemm_wide_t(const GemmArgs& g, int variant, int splits, hipStream_t stream) {
   // in-kernel E keeps a copy of E per wavefront and stage, which fits the LDS
   // with four wavefronts (2 x 2, blocks twice as wide) but not with eight
@@ -1238,18 +1240,21 @@ hipError_t launch_gemm_wide_t(const GemmArgs& g, int variant, int splits, hipStr
   const int tn = (g.N + kWideBN[variant] - 1) / kWideBN[variant];
   const dim3 grid(tm * tn * splits), block(128 * W);
   switch (variant) {
-    case 0: hipLaunchKernelGGL((gemm_wide_kernel<4, 2 * X, 32, 4, HAS_E, W>), grid, block, 0, stream, g, tm, tn); break;
-    case 1: hipLaunchKernelGGL((gemm_wide_kernel<4, X, 32, 4, HAS_E, W>), grid, block, 0, stream, g, tm, tn); break;
-    case 2: hipLaunchKernelGGL((gemm_wide_kernel<2, 2 * X, 32, 4, HAS_E, W>), grid, block, 0, stream, g, tm, tn); break;
-    case 3: hipLaunchKernelGGL((gemm_wide_kernel<4, 2 * X, 64, 2, HAS_E, W>), grid, block, 0, stream, g, tm, tn); break;
-    case 4: hipLaunchKernelGGL((gemm_wide_kernel<4, X, 64, 3, HAS_E, W>), grid, block, 0, stream, g, tm, tn); break;
-    case 5: hipLaunchKernelGGL((gemm_wide_kernel<2, 2 * X, 64, 3, HAS_E, W>), grid, block, 0, stream, g, tm, tn); break;
-    default: hipLaunchKernelGGL((gemm_wide_kernel<2, X, 64, 4, HAS_E, W>), grid, block, 0, stream, g, tm, tn); break;
+    case 0: hipLaunchKernelGGL((gemm_wide_kernel<4, 2 * X, 32, 4, HAS_E, W, PLAIN>), grid, block, 0, stream, g, tm, tn); break;
+    case 1: hipLaunchKernelGGL((gemm_wide_kernel<4, X, 32, 4, HAS_E, W, PLAIN>), grid, block, 0, stream, g, tm, tn); break;
+    case 2: hipLaunchKernelGGL((gemm_wide_kernel<2, 2 * X, 32, 4, HAS_E, W, PLAIN>), grid, block, 0, stream, g, tm, tn); break;
+    case 3: hipLaunchKernelGGL((gemm_wide_kernel<4, 2 * X, 64, 2, HAS_E, W, PLAIN>), grid, block, 0, stream, g, tm, tn); break;
+    case 4: hipLaunchKernelGGL((gemm_wide_kernel<4, X, 64, 3, HAS_E, W, PLAIN>), grid, block, 0, stream, g, tm, tn); break;
+    case 5: hipLaunchKernelGGL((gemm_wide_kernel<2, 2 * X, 64, 3, HAS_E, W, PLAIN>), grid, block, 0, stream, g, tm, tn); break;
+    default: hipLaunchKernelGGL((gemm_wide_kernel<2, X, 64, 4, HAS_E, W, PLAIN>), grid, block, 0, stream, g, tm, tn); break;
   }
   return hipGetLastError();
 }
 
 hipError_t launch_gemm_bf16(const GemmArgs& g, int tile, int splits, hipStream_t stream) {
+  if (g.mode == kModeKV && g.kv.k_rows != nullptr)   // (carries no E)
+    return tile >= kWide ? launch_gemm_wide_t<false, true>(g, tile - kWide, splits, stream)
+                         : launch_gemm_bf16_t<false, true>(g, tile, splits, stream);
   if (tile >= kWide)
     return g.e ? launch_gemm_wide_t<true>(g, tile - kWide, splits, stream)
                : launch_gemm_wide_t<false>(g, tile - kWide, splits, stream);
@@ -1456,8 +1461,9 @@ hipError_t launch_project(const ProjectArgs& a, const ProjectPlan& p, hipStream_
 
   if (!sep && a.znorm == nullptr && a.dst.knorm == nullptr && p.fused &&
       (a.fe != nullptr || a.e == nullptr)) {
-    hipLaunchKernelGGL(proj_fused_kernel, dim3((a.M + kFusedBM - 1) / kFusedBM), dim3(256), 0,
-                       stream, a);
+    const dim3 grid((a.M + kFusedBM - 1) / kFusedBM);
+    if (a.dst.k_rows != nullptr) hipLaunchKernelGGL(proj_fused_kernel<true>, grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(proj_fused_kernel<false>, grid, dim3(256), 0, stream, a);
     return hipGetLastError();
   }
   if (a.fe != nullptr && !sep) {   // F(E) folded beforehand: the GEMM carries no E
@@ -1497,8 +1503,13 @@ hipError_t launch_project(const ProjectArgs& a, const ProjectPlan& p, hipStream_
   if ((err = launch_gemm_bf16(kv, p.kv_tile, p.kv_split, stream)) != hipSuccess) return err;
   if (p.kv_split > 1) {
     const int64_t items = static_cast<int64_t>(a.M) * (n_kv / 2);
-    hipLaunchKernelGGL(epi_kv_kernel<uint16_t>, dim3(static_cast<unsigned>((items + 255) / 256)),
-                       dim3(256), 0, stream, part, p.kv_split, a.M, n_kv, a.dst);
+    const dim3 grid(static_cast<unsigned>((items + 255) / 256));
+    if (a.dst.k_rows != nullptr)
+      hipLaunchKernelGGL((epi_kv_kernel<uint16_t, true>), grid, dim3(256), 0, stream, part, p.kv_split, a.M,
+                         n_kv, a.dst);
+    else
+      hipLaunchKernelGGL(epi_kv_kernel<uint16_t>, grid, dim3(256), 0, stream, part, p.kv_split, a.M, n_kv,
+                         a.dst);
   }
   return hipGetLastError();
 }
