@@ -426,6 +426,7 @@ co_status carryover_project_kv_backward(const co_dims* dims, const co_weights* w
  * q as for drafter_block_attention; lse (input) and mass (output) fp32
  * [layer_count][num_seqs][block][num_q_heads].  flags: CO_Q_PREROTATED.
  * Enqueue after the attention call, before anything changes the state.
+ * state->k_cache and v_cache are not used and may be NULL.
  * Supported shapes: those of drafter_block_attention with block <= 64.
  * Device errors: CO_ERR_LENGTH (a negative length, or carry_len > the carry
  * segment); that sequence's mass is then 0.
@@ -445,9 +446,9 @@ co_status drafter_carry_mass(const co_dims* dims, int32_t layer_begin, int32_t l
  * rule, so that they hold the attention over [C;U;S] in one softmax.
  * k_self, v_self: [layer_count][num_seqs][block][num_kv_heads][head_dim] in
  * the call's dtype, keys unrotated.  out, lse: as written by the attention
- * call.  flags: CO_Q_PREROTATED.  Supported: the attention call's shapes with
- * block <= 64.  Device errors: CO_ERR_LENGTH (negative ctx_len); that
- * sequence is left as it was.
+ * call.  flags: CO_Q_PREROTATED.  state->k_cache and v_cache are not used and
+ * may be NULL.  Supported: the attention call's shapes with block <= 64.  Device
+ * errors: CO_ERR_LENGTH (negative ctx_len); that sequence is left as it was.
  */
 co_status drafter_self_merge(const co_dims* dims, int32_t layer_begin, int32_t layer_count,
                              const void* q, const void* k_self, const void* v_self,
@@ -561,7 +562,11 @@ co_status carryover_project_kv8(const co_dims* dims, const co_weights* w, const 
  * keys and values read as code * 2^(b - 127) and U and S in bf16; block 1 is a
  * single token's.  Values enter the products exactly, but for entries below 2^-35 of
  * the largest that their page scales allow in the sequence and head (448 * 2^e), which
- * are off by up to 2^-40 of it.  k_self, v_self, lse and
+ * are off by up to 2^-40 of it.  Queries, rotated and scaled in fp32, enter them off by
+ * up to 2^-9 of an entry (bf16 would be 2^-8), entries below 2^-14 of their row's
+ * largest by up to 2^-22 of that; the weights of committed keys off by up to 2^-11
+ * (below 2^-21 of the row's largest by up to 2^-32 of that), those of U and S by up to
+ * 2^-16.  k_self, v_self, lse and
  * carry_mass are optional (NULL).  state->k_cache and v_cache are not used and
  * may be NULL.  Supported: bf16; the shapes of drafter_block_attention.
  * `ws`: carryover_workspace_bytes(dims, CO_WS_ATTENTION_KV8) bytes, 256-byte

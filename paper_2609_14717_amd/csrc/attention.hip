@@ -1620,13 +1620,17 @@ __global__ __launch_bounds__(256) void attn_bf16_combine_kernel(AttnArgs a, int 
 //   Scores: v_mfma_scale_f32_32x32x64_f8f6f4 takes the keys' codes as they are, with
 //   the page's scale byte as its own block scale (the same format).  A query
 //   is the sum of two codes of 4 significant bits, the second under 2^-4 of the
-//   first's scale, one power of two per row: rounded to 8 bits, as in bf16 (entries
-//   under 2^-14 of a row's largest: to 2^-22 of that).  Two such products at twice
-//   the bf16 rate.  Widening the keys to bf16 took 64 of the 540 vector instructions
-//   of a tile.
+//   first's scale, one power of two per row: off by up to 2^-9 of an entry, 0.6e-3 of a
+//   row, where a bf16 query is off by up to 2^-8 and 1.7e-3 (entries under 2^-14 of a
+//   row's largest: by up to 2^-22 of that).  Two such products at twice the bf16 rate.
+//   Chosen over a third code (e2m1): outputs 1.7e-3 from 64 bits in place of 1.9e-3, where
+//   their own rounding leaves 1.66e-3 and the bf16 attention over the same values
+//   2.7e-3 to 3.5e-3, at 4 % more time in long calls, 6 % at batch 32, 5 % for one block
+//   and 3 % for one token.  Widening the keys to bf16 took 64 of the 540 vector
+//   instructions of a tile.
 //   Values: codes to fp16 in registers (v_cvt_scalef32_pk_f16_fp8), exactly, against
-//   fp16 weights.  Weights of 11 bits in place of 8 leave the output's own rounding:
-//   1.8e-3 from 64 bits (bf16 weights 2.4e-3), at the same rate.  fp16's range is met
+//   fp16 weights.  Weights of 11 bits in place of 8 add 0.3e-3 to the output's own rounding
+//   (bf16 weights: 2.4e-3 from 64 bits together), at the same rate.  fp16's range is met
 //   by two references.  The values' is the largest scale byte seen (v_ref): codes
 //   enter as code * 2^(b - v_ref + 7), at most 57344, exact down to b = v_ref - 22,
 //   and o is in its units, times 2^-15 with the weights'.  The weights' is 2^7 below

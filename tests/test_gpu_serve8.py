@@ -4,8 +4,10 @@ cache, attention over it, and the round of all of them) with the fp64 oracle.
 Whole numbers, codes and scale bytes are equal to the oracle's.  Attention is held to
 the rule of the other bf16 paths, 2e-2 of a head vector's largest entry and 2e-2 of a
 log-sum-exp or share: the queries are rounded to two codes after their rotation (2^-9 of
-the value: a logit of a few units moves by a few 2^-9) and the softmax weights and the
-output to bf16 once each (half a step, 2^-8 of their size); the codes are exact in bf16.
+the value: a logit of a few units moves by a few 2^-9), the softmax weights to fp16 against
+codes (half a step, 2^-11 of their size) and to two bf16 parts against carry and own rows
+(2^-16), and the output to bf16 (2^-8).  The codes are exact in fp16 under the largest value
+scale of the sequence and head, down to 2^-35 of the largest entry that it allows.
 """
 import math
 import random
