@@ -75,7 +75,9 @@ enum {
   CO_ERR_PAGE_RANGE = 5,    /* device: page id outside [0, num_pages)          */
   CO_ERR_HIP = 6,           /* a HIP runtime call or launch failed             */
   CO_ERR_LENGTH = 7,        /* device: ctx_len outside [0, max_pages_per_seq * 16] or
-                               carry_len outside [0, 16 * ceil(block / 16)]        */
+                               carry_len outside [0, 16 * ceil(block / 16)]; a length,
+                               holding or row start of the page tables' calls that
+                               cannot be                                           */
   CO_ERR_GROUP = 8,         /* device: a sequence's committed page ids differ from its
                                group's first sequence (attention backward)          */
   CO_ERR_TOKEN = 9,         /* device: a proposed token outside [0, vocab)
@@ -514,7 +516,8 @@ co_status carryover_assign_pages(const co_dims* dims, const int32_t* want_len, i
  * valid).  Device errors, written to *status; the row then gets INT32_MIN and 0:
  * CO_ERR_LENGTH (pos0 < 0), CO_ERR_CAPACITY (a position >= max_pages_per_seq *
  * 16), CO_ERR_PAGE_RANGE (a page id outside [0, num_pages)).  With a start that
- * decreases (CO_ERR_LENGTH) every row gets them.  Host: num_pages * 16 below 2^31 (CO_ERR_UNSUPPORTED).
+ * decreases (CO_ERR_LENGTH) every row gets them.  Host: num_pages * 16 below 2^31
+ * (CO_ERR_UNSUPPORTED).
  */
 co_status carryover_slot_map(const co_dims* dims, int32_t num_rows, const int32_t* row_start,
                              const int32_t* pos0, const int32_t* page_table, int32_t* row_pos,
