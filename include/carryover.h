@@ -80,11 +80,13 @@ enum {
                                cannot be                                           */
   CO_ERR_GROUP = 8,         /* device: a sequence's committed page ids differ from its
                                group's first sequence (attention backward)          */
-  CO_ERR_TOKEN = 9,         /* device: a proposed token outside [0, vocab)
-                               (carryover_verify_sample)                            */
-  CO_ERR_POOL = 10          /* device: the page pool has too few free pages, or a free
+  CO_ERR_TOKEN = 9,         /* device: a proposed, biased or counted token outside
+                               [0, vocab)                                           */
+  CO_ERR_POOL = 10,         /* device: the page pool has too few free pages, or a free
                                count or holdings that it cannot have
                                (carryover_assign_pages)                             */
+  CO_ERR_MASK = 11          /* device: a row names a mask that is not there
+                               (co_logit_rules)                                     */
 };
 
 enum { CO_DTYPE_F32 = 0, CO_DTYPE_BF16 = 1 };
@@ -190,6 +192,54 @@ typedef struct co_page_pool {
   int32_t* free_pages;        /* [num_pages] the free pages' ids, in entries 0 .. *free_count - 1 */
   int32_t* free_count;        /* one int32                                                  */
 } co_page_pool;
+
+/*
+ * The projection's weights in 8 bits (next to the paper): rows quantised by
+ * carryover_quantize_i8, each with its scale; norms and F E as in co_weights.
+ */
+typedef struct co_weights_i8 {
+  const int8_t* w_f;          /* [model_dim][feat_dim], 16-byte aligned               */
+  const float* w_f_scale;     /* [model_dim]                                          */
+  const int8_t* w_kv;         /* [NKV][model_dim], rows as in co_weights, 16-byte aligned */
+  const float* w_kv_scale;    /* [NKV]                                                */
+  const float* f_e;           /* F e_carry, fp32 [model_dim] (carryover_fold_e on the weights
+                                 before their quantisation), added on carry rows; NULL: no
+                                 embedding                                            */
+  const float* z_norm;        /* optional, as in co_weights                           */
+  const float* k_norm;        /* optional, as in co_weights                           */
+} co_weights_i8;
+
+/*
+ * What the requests of a batch ask of their logits (carryover_logit_rules,
+ * carryover_probabilities); every part is optional.  Let c be how often token v
+ * was generated before a row: the count of its history word, and in row j of a
+ * window the proposals before j that are v.  In this order, each operation
+ * rounded to fp32:
+ *   x = x > 0 ? x / repetition : x * repetition   where v is in the prompt or c > 0
+ *   x = x - frequency * c;  x = x - presence       where c > 0
+ *   x = x + bias                                   where v has an entry
+ *   x = -inf                                       where the row's mask has v's bit clear
+ */
+typedef struct co_logit_rules {
+  const uint16_t* seen;       /* [num_seqs][vocab] token history (carryover_count_tokens):
+                                 bit 15: in the prompt; bits 0 .. 14: times generated.
+                                 NULL: no penalties                                   */
+  const float* repetition;    /* [num_seqs], positive (1: none); these three need `seen`
+                                 and may be NULL                                      */
+  const float* presence;      /* [num_seqs] (0: none)                                 */
+  const float* frequency;     /* [num_seqs] (0: none)                                 */
+  const int32_t* bias_start;  /* [num_seqs + 1]: sequence s has entries bias_start[s] ..
+                                 bias_start[s + 1] - 1; a token's last entry counts.
+                                 These three are all given or all NULL                */
+  const int32_t* bias_tok;    /* [num_bias]                                           */
+  const float* bias_val;      /* [num_bias]                                           */
+  const int32_t* mask_row;    /* [num_seqs][rows]: the mask of each row, negative: none;
+                                 both of these are given or NULL                      */
+  const uint32_t* mask_bits;  /* [num_masks][ceil(vocab / 32)]: bit v % 32 of word v / 32 set
+                                 allows token v; bits past the vocabulary are ignored */
+  int32_t num_bias;
+  int32_t num_masks;
+} co_logit_rules;
 
 /*
  * Route (Algorithm 1 "Given"; greedy verification, Section 2
@@ -597,9 +647,114 @@ co_status carryover_round_kv8(const co_dims* dims, const co_weights* w, const vo
                               void* out, float* lse, uint32_t flags, void* ws, size_t ws_bytes,
                               hipStream_t stream);
 
+/*
+ * Rows into 8-bit codes with a scale for each row: the tokens of a product, or the
+ * output channels of its weights.  With a = the largest magnitude of row i, at
+ * least 127 * 2^-126:
+ *   scale[i] = a / 127;  code = the integer nearest to 127 x / a, ties to even
+ * (exactly), from -127 to 127.  A row with an infinity or a NaN gets scale NaN and
+ * codes 0, so that every product with it is NaN.  x [num_rows][num_cols] of
+ * `dtype` (CO_DTYPE_F32 or CO_DTYPE_BF16) and codes of the same shape, 16-byte
+ * aligned; scale fp32 [num_rows].  num_cols: a multiple of 64; num_rows * num_cols
+ * any, num_rows below 2^24 (CO_ERR_UNSUPPORTED otherwise).
+ */
+co_status carryover_quantize_i8(int32_t num_rows, int32_t num_cols, int32_t dtype, const void* x,
+                                int8_t* codes, float* scale, hipStream_t stream);
+
+/*
+ * Product of 8-bit integers with a scale for each row of both operands:
+ *   out[i][j] = float(sum_k a[i][k] * w[j][k]) * (a_scale[i] * w_scale[j]) + bias[j]
+ * for i < m, j < n; the sum is exact, each other operation is rounded to fp32, the
+ * result to `dtype`.  a [m][k] and w [n][k] int8 (any codes, -128 too), 16-byte
+ * aligned; a_scale fp32 [m], w_scale fp32 [n]; bias fp32 [n] or NULL; out [m][n] of
+ * `dtype` (CO_DTYPE_F32 or CO_DTYPE_BF16), 16-byte aligned.  m and n from 0 to 2^24 - 1,
+ * k a multiple of 64 from 64 to 131008 (CO_ERR_UNSUPPORTED otherwise).  `ws`:
+ * carryover_matmul_i8_workspace_bytes(m, n, k) bytes of scratch, 256-byte
+ * aligned (any contents; NULL where that is 0).
+ */
+co_status carryover_matmul_i8(int32_t m, int32_t n, int32_t k, const int8_t* a,
+                              const float* a_scale, const int8_t* w, const float* w_scale,
+                              const float* bias, int32_t dtype, void* out, void* ws,
+                              size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of carryover_matmul_i8 (0 also on unsupported sizes). */
+size_t carryover_matmul_i8_workspace_bytes(int32_t m, int32_t n, int32_t k);
+
+/*
+ * carryover_project_kv with F and the K/V weights in 8 bits: the rows of `hidden`,
+ * and those of z = F x, are quantised as carryover_quantize_i8 does (z from its
+ * fp32 sums, after F E and the norm), both products are carryover_matmul_i8's in
+ * fp32, keys are normalised and rotated and rows stored as ever, in bf16.  No
+ * separate carry projector.  Supported: bf16, feat_dim and model_dim up to 131008.
+ * `ws`: carryover_workspace_bytes(dims, CO_WS_PROJECT_I8) bytes, 256-byte aligned.
+ * Other arguments and errors as carryover_project_kv.
+ */
+co_status carryover_project_kv_i8(const co_dims* dims, const co_weights_i8* w, const void* hidden,
+                                  const co_route* route, const co_state* state, void* ws,
+                                  size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Tokens into the history that co_logit_rules reads.  Sequence s has the tokens
+ * tokens[s][0 .. len[s] - 1] (int32 [num_seqs][width]; len NULL: all of them);
+ * negative ones are padding.  With CO_COUNT_PROMPT they are marked as of the
+ * prompt, otherwise counted as generated (a count stops at 32767).  With
+ * CO_COUNT_FRESH the words of every sequence whose length is not 0 start at 0 (a
+ * request enters).  After a verification: the proposals with len = accept_len, then
+ * next_tok with width 1.  seen [num_seqs][vocab], 2-byte aligned.  Only num_seqs of
+ * dims is used (the rest must still be valid).  Device errors, written to *status:
+ * CO_ERR_LENGTH (len outside [0, width]; the sequence stays as it is), CO_ERR_TOKEN
+ * (a token >= vocab; it is left out).  Calls on one history must not overlap.
+ * Host: vocab >= 1, num_seqs * ceil(vocab / 8192) below 2^23 (CO_ERR_UNSUPPORTED).
+ */
+enum { CO_COUNT_PROMPT = 1, CO_COUNT_FRESH = 2 };
+co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t width,
+                                 const int32_t* tokens, const int32_t* len, uint32_t flags,
+                                 uint16_t* seen, int32_t* status, hipStream_t stream);
+
+/*
+ * The rules on a batch's logits: out = logits [num_seqs][rows][vocab] after
+ * co_logit_rules, of `dtype` (CO_DTYPE_F32 or CO_DTYPE_BF16); out may be logits itself,
+ * and must not overlap it otherwise.  rows from 1 to block + 1: a verified window
+ * has block + 1, single tokens 1.  draft_tok int32 [num_seqs][block]: the window's
+ * proposals, of which row j has the first j behind it (NULL: rows do not follow each
+ * other).  Only num_seqs and block of dims are used (the rest must still be valid).
+ * Device errors, written to *status: CO_ERR_TOKEN (a proposal or a bias's token outside
+ * [0, vocab); it is left out), CO_ERR_LENGTH (bias_start that decreases or lies outside
+ * [0, num_bias]; the sequence has no biases), CO_ERR_MASK (mask_row >= num_masks; the row
+ * allows no token).
+ * Host: vocab >= 1, block <= 1024, num_seqs * rows * vocab <= 2^40, and a grid of
+ * workgroups below 2^24 (CO_ERR_UNSUPPORTED).
+ */
+co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,
+                                const void* logits, const int32_t* draft_tok,
+                                const co_logit_rules* rules, void* out, int32_t* status,
+                                hipStream_t stream);
+
+/*
+ * Probabilities of a batch's logits after the rules (NULL: none), as
+ * carryover_verify_sample takes them: with x the logits of a row after
+ * co_logit_rules (kept in fp32) and T = temperature[s] (fp32 [num_seqs]; NULL: 1),
+ *   probs[s][j][v] = exp((x_v - max) / T) / sum   (fp32)
+ * or, for T <= 0 (greedy), 1 at the lowest token of the largest x and 0 elsewhere.
+ * top_tok int32 [num_seqs][rows] (NULL: not wanted): that token of every row (target_tok
+ * of carryover_route).  A NaN among the logits is left out, as if masked; infinite ones
+ * share the row.  A row with nothing left has probabilities 0 and top_tok -1.  The
+ * logits are not changed; probs must not overlap them.  `ws`:
+ * carryover_probabilities_workspace_bytes(dims, vocab, rows) bytes of scratch,
+ * 256-byte aligned.  Other arguments and errors as carryover_logit_rules.
+ */
+co_status carryover_probabilities(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,
+                                  const void* logits, const int32_t* draft_tok,
+                                  const co_logit_rules* rules, const float* temperature,
+                                  float* probs, int32_t* top_tok, int32_t* status, void* ws,
+                                  size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of carryover_probabilities (0 on unsupported sizes). */
+size_t carryover_probabilities_workspace_bytes(const co_dims* dims, int32_t vocab, int32_t rows);
+
 enum { CO_WS_PROJECT = 0, CO_WS_ATTENTION = 1, CO_WS_ROUND = 2, CO_WS_ATTENTION_BACKWARD = 3,
        CO_WS_PROJECT_BACKWARD = 4, CO_WS_PROJECT_KV8 = 5, CO_WS_ATTENTION_KV8 = 6,
-       CO_WS_ROUND_KV8 = 7, CO_WS_ASSIGN_PAGES = 8 };
+       CO_WS_ROUND_KV8 = 7, CO_WS_ASSIGN_PAGES = 8, CO_WS_PROJECT_I8 = 9 };
 
 /* Workspace bytes a call needs for these dims (0 on unsupported dims). */
 size_t carryover_workspace_bytes(const co_dims* dims, int32_t which);

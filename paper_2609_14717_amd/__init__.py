@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(HERE, "libcarryover.so")
 
 CO_OK, CO_ERR_INVALID_ARG, CO_ERR_UNSUPPORTED, CO_ERR_WORKSPACE = 0, 1, 2, 3
 CO_ERR_CAPACITY, CO_ERR_PAGE_RANGE, CO_ERR_HIP, CO_ERR_LENGTH, CO_ERR_GROUP = 4, 5, 6, 7, 8
-CO_ERR_TOKEN, CO_ERR_POOL = 9, 10
+CO_ERR_TOKEN, CO_ERR_POOL, CO_ERR_MASK = 9, 10, 11
 CO_DTYPE_F32, CO_DTYPE_BF16 = 0, 1
 CO_BASELINE_MODE, CO_ROUTE_ACCEPT_ALL, CO_ROUTE_CARRY_ONLY, CO_Q_PREROTATED = 1, 2, 4, 8
 CO_ATTN_SHARED_PREFIX = 16
@@ -25,6 +25,8 @@ CO_ROUTE_ACCEPT_BITS = 32
 CO_WS_PROJECT, CO_WS_ATTENTION, CO_WS_ROUND, CO_WS_ATTENTION_BACKWARD = 0, 1, 2, 3
 CO_WS_PROJECT_BACKWARD = 4
 CO_WS_PROJECT_KV8, CO_WS_ATTENTION_KV8, CO_WS_ROUND_KV8, CO_WS_ASSIGN_PAGES = 5, 6, 7, 8
+CO_WS_PROJECT_I8 = 9
+CO_COUNT_PROMPT, CO_COUNT_FRESH = 1, 2
 # launch-shape overrides (carryover_set_tuning)
 TUNING = {"gemm_wide_variant": 0, "gemm_no_wide": 1, "project_fused_min_rows": 2, "attn_wave": 3,
           "attn_workgroups": 4, "attn_round_tiles": 5, "attn_group_split_tiles": 6}
@@ -77,9 +79,26 @@ class co_page_pool(ctypes.Structure):
                 ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p)]
 
 
+class co_weights_i8(ctypes.Structure):
+    _fields_ = [("w_f", ctypes.c_void_p), ("w_f_scale", ctypes.c_void_p),
+                ("w_kv", ctypes.c_void_p), ("w_kv_scale", ctypes.c_void_p),
+                ("f_e", ctypes.c_void_p), ("z_norm", ctypes.c_void_p),
+                ("k_norm", ctypes.c_void_p)]
+
+
+class co_logit_rules(ctypes.Structure):
+    _fields_ = [("seen", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p),
+                ("bias_start", ctypes.c_void_p), ("bias_tok", ctypes.c_void_p),
+                ("bias_val", ctypes.c_void_p), ("mask_row", ctypes.c_void_p),
+                ("mask_bits", ctypes.c_void_p), ("num_bias", ctypes.c_int32),
+                ("num_masks", ctypes.c_int32)]
+
+
 _lib = None
 _P = ctypes.POINTER
 _v = ctypes.c_void_p
+_i = ctypes.c_int32
 
 
 def lib():
@@ -130,6 +149,18 @@ def lib():
             "carryover_round_kv8": [_P(co_dims), _P(co_weights), _v, _v, _v, _v, _P(co_state),
                                     _P(co_kv8), _P(co_route), _v, _v, ctypes.c_uint32, _v,
                                     ctypes.c_size_t, _v],
+            "carryover_quantize_i8": [_i, _i, _i, _v, _v, _v, _v],
+            "carryover_matmul_i8": [_i, _i, _i, _v, _v, _v, _v, _v, _i, _v, _v, ctypes.c_size_t,
+                                    _v],
+            "carryover_matmul_i8_workspace_bytes": [_i, _i, _i],
+            "carryover_project_kv_i8": [_P(co_dims), _P(co_weights_i8), _v, _P(co_route),
+                                        _P(co_state), _v, ctypes.c_size_t, _v],
+            "carryover_count_tokens": [_P(co_dims), _i, _i, _v, _v, ctypes.c_uint32, _v, _v, _v],
+            "carryover_logit_rules": [_P(co_dims), _i, _i, _i, _v, _v, _P(co_logit_rules), _v, _v,
+                                      _v],
+            "carryover_probabilities": [_P(co_dims), _i, _i, _i, _v, _v, _P(co_logit_rules), _v,
+                                        _v, _v, _v, _v, ctypes.c_size_t, _v],
+            "carryover_probabilities_workspace_bytes": [_P(co_dims), _i, _i],
             "carryover_set_tuning": [ctypes.c_int32, ctypes.c_int64],
             "carryover_round_noalloc": [_P(co_dims), _P(co_weights), _v, _v, _v, _v,
                                         _P(co_state), _P(co_route), _v, _v, ctypes.c_uint32, _v],
@@ -141,7 +172,9 @@ def lib():
             f = getattr(L, name)
             f.argtypes = args
             f.restype = ctypes.c_int32
-        L.carryover_workspace_bytes.restype = ctypes.c_size_t
+        for name in ("carryover_workspace_bytes", "carryover_matmul_i8_workspace_bytes",
+                     "carryover_probabilities_workspace_bytes"):
+            getattr(L, name).restype = ctypes.c_size_t
         L.carryover_status_string.restype = ctypes.c_char_p
         _lib = L
     return _lib
@@ -154,7 +187,10 @@ EXPORTED = ("carryover_route", "carryover_project_kv", "drafter_block_attention"
             "carryover_import_kv", "carryover_verify_sample", "carryover_set_tuning",
             "carryover_assign_pages", "carryover_slot_map", "carryover_store_kv8",
             "carryover_project_kv8", "drafter_block_attention_kv8", "carryover_round_kv8",
-            "carryover_round_noalloc",
+            "carryover_quantize_i8", "carryover_matmul_i8",
+            "carryover_matmul_i8_workspace_bytes", "carryover_project_kv_i8",
+            "carryover_count_tokens", "carryover_logit_rules", "carryover_probabilities",
+            "carryover_probabilities_workspace_bytes", "carryover_round_noalloc",
             "carryover_workspace_bytes", "carryover_read_status", "carryover_status_string")
 
 
@@ -164,6 +200,19 @@ def _ptr(x):
     if isinstance(x, int):
         return x
     return x.data_ptr()
+
+
+def _dense(x, name):
+    """The address of a tensor whose elements lie next to each other, in order."""
+    if x is None or isinstance(x, int):
+        return x
+    if not x.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    return x.data_ptr()
+
+
+def _dtype(dtype):
+    return CO_DTYPE_BF16 if dtype == "bf16" else CO_DTYPE_F32 if dtype == "f32" else dtype
 
 
 def _stream(stream):
@@ -226,8 +275,37 @@ def page_pool(t):
                         _ptr(t["free_count"]))
 
 
+def weights_i8(w_f, w_f_scale, w_kv, w_kv_scale, f_e=None, z_norm=None, k_norm=None):
+    """co_weights_i8 over device tensors: codes and scales of ``carryover_quantize_i8``; f_e
+    from ``carryover_fold_e``, z_norm and k_norm as in ``weights``."""
+    return co_weights_i8(*(_dense(x, n) for x, n in (
+        (w_f, "w_f"), (w_f_scale, "w_f_scale"), (w_kv, "w_kv"), (w_kv_scale, "w_kv_scale"),
+        (f_e, "f_e"), (z_norm, "z_norm"), (k_norm, "k_norm"))))
+
+
+def logit_rules(seen=None, repetition=None, presence=None, frequency=None, bias_start=None,
+                bias_tok=None, bias_val=None, mask_row=None, mask_bits=None):
+    """co_logit_rules over device tensors; num_bias and num_masks are their lengths.  Masks
+    are ``mask_bits`` [masks][ceil(vocab / 32)] of 32-bit words.  The tensors must outlive it."""
+    r = co_logit_rules(*(_dense(x, n) for x, n in (
+        (seen, "seen"), (repetition, "repetition"), (presence, "presence"),
+        (frequency, "frequency"), (bias_start, "bias_start"), (bias_tok, "bias_tok"),
+        (bias_val, "bias_val"), (mask_row, "mask_row"), (mask_bits, "mask_bits"))))
+    r.num_bias = 0 if bias_tok is None else len(bias_tok)
+    r.num_masks = 0 if mask_bits is None else len(mask_bits)
+    return r
+
+
 def workspace_bytes(dims, which=CO_WS_ROUND) -> int:
     return lib().carryover_workspace_bytes(ctypes.byref(dims), which)
+
+
+def matmul_i8_workspace_bytes(m, n, k) -> int:
+    return lib().carryover_matmul_i8_workspace_bytes(m, n, k)
+
+
+def probabilities_workspace_bytes(dims, vocab, rows) -> int:
+    return lib().carryover_probabilities_workspace_bytes(ctypes.byref(dims), vocab, rows)
 
 
 def alloc_state(dims, page_table, device="cuda", committed=True):
@@ -424,6 +502,67 @@ def carryover_round_kv8(dims, w, hidden, draft_tok, target_tok, q, st, cache, rt
                                      _ptr(draft_tok), _ptr(target_tok), _ptr(q), ctypes.byref(s),
                                      ctypes.byref(c), ctypes.byref(r), _ptr(out), _ptr(lse), flags,
                                      _ptr(ws), nb, _stream(stream)), "carryover_round_kv8")
+
+
+def carryover_quantize_i8(num_rows, num_cols, dtype, x, codes, scale, stream=None):
+    """Rows of x (``dtype`` "bf16" or "f32") into 8-bit codes with a scale for each row."""
+    _check(lib().carryover_quantize_i8(num_rows, num_cols, _dtype(dtype), _dense(x, "x"),
+                                       _dense(codes, "codes"), _dense(scale, "scale"),
+                                       _stream(stream)), "carryover_quantize_i8")
+
+
+def carryover_matmul_i8(m, n, k, a, a_scale, w, w_scale, bias, dtype, out, ws, stream=None,
+                        ws_bytes=None):
+    """out [m][n] (``dtype`` "bf16" or "f32") = a [m][k] times w [n][k] transposed, both int8
+    with a scale for each row, plus bias [n] (or None)."""
+    nb = ws_bytes if ws_bytes is not None else 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib().carryover_matmul_i8(m, n, k, _dense(a, "a"), _dense(a_scale, "a_scale"),
+                                     _dense(w, "w"), _dense(w_scale, "w_scale"),
+                                     _dense(bias, "bias"), _dtype(dtype), _dense(out, "out"),
+                                     _dense(ws, "ws"), nb, _stream(stream)),
+           "carryover_matmul_i8")
+
+
+def carryover_project_kv_i8(dims, w, hidden, rt, st, ws, stream=None, ws_bytes=None):
+    """carryover_project_kv with weights of ``weights_i8``."""
+    s, r = state(st), route(rt)
+    nb = ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    _check(lib().carryover_project_kv_i8(ctypes.byref(dims), ctypes.byref(w),
+                                         _dense(hidden, "hidden"), ctypes.byref(r),
+                                         ctypes.byref(s), _dense(ws, "ws"), nb, _stream(stream)),
+           "carryover_project_kv_i8")
+
+
+def carryover_count_tokens(dims, vocab, width, tokens, lens, flags, seen, status, stream=None):
+    """tokens [num_seqs][width], the first lens of each sequence, into the history words seen
+    [num_seqs][vocab] (16 bits): of the prompt (CO_COUNT_PROMPT) or generated."""
+    _check(lib().carryover_count_tokens(ctypes.byref(dims), vocab, width, _dense(tokens, "tokens"),
+                                        _dense(lens, "lens"), flags, _dense(seen, "seen"),
+                                        _dense(status, "status"), _stream(stream)),
+           "carryover_count_tokens")
+
+
+def carryover_logit_rules(dims, vocab, rows, dtype, logits, draft_tok, rules, out, status,
+                          stream=None):
+    """Penalties, biases and masks of ``logit_rules`` on logits [num_seqs][rows][vocab]."""
+    _check(lib().carryover_logit_rules(ctypes.byref(dims), vocab, rows, _dtype(dtype),
+                                       _dense(logits, "logits"), _dense(draft_tok, "draft_tok"),
+                                       ctypes.byref(rules), _dense(out, "out"),
+                                       _dense(status, "status"), _stream(stream)),
+           "carryover_logit_rules")
+
+
+def carryover_probabilities(dims, vocab, rows, dtype, logits, draft_tok, rules, temperature, probs,
+                            top_tok, status, ws, stream=None, ws_bytes=None):
+    """Probabilities (fp32) of the logits after ``logit_rules`` (or None) at each sequence's
+    temperature, as carryover_verify_sample takes them."""
+    nb = ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    _check(lib().carryover_probabilities(
+        ctypes.byref(dims), vocab, rows, _dtype(dtype), _dense(logits, "logits"),
+        _dense(draft_tok, "draft_tok"), None if rules is None else ctypes.byref(rules),
+        _dense(temperature, "temperature"), _dense(probs, "probs"), _dense(top_tok, "top_tok"),
+        _dense(status, "status"), _dense(ws, "ws"), nb, _stream(stream)),
+        "carryover_probabilities")
 
 
 NOALLOC_SCRATCH_BYTES = 136 << 20

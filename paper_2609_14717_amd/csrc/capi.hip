@@ -197,6 +197,92 @@ co_status check_attention_kv8_dims(const co_dims* d) {
                                                                              : CO_ERR_UNSUPPORTED;
 }
 
+bool dtype_ok(int32_t dtype) { return dtype == CO_DTYPE_F32 || dtype == CO_DTYPE_BF16; }
+
+// Shapes of the projection with 8-bit weights: dims are already checked.
+co_status check_project_i8_dims(const co_dims* d) {
+  if (d->dtype != CO_DTYPE_BF16 || d->feat_dim > kMaxSumI8 || d->model_dim > kMaxSumI8)
+    return CO_ERR_UNSUPPORTED;
+  const int64_t n_kv = 2ll * d->num_layers * d->num_kv_heads * d->head_dim;
+  const int64_t rows = static_cast<int64_t>(d->num_seqs) * d->block;
+  if (rows > kMaxSideI8 || n_kv > kMaxSideI8 || rows * n_kv >= int64_t{1} << 32 ||
+      rows * d->model_dim >= int64_t{1} << 32)
+    return CO_ERR_UNSUPPORTED;
+  return CO_OK;
+}
+
+size_t project_i8_bytes(const co_dims* d) {
+  return project_i8_ws_bytes(d->num_seqs * d->block, d->feat_dim, d->model_dim,
+                             2 * d->num_layers * d->num_kv_heads * d->head_dim, num_cus());
+}
+
+co_status check_matmul_i8(int32_t m, int32_t n, int32_t k) {
+  if (m < 0 || n < 0) return CO_ERR_INVALID_ARG;
+  if (m > kMaxSideI8 || n > kMaxSideI8 || k < 64 || k % 64 || k > kMaxSumI8)
+    return CO_ERR_UNSUPPORTED;
+  return plan_matmul_i8(m, n, k, num_cus()).workgroups < kMaxGrid ? CO_OK : CO_ERR_UNSUPPORTED;
+}
+
+// Sizes of the logits' calls: dims are already checked.
+co_status check_logits(const co_dims* d, int32_t vocab, int32_t rows, int32_t dtype) {
+  if (rows < 1 || rows > static_cast<int64_t>(d->block) + 1) return CO_ERR_INVALID_ARG;
+  if (vocab < 1 || d->block > 1024 || !dtype_ok(dtype) ||
+      static_cast<int64_t>(d->num_seqs) * rows > (int64_t{1} << 40) / vocab)
+    return CO_ERR_UNSUPPORTED;
+  return plan_logits(d->num_seqs, rows, vocab, num_cus()).workgroups < kMaxGrid
+             ? CO_OK
+             : CO_ERR_UNSUPPORTED;
+}
+
+bool rules_ok(const co_logit_rules* r) {
+  if (!r->seen && (r->repetition || r->presence || r->frequency)) return false;
+  if (!aligned(r->seen, 2) || !aligned(r->repetition, 4) || !aligned(r->presence, 4) ||
+      !aligned(r->frequency, 4) || !aligned(r->bias_start, 4) || !aligned(r->bias_tok, 4) ||
+      !aligned(r->bias_val, 4) || !aligned(r->mask_row, 4) || !aligned(r->mask_bits, 4))
+    return false;
+  if ((r->bias_start == nullptr) != (r->bias_tok == nullptr) ||
+      (r->bias_start == nullptr) != (r->bias_val == nullptr) ||
+      (r->mask_row == nullptr) != (r->mask_bits == nullptr))
+    return false;
+  return r->num_bias >= 0 && r->num_masks >= 0;
+}
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y ? y - x < na : x - y < nb;
+}
+
+LogitArgs logit_args(const co_dims* d, int32_t vocab, int32_t rows, const void* logits,
+                     const int32_t* draft_tok, const co_logit_rules* r, int32_t* status) {
+  const LogitPlan p = plan_logits(d->num_seqs, rows, vocab, num_cus());
+  LogitArgs a{};
+  a.S = d->num_seqs;
+  a.B = d->block;
+  a.R = rows;
+  a.V = vocab;
+  a.logits = logits;
+  a.draft = draft_tok;
+  if (r) {
+    a.seen = r->seen;
+    a.repetition = r->repetition;
+    a.presence = r->presence;
+    a.frequency = r->frequency;
+    a.bias_start = r->bias_start;
+    a.bias_tok = r->bias_tok;
+    a.bias_val = r->bias_val;
+    a.mask_row = r->mask_row;
+    a.mask_bits = r->mask_bits;
+    a.num_bias = r->num_bias;
+    a.num_masks = r->num_masks;
+  }
+  a.status = status;
+  a.groups = p.groups;
+  a.rows_per = p.rows_per;
+  a.tiles = p.tiles;
+  a.chunks = p.chunks;
+  return a;
+}
+
 co_status hip_status(hipError_t e) { return e == hipSuccess ? CO_OK : CO_ERR_HIP; }
 
 // The launch functions report hipGetLastError() after their launches; an
@@ -421,6 +507,8 @@ size_t carryover_workspace_bytes(const co_dims* dims, int32_t which) {
       return which == CO_WS_ATTENTION_KV8 ? kw : pw + 2 * rows_bytes(dims) + kw;
     }
     case CO_WS_ASSIGN_PAGES: return assign_ws_bytes(dims->num_seqs);
+    case CO_WS_PROJECT_I8:
+      return check_project_i8_dims(dims) == CO_OK ? project_i8_bytes(dims) : 0;
     case CO_WS_ATTENTION_BACKWARD:
       return bwd_workspace_bytes(dims->num_seqs, dims->num_layers, dims->num_kv_heads,
                                  dims->head_dim, dims->num_pages, carry_pages(dims));
@@ -899,6 +987,155 @@ co_status carryover_round_kv8(const co_dims* dims, const co_weights* w, const vo
                       nullptr, nullptr, cache);
 }
 
+co_status carryover_quantize_i8(int32_t num_rows, int32_t num_cols, int32_t dtype, const void* x,
+                                int8_t* codes, float* scale, hipStream_t stream) {
+  if (num_rows < 0 || num_cols < 1) return CO_ERR_INVALID_ARG;
+  if (num_rows > kMaxSideI8 || num_cols % 64 || !dtype_ok(dtype)) return CO_ERR_UNSUPPORTED;
+  if (!x || !codes || !scale || !aligned(x, 16) || !aligned(codes, 16) || !aligned(scale, 4))
+    return CO_ERR_INVALID_ARG;
+  clear_stale_error();
+  return hip_status(launch_quantize_i8(x, num_rows, num_cols, dtype, codes, scale, stream));
+}
+
+size_t carryover_matmul_i8_workspace_bytes(int32_t m, int32_t n, int32_t k) {
+  return check_matmul_i8(m, n, k) == CO_OK ? plan_matmul_i8(m, n, k, num_cus()).ws_bytes : 0;
+}
+
+co_status carryover_matmul_i8(int32_t m, int32_t n, int32_t k, const int8_t* a,
+                              const float* a_scale, const int8_t* w, const float* w_scale,
+                              const float* bias, int32_t dtype, void* out, void* ws,
+                              size_t ws_bytes, hipStream_t stream) {
+  co_status s = check_matmul_i8(m, n, k);
+  if (s != CO_OK) return s;
+  if (!dtype_ok(dtype)) return CO_ERR_UNSUPPORTED;
+  if (!a || !a_scale || !w || !w_scale || !out || !aligned(a, 16) || !aligned(w, 16) ||
+      !aligned(out, 16) || !aligned(a_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4))
+    return CO_ERR_INVALID_ARG;
+  const MatmulI8Plan p = plan_matmul_i8(m, n, k, num_cus());
+  if (p.ws_bytes && (!ws || !aligned(ws, 256))) return CO_ERR_INVALID_ARG;
+  if (ws_bytes < p.ws_bytes) return CO_ERR_WORKSPACE;
+  MatmulI8Args g{};
+  g.M = m;
+  g.N = n;
+  g.K = k;
+  g.dtype = dtype;
+  g.A = a;
+  g.W = w;
+  g.a_scale = a_scale;
+  g.w_scale = w_scale;
+  g.bias = bias;
+  g.out = out;
+  g.ws = ws;
+  clear_stale_error();
+  return hip_status(launch_matmul_i8(g, p, stream));
+}
+
+co_status carryover_project_kv_i8(const co_dims* dims, const co_weights_i8* w, const void* hidden,
+                                  const co_route* route, const co_state* state, void* ws,
+                                  size_t ws_bytes, hipStream_t stream) {
+  co_status s = check_dims(dims);
+  if (s != CO_OK) return s;
+  if ((s = check_project_i8_dims(dims)) != CO_OK) return s;
+  if (!w || !w->w_f || !w->w_f_scale || !w->w_kv || !w->w_kv_scale || !hidden ||
+      !route_ok(route) || !state_ok(state))
+    return CO_ERR_INVALID_ARG;
+  if (!aligned(hidden, 16) || !aligned(w->w_f, 16) || !aligned(w->w_kv, 16) ||
+      !aligned(w->w_f_scale, 4) || !aligned(w->w_kv_scale, 4) || !aligned(w->f_e, 16) ||
+      !aligned(w->z_norm, 4) || !aligned(w->k_norm, 4))
+    return CO_ERR_INVALID_ARG;
+  if (w->z_norm && dims->model_dim > kNormMaxCols) return CO_ERR_UNSUPPORTED;
+  if (!ws || !aligned(ws, 256)) return CO_ERR_INVALID_ARG;
+  if (ws_bytes < project_i8_bytes(dims)) return CO_ERR_WORKSPACE;
+  ProjectI8Args a{};
+  a.M = dims->num_seqs * dims->block;
+  a.Dcat = dims->feat_dim;
+  a.d = dims->model_dim;
+  a.hidden = hidden;
+  a.wf = w->w_f;
+  a.wf_scale = w->w_f_scale;
+  a.wkv = w->w_kv;
+  a.wkv_scale = w->w_kv_scale;
+  a.fe = w->f_e;
+  a.znorm = w->z_norm;
+  a.dst = make_dest(dims, route, state);
+  a.dst.knorm = w->k_norm;
+  a.ws = ws;
+  clear_stale_error();
+  return hip_status(launch_project_i8(a, num_cus(), stream));
+}
+
+co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t width,
+                                 const int32_t* tokens, const int32_t* len, uint32_t flags,
+                                 uint16_t* seen, int32_t* status, hipStream_t stream) {
+  co_status s = check_dims(dims);
+  if (s != CO_OK) return s;
+  if (vocab < 1 || count_workgroups(dims->num_seqs, vocab) >= kMaxGrid) return CO_ERR_UNSUPPORTED;
+  if (width < 0 || !tokens || !seen || !status || !aligned(tokens, 4) || !aligned(len, 4) ||
+      !aligned(seen, 2) || !aligned(status, 4) || (flags & ~(CO_COUNT_PROMPT | CO_COUNT_FRESH)))
+    return CO_ERR_INVALID_ARG;
+  CountArgs a{};
+  a.S = dims->num_seqs;
+  a.V = vocab;
+  a.width = width;
+  a.flags = flags;
+  a.tokens = tokens;
+  a.len = len;
+  a.seen = seen;
+  a.status = status;
+  clear_stale_error();
+  return hip_status(launch_count_tokens(a, stream));
+}
+
+co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,
+                                const void* logits, const int32_t* draft_tok,
+                                const co_logit_rules* rules, void* out, int32_t* status,
+                                hipStream_t stream) {
+  co_status s = check_dims(dims);
+  if (s != CO_OK) return s;
+  if ((s = check_logits(dims, vocab, rows, dtype)) != CO_OK) return s;
+  const size_t es = dtype == CO_DTYPE_BF16 ? 2 : 4;
+  const size_t bytes = static_cast<size_t>(dims->num_seqs) * rows * vocab * es;
+  if (!logits || !rules || !out || !status || !rules_ok(rules) || !aligned(logits, es) ||
+      !aligned(out, es) || !aligned(draft_tok, 4) || !aligned(status, 4) ||
+      (out != logits && overlap(logits, bytes, out, bytes)))
+    return CO_ERR_INVALID_ARG;
+  LogitArgs a = logit_args(dims, vocab, rows, logits, draft_tok, rules, status);
+  a.out = out;
+  clear_stale_error();
+  return hip_status(launch_logit_rules(a, dtype, stream));
+}
+
+size_t carryover_probabilities_workspace_bytes(const co_dims* dims, int32_t vocab, int32_t rows) {
+  if (check_dims(dims) != CO_OK || check_logits(dims, vocab, rows, CO_DTYPE_F32) != CO_OK) return 0;
+  return plan_logits(dims->num_seqs, rows, vocab, num_cus()).ws_bytes;
+}
+
+co_status carryover_probabilities(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,
+                                  const void* logits, const int32_t* draft_tok,
+                                  const co_logit_rules* rules, const float* temperature,
+                                  float* probs, int32_t* top_tok, int32_t* status, void* ws,
+                                  size_t ws_bytes, hipStream_t stream) {
+  co_status s = check_dims(dims);
+  if (s != CO_OK) return s;
+  if ((s = check_logits(dims, vocab, rows, dtype)) != CO_OK) return s;
+  const size_t es = dtype == CO_DTYPE_BF16 ? 2 : 4;
+  const size_t n = static_cast<size_t>(dims->num_seqs) * rows * vocab;
+  if (!logits || !probs || !status || (rules && !rules_ok(rules)) || !aligned(logits, es) ||
+      !aligned(draft_tok, 4) || !aligned(temperature, 4) || !aligned(probs, 4) ||
+      !aligned(top_tok, 4) || !aligned(status, 4) || overlap(logits, n * es, probs, n * 4))
+    return CO_ERR_INVALID_ARG;
+  if (!ws || !aligned(ws, 256)) return CO_ERR_INVALID_ARG;
+  if (ws_bytes < plan_logits(dims->num_seqs, rows, vocab, num_cus()).ws_bytes)
+    return CO_ERR_WORKSPACE;
+  LogitArgs a = logit_args(dims, vocab, rows, logits, draft_tok, rules, status);
+  a.temperature = temperature;
+  a.probs = probs;
+  a.top = top_tok;
+  a.ws = static_cast<float4*>(ws);
+  clear_stale_error();
+  return hip_status(launch_probabilities(a, dtype, stream));
+}
+
 co_status carryover_set_tuning(int32_t knob, int64_t value) {
   if (knob < 0 || knob >= CO_TUNE_COUNT) return CO_ERR_INVALID_ARG;
   g_tuning.v[knob] = value < 0 ? -1 : value;
@@ -940,7 +1177,8 @@ const char* carryover_status_string(co_status status) {
     case CO_ERR_LENGTH: return "invalid sequence length";
     case CO_ERR_GROUP: return "page rows differ within a sequence group";
     case CO_ERR_POOL: return "page pool exhausted or corrupt";
-    case CO_ERR_TOKEN: return "proposed token outside the vocabulary";
+    case CO_ERR_TOKEN: return "token outside the vocabulary";
+    case CO_ERR_MASK: return "mask index out of range";
     default: return "unknown status";
   }
 }

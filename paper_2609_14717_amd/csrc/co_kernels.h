@@ -262,6 +262,101 @@ struct StoreArgs {
   int32_t* status;
 };
 
+// Products of 8-bit integers with a scale for each row of both operands.
+constexpr int kMaxSumI8 = 131008;         // of codes from -128 on: the sum fits 32 bits
+constexpr int kMaxSideI8 = (1 << 24) - 1; // rows of an operand
+constexpr int64_t kMaxGrid = 1 << 23;     // workgroups of up to 511 threads in one launch
+
+struct MatmulI8Args {
+  int M, N, K, dtype;                     // dtype of out
+  const int8_t* A;                        // [M][K]
+  const int8_t* W;                        // [N][K]
+  const float* a_scale;                   // [M]
+  const float* w_scale;                   // [N]
+  const float* bias;                      // [N] or null
+  void* out;                              // [M][N]
+  void* ws;
+};
+
+struct MatmulI8Plan {
+  int64_t workgroups;
+  size_t ws_bytes;
+};
+
+MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus);
+hipError_t launch_matmul_i8(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream);
+hipError_t launch_quantize_i8(const void* x, int64_t rows, int cols, int dtype, int8_t* codes,
+                              float* scale, hipStream_t stream);
+
+// The projection with 8-bit weights (carryover_project_kv_i8).
+struct ProjectI8Args {
+  int M, Dcat, d;
+  const void* hidden;        // [M][Dcat] bf16
+  const int8_t* wf;          // [d][Dcat]
+  const float* wf_scale;     // [d]
+  const int8_t* wkv;         // [n_kv][d]
+  const float* wkv_scale;    // [n_kv]
+  const float* fe;           // F(E) [d], or null
+  const float* znorm;        // [d], or null
+  KvDest dst;
+  void* ws;
+};
+
+size_t project_i8_ws_bytes(int M, int Dcat, int d, int n_kv, int num_cus);
+hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t stream);
+// Rows of K/V products in fp32 [splits][M][n_kv], summed over the splits, to their
+// destinations as bf16: keys normalised and rotated.
+hipError_t launch_store_products(const float* y, int splits, int M, int n_kv, const KvDest& dst,
+                                 hipStream_t stream);
+
+// Rules on logits and probabilities (carryover_logit_rules, carryover_probabilities).
+struct LogitArgs {
+  int S, B, R, V;                         // R rows of logits per sequence
+  const void* logits;                     // [S][R][V]
+  void* out;                              // the same, rules applied
+  const int32_t* draft;                   // [S][B] or null
+  const uint16_t* seen;                   // [S][V] or null
+  const float* repetition;                // [S] or null, as the next two
+  const float* presence;
+  const float* frequency;
+  const int32_t* bias_start;              // [S + 1] or null
+  const int32_t* bias_tok;                // [num_bias]
+  const float* bias_val;
+  const int32_t* mask_row;                // [S][R] or null
+  const uint32_t* mask_bits;              // [num_masks][ceil(V / 32)]
+  int num_bias, num_masks;
+  const float* temperature;               // [S] or null
+  float* probs;                           // [S][R][V]
+  int32_t* top;                           // [S][R] or null
+  float4* ws;                             // [S][R][tiles]
+  int32_t* status;
+  int groups, rows_per, tiles, chunks;    // of the plan
+};
+
+struct LogitPlan {
+  int groups, rows_per;      // row groups of a sequence, rows of each
+  int tiles, chunks;         // tiles of a row, chunks of each
+  int64_t workgroups;
+  size_t ws_bytes;
+};
+
+LogitPlan plan_logits(int S, int R, int V, int num_cus);
+hipError_t launch_logit_rules(const LogitArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_probabilities(const LogitArgs& a, int dtype, hipStream_t stream);
+
+// Token history (carryover_count_tokens).
+struct CountArgs {
+  int S, V, width, tiles;
+  uint32_t flags;
+  const int32_t* tokens;     // [S][width]
+  const int32_t* len;        // [S] or null
+  uint16_t* seen;            // [S][V]
+  int32_t* status;
+};
+
+int64_t count_workgroups(int S, int V);
+hipError_t launch_count_tokens(CountArgs a, hipStream_t stream);
+
 // Launch-shape override in force (-1: automatic); see carryover_set_tuning.
 int64_t tuning(int knob);
 

@@ -1,0 +1,343 @@
+"""8-bit products, logit rules and probabilities without a GPU: the oracle's pins and the
+host checks of the entry points (refusals return before anything is enqueued; no compute
+call runs here)."""
+import os
+from fractions import Fraction
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2609_14717_amd as co
+from oracle import head
+
+needs_lib = pytest.mark.skipif(not os.path.exists(co.LIB_PATH), reason="library not built")
+FAKE = 1 << 20      # an aligned, non-null address that is never dereferenced here
+
+
+# ------------------------------------------------------------------ the oracle
+
+def test_codes_are_the_nearest_integers_of_the_exact_quotient():
+    rng = np.random.default_rng(7)
+    x = rng.standard_normal((6, 64)).astype(np.float32)
+    x[1] = torch.tensor(x[1]).bfloat16().float().numpy()
+    x[2] = np.arange(64) * 0.5                  # many middles: 127 x / 31.5 = 4.03.. x
+    x[3] = (np.arange(64) - 32) / 254.0 * 127   # 127 x / a with a = 16: exact quarters
+    x[3, 0] = 63.5                              # a = 63.5: 127 x / a = 2 x, exact halves
+    x[4] = 0.0
+    codes, scale = head.quantize(x)
+    for i in range(len(x)):
+        a = max(Fraction(float(np.abs(x[i]).max())), Fraction(127, 2 ** 126))
+        for k in range(64):
+            q = Fraction(127) * Fraction(float(x[i, k])) / a
+            assert codes[i, k] == round(q)      # (of a fraction: ties to even)
+        assert scale[i] == pytest.approx(float(a) / 127, rel=1e-15)
+    codes, scale = head.quantize([[1.0] * 63 + [np.inf], [np.nan] * 64, [-2.0] + [0.0] * 63])
+    assert not codes[:2].any() and np.isnan(scale[:2]).all()
+    assert codes[2, 0] == -127 and scale[2] == 2 / 127
+
+
+def test_product_of_codes_is_the_scaled_integer_sum():
+    a = np.array([[1, -2, 3], [127, 127, 127]])
+    w = np.array([[4, 5, -6], [-128, -128, -128]])
+    y, _ = head.matmul_i8(a, [0.5, 1.0], w, [2.0, 1.0], [10.0, 0.0])
+    np.testing.assert_array_equal(y, [[-24 * 1.0 + 10, -256 * 0.5], [381 * 2.0 + 10, -48768.0]])
+
+
+def test_projection_with_exact_codes_is_the_plain_projection():
+    """Integer rows whose largest entry is 127 are their own codes at the first product; with
+    F = 127 e_k selections z keeps them, so that both products are exact."""
+    rng = np.random.default_rng(3)
+    M, D, L, Hkv, hd = 4, 128, 1, 1, 64
+    H = rng.integers(-127, 128, (M, D)).astype(np.float64)
+    H[:, 5] = 127
+    perm = rng.permutation(D)
+    wf = np.zeros((D, D), np.int64)
+    wf[np.arange(D), perm] = 1
+    wkv = rng.integers(-127, 128, (2 * hd, D))
+    sf, skv = np.ones(D), np.full(2 * hd, 0.01)
+    pos = np.array([0, 3, 70, 5000])
+    k, v, *_ = head.project_i8(H, wf, sf, wkv, skv, None, np.zeros(M), pos, L, Hkv, hd, 1e4)
+    K, V = oracle.project(H, np.zeros(D), np.zeros(M, bool), wf.astype(float), wkv * skv[:, None],
+                          pos, L, Hkv, hd, 1e4)
+    np.testing.assert_allclose(k.reshape(-1), np.asarray(K).reshape(k.shape).reshape(-1), rtol=1e-12, atol=1e-12)
+    np.testing.assert_allclose(v.reshape(-1), np.asarray(V).reshape(v.shape).reshape(-1), rtol=1e-12, atol=1e-12)
+
+
+def test_history_words():
+    seen = np.zeros((3, 5), np.uint16)
+    seen[1] = 9
+    seen[2, 4] = 32766
+    tok = np.array([[1, 1, -1, 4], [0, 2, 2, 2], [4, 4, 4, 0]])
+    w, st = head.count_tokens(seen, tok, [3, 0, 3], prompt=False, fresh=False)
+    np.testing.assert_array_equal(w, [[0, 2, 0, 0, 0], [9] * 5, [0, 0, 0, 0, 32767]])
+    assert st == oracle.OK
+    w, st = head.count_tokens(w, tok, [4, 0, 4], prompt=True, fresh=True)
+    np.testing.assert_array_equal(w, [[0, 0x8000, 0, 0, 0x8000], [9] * 5, [0x8000, 0, 0, 0, 0x8000]])
+    _, st = head.count_tokens(w, tok + 1, [4, 5, 0], prompt=True, fresh=False)
+    assert st == oracle.ERR_LENGTH
+    _, st = head.count_tokens(w, tok + 1, [4, 0, 0], prompt=True, fresh=False)
+    assert st == oracle.ERR_TOKEN
+
+
+def test_rules_by_hand():
+    x = [2.0, -2.0, 2.0, 2.0, 0.5, np.nan]
+    word = [0x8000, 0x8000 | 1, 0, 3, 0, 0]
+    y, err = head.rules_row(x, word, window=[2, 2, 0, 99, -1], repetition=2.0, presence=0.25,
+                            frequency=0.5, biases=[(4, 7.0), (3, -1.0), (4, 1.0), (77, 3.0)],
+                            allowed=[1, 1, 1, 1, 1, 0])
+    np.testing.assert_array_equal(y, [1 - 0.5 - 0.25, -4 - 0.5 - 0.25, 1 - 1.0 - 0.25,
+                                      1 - 1.5 - 0.25 - 1, 1.5, -np.inf])
+    assert err[4] == 1.5 * 2.0 ** -24 and err[5] == 0 and (err[:4] > 0).all()
+
+
+def test_probabilities_by_hand():
+    p, tol, top = head.probabilities_row(np.array([0.0, np.log(3.0), -np.inf]), np.zeros(3))
+    np.testing.assert_allclose(p, [0.25, 0.75, 0.0], rtol=1e-15)
+    assert top == 1 and tol[0] < 1e-4
+    p, _, top = head.probabilities_row(np.array([1.0, 5.0, 5.0]), np.zeros(3), temperature=0.0)
+    np.testing.assert_array_equal(p, [0, 1, 0])
+    assert top == 1
+    p, _, top = head.probabilities_row(np.array([-np.inf, np.nan]), np.zeros(2))
+    assert top == -1 and not p.any()
+    p, _, top = head.probabilities_row(np.array([np.inf, 3.0, np.inf]), np.zeros(3))
+    np.testing.assert_array_equal(p, [0.5, 0, 0.5])
+    assert top == 0
+
+
+# ------------------------------------------------------------------ refusals
+
+def _rc(fn):
+    try:
+        fn()
+    except co.CarryoverError as e:
+        return e.code
+    return co.CO_OK
+
+
+def dims(S=2, B=16, **kw):
+    base = dict(Dcat=768, d=256, L=1, Hq=4, Hkv=2, hd=64, max_pages_per_seq=8, num_pages=16,
+                dtype="bf16", theta=1e4)
+    base.update(kw)
+    return co.make_dims(S, B, **base)
+
+
+@needs_lib
+@pytest.mark.parametrize("rows,cols,dtype,kw,code", [
+    (-1, 64, "bf16", {}, co.CO_ERR_INVALID_ARG),
+    (1, 0, "bf16", {}, co.CO_ERR_INVALID_ARG),
+    (1, 65, "bf16", {}, co.CO_ERR_UNSUPPORTED),
+    (1 << 24, 64, "bf16", {}, co.CO_ERR_UNSUPPORTED),
+    (1, 64, 7, {}, co.CO_ERR_UNSUPPORTED),
+    (1, 64, "f32", dict(x=0), co.CO_ERR_INVALID_ARG),
+    (1, 64, "f32", dict(x=FAKE + 4), co.CO_ERR_INVALID_ARG),
+    (1, 64, "f32", dict(codes=FAKE + 8), co.CO_ERR_INVALID_ARG),
+    (1, 64, "f32", dict(scale=FAKE + 2), co.CO_ERR_INVALID_ARG),
+    (1, 64, "f32", dict(scale=0), co.CO_ERR_INVALID_ARG),
+])
+def test_quantize_refusals(rows, cols, dtype, kw, code):
+    p = dict(x=FAKE, codes=FAKE, scale=FAKE, **{})
+    p.update(kw)
+    assert _rc(lambda: co.carryover_quantize_i8(rows, cols, dtype, p["x"], p["codes"], p["scale"],
+                                                stream=0)) == code
+
+
+@needs_lib
+@pytest.mark.parametrize("m,n,k,kw,code", [
+    (-1, 64, 64, {}, co.CO_ERR_INVALID_ARG),
+    (1, -1, 64, {}, co.CO_ERR_INVALID_ARG),
+    (1, 64, 0, {}, co.CO_ERR_UNSUPPORTED),
+    (1, 64, 32, {}, co.CO_ERR_UNSUPPORTED),
+    (1, 64, 131072, {}, co.CO_ERR_UNSUPPORTED),
+    (1 << 24, 1, 64, {}, co.CO_ERR_UNSUPPORTED),
+    (1, 1 << 24, 64, {}, co.CO_ERR_UNSUPPORTED),
+    ((1 << 24) - 1, (1 << 24) - 1, 64, {}, co.CO_ERR_UNSUPPORTED),
+    (1, 64, 64, dict(dtype=2), co.CO_ERR_UNSUPPORTED),
+    (1, 64, 64, dict(a=0), co.CO_ERR_INVALID_ARG),
+    (1, 64, 64, dict(a=FAKE + 8), co.CO_ERR_INVALID_ARG),
+    (1, 64, 64, dict(w=FAKE + 1), co.CO_ERR_INVALID_ARG),
+    (1, 64, 64, dict(a_scale=0), co.CO_ERR_INVALID_ARG),
+    (1, 64, 64, dict(w_scale=FAKE + 2), co.CO_ERR_INVALID_ARG),
+    (1, 64, 64, dict(bias=FAKE + 2), co.CO_ERR_INVALID_ARG),
+    (1, 64, 64, dict(out=0), co.CO_ERR_INVALID_ARG),
+    (1, 64, 64, dict(out=FAKE + 4), co.CO_ERR_INVALID_ARG),
+])
+def test_matmul_refusals(m, n, k, kw, code):
+    p = dict(a=FAKE, a_scale=FAKE, w=FAKE, w_scale=FAKE, bias=None, dtype="bf16", out=FAKE)
+    p.update(kw)
+    assert _rc(lambda: co.carryover_matmul_i8(m, n, k, p["a"], p["a_scale"], p["w"], p["w_scale"],
+                                              p["bias"], p["dtype"], p["out"], FAKE, stream=0,
+                                              ws_bytes=1 << 40)) == code
+    if not kw:
+        assert co.matmul_i8_workspace_bytes(m, n, k) == 0
+
+
+@needs_lib
+@pytest.mark.parametrize("m,n,k", [(1, 256, 768), (16, 4096, 20480), (17, 128000, 4096)])
+def test_matmul_workspace_is_checked(m, n, k):
+    need = co.matmul_i8_workspace_bytes(m, n, k)
+    call = lambda ws, nb: _rc(lambda: co.carryover_matmul_i8(  # noqa: E731
+        m, n, k, FAKE, FAKE, FAKE, FAKE, None, "bf16", FAKE, ws, stream=0, ws_bytes=nb))
+    if need:
+        assert call(FAKE, need - 1) == co.CO_ERR_WORKSPACE
+        assert call(FAKE + 16, need) == co.CO_ERR_INVALID_ARG
+        assert call(0, need) == co.CO_ERR_INVALID_ARG
+
+
+def _weights_i8(**kw):
+    p = dict(w_f=FAKE, w_f_scale=FAKE, w_kv=FAKE, w_kv_scale=FAKE)
+    p.update(kw)
+    return co.weights_i8(**p)
+
+
+@needs_lib
+@pytest.mark.parametrize("d,w,code", [
+    (dict(dtype="f32"), {}, co.CO_ERR_UNSUPPORTED),
+    (dict(Dcat=131072), {}, co.CO_ERR_UNSUPPORTED),
+    (dict(d=131072), {}, co.CO_ERR_UNSUPPORTED),
+    (dict(d=16448), dict(z_norm=FAKE), co.CO_ERR_UNSUPPORTED),
+    (dict(S=1 << 20), {}, co.CO_ERR_UNSUPPORTED),
+    ({}, dict(w_f=0), co.CO_ERR_INVALID_ARG),
+    ({}, dict(w_f_scale=0), co.CO_ERR_INVALID_ARG),
+    ({}, dict(w_kv=FAKE + 8), co.CO_ERR_INVALID_ARG),
+    ({}, dict(w_kv_scale=FAKE + 2), co.CO_ERR_INVALID_ARG),
+    ({}, dict(f_e=FAKE + 4), co.CO_ERR_INVALID_ARG),
+])
+def test_project_refusals(d, w, code):
+    d = dims(**d)
+    st = {k: FAKE for k in ("ctx_len", "carry_len", "page_table", "k_cache", "v_cache", "k_carry",
+                            "v_carry", "status")}
+    rt = {k: FAKE for k in ("accept_len", "row_pos", "row_dst")}
+    assert _rc(lambda: co.carryover_project_kv_i8(d, _weights_i8(**w), FAKE, rt, st, FAKE, stream=0,
+                                                  ws_bytes=1 << 50)) == code
+
+
+@needs_lib
+def test_project_workspace_is_checked():
+    d = dims()
+    st = {k: FAKE for k in ("ctx_len", "carry_len", "page_table", "k_cache", "v_cache", "k_carry",
+                            "v_carry", "status")}
+    rt = {k: FAKE for k in ("accept_len", "row_pos", "row_dst")}
+    need = co.workspace_bytes(d, co.CO_WS_PROJECT_I8)
+    call = lambda ws, nb: _rc(lambda: co.carryover_project_kv_i8(  # noqa: E731
+        d, _weights_i8(), FAKE, rt, st, ws, stream=0, ws_bytes=nb))
+    assert need > 0 and call(FAKE, need - 1) == co.CO_ERR_WORKSPACE
+    assert call(FAKE + 128, need) == co.CO_ERR_INVALID_ARG
+    assert call(0, need) == co.CO_ERR_INVALID_ARG
+    assert co.workspace_bytes(dims(dtype="f32"), co.CO_WS_PROJECT_I8) == 0
+    st["status"] = 0
+    assert call(FAKE, need) == co.CO_ERR_INVALID_ARG
+
+
+@needs_lib
+@pytest.mark.parametrize("kw,code", [
+    (dict(vocab=0), co.CO_ERR_UNSUPPORTED),
+    (dict(width=-1), co.CO_ERR_INVALID_ARG),
+    (dict(tokens=0), co.CO_ERR_INVALID_ARG),
+    (dict(lens=FAKE + 2), co.CO_ERR_INVALID_ARG),
+    (dict(flags=4), co.CO_ERR_INVALID_ARG),
+    (dict(seen=0), co.CO_ERR_INVALID_ARG),
+    (dict(seen=FAKE + 1), co.CO_ERR_INVALID_ARG),
+    (dict(status=0), co.CO_ERR_INVALID_ARG),
+    (dict(dims=dims(B=0)), co.CO_ERR_INVALID_ARG),
+    (dict(dims=dims(S=1 << 20), vocab=1 << 20), co.CO_ERR_UNSUPPORTED),
+])
+def test_count_refusals(kw, code):
+    p = dict(dims=dims(), vocab=1000, width=16, tokens=FAKE, lens=None, flags=0, seen=FAKE, status=FAKE)
+    p.update(kw)
+    assert _rc(lambda: co.carryover_count_tokens(*p.values(), stream=0)) == code
+
+
+def _rules(**kw):
+    return co.logit_rules(**{k: v for k, v in kw.items() if k not in ("num_bias", "num_masks")})
+
+
+RULE_CASES = [
+    (dict(repetition=FAKE), co.CO_ERR_INVALID_ARG),                      # penalties need a history
+    (dict(frequency=FAKE), co.CO_ERR_INVALID_ARG),
+    (dict(seen=FAKE + 1), co.CO_ERR_INVALID_ARG),
+    (dict(seen=FAKE, presence=FAKE + 2), co.CO_ERR_INVALID_ARG),
+    (dict(bias_start=FAKE), co.CO_ERR_INVALID_ARG),                      # three or none
+    (dict(mask_row=FAKE), co.CO_ERR_INVALID_ARG),                        # both or none
+]
+
+
+def _raw_rules(**kw):
+    r = co.co_logit_rules()
+    for k, v in kw.items():
+        setattr(r, k, v)
+    return r
+
+
+@needs_lib
+@pytest.mark.parametrize("probs", [False, True])
+@pytest.mark.parametrize("kw,code", [
+    (dict(vocab=0), co.CO_ERR_UNSUPPORTED),
+    (dict(rows=0), co.CO_ERR_INVALID_ARG),
+    (dict(rows=18), co.CO_ERR_INVALID_ARG),                              # block + 1 at most
+    (dict(dtype=3), co.CO_ERR_UNSUPPORTED),
+    (dict(logits=0), co.CO_ERR_INVALID_ARG),
+    (dict(logits=FAKE + 2), co.CO_ERR_INVALID_ARG),
+    (dict(draft=FAKE + 2), co.CO_ERR_INVALID_ARG),
+    (dict(out=0), co.CO_ERR_INVALID_ARG),
+    (dict(out=FAKE + 64), co.CO_ERR_INVALID_ARG),                        # overlaps the logits
+    (dict(status=0), co.CO_ERR_INVALID_ARG),
+    (dict(dims=dims(B=1025)), co.CO_ERR_UNSUPPORTED),
+    (dict(dims=dims(S=1 << 20), vocab=1 << 20), co.CO_ERR_UNSUPPORTED),
+] + [(dict(rules=_raw_rules(**r)), c) for r, c in RULE_CASES] + [
+    (dict(rules=_raw_rules(num_bias=-1)), co.CO_ERR_INVALID_ARG),
+    (dict(rules=_raw_rules(num_masks=-1)), co.CO_ERR_INVALID_ARG),
+])
+def test_logit_refusals(probs, kw, code):
+    p = dict(dims=dims(), vocab=1000, rows=17, dtype="f32", logits=FAKE, draft=None, rules=_raw_rules(),
+             out=1 << 30, status=FAKE)
+    p.update(kw)
+    if probs:
+        call = lambda: co.carryover_probabilities(  # noqa: E731
+            p["dims"], p["vocab"], p["rows"], p["dtype"], p["logits"], p["draft"], p["rules"], None,
+            p["out"], None, p["status"], FAKE, stream=0, ws_bytes=1 << 50)
+    else:
+        call = lambda: co.carryover_logit_rules(*p.values(), stream=0)  # noqa: E731
+    assert _rc(call) == code
+
+
+@needs_lib
+def test_probabilities_workspace_temperature_and_top():
+    d = dims()
+    need = co.probabilities_workspace_bytes(d, 1000, 17)
+    assert need > 0 and co.probabilities_workspace_bytes(d, 0, 17) == 0
+    assert co.probabilities_workspace_bytes(d, 1000, 18) == 0
+
+    def call(ws=FAKE, nb=need, t=None, top=None, out=1 << 30):
+        return _rc(lambda: co.carryover_probabilities(d, 1000, 17, "f32", FAKE, None, None, t, out, top,
+                                                      FAKE, ws, stream=0, ws_bytes=nb))
+    assert call(nb=need - 1) == co.CO_ERR_WORKSPACE
+    assert call(ws=FAKE + 64) == co.CO_ERR_INVALID_ARG
+    assert call(ws=0) == co.CO_ERR_INVALID_ARG
+    assert call(t=FAKE + 1) == co.CO_ERR_INVALID_ARG
+    assert call(top=FAKE + 1) == co.CO_ERR_INVALID_ARG
+    assert call(out=FAKE) == co.CO_ERR_INVALID_ARG          # in place is the rules' call
+
+
+@needs_lib
+def test_rules_call_needs_rules():
+    import ctypes
+    d = dims()
+    assert co.lib().carryover_logit_rules(ctypes.byref(d), 1000, 17, 0, FAKE, None, None, 1 << 30, FAKE,
+                                          0) == co.CO_ERR_INVALID_ARG
+
+
+def test_strided_tensors_are_refused():
+    x = torch.zeros(4, 128)[:, ::2]
+    with pytest.raises(ValueError, match="x is not contiguous"):
+        co._dense(x, "x")
+    with pytest.raises(ValueError, match="seen is not contiguous"):
+        co.logit_rules(seen=torch.zeros(4, 6, dtype=torch.int16).t())
+    with pytest.raises(ValueError, match="w_f is not contiguous"):
+        co.weights_i8(torch.zeros(64, 64, dtype=torch.int8).t(), None, None, None)
+
+
+@needs_lib
+def test_mask_status_has_a_message():
+    assert "mask" in co.status_string(co.CO_ERR_MASK)
