@@ -779,12 +779,14 @@ co_status carryover_read_status(const co_state* state, int32_t* host_out, hipStr
  *                                   attention kernel
  *   CO_TUNE_ATTN_GROUP_SPLIT_TILES  committed tiles per share, grouped-prefix
  *                                   attention
+ *   CO_TUNE_MATMUL_I8               8-bit product: tile variant 0..6 at any size, or 7: the
+ *                                   kernel for up to 32 rows where it applies
  * Returns CO_ERR_INVALID_ARG for an unknown knob.  Workspace sizes follow the
  * overrides in force when carryover_workspace_bytes is called.
  */
 enum { CO_TUNE_GEMM_WIDE_VARIANT = 0, CO_TUNE_GEMM_NO_WIDE = 1, CO_TUNE_PROJECT_FUSED_MIN_ROWS = 2,
        CO_TUNE_ATTN_WAVE = 3, CO_TUNE_ATTN_WORKGROUPS = 4, CO_TUNE_ATTN_ROUND_TILES = 5,
-       CO_TUNE_ATTN_GROUP_SPLIT_TILES = 6, CO_TUNE_COUNT = 7 };
+       CO_TUNE_ATTN_GROUP_SPLIT_TILES = 6, CO_TUNE_MATMUL_I8 = 7, CO_TUNE_COUNT = 8 };
 co_status carryover_set_tuning(int32_t knob, int64_t value);
 
 /* Static message for a status code. */

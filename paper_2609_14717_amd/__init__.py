@@ -29,7 +29,8 @@ CO_WS_PROJECT_I8 = 9
 CO_COUNT_PROMPT, CO_COUNT_FRESH = 1, 2
 # launch-shape overrides (carryover_set_tuning)
 TUNING = {"gemm_wide_variant": 0, "gemm_no_wide": 1, "project_fused_min_rows": 2, "attn_wave": 3,
-          "attn_workgroups": 4, "attn_round_tiles": 5, "attn_group_split_tiles": 6}
+          "attn_workgroups": 4, "attn_round_tiles": 5, "attn_group_split_tiles": 6,
+          "matmul_i8": 7}
 SKIP = -(2 ** 31)
 PAGE = 16
 

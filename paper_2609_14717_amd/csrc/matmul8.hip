@@ -66,38 +66,391 @@ __device__ __forceinline__ i32x16 mfma_i8(i32x4 a, i32x4 b, i32x16 c) {
 #endif
 }
 
+__device__ __forceinline__ i32x4 mfma_i8(i32x4 a, i32x4 b, i32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+
+// One result; the operations are rounded one by one.
 __device__ __forceinline__ float scaled(int sum, float sa, float sw) {
 #pragma clang fp contract(off)
   return static_cast<float>(sum) * (sa * sw);
 }
 
-// A wavefront: 32 x 32 outputs, fragments from memory.  Lane l holds 16 k of row l % 32
-// of each operand; result register r is column l % 32 of row 8 (r / 4) + 4 (l / 32) + r % 4.
-template <typename T>
-__global__ __launch_bounds__(256) void matmul_i8_kernel(MatmulI8Args g, int tiles_n) {
+__device__ __forceinline__ float scaled(int sum, float sa, float sw, float bias) {
 #pragma clang fp contract(off)
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int m0 = static_cast<int>(blockIdx.x / tiles_n) * 64 + (wave >> 1) * 32;
-  const int n0 = static_cast<int>(blockIdx.x % tiles_n) * 64 + (wave & 1) * 32;
-  const int am = min(m0 + (lane & 31), g.M - 1), bn = min(n0 + (lane & 31), g.N - 1);
-  const int8_t* pa = g.A + static_cast<int64_t>(am) * g.K + (lane >> 5) * 16;
-  const int8_t* pb = g.W + static_cast<int64_t>(bn) * g.K + (lane >> 5) * 16;
-  i32x16 acc = {};
-  for (int k = 0; k < g.K; k += 32)
-    acc = mfma_i8(*reinterpret_cast<const i32x4*>(pa + k), *reinterpret_cast<const i32x4*>(pb + k), acc);
-  const int col = n0 + (lane & 31);
-  if (col >= g.N) return;
-  const float sw = g.w_scale[col];
-  const float bias = g.bias ? g.bias[col] : 0.f;
+  const float v = static_cast<float>(sum) * (sa * sw);
+  return v + bias;
+}
+
+template <typename T> __device__ __forceinline__ void put(T* p, float v);
+template <> __device__ __forceinline__ void put<float>(float* p, float v) { *p = v; }
+template <> __device__ __forceinline__ void put<uint16_t>(uint16_t* p, float v) {
+  *p = static_cast<uint16_t>(cvt_pk_bf16(v, v));
+}
+
+// Workgroups are dealt to the eight XCDs in turn: renumbered, each XCD gets a run of
+// consecutive indices, whose shared panels then stay in its L2.
+__device__ __forceinline__ int xcd_run(int t, int total) {
+  const int q = total >> 3, r = total & 7, x = t & 7;
+  return x * q + min(x, r) + (t >> 3);
+}
+
+// Few rows (16 MT of them): bound by reading the weights once.  A workgroup's NW
+// wavefronts share 16 TN columns and split K: a wavefront takes every NW-th unit of 256
+// bytes of K, straight into the operand registers of v_mfma_i32_16x16x64_i8 (lane l holds
+// row or column l % 16, 16 k from 16 (l / 16) on; result register r is row 4 (l / 16) + r,
+// column l % 16), the next unit's loads in flight while one is multiplied.  The NW partial
+// tiles are added in LDS: whole numbers, so the order does not matter.
+constexpr int kUnit = 256;
+
+template <int MT, int TN, int NW, typename T>
+__global__ __launch_bounds__(64 * NW) void matmul_i8_few_kernel(MatmulI8Args g) {
+  __shared__ int red[NW][MT * TN * 256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n0 = static_cast<int>(blockIdx.x) * 16 * TN;
+  const int quad = (lane >> 4) * 16;
+  const int8_t* pa[MT];
+  const int8_t* pw[TN];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int row = m0 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-    if (row >= g.M) continue;
-    float v = scaled(acc[r], g.a_scale[row], sw);
-    if (g.bias) v = v + bias;
-    T* out = static_cast<T*>(g.out) + static_cast<int64_t>(row) * g.N + col;
-    if constexpr (sizeof(T) == 2) *out = static_cast<T>(cvt_pk_bf16(v, v)); else *out = v;
+  for (int i = 0; i < MT; ++i)
+    pa[i] = g.A + static_cast<int64_t>(min(16 * i + (lane & 15), g.M - 1)) * g.K + quad;
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+    pw[j] = g.W + static_cast<int64_t>(min(n0 + 16 * j + (lane & 15), g.N - 1)) * g.K + quad;
+  i32x4 acc[MT][TN] = {};
+  struct Unit {
+    i32x4 a[4][MT], w[4][TN];
+  };
+  const int units = g.K / kUnit;
+  auto load = [&](int u, Unit& f) {
+    const int64_t k = static_cast<int64_t>(u) * kUnit;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) f.w[t][j] = *reinterpret_cast<const i32x4*>(pw[j] + k + 64 * t);
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) f.a[t][i] = *reinterpret_cast<const i32x4*>(pa[i] + k + 64 * t);
+    }
+  };
+  auto compute = [&](const Unit& f) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mfma_i8(f.a[t][i], f.w[t][j], acc[i][j]);
+  };
+  Unit f0, f1;
+  int u = wave;
+  if (u < units) load(u, f0);
+  while (u < units) {
+    if (u + NW < units) load(u + NW, f1);
+    compute(f0);
+    u += NW;
+    if (u >= units) break;
+    if (u + NW < units) load(u + NW, f0);
+    compute(f1);
+    u += NW;
   }
+  for (int k = units * kUnit + 64 * wave; k < g.K; k += 64 * NW) {   // up to three steps of 64
+    i32x4 w[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) w[j] = *reinterpret_cast<const i32x4*>(pw[j] + k);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const i32x4 a = *reinterpret_cast<const i32x4*>(pa[i] + k);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma_i8(a, w[j], acc[i][j]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        red[wave][(16 * i + 4 * (lane >> 4) + r) * (16 * TN) + 16 * j + (lane & 15)] = acc[i][j][r];
+  __syncthreads();
+  for (int o = tid; o < MT * TN * 256; o += 64 * NW) {
+    const int row = o / (16 * TN), col = n0 + o % (16 * TN);
+    if (row >= g.M || col >= g.N) continue;
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) sum += red[w][o];
+    const float sa = g.a_scale[row], sw = g.w_scale[col];
+    put(static_cast<T*>(g.out) + static_cast<int64_t>(row) * g.N + col,
+        g.bias ? scaled(sum, sa, sw, g.bias[col]) : scaled(sum, sa, sw));
+  }
+}
+
+// Many rows: a tile of BM x BN outputs, eight wavefronts (2 x 4) of TMW x TNW tiles of
+// v_mfma_i32_32x32x32_i8 (lane l holds row or column l % 32, 16 k from 16 (l / 32) on;
+// result register r is row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32).  K advances in
+// stages of 64 bytes through a ring of NS in LDS, filled by direct-to-LDS loads that the
+// compiler does not see: a wavefront waits for its own with an exact count and a barrier
+// publishes a stage.  Staged rows are 64 bytes, their 16-byte chunks permuted by row / 4 so
+// that 16 lanes reading a fragment hit 16 bank groups.  Fragments of a step of 32 k are read
+// while the step before multiplies.
+typedef uint16_t u16x8u __attribute__((ext_vector_type(8), aligned(2)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
+template <int TMW, int TNW, int NS>
+struct WideTile {
+  static constexpr int BM = 64 * TMW, BN = 128 * TNW, ROWS = BM + BN;
+  static constexpr int STAGE = ROWS * 64;
+};
+
+template <int TMW, int TNW, int NS, typename T>
+__global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, int tiles_m,
+                                                                int tiles_n, int k_per_split) {
+  using Tile = WideTile<TMW, TNW, NS>;
+  constexpr int BM = Tile::BM, BN = Tile::BN, ROWS = Tile::ROWS, STAGE = Tile::STAGE;
+  constexpr int LOADS = ROWS / 16;                       // 1 KiB loads of a stage
+  constexpr int LPW = (LOADS + 7) / 8;                   // of a wavefront, at most
+  constexpr int FULL = LOADS - 8 * (LPW - 1);            // wavefronts that issue LPW of them
+  constexpr int PASS = 64, LDC = BN + 4;                 // epilogue: 64 rows at a time
+  static_assert(LPW * (NS - 1) < 64 && NS >= 2 && NS <= 8, "vmcnt");
+  static_assert(PASS * LDC * 4 <= NS * STAGE, "the epilogue's rows must fit in the ring");
+  static_assert(NS * STAGE <= 160 * 1024, "LDS");
+  __shared__ __align__(16) unsigned char smem[NS * STAGE];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 2, wn = wave & 3;
+  const bool full = wave < FULL;
+  // Splits of K one after the other; within one, groups of up to four row tiles sweep the
+  // column tiles, so that consecutive indices share panels of both operands.
+  const int t = xcd_run(blockIdx.x, gridDim.x);
+  const int per_split = tiles_m * tiles_n;
+  const int sp = t / per_split, r0 = t % per_split;
+  const int gm = min(4, tiles_m), grp = r0 / (gm * tiles_n);
+  const int gsz = min(gm, tiles_m - grp * gm), rg = r0 % (gm * tiles_n);
+  const int m0 = (grp * gm + rg % gsz) * BM, n0 = rg / gsz * BN;
+  const int kbeg = sp * k_per_split;
+  const int nk = min(g.K - kbeg, k_per_split) / 64;
+
+  // load j of the wavefront fills rows 16 (8 j + wave) .. + 15
+  const int8_t* src[LPW];
+#pragma unroll
+  for (int j = 0; j < LPW; ++j) {
+    const int row = min(8 * j + wave, LOADS - 1) * 16 + lane / 4;
+    const int chunk = (lane & 3) ^ ((row >> 2) & 3);
+    const int8_t* base = row < BM ? g.A + static_cast<int64_t>(min(m0 + row, g.M - 1)) * g.K
+                                  : g.W + static_cast<int64_t>(min(n0 + row - BM, g.N - 1)) * g.K;
+    src[j] = base + kbeg + chunk * 16;
+  }
+  const uint32_t ring = lds_addr(smem);
+  auto issue = [&](int kt) {
+    const uint32_t st = ring + (kt % NS) * STAGE;
+#pragma unroll
+    for (int j = 0; j < LPW; ++j)
+      if (j < LPW - 1 || full) lds_dma16_opaque(src[j] + kt * 64, st + (8 * j + wave) * 1024);
+  };
+  // Waits until the stage `ahead` stages before the newest one issued has landed.
+  auto wait_stage = [&](int ahead) {
+    switch (ahead) {
+#define CO_WAIT(n)                                              \
+  case n:                                                       \
+    if constexpr (NS > n) {                                     \
+      if (full) wait_vm_lgkm_barrier<n * LPW>();                \
+      else wait_vm_lgkm_barrier<n * (LPW - 1)>();               \
+    }                                                           \
+    break;
+      CO_WAIT(7) CO_WAIT(6) CO_WAIT(5) CO_WAIT(4) CO_WAIT(3) CO_WAIT(2) CO_WAIT(1)
+#undef CO_WAIT
+      default: wait_vm_lgkm_barrier<0>();
+    }
+  };
+
+  i32x16 acc[TMW][TNW] = {};
+  const int frow = (lane & 31) * 64;
+  const int fswz = ((lane & 31) >> 2) & 3;
+  struct Frags {
+    i32x4 a[TMW], b[TNW];
+  };
+  auto load = [&](int kt, int h, Frags& f) {
+    const unsigned char* st = smem + (kt % NS) * STAGE;
+    const int off = frow + (((2 * h + (lane >> 5)) ^ fswz) << 4);
+#pragma unroll
+    for (int a = 0; a < TMW; ++a)
+      f.a[a] = *reinterpret_cast<const i32x4*>(st + (wm * TMW + a) * 2048 + off);
+#pragma unroll
+    for (int b = 0; b < TNW; ++b)
+      f.b[b] = *reinterpret_cast<const i32x4*>(st + BM * 64 + (wn * TNW + b) * 2048 + off);
+  };
+  auto settle = [&](Frags& f) {   // the LDS reads are waited for here, not at the products
+#pragma unroll
+    for (int a = 0; a < TMW; ++a) asm volatile("" : "+v"(f.a[a]));
+#pragma unroll
+    for (int b = 0; b < TNW; ++b) asm volatile("" : "+v"(f.b[b]));
+  };
+  auto compute = [&](const Frags& f) {
+#pragma unroll
+    for (int a = 0; a < TMW; ++a)
+#pragma unroll
+      for (int b = 0; b < TNW; ++b) acc[a][b] = mfma_i8(f.a[a], f.b[b], acc[a][b]);
+  };
+
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+    if (s < nk) issue(s);
+  Frags f0, f1;
+  wait_stage(min(NS - 1, nk - 1));
+  load(0, 0, f0);
+  for (int kt = 0; kt < nk; ++kt) {
+    load(kt, 1, f1);
+    __builtin_amdgcn_sched_barrier(0);
+    compute(f0);
+    __builtin_amdgcn_sched_barrier(0);
+    settle(f1);
+    // every wavefront holds all of stage kt: its slot takes stage kt + NS
+    if (kt + 1 < nk) {
+      wait_stage(min(NS - 2, nk - 2 - kt));
+      if (kt + NS < nk) issue(kt + NS);
+      load(kt + 1, 0, f0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    compute(f1);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  wait_vm_lgkm_barrier<0>();   // the ring is reused below
+
+  if (gridDim.x > static_cast<unsigned>(per_split)) {   // a part of K: sums to the workspace
+    int* out = static_cast<int*>(g.ws) + static_cast<int64_t>(sp) * g.M * g.N;
+#pragma unroll
+    for (int a = 0; a < TMW; ++a)
+#pragma unroll
+      for (int b = 0; b < TNW; ++b) {
+        const int col = n0 + (wn * TNW + b) * 32 + (lane & 31);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = m0 + (wm * TMW + a) * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+          if (row < g.M && col < g.N) out[static_cast<int64_t>(row) * g.N + col] = acc[a][b][r];
+        }
+      }
+    return;
+  }
+  int* sc = reinterpret_cast<int*>(smem);
+#pragma unroll
+  for (int p = 0; p < BM / PASS; ++p) {
+#pragma unroll
+    for (int a = 0; a < TMW; ++a) {
+      if ((wm * TMW + a) * 32 / PASS != p) continue;
+#pragma unroll
+      for (int b = 0; b < TNW; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = (wm * TMW + a) * 32 - p * PASS + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+          sc[row * LDC + (wn * TNW + b) * 32 + (lane & 31)] = acc[a][b][r];
+        }
+    }
+    __syncthreads();
+    for (int c = tid; c < PASS * BN / 8; c += 512) {
+      const int rl = c / (BN / 8), cc = c % (BN / 8) * 8;
+      const int row = m0 + p * PASS + rl, col = n0 + cc;
+      if (row >= g.M || col >= g.N) continue;
+      const float sa = g.a_scale[row];
+      T* out = static_cast<T*>(g.out) + static_cast<int64_t>(row) * g.N + col;
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int cq = min(col + q, g.N - 1);
+        const int sum = sc[rl * LDC + cc + q];
+        v[q] = g.bias ? scaled(sum, sa, g.w_scale[cq], g.bias[cq]) : scaled(sum, sa, g.w_scale[cq]);
+      }
+      if (col + 8 > g.N) {
+        for (int q = 0; col + q < g.N; ++q) put(out + q, v[q]);
+      } else if constexpr (sizeof(T) == 2) {
+        u16x8u o;
+#pragma unroll
+        for (int q = 0; q < 8; q += 2) {
+          const uint32_t w = cvt_pk_bf16(v[q], v[q + 1]);
+          o[q] = static_cast<uint16_t>(w);
+          o[q + 1] = static_cast<uint16_t>(w >> 16);
+        }
+        *reinterpret_cast<u16x8u*>(out) = o;
+      } else {
+        *reinterpret_cast<f32x4u*>(out) = f32x4u{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4u*>(out + 4) = f32x4u{v[4], v[5], v[6], v[7]};
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// The parts of K added up and scaled.
+template <typename T>
+__global__ __launch_bounds__(256) void sum_parts_i8_kernel(MatmulI8Args g, int splits) {
+  const int64_t n = static_cast<int64_t>(g.M) * g.N;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int* part = static_cast<const int*>(g.ws);
+  int sum = 0;
+  for (int s = 0; s < splits; ++s) sum += part[s * n + i];
+  const int row = static_cast<int>(i / g.N), col = static_cast<int>(i % g.N);
+  const float sa = g.a_scale[row], sw = g.w_scale[col];
+  put(static_cast<T*>(g.out) + i, g.bias ? scaled(sum, sa, sw, g.bias[col]) : scaled(sum, sa, sw));
+}
+
+// Tile variants of the wide kernel; kFew: the kernel for few rows.
+constexpr int kVariants = 7, kFew = kVariants;
+constexpr int kBM[kVariants] = {256, 256, 128, 192, 128, 64, 64};
+constexpr int kBN[kVariants] = {256, 128, 256, 256, 128, 256, 128};
+
+template <typename T>
+hipError_t launch_wide(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
+  const int tm = (g.M + kBM[p.variant] - 1) / kBM[p.variant];
+  const int tn = (g.N + kBN[p.variant] - 1) / kBN[p.variant];
+  const dim3 grid(static_cast<unsigned>(p.workgroups)), block(512);
+  const int k = p.k_per_split;
+  switch (p.variant) {
+    case 0: hipLaunchKernelGGL((matmul_i8_wide_kernel<4, 2, 4, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 1: hipLaunchKernelGGL((matmul_i8_wide_kernel<4, 1, 5, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 2: hipLaunchKernelGGL((matmul_i8_wide_kernel<2, 2, 5, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 3: hipLaunchKernelGGL((matmul_i8_wide_kernel<3, 2, 5, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 4: hipLaunchKernelGGL((matmul_i8_wide_kernel<2, 1, 8, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 5: hipLaunchKernelGGL((matmul_i8_wide_kernel<1, 2, 6, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    default: hipLaunchKernelGGL((matmul_i8_wide_kernel<1, 1, 8, T>), grid, block, 0, stream, g, tm, tn, k); break;
+  }
+  if (p.splits > 1) {
+    const int64_t n = static_cast<int64_t>(g.M) * g.N;
+    hipLaunchKernelGGL(sum_parts_i8_kernel<T>, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256),
+                       0, stream, g, p.splits);
+  }
+  return hipGetLastError();
+}
+
+template <int MT, int TN, typename T>
+hipError_t launch_few_nw(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(p.workgroups));
+  if constexpr (MT * TN <= 2) {   // (more tiles need more than the 128 registers of sixteen wavefronts)
+    if (p.waves == 16) {
+      hipLaunchKernelGGL((matmul_i8_few_kernel<MT, TN, 16, T>), grid, dim3(1024), 0, stream, g);
+      return hipGetLastError();
+    }
+  }
+  if (p.waves == 8) hipLaunchKernelGGL((matmul_i8_few_kernel<MT, TN, 8, T>), grid, dim3(512), 0, stream, g);
+  else hipLaunchKernelGGL((matmul_i8_few_kernel<MT, TN, 4, T>), grid, dim3(256), 0, stream, g);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_few(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
+  if (g.M <= 16) {
+    if (p.cols == 4) return launch_few_nw<1, 4, T>(g, p, stream);
+    if (p.cols == 2) return launch_few_nw<1, 2, T>(g, p, stream);
+    return launch_few_nw<1, 1, T>(g, p, stream);
+  }
+  if (p.cols == 4) return launch_few_nw<2, 4, T>(g, p, stream);
+  if (p.cols == 2) return launch_few_nw<2, 2, T>(g, p, stream);
+  return launch_few_nw<2, 1, T>(g, p, stream);
 }
 
 }  // namespace
@@ -115,24 +468,58 @@ hipError_t launch_quantize_i8(const void* x, int64_t rows, int cols, int dtype, 
   return hipGetLastError();
 }
 
+constexpr int kFewRows = 32;
+
 MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
-  (void)K;
-  (void)num_cus;
   MatmulI8Plan p{};
-  p.workgroups = static_cast<int64_t>((M + 63) / 64) * ((N + 63) / 64);
-  p.ws_bytes = 0;
+  p.splits = 1;
+  p.k_per_split = K;
+  const int64_t force = tuning(CO_TUNE_MATMUL_I8);
+  if (force < 0 ? M <= kFewRows : force == kFew && M <= kFewRows) {
+    p.variant = kFew;
+    // columns of a workgroup: as many (the rows' codes are read once for them) as leave
+    // two workgroups to a compute unit
+    p.cols = N >= 128 * num_cus ? 4 : (N >= 64 * num_cus ? 2 : 1);
+    p.workgroups = (N + 16 * p.cols - 1) / (16 * p.cols);
+    // wavefronts: enough of them on the chip, each with a unit of K or more
+    p.waves = 4;
+    while (p.waves < 16 && p.workgroups * p.waves < 16ll * num_cus && K / kUnit > p.waves) p.waves *= 2;
+    if (p.cols * (M > 16 ? 2 : 1) > 2 && p.waves == 16) p.waves = 8;
+    return p;
+  }
+  double best = 1e30;
+  for (int v = 0; v < kVariants; ++v) {
+    if (force >= 0 && force < kFew && force != v) continue;
+    const int64_t tm = (static_cast<int64_t>(M) + kBM[v] - 1) / kBM[v];
+    const int64_t tiles = tm * ((static_cast<int64_t>(N) + kBN[v] - 1) / kBN[v]);
+    for (int s = 1; s <= 8; ++s) {
+      const int kps = ((K + s - 1) / s + 63) / 64 * 64;
+      if (s > 1 && (kps < 512 || (K + kps - 1) / kps != s || static_cast<int64_t>(M) * N * s > (1ll << 28)))
+        continue;
+      const int64_t wgs = tiles * s, waves = (wgs + num_cus - 1) / num_cus;
+      constexpr double kEff[kVariants] = {1.0, 0.8, 0.85, 0.95, 0.7, 0.6, 0.45};
+      const double t_mfma = static_cast<double>(waves) * kBM[v] * kBN[v] * (kps + 256.0) * 2.0 / (8.0e12 * kEff[v]);
+      const double t_mem = static_cast<double>(tm) * N * K / 8.0e12 + static_cast<double>(N) * K / 8e12;
+      const double t_part = s > 1 ? static_cast<double>(s) * M * N * 8.0 / 4.0e12 + 3e-6 : 0.0;
+      const double t = (t_mfma > t_mem ? t_mfma : t_mem) + t_part;
+      if (t < best) {
+        best = t;
+        p.variant = v;
+        p.splits = s;
+        p.k_per_split = kps;
+        p.workgroups = wgs;
+      }
+    }
+  }
+  p.ws_bytes = p.splits > 1 ? (static_cast<size_t>(p.splits) * M * N * 4 + 255) / 256 * 256 : 0;
   return p;
 }
 
 hipError_t launch_matmul_i8(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
   if (g.M == 0 || g.N == 0) return hipSuccess;
-  const int tiles_n = (g.N + 63) / 64;
-  const dim3 grid(static_cast<unsigned>(p.workgroups)), block(256);
-  if (g.dtype == CO_DTYPE_BF16)
-    hipLaunchKernelGGL(matmul_i8_kernel<uint16_t>, grid, block, 0, stream, g, tiles_n);
-  else
-    hipLaunchKernelGGL(matmul_i8_kernel<float>, grid, block, 0, stream, g, tiles_n);
-  return hipGetLastError();
+  if (p.variant == kFew)
+    return g.dtype == CO_DTYPE_BF16 ? launch_few<uint16_t>(g, p, stream) : launch_few<float>(g, p, stream);
+  return g.dtype == CO_DTYPE_BF16 ? launch_wide<uint16_t>(g, p, stream) : launch_wide<float>(g, p, stream);
 }
 
 // -------------------------------------------- projection with 8-bit weights
@@ -189,9 +576,10 @@ size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
 
 size_t project_i8_ws_bytes(int M, int Dcat, int d, int n_kv, int num_cus) {
   const int wide = Dcat > d ? Dcat : d, out = d > n_kv ? d : n_kv;
-  (void)num_cus;
+  const size_t pf = plan_matmul_i8(M, d, Dcat, num_cus).ws_bytes;
+  const size_t pk = plan_matmul_i8(M, n_kv, d, num_cus).ws_bytes;
   return pad256(static_cast<size_t>(M) * wide) + pad256(static_cast<size_t>(M) * 4) +
-         pad256(static_cast<size_t>(M) * out * 4);
+         pad256(static_cast<size_t>(M) * out * 4) + (pf > pk ? pf : pk);
 }
 
 hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t stream) {
@@ -202,6 +590,7 @@ hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t st
   int8_t* codes = reinterpret_cast<int8_t*>(ws);
   float* scale = reinterpret_cast<float*>(ws + pad256(static_cast<size_t>(a.M) * wide));
   float* y = reinterpret_cast<float*>(reinterpret_cast<char*>(scale) + pad256(static_cast<size_t>(a.M) * 4));
+  const int out = a.d > n_kv ? a.d : n_kv;
   hipError_t err = launch_quantize_i8(a.hidden, a.M, a.Dcat, CO_DTYPE_BF16, codes, scale, stream);
   if (err != hipSuccess) return err;
   MatmulI8Args g{};
@@ -214,6 +603,7 @@ hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t st
   g.W = a.wf;
   g.w_scale = a.wf_scale;
   g.out = y;
+  g.ws = reinterpret_cast<char*>(y) + pad256(static_cast<size_t>(a.M) * out * 4);
   if ((err = launch_matmul_i8(g, plan_matmul_i8(g.M, g.N, g.K, num_cus), stream)) != hipSuccess) return err;
   hipLaunchKernelGGL(z_codes_kernel, dim3(a.M), dim3(256), 0, stream, y, a.d, a.fe, a.znorm,
                      a.dst.row_dst, codes, scale);

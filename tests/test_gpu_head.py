@@ -142,6 +142,18 @@ def test_product(m, n, k, dtype, bias):
     check_product(*ops, dtype, product(*ops, dtype), f"{m} x {n} x {k}")
 
 
+@pytest.mark.parametrize("variant", range(8))
+def test_product_variants(variant, tune):
+    """Every tile at sizes that end inside it, with one stage of K, few and many, with and
+    without a split of K."""
+    tune("matmul_i8", variant)
+    for m, n, k in ((1, 1, 64), (31, 255, 128), (70, 300, 256), (257, 129, 640), (193, 513, 4096), (20, 70, 8256),
+                    (513, 260, 1088)):
+        print(f"[product] variant {variant}: {m} x {n} x {k}", flush=True)
+        ops = operands(m, n, k, m + n + k, True)
+        check_product(*ops, "f32", product(*ops, "f32"), f"variant {variant}: {m} x {n} x {k}")
+
+
 def test_product_of_the_largest_sums():
     """-128 times -128 at the longest rows: 131008 * 2^14, the sum that fits 32 bits."""
     m, n, k = 3, 5, 131008
