@@ -193,30 +193,24 @@ __global__ __launch_bounds__(64 * NW) void matmul_i8_few_kernel(MatmulI8Args g) 
 // Many rows: a tile of BM x BN outputs, eight wavefronts (2 x 4) of TMW x TNW tiles of
 // v_mfma_i32_32x32x32_i8 (lane l holds row or column l % 32, 16 k from 16 (l / 32) on;
 // result register r is row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32).  K advances in
-// stages of 64 bytes through a ring of NS in LDS, filled by direct-to-LDS loads that the
-// compiler does not see: a wavefront waits for its own with an exact count and a barrier
-// publishes a stage.  Staged rows are 64 bytes, their 16-byte chunks permuted by row / 4 so
-// that 16 lanes reading a fragment hit 16 bank groups.  Fragments of a step of 32 k are read
-// while the step before multiplies.
+// stages of 128 bytes (whole cache lines: stages of 64 fetch every line twice) through a
+// ring of NS in LDS, filled by direct-to-LDS loads that the compiler does not see: a
+// wavefront waits for its own with an exact count and a barrier publishes a stage.  The
+// 16-byte chunks of a staged row are permuted by row / 2, so that 16 lanes reading a
+// fragment hit 16 bank groups.  Fragments of a step of 32 k are read while the step before
+// multiplies.
 typedef uint16_t u16x8u __attribute__((ext_vector_type(8), aligned(2)));
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
-template <int TMW, int TNW, int NS>
-struct WideTile {
-  static constexpr int BM = 64 * TMW, BN = 128 * TNW, ROWS = BM + BN;
-  static constexpr int STAGE = ROWS * 64;
-};
+constexpr int kStageK = 128;
 
 template <int TMW, int TNW, int NS, typename T>
 __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, int tiles_m,
                                                                 int tiles_n, int k_per_split) {
-  using Tile = WideTile<TMW, TNW, NS>;
-  constexpr int BM = Tile::BM, BN = Tile::BN, ROWS = Tile::ROWS, STAGE = Tile::STAGE;
-  constexpr int LOADS = ROWS / 16;                       // 1 KiB loads of a stage
-  constexpr int LPW = (LOADS + 7) / 8;                   // of a wavefront, at most
-  constexpr int FULL = LOADS - 8 * (LPW - 1);            // wavefronts that issue LPW of them
+  constexpr int BM = 64 * TMW, BN = 128 * TNW, ROWS = BM + BN, STAGE = ROWS * kStageK;
+  constexpr int LPW = ROWS / 64;                         // 1 KiB loads of a wavefront, a stage
   constexpr int PASS = 64, LDC = BN + 4;                 // epilogue: 64 rows at a time
-  static_assert(LPW * (NS - 1) < 64 && NS >= 2 && NS <= 8, "vmcnt");
+  static_assert(LPW * (NS - 1) < 64 && NS >= 2 && NS <= 4, "vmcnt");
   static_assert(PASS * LDC * 4 <= NS * STAGE, "the epilogue's rows must fit in the ring");
   static_assert(NS * STAGE <= 160 * 1024, "LDS");
   __shared__ __align__(16) unsigned char smem[NS * STAGE];
@@ -224,7 +218,6 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 2, wn = wave & 3;
-  const bool full = wave < FULL;
   // Splits of K one after the other; within one, groups of up to four row tiles sweep the
   // column tiles, so that consecutive indices share panels of both operands.
   const int t = xcd_run(blockIdx.x, gridDim.x);
@@ -234,44 +227,47 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
   const int gsz = min(gm, tiles_m - grp * gm), rg = r0 % (gm * tiles_n);
   const int m0 = (grp * gm + rg % gsz) * BM, n0 = rg / gsz * BN;
   const int kbeg = sp * k_per_split;
-  const int nk = min(g.K - kbeg, k_per_split) / 64;
+  const int klen = min(g.K - kbeg, k_per_split);
+  const int nk = (klen + kStageK - 1) / kStageK;
+  const bool half = (klen & 64) != 0;                    // the last stage is half a one
 
-  // load j of the wavefront fills rows 16 (8 j + wave) .. + 15
+  // load j of the wavefront fills rows 8 (LPW wave + j) .. + 7
   const int8_t* src[LPW];
 #pragma unroll
   for (int j = 0; j < LPW; ++j) {
-    const int row = min(8 * j + wave, LOADS - 1) * 16 + lane / 4;
-    const int chunk = (lane & 3) ^ ((row >> 2) & 3);
+    const int row = (LPW * wave + j) * 8 + lane / 8;
+    const int chunk = (lane & 7) ^ ((row >> 1) & 7);
     const int8_t* base = row < BM ? g.A + static_cast<int64_t>(min(m0 + row, g.M - 1)) * g.K
                                   : g.W + static_cast<int64_t>(min(n0 + row - BM, g.N - 1)) * g.K;
     src[j] = base + kbeg + chunk * 16;
   }
+  // chunks past a half stage are not read: they take the half before
+  auto back = [&](int j) {
+    const int row = (LPW * wave + j) * 8 + lane / 8;
+    return (((lane & 7) ^ ((row >> 1) & 7)) & 4) << 4;
+  };
   const uint32_t ring = lds_addr(smem);
   auto issue = [&](int kt) {
-    const uint32_t st = ring + (kt % NS) * STAGE;
+    const uint32_t st = ring + (kt % NS) * STAGE + LPW * wave * 1024;
+    if (half && kt + 1 == nk) {
 #pragma unroll
-    for (int j = 0; j < LPW; ++j)
-      if (j < LPW - 1 || full) lds_dma16_opaque(src[j] + kt * 64, st + (8 * j + wave) * 1024);
+      for (int j = 0; j < LPW; ++j) lds_dma16_opaque(src[j] + kt * kStageK - back(j), st + j * 1024);
+    } else {
+#pragma unroll
+      for (int j = 0; j < LPW; ++j) lds_dma16_opaque(src[j] + kt * kStageK, st + j * 1024);
+    }
   };
   // Waits until the stage `ahead` stages before the newest one issued has landed.
   auto wait_stage = [&](int ahead) {
-    switch (ahead) {
-#define CO_WAIT(n)                                              \
-  case n:                                                       \
-    if constexpr (NS > n) {                                     \
-      if (full) wait_vm_lgkm_barrier<n * LPW>();                \
-      else wait_vm_lgkm_barrier<n * (LPW - 1)>();               \
-    }                                                           \
-    break;
-      CO_WAIT(7) CO_WAIT(6) CO_WAIT(5) CO_WAIT(4) CO_WAIT(3) CO_WAIT(2) CO_WAIT(1)
-#undef CO_WAIT
-      default: wait_vm_lgkm_barrier<0>();
-    }
+    if (NS >= 4 && ahead >= 3) wait_vm_lgkm_barrier<(NS >= 4 ? 3 * LPW : 0)>();
+    else if (NS >= 3 && ahead >= 2) wait_vm_lgkm_barrier<(NS >= 3 ? 2 * LPW : 0)>();
+    else if (ahead >= 1) wait_vm_lgkm_barrier<LPW>();
+    else wait_vm_lgkm_barrier<0>();
   };
 
   i32x16 acc[TMW][TNW] = {};
-  const int frow = (lane & 31) * 64;
-  const int fswz = ((lane & 31) >> 2) & 3;
+  const int frow = (lane & 31) * kStageK;
+  const int fswz = ((lane & 31) >> 1) & 7;
   struct Frags {
     i32x4 a[TMW], b[TNW];
   };
@@ -280,10 +276,10 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
     const int off = frow + (((2 * h + (lane >> 5)) ^ fswz) << 4);
 #pragma unroll
     for (int a = 0; a < TMW; ++a)
-      f.a[a] = *reinterpret_cast<const i32x4*>(st + (wm * TMW + a) * 2048 + off);
+      f.a[a] = *reinterpret_cast<const i32x4*>(st + (wm * TMW + a) * 32 * kStageK + off);
 #pragma unroll
     for (int b = 0; b < TNW; ++b)
-      f.b[b] = *reinterpret_cast<const i32x4*>(st + BM * 64 + (wn * TNW + b) * 2048 + off);
+      f.b[b] = *reinterpret_cast<const i32x4*>(st + (BM + (wn * TNW + b) * 32) * kStageK + off);
   };
   auto settle = [&](Frags& f) {   // the LDS reads are waited for here, not at the products
 #pragma unroll
@@ -304,21 +300,32 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
   Frags f0, f1;
   wait_stage(min(NS - 1, nk - 1));
   load(0, 0, f0);
-  for (int kt = 0; kt < nk; ++kt) {
-    load(kt, 1, f1);
-    __builtin_amdgcn_sched_barrier(0);
-    compute(f0);
-    __builtin_amdgcn_sched_barrier(0);
-    settle(f1);
-    // every wavefront holds all of stage kt: its slot takes stage kt + NS
-    if (kt + 1 < nk) {
-      wait_stage(min(NS - 2, nk - 2 - kt));
-      if (kt + NS < nk) issue(kt + NS);
-      load(kt + 1, 0, f0);
+  const int whole = half ? nk - 1 : nk;
+  for (int kt = 0; kt < whole; ++kt) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      Frags& cur = (h & 1) ? f1 : f0;
+      Frags& nxt = (h & 1) ? f0 : f1;
+      if (h < 3) load(kt, h + 1, nxt);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(cur);
+      __builtin_amdgcn_sched_barrier(0);
+      if (h == 2) {
+        // every wavefront holds the rest of stage kt: its slot takes stage kt + NS
+        settle(nxt);
+        if (kt + 1 < nk) {
+          wait_stage(min(NS - 2, nk - 2 - kt));
+          if (kt + NS < nk) issue(kt + NS);
+          load(kt + 1, 0, cur);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
-    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (half) {
+    load(nk - 1, 1, f1);
+    compute(f0);
     compute(f1);
-    __builtin_amdgcn_sched_barrier(0);
   }
   wait_vm_lgkm_barrier<0>();   // the ring is reused below
 
@@ -411,13 +418,13 @@ hipError_t launch_wide(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t
   const dim3 grid(static_cast<unsigned>(p.workgroups)), block(512);
   const int k = p.k_per_split;
   switch (p.variant) {
-    case 0: hipLaunchKernelGGL((matmul_i8_wide_kernel<4, 2, 4, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    case 1: hipLaunchKernelGGL((matmul_i8_wide_kernel<4, 1, 5, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    case 2: hipLaunchKernelGGL((matmul_i8_wide_kernel<2, 2, 5, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    case 3: hipLaunchKernelGGL((matmul_i8_wide_kernel<3, 2, 5, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    case 4: hipLaunchKernelGGL((matmul_i8_wide_kernel<2, 1, 8, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    case 5: hipLaunchKernelGGL((matmul_i8_wide_kernel<1, 2, 6, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    default: hipLaunchKernelGGL((matmul_i8_wide_kernel<1, 1, 8, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 0: hipLaunchKernelGGL((matmul_i8_wide_kernel<4, 2, 2, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 1: hipLaunchKernelGGL((matmul_i8_wide_kernel<4, 1, 3, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 2: hipLaunchKernelGGL((matmul_i8_wide_kernel<2, 2, 3, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 3: hipLaunchKernelGGL((matmul_i8_wide_kernel<3, 2, 2, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 4: hipLaunchKernelGGL((matmul_i8_wide_kernel<2, 1, 4, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    case 5: hipLaunchKernelGGL((matmul_i8_wide_kernel<1, 2, 3, T>), grid, block, 0, stream, g, tm, tn, k); break;
+    default: hipLaunchKernelGGL((matmul_i8_wide_kernel<1, 1, 4, T>), grid, block, 0, stream, g, tm, tn, k); break;
   }
   if (p.splits > 1) {
     const int64_t n = static_cast<int64_t>(g.M) * g.N;
