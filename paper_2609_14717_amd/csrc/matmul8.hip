@@ -191,29 +191,41 @@ __global__ __launch_bounds__(64 * NW) void matmul_i8_few_kernel(MatmulI8Args g) 
 }
 
 // Many rows: a tile of BM x BN outputs, eight wavefronts (2 x 4) of TMW x TNW tiles of
-// v_mfma_i32_32x32x32_i8 (lane l holds row or column l % 32, 16 k from 16 (l / 32) on;
-// result register r is row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32).  K advances in
+// v_mfma_i32_32x32x32_i8 (lane l holds row or column l % 32, 16 k from 16 (l / 32) on).
+// The weights are its first operand, so that a lane ends with one output row, l % 32, and
+// in registers 4 q .. 4 q + 3 four columns next to each other, from 8 q + 4 (l / 32) on,
+// which go to memory from the registers.  K advances in
 // stages of 128 bytes (whole cache lines: stages of 64 fetch every line twice) through a
 // ring of NS in LDS, filled by direct-to-LDS loads that the compiler does not see: a
 // wavefront waits for its own with an exact count and a barrier publishes a stage.  The
 // 16-byte chunks of a staged row are permuted by row / 2, so that 16 lanes reading a
 // fragment hit 16 bank groups.  Fragments of a step of 32 k are read while the step before
 // multiplies.
-typedef uint16_t u16x8u __attribute__((ext_vector_type(8), aligned(2)));
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
-
 constexpr int kStageK = 128;
+
+// Columns col .. col + C - 1 of a row that starts anywhere, those below N.
+template <int C, typename E, typename V>
+__device__ __forceinline__ void put_cols(E* row, int col, int N, const V& v) {
+  typedef E out_t __attribute__((ext_vector_type(C), aligned(sizeof(E))));
+  if (col + C <= N) {
+    *reinterpret_cast<out_t*>(row + col) = v;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < C; ++i)
+    if (col + i < N) row[col + i] = v[i];
+}
 
 template <int TMW, int TNW, int NS, typename T>
 __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, int tiles_m,
                                                                 int tiles_n, int k_per_split) {
+#pragma clang fp contract(off)
   constexpr int BM = 64 * TMW, BN = 128 * TNW, ROWS = BM + BN, STAGE = ROWS * kStageK;
   constexpr int LPW = ROWS / 64;                         // 1 KiB loads of a wavefront, a stage
-  constexpr int PASS = 64, LDC = BN + 4;                 // epilogue: 64 rows at a time
   static_assert(LPW * (NS - 1) < 64 && NS >= 2 && NS <= 4, "vmcnt");
-  static_assert(PASS * LDC * 4 <= NS * STAGE, "the epilogue's rows must fit in the ring");
-  static_assert(NS * STAGE <= 160 * 1024, "LDS");
+  static_assert(NS * STAGE + 8 * BN <= 160 * 1024, "LDS");
   __shared__ __align__(16) unsigned char smem[NS * STAGE];
+  __shared__ __align__(16) float col_scale[BN], col_bias[BN];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -291,9 +303,14 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
 #pragma unroll
     for (int a = 0; a < TMW; ++a)
 #pragma unroll
-      for (int b = 0; b < TNW; ++b) acc[a][b] = mfma_i8(f.a[a], f.b[b], acc[a][b]);
+      for (int b = 0; b < TNW; ++b) acc[a][b] = mfma_i8(f.b[b], f.a[a], acc[a][b]);
   };
 
+  for (int c = tid; c < BN; c += 512) {   // (read behind the main loop's barriers)
+    const int col = min(n0 + c, g.N - 1);
+    col_scale[c] = g.w_scale[col];
+    col_bias[c] = g.bias ? g.bias[col] : 0.f;
+  }
 #pragma unroll
   for (int s = 0; s < NS; ++s)
     if (s < nk) issue(s);
@@ -327,68 +344,60 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
     compute(f0);
     compute(f1);
   }
-  wait_vm_lgkm_barrier<0>();   // the ring is reused below
 
-  if (gridDim.x > static_cast<unsigned>(per_split)) {   // a part of K: sums to the workspace
-    int* out = static_cast<int*>(g.ws) + static_cast<int64_t>(sp) * g.M * g.N;
+  const bool parts = gridDim.x > static_cast<unsigned>(per_split);   // of K: sums to the workspace
+  int* part = static_cast<int*>(g.ws) + static_cast<int64_t>(sp) * g.M * g.N;
 #pragma unroll
-    for (int a = 0; a < TMW; ++a)
+  for (int a = 0; a < TMW; ++a) {
+    const int row = m0 + (wm * TMW + a) * 32 + (lane & 31);
+    const bool in = row < g.M;
+    const int64_t at = static_cast<int64_t>(in ? row : 0) * g.N;
+    const float sa = parts ? 0.f : g.a_scale[in ? row : 0];
 #pragma unroll
-      for (int b = 0; b < TNW; ++b) {
-        const int col = n0 + (wn * TNW + b) * 32 + (lane & 31);
+    for (int b = 0; b < TNW; ++b) {
+      const int cb = (wn * TNW + b) * 32;
+      if (parts) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int row = m0 + (wm * TMW + a) * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-          if (row < g.M && col < g.N) out[static_cast<int64_t>(row) * g.N + col] = acc[a][b][r];
+        for (int q = 0; q < 4; ++q) {
+          const int col = n0 + cb + 8 * q + 4 * (lane >> 5);
+          const i32x4 v = {acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
+          if (in) put_cols<4>(part + at, col, g.N, v);
+        }
+        continue;
+      }
+      f32x4 v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = cb + 8 * q + 4 * (lane >> 5);
+        const f32x4 sw = *reinterpret_cast<const f32x4*>(col_scale + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[q][i] = scaled(acc[a][b][4 * q + i], sa, sw[i]);
+        if (g.bias) {
+          const f32x4 bv = *reinterpret_cast<const f32x4*>(col_bias + c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[q][i] = v[q][i] + bv[i];
         }
       }
-    return;
-  }
-  int* sc = reinterpret_cast<int*>(smem);
+      if constexpr (sizeof(T) == 4) {
 #pragma unroll
-  for (int p = 0; p < BM / PASS; ++p) {
-#pragma unroll
-    for (int a = 0; a < TMW; ++a) {
-      if ((wm * TMW + a) * 32 / PASS != p) continue;
-#pragma unroll
-      for (int b = 0; b < TNW; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int row = (wm * TMW + a) * 32 - p * PASS + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-          sc[row * LDC + (wn * TNW + b) * 32 + (lane & 31)] = acc[a][b][r];
-        }
-    }
-    __syncthreads();
-    for (int c = tid; c < PASS * BN / 8; c += 512) {
-      const int rl = c / (BN / 8), cc = c % (BN / 8) * 8;
-      const int row = m0 + p * PASS + rl, col = n0 + cc;
-      if (row >= g.M || col >= g.N) continue;
-      const float sa = g.a_scale[row];
-      T* out = static_cast<T*>(g.out) + static_cast<int64_t>(row) * g.N + col;
-      float v[8];
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const int cq = min(col + q, g.N - 1);
-        const int sum = sc[rl * LDC + cc + q];
-        v[q] = g.bias ? scaled(sum, sa, g.w_scale[cq], g.bias[cq]) : scaled(sum, sa, g.w_scale[cq]);
-      }
-      if (col + 8 > g.N) {
-        for (int q = 0; col + q < g.N; ++q) put(out + q, v[q]);
-      } else if constexpr (sizeof(T) == 2) {
-        u16x8u o;
-#pragma unroll
-        for (int q = 0; q < 8; q += 2) {
-          const uint32_t w = cvt_pk_bf16(v[q], v[q + 1]);
-          o[q] = static_cast<uint16_t>(w);
-          o[q + 1] = static_cast<uint16_t>(w >> 16);
-        }
-        *reinterpret_cast<u16x8u*>(out) = o;
+        for (int q = 0; q < 4; ++q)
+          if (in) put_cols<4>(static_cast<float*>(g.out) + at, n0 + cb + 8 * q + 4 * (lane >> 5), g.N, v[q]);
       } else {
-        *reinterpret_cast<f32x4u*>(out) = f32x4u{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4u*>(out + 4) = f32x4u{v[4], v[5], v[6], v[7]};
+        // lanes l and l ^ 32 hold every other four columns of a row: exchanged, each has eight
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+          typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+          const auto lo = __builtin_amdgcn_permlane32_swap(cvt_pk_bf16(v[q][0], v[q][1]),
+                                                           cvt_pk_bf16(v[q + 1][0], v[q + 1][1]), false, false);
+          const auto hi = __builtin_amdgcn_permlane32_swap(cvt_pk_bf16(v[q][2], v[q][3]),
+                                                           cvt_pk_bf16(v[q + 1][2], v[q + 1][3]), false, false);
+          const u32x4 w = {static_cast<uint32_t>(lo[0]), static_cast<uint32_t>(hi[0]),
+                           static_cast<uint32_t>(lo[1]), static_cast<uint32_t>(hi[1])};
+          const int col = n0 + cb + 8 * q + 8 * (lane >> 5);
+          if (in) put_cols<8>(static_cast<uint16_t*>(g.out) + at, col, g.N, __builtin_bit_cast(u16x8, w));
+        }
       }
     }
-    __syncthreads();
   }
 }
 
