@@ -216,10 +216,58 @@ __device__ __forceinline__ void put_cols(E* row, int col, int N, const V& v) {
     if (col + i < N) row[col + i] = v[i];
 }
 
+// A wavefront's 32 x 32 results: scaled, the bias added, stored.
+template <typename T>
+__device__ __forceinline__ void put_tile(const MatmulI8Args& g, const i32x16& acc, int row, float sa,
+                                         int n0, int lane, const float* col_scale, const float* col_bias) {
+#pragma clang fp contract(off)
+  f32x4 v[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int c = 8 * q + 4 * (lane >> 5);
+    const f32x4 sw = *reinterpret_cast<const f32x4*>(col_scale + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[q][i] = scaled(acc[4 * q + i], sa, sw[i]);
+    if (g.bias) {
+      const f32x4 bv = *reinterpret_cast<const f32x4*>(col_bias + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[q][i] = v[q][i] + bv[i];
+    }
+  }
+  T* out = static_cast<T*>(g.out) + static_cast<int64_t>(row) * g.N;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (row < g.M) put_cols<4>(out, n0 + 8 * q + 4 * (lane >> 5), g.N, v[q]);
+  } else {
+    // lanes l and l ^ 32 hold every other four columns of a row: exchanged, each has eight
+#pragma unroll
+    for (int q = 0; q < 4; q += 2) {
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      const auto lo = __builtin_amdgcn_permlane32_swap(cvt_pk_bf16(v[q][0], v[q][1]),
+                                                       cvt_pk_bf16(v[q + 1][0], v[q + 1][1]), false, false);
+      const auto hi = __builtin_amdgcn_permlane32_swap(cvt_pk_bf16(v[q][2], v[q][3]),
+                                                       cvt_pk_bf16(v[q + 1][2], v[q + 1][3]), false, false);
+      const u32x4 w = {static_cast<uint32_t>(lo[0]), static_cast<uint32_t>(hi[0]),
+                       static_cast<uint32_t>(lo[1]), static_cast<uint32_t>(hi[1])};
+      if (row < g.M) put_cols<8>(out, n0 + 8 * q + 8 * (lane >> 5), g.N, __builtin_bit_cast(u16x8, w));
+    }
+  }
+}
+
+// Tile r of a part of K: groups of up to four row tiles sweep the column tiles, so that
+// consecutive indices share panels of both operands.
+template <int BM, int BN>
+__device__ __forceinline__ void tile_of(int r, int tiles_m, int tiles_n, int* m0, int* n0) {
+  const int gm = min(4, tiles_m), grp = r / (gm * tiles_n);
+  const int gsz = min(gm, tiles_m - grp * gm), rg = r % (gm * tiles_n);
+  *m0 = (grp * gm + rg % gsz) * BM;
+  *n0 = rg / gsz * BN;
+}
+
 template <int TMW, int TNW, int NS, typename T>
 __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, int tiles_m,
                                                                 int tiles_n, int k_per_split) {
-#pragma clang fp contract(off)
   constexpr int BM = 64 * TMW, BN = 128 * TNW, ROWS = BM + BN, STAGE = ROWS * kStageK;
   constexpr int LPW = ROWS / 64;                         // 1 KiB loads of a wavefront, a stage
   static_assert(LPW * (NS - 1) < 64 && NS >= 2 && NS <= 4, "vmcnt");
@@ -230,14 +278,11 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 2, wn = wave & 3;
-  // Splits of K one after the other; within one, groups of up to four row tiles sweep the
-  // column tiles, so that consecutive indices share panels of both operands.
-  const int t = xcd_run(blockIdx.x, gridDim.x);
+  const int t = xcd_run(blockIdx.x, gridDim.x);   // parts of K one after the other
   const int per_split = tiles_m * tiles_n;
-  const int sp = t / per_split, r0 = t % per_split;
-  const int gm = min(4, tiles_m), grp = r0 / (gm * tiles_n);
-  const int gsz = min(gm, tiles_m - grp * gm), rg = r0 % (gm * tiles_n);
-  const int m0 = (grp * gm + rg % gsz) * BM, n0 = rg / gsz * BN;
+  const int sp = t / per_split;
+  int m0, n0;
+  tile_of<BM, BN>(t % per_split, tiles_m, tiles_n, &m0, &n0);
   const int kbeg = sp * k_per_split;
   const int klen = min(g.K - kbeg, k_per_split);
   const int nk = (klen + kStageK - 1) / kStageK;
@@ -345,74 +390,63 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
     compute(f1);
   }
 
-  const bool parts = gridDim.x > static_cast<unsigned>(per_split);   // of K: sums to the workspace
-  int* part = static_cast<int*>(g.ws) + static_cast<int64_t>(sp) * g.M * g.N;
+  if (gridDim.x > static_cast<unsigned>(per_split)) {
+    // a part of K: the sums to the workspace in the order of the registers, 16 bytes a lane
+    i32x4* part = reinterpret_cast<i32x4*>(g.ws) + static_cast<int64_t>(t) * (BM * BN / 4) + tid;
+#pragma unroll
+    for (int a = 0; a < TMW; ++a)
+#pragma unroll
+      for (int b = 0; b < TNW; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          part[((a * TNW + b) * 4 + q) * 512] = i32x4{acc[a][b][4 * q], acc[a][b][4 * q + 1],
+                                                      acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
+    return;
+  }
 #pragma unroll
   for (int a = 0; a < TMW; ++a) {
     const int row = m0 + (wm * TMW + a) * 32 + (lane & 31);
-    const bool in = row < g.M;
-    const int64_t at = static_cast<int64_t>(in ? row : 0) * g.N;
-    const float sa = parts ? 0.f : g.a_scale[in ? row : 0];
+    const float sa = row < g.M ? g.a_scale[row] : 0.f;
 #pragma unroll
     for (int b = 0; b < TNW; ++b) {
       const int cb = (wn * TNW + b) * 32;
-      if (parts) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int col = n0 + cb + 8 * q + 4 * (lane >> 5);
-          const i32x4 v = {acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
-          if (in) put_cols<4>(part + at, col, g.N, v);
-        }
-        continue;
-      }
-      f32x4 v[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = cb + 8 * q + 4 * (lane >> 5);
-        const f32x4 sw = *reinterpret_cast<const f32x4*>(col_scale + c);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[q][i] = scaled(acc[a][b][4 * q + i], sa, sw[i]);
-        if (g.bias) {
-          const f32x4 bv = *reinterpret_cast<const f32x4*>(col_bias + c);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[q][i] = v[q][i] + bv[i];
-        }
-      }
-      if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (in) put_cols<4>(static_cast<float*>(g.out) + at, n0 + cb + 8 * q + 4 * (lane >> 5), g.N, v[q]);
-      } else {
-        // lanes l and l ^ 32 hold every other four columns of a row: exchanged, each has eight
-#pragma unroll
-        for (int q = 0; q < 4; q += 2) {
-          typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-          const auto lo = __builtin_amdgcn_permlane32_swap(cvt_pk_bf16(v[q][0], v[q][1]),
-                                                           cvt_pk_bf16(v[q + 1][0], v[q + 1][1]), false, false);
-          const auto hi = __builtin_amdgcn_permlane32_swap(cvt_pk_bf16(v[q][2], v[q][3]),
-                                                           cvt_pk_bf16(v[q + 1][2], v[q + 1][3]), false, false);
-          const u32x4 w = {static_cast<uint32_t>(lo[0]), static_cast<uint32_t>(hi[0]),
-                           static_cast<uint32_t>(lo[1]), static_cast<uint32_t>(hi[1])};
-          const int col = n0 + cb + 8 * q + 8 * (lane >> 5);
-          if (in) put_cols<8>(static_cast<uint16_t*>(g.out) + at, col, g.N, __builtin_bit_cast(u16x8, w));
-        }
-      }
+      put_tile<T>(g, acc[a][b], row, sa, n0 + cb, lane, col_scale + cb, col_bias + cb);
     }
   }
 }
 
-// The parts of K added up and scaled.
-template <typename T>
-__global__ __launch_bounds__(256) void sum_parts_i8_kernel(MatmulI8Args g, int splits) {
-  const int64_t n = static_cast<int64_t>(g.M) * g.N;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= n) return;
-  const int* part = static_cast<const int*>(g.ws);
-  int sum = 0;
-  for (int s = 0; s < splits; ++s) sum += part[s * n + i];
-  const int row = static_cast<int>(i / g.N), col = static_cast<int>(i % g.N);
-  const float sa = g.a_scale[row], sw = g.w_scale[col];
-  put(static_cast<T*>(g.out) + i, g.bias ? scaled(sum, sa, sw, g.bias[col]) : scaled(sum, sa, sw));
+// The parts of K of one 32 x 32 tile for each wavefront, added up, scaled and stored.
+template <int TMW, int TNW, typename T>
+__global__ __launch_bounds__(512) void sum_parts_i8_kernel(MatmulI8Args g, int tiles_m, int tiles_n,
+                                                           int splits) {
+  constexpr int BM = 64 * TMW, BN = 128 * TNW;
+  __shared__ __align__(16) float col_scale[BN], col_bias[BN];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave >> 2, wn = wave & 3;
+  const int frag = blockIdx.x % (TMW * TNW), r0 = blockIdx.x / (TMW * TNW);
+  int m0, n0;
+  tile_of<BM, BN>(r0, tiles_m, tiles_n, &m0, &n0);
+  for (int c = tid; c < BN; c += 512) {
+    const int col = min(n0 + c, g.N - 1);
+    col_scale[c] = g.w_scale[col];
+    col_bias[c] = g.bias ? g.bias[col] : 0.f;
+  }
+  const int64_t step = static_cast<int64_t>(tiles_m) * tiles_n * (BM * BN / 4);
+  const i32x4* part = reinterpret_cast<const i32x4*>(g.ws) + static_cast<int64_t>(r0) * (BM * BN / 4) +
+                      frag * 4 * 512 + tid;
+  i32x4 sum[4] = {};
+  for (int s = 0; s < splits; ++s) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum[q] += part[s * step + q * 512];
+  }
+  __syncthreads();
+  i32x16 acc;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = sum[r >> 2][r & 3];
+  const int a = frag / TNW, b = frag % TNW;
+  const int row = m0 + (wm * TMW + a) * 32 + (lane & 31);
+  const int cb = (wn * TNW + b) * 32;
+  put_tile<T>(g, acc, row, row < g.M ? g.a_scale[row] : 0.f, n0 + cb, lane, col_scale + cb, col_bias + cb);
 }
 
 // Tile variants of the wide kernel; kFew: the kernel for few rows.
@@ -420,25 +454,26 @@ constexpr int kVariants = 7, kFew = kVariants;
 constexpr int kBM[kVariants] = {256, 256, 128, 192, 128, 64, 64};
 constexpr int kBN[kVariants] = {256, 128, 256, 256, 128, 256, 128};
 
+template <int TMW, int TNW, int NS, typename T>
+void launch_wide_t(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
+  const int tm = (g.M + 64 * TMW - 1) / (64 * TMW), tn = (g.N + 128 * TNW - 1) / (128 * TNW);
+  hipLaunchKernelGGL((matmul_i8_wide_kernel<TMW, TNW, NS, T>), dim3(static_cast<unsigned>(p.workgroups)),
+                     dim3(512), 0, stream, g, tm, tn, p.k_per_split);
+  if (p.splits > 1)
+    hipLaunchKernelGGL((sum_parts_i8_kernel<TMW, TNW, T>), dim3(static_cast<unsigned>(tm) * tn * TMW * TNW),
+                       dim3(512), 0, stream, g, tm, tn, p.splits);
+}
+
 template <typename T>
 hipError_t launch_wide(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
-  const int tm = (g.M + kBM[p.variant] - 1) / kBM[p.variant];
-  const int tn = (g.N + kBN[p.variant] - 1) / kBN[p.variant];
-  const dim3 grid(static_cast<unsigned>(p.workgroups)), block(512);
-  const int k = p.k_per_split;
   switch (p.variant) {
-    case 0: hipLaunchKernelGGL((matmul_i8_wide_kernel<4, 2, 2, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    case 1: hipLaunchKernelGGL((matmul_i8_wide_kernel<4, 1, 3, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    case 2: hipLaunchKernelGGL((matmul_i8_wide_kernel<2, 2, 3, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    case 3: hipLaunchKernelGGL((matmul_i8_wide_kernel<3, 2, 2, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    case 4: hipLaunchKernelGGL((matmul_i8_wide_kernel<2, 1, 4, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    case 5: hipLaunchKernelGGL((matmul_i8_wide_kernel<1, 2, 3, T>), grid, block, 0, stream, g, tm, tn, k); break;
-    default: hipLaunchKernelGGL((matmul_i8_wide_kernel<1, 1, 4, T>), grid, block, 0, stream, g, tm, tn, k); break;
-  }
-  if (p.splits > 1) {
-    const int64_t n = static_cast<int64_t>(g.M) * g.N;
-    hipLaunchKernelGGL(sum_parts_i8_kernel<T>, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256),
-                       0, stream, g, p.splits);
+    case 0: launch_wide_t<4, 2, 2, T>(g, p, stream); break;
+    case 1: launch_wide_t<4, 1, 3, T>(g, p, stream); break;
+    case 2: launch_wide_t<2, 2, 3, T>(g, p, stream); break;
+    case 3: launch_wide_t<3, 2, 2, T>(g, p, stream); break;
+    case 4: launch_wide_t<2, 1, 4, T>(g, p, stream); break;
+    case 5: launch_wide_t<1, 2, 3, T>(g, p, stream); break;
+    default: launch_wide_t<1, 1, 4, T>(g, p, stream); break;
   }
   return hipGetLastError();
 }
@@ -527,7 +562,7 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
       }
     }
   }
-  p.ws_bytes = p.splits > 1 ? (static_cast<size_t>(p.splits) * M * N * 4 + 255) / 256 * 256 : 0;
+  p.ws_bytes = p.splits > 1 ? static_cast<size_t>(p.workgroups) * kBM[p.variant] * kBN[p.variant] * 4 : 0;
   return p;
 }
 
