@@ -307,10 +307,6 @@ struct ProjectI8Args {
 
 size_t project_i8_ws_bytes(int M, int Dcat, int d, int n_kv, int num_cus);
 hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t stream);
-// Rows of K/V products in fp32 [splits][M][n_kv], summed over the splits, to their
-// destinations as bf16: keys normalised and rotated.
-hipError_t launch_store_products(const float* y, int splits, int M, int n_kv, const KvDest& dst,
-                                 hipStream_t stream);
 
 // Rules on logits and probabilities (carryover_logit_rules, carryover_probabilities).
 struct LogitArgs {

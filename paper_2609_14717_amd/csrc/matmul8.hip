@@ -5,7 +5,7 @@
 //   out[i][j]  = float(sum_k a[i][k] w[j][k]) (a_scale[i] w_scale[j]) + bias[j]
 //
 // Sums are exact: int32, for k up to 131008.
-#include "co_kernels.h"
+#include "co_store.h"
 
 namespace co {
 
@@ -13,6 +13,7 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr float kLeast = 0x1.fcp-120f;   // 127 * 2^-126: smallest magnitude that scales a row
 
@@ -31,29 +32,107 @@ __device__ __forceinline__ int code_of(float x, float a, float r) {
   return static_cast<int>(n);
 }
 
-// One workgroup per row: its largest magnitude, then its codes.
-template <typename T>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const T* x, int cols, int8_t* codes,
-                                                            float* scale) {
-  __shared__ uint32_t red[4];
-  const int64_t row = blockIdx.x;
-  const int tid = threadIdx.x;
-  const T* xr = x + row * cols;
-  auto get = [&](int c) {
-    if constexpr (sizeof(T) == 2) return bf2f(xr[c]); else return xr[c];
-  };
-  uint32_t top = 0;   // magnitudes compare as their bits; infinities and NaNs are largest
-  for (int c = tid; c < cols; c += 256) top = max(top, __float_as_uint(get(c)) & 0x7FFFFFFFu);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off)));
-  if ((tid & 63) == 0) red[tid >> 6] = top;
+// Largest of the workgroup's values, in every thread.
+template <int NT>
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* red) {
+  v = static_cast<uint32_t>(wave_max(static_cast<int>(v)));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  top = max(max(red[0], red[1]), max(red[2], red[3]));
-  const bool fine = top < 0x7F800000u;
-  const float a = fmaxf(__uint_as_float(top), kLeast), r = 127.f / a;
+  v = red[0];
+#pragma unroll
+  for (int w = 1; w < NT / 64; ++w) v = max(v, red[w]);
+  return v;
+}
+
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// Eight elements as fp32.
+__device__ __forceinline__ void eight(const uint16_t* p, float (&x)[8]) {
+  const u16x8 v = *reinterpret_cast<const u16x8*>(p);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = bf2f(v[e]);
+}
+__device__ __forceinline__ void eight(const float* p, float (&x)[8]) {
+  const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = lo[e];
+    x[4 + e] = hi[e];
+  }
+}
+
+// The scale of a row and what its entries are multiplied by; bad: not finite.
+struct RowScale {
+  float a, r, scale;
+  bool bad;
+  __device__ __forceinline__ explicit RowScale(uint32_t top) {
+    bad = top >= 0x7F800000u;
+    a = fmaxf(__uint_as_float(bad ? 0u : top), kLeast);
+    r = 127.f / a;
+    scale = bad ? NAN : a / 127.f;
+  }
+  __device__ __forceinline__ void codes(const float (&x)[8], int8_t* out) const {
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      w[e >> 2] |= (bad ? 0u : static_cast<uint32_t>(code_of(x[e], a, r)) & 0xFFu) << (8 * (e & 3));
+    *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+  }
+};
+
+// One workgroup per row, which it holds in registers (Q times eight entries a thread) from
+// the search for its largest magnitude to its codes; Q = 0: rows of any length, read twice.
+// Magnitudes compare as their bits, infinities and NaNs as the largest.
+template <typename T, int NT, int Q>
+__global__ __launch_bounds__(NT) void quantize_rows_kernel(const T* x, int cols, int8_t* codes,
+                                                           float* scale) {
+  __shared__ uint32_t red[NT / 64];
+  const int64_t row = blockIdx.x;
+  const T* xr = x + row * cols;
   int8_t* cr = codes + row * cols;
-  for (int c = tid; c < cols; c += 256) cr[c] = fine ? static_cast<int8_t>(code_of(get(c), a, r)) : 0;
-  if (tid == 0) scale[row] = fine ? a / 127.f : NAN;
+  uint32_t top = 0;
+  if constexpr (Q > 0) {
+    float v[Q][8];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int c = (q * NT + threadIdx.x) * 8;
+      if (c < cols) eight(xr + c, v[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+      if ((q * NT + threadIdx.x) * 8 < cols)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[q][e]));
+    const RowScale s(block_max<NT>(top, red));
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int c = (q * NT + threadIdx.x) * 8;
+      if (c < cols) s.codes(v[q], cr + c);
+    }
+    if (threadIdx.x == 0) scale[row] = s.scale;
+  } else {
+    float v[8];
+    for (int c = threadIdx.x * 8; c < cols; c += NT * 8) {
+      eight(xr + c, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
+    }
+    const RowScale s(block_max<NT>(top, red));
+    for (int c = threadIdx.x * 8; c < cols; c += NT * 8) {
+      eight(xr + c, v);
+      s.codes(v, cr + c);
+    }
+    if (threadIdx.x == 0) scale[row] = s.scale;
+  }
+}
+
+template <typename T>
+void launch_quantize_t(const T* x, int64_t rows, int cols, int8_t* codes, float* scale, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(rows));
+  if (cols <= 2048) hipLaunchKernelGGL((quantize_rows_kernel<T, 256, 1>), grid, dim3(256), 0, stream, x, cols, codes, scale);
+  else if (cols <= 8192) hipLaunchKernelGGL((quantize_rows_kernel<T, 512, 2>), grid, dim3(512), 0, stream, x, cols, codes, scale);
+  else if (cols <= 32768) hipLaunchKernelGGL((quantize_rows_kernel<T, 1024, 4>), grid, dim3(1024), 0, stream, x, cols, codes, scale);
+  else hipLaunchKernelGGL((quantize_rows_kernel<T, 1024, 0>), grid, dim3(1024), 0, stream, x, cols, codes, scale);
 }
 
 // ------------------------------------------------------------------- product
@@ -190,19 +269,6 @@ __global__ __launch_bounds__(64 * NW) void matmul_i8_few_kernel(MatmulI8Args g) 
   }
 }
 
-// Many rows: a tile of BM x BN outputs, eight wavefronts (2 x 4) of TMW x TNW tiles of
-// v_mfma_i32_32x32x32_i8 (lane l holds row or column l % 32, 16 k from 16 (l / 32) on).
-// The weights are its first operand, so that a lane ends with one output row, l % 32, and
-// in registers 4 q .. 4 q + 3 four columns next to each other, from 8 q + 4 (l / 32) on,
-// which go to memory from the registers.  K advances in
-// stages of 128 bytes (whole cache lines: stages of 64 fetch every line twice) through a
-// ring of NS in LDS, filled by direct-to-LDS loads that the compiler does not see: a
-// wavefront waits for its own with an exact count and a barrier publishes a stage.  The
-// 16-byte chunks of a staged row are permuted by row / 2, so that 16 lanes reading a
-// fragment hit 16 bank groups.  Fragments of a step of 32 k are read while the step before
-// multiplies.
-constexpr int kStageK = 128;
-
 // Columns col .. col + C - 1 of a row that starts anywhere, those below N.
 template <int C, typename E, typename V>
 __device__ __forceinline__ void put_cols(E* row, int col, int N, const V& v) {
@@ -215,6 +281,130 @@ __device__ __forceinline__ void put_cols(E* row, int col, int N, const V& v) {
   for (int i = 0; i < C; ++i)
     if (col + i < N) row[col + i] = v[i];
 }
+
+// Few rows through LDS: a workgroup's four wavefronts take 16 columns each and share 16 MT
+// rows; K advances in stages of 256 bytes a row (long runs of memory) through a ring of NS,
+// and is split over workgroups until the chip is full.  The weights are the first operand: a
+// lane ends with row l % 16 and four columns from 4 (l / 16) on.
+template <int MT, int NS, typename T>
+__global__ __launch_bounds__(256) void matmul_i8_stream_kernel(MatmulI8Args g, int tiles_n, int k_per_split) {
+  constexpr int ROWS = 64 + 16 * MT, STAGE = ROWS * kUnit;
+  constexpr int LPW = ROWS / 16;                 // 1 KiB loads (four rows) of a wavefront, a stage
+  static_assert(LPW * (NS - 1) < 64 && NS >= 2 && NS <= 4, "vmcnt");
+  __shared__ __align__(16) unsigned char smem[NS * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = static_cast<int>(blockIdx.x % tiles_n) * 64, sp = blockIdx.x / tiles_n;
+  const int kbeg = sp * k_per_split, klen = min(g.K - kbeg, k_per_split);
+  const int nk = (klen + kUnit - 1) / kUnit;
+  const int8_t* src[LPW];
+  int chunk[LPW];
+#pragma unroll
+  for (int j = 0; j < LPW; ++j) {
+    const int row = (LPW * wave + j) * 4 + (lane >> 4);
+    chunk[j] = ((lane & 15) ^ (row & 15)) * 16;
+    src[j] = (row < 64 ? g.W + static_cast<int64_t>(min(n0 + row, g.N - 1)) * g.K
+                       : g.A + static_cast<int64_t>(min(row - 64, g.M - 1)) * g.K) + kbeg;
+  }
+  const uint32_t ring = lds_addr(smem);
+  auto issue = [&](int kt) {
+    const uint32_t st = ring + (kt % NS) * STAGE + LPW * wave * 1024;
+    const int left = klen - kt * kUnit;
+    if (left >= kUnit) {
+#pragma unroll
+      for (int j = 0; j < LPW; ++j) lds_dma16_opaque(src[j] + kt * kUnit + chunk[j], st + j * 1024);
+    } else {   // chunks past the end are not read: they take the first
+#pragma unroll
+      for (int j = 0; j < LPW; ++j)
+        lds_dma16_opaque(src[j] + kt * kUnit + (chunk[j] < left ? chunk[j] : 0), st + j * 1024);
+    }
+  };
+  auto wait_stage = [&](int ahead) {
+    if (NS >= 4 && ahead >= 3) wait_vm_lgkm_barrier<(NS >= 4 ? 3 * LPW : 0)>();
+    else if (NS >= 3 && ahead >= 2) wait_vm_lgkm_barrier<(NS >= 3 ? 2 * LPW : 0)>();
+    else if (ahead >= 1) wait_vm_lgkm_barrier<LPW>();
+    else wait_vm_lgkm_barrier<0>();
+  };
+  i32x4 acc[MT] = {};
+  auto step = [&](const unsigned char* st, int h) {
+    const int off = (lane & 15) * kUnit + (((4 * h + (lane >> 4)) ^ (lane & 15)) << 4);
+    const i32x4 w = *reinterpret_cast<const i32x4*>(st + 16 * wave * kUnit + off);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const i32x4 a = *reinterpret_cast<const i32x4*>(st + (64 + 16 * i) * kUnit + off);
+      acc[i] = mfma_i8(w, a, acc[i]);
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s)
+    if (s < nk) issue(s);
+  for (int kt = 0; kt < nk; ++kt) {
+    wait_stage(min(NS - 2, nk - 1 - kt));
+    // (every wavefront is done with stage kt - 1: its slot takes stage kt + NS - 1)
+    if (kt + NS - 1 < nk) issue(kt + NS - 1);
+    const unsigned char* st = smem + (kt % NS) * STAGE;
+    const int steps = min(klen - kt * kUnit, kUnit) / 64;
+    if (steps == 4) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) step(st, h);
+    } else {
+      for (int h = 0; h < steps; ++h) step(st, h);
+    }
+  }
+  const int col = n0 + 16 * wave + 4 * (lane >> 4);
+  const bool parts = gridDim.x > static_cast<unsigned>(tiles_n);
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int row = 16 * i + (lane & 15);
+    if (row >= g.M) continue;
+    if (parts) {
+      put_cols<4>(static_cast<int*>(g.ws) + (static_cast<int64_t>(sp) * g.M + row) * g.N, col, g.N, acc[i]);
+      continue;
+    }
+    const float sa = g.a_scale[row];
+    T* out = static_cast<T*>(g.out) + static_cast<int64_t>(row) * g.N;
+    f32x4 v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int c = min(col + q, g.N - 1);
+      v[q] = g.bias ? scaled(acc[i][q], sa, g.w_scale[c], g.bias[c]) : scaled(acc[i][q], sa, g.w_scale[c]);
+    }
+    if constexpr (sizeof(T) == 4) {
+      put_cols<4>(out, col, g.N, v);
+    } else {
+      typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+      const u32x2 w = {cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
+      put_cols<4>(out, col, g.N, __builtin_bit_cast(u16x4, w));
+    }
+  }
+}
+
+// Its parts of K, rows by rows, added up and scaled.
+template <typename T>
+__global__ __launch_bounds__(256) void sum_rows_i8_kernel(MatmulI8Args g, int splits) {
+  const int64_t n = static_cast<int64_t>(g.M) * g.N;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int* part = static_cast<const int*>(g.ws);
+  int sum = 0;
+  for (int s = 0; s < splits; ++s) sum += part[s * n + i];
+  const int row = static_cast<int>(i / g.N), col = static_cast<int>(i % g.N);
+  const float sa = g.a_scale[row], sw = g.w_scale[col];
+  put(static_cast<T*>(g.out) + i, g.bias ? scaled(sum, sa, sw, g.bias[col]) : scaled(sum, sa, sw));
+}
+
+// Many rows: a tile of BM x BN outputs, eight wavefronts (2 x 4) of TMW x TNW tiles of
+// v_mfma_i32_32x32x32_i8 (lane l holds row or column l % 32, 16 k from 16 (l / 32) on).
+// The weights are its first operand, so that a lane ends with one output row, l % 32, and
+// in registers 4 q .. 4 q + 3 four columns next to each other, from 8 q + 4 (l / 32) on,
+// which go to memory from the registers.  K advances in
+// stages of 128 bytes (whole cache lines: stages of 64 fetch every line twice) through a
+// ring of NS in LDS, filled by direct-to-LDS loads that the compiler does not see: a
+// wavefront waits for its own with an exact count and a barrier publishes a stage.  The
+// 16-byte chunks of a staged row are permuted by row / 2, so that 16 lanes reading a
+// fragment hit 16 bank groups.  Fragments of a step of 32 k are read while the step before
+// multiplies.
+constexpr int kStageK = 128;
 
 // A wavefront's 32 x 32 results: scaled, the bias added, stored.
 template <typename T>
@@ -450,7 +640,7 @@ __global__ __launch_bounds__(512) void sum_parts_i8_kernel(MatmulI8Args g, int t
 }
 
 // Tile variants of the wide kernel; kFew: the kernel for few rows.
-constexpr int kVariants = 7, kFew = kVariants;
+constexpr int kVariants = 7, kFew = kVariants, kStream = kVariants + 1;
 constexpr int kBM[kVariants] = {256, 256, 128, 192, 128, 64, 64};
 constexpr int kBN[kVariants] = {256, 128, 256, 256, 128, 256, 128};
 
@@ -474,6 +664,21 @@ hipError_t launch_wide(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t
     case 4: launch_wide_t<2, 1, 4, T>(g, p, stream); break;
     case 5: launch_wide_t<1, 2, 3, T>(g, p, stream); break;
     default: launch_wide_t<1, 1, 4, T>(g, p, stream); break;
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_stream(const MatmulI8Args& g, const MatmulI8Plan& p, bool keep_parts, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(p.workgroups)), block(256);
+  const int tn = (g.N + 63) / 64, k = p.k_per_split;
+  if (g.M <= 16) hipLaunchKernelGGL((matmul_i8_stream_kernel<1, 4, T>), grid, block, 0, stream, g, tn, k);
+  else if (g.M <= 32) hipLaunchKernelGGL((matmul_i8_stream_kernel<2, 3, T>), grid, block, 0, stream, g, tn, k);
+  else hipLaunchKernelGGL((matmul_i8_stream_kernel<4, 2, T>), grid, block, 0, stream, g, tn, k);
+  if (p.splits > 1 && !keep_parts) {
+    const int64_t n = static_cast<int64_t>(g.M) * g.N;
+    hipLaunchKernelGGL(sum_rows_i8_kernel<T>, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256),
+                       0, stream, g, p.splits);
   }
   return hipGetLastError();
 }
@@ -509,13 +714,8 @@ hipError_t launch_few(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t 
 hipError_t launch_quantize_i8(const void* x, int64_t rows, int cols, int dtype, int8_t* codes,
                               float* scale, hipStream_t stream) {
   if (rows == 0) return hipSuccess;
-  const dim3 grid(static_cast<unsigned>(rows)), block(256);
-  if (dtype == CO_DTYPE_BF16)
-    hipLaunchKernelGGL(quantize_rows_kernel<uint16_t>, grid, block, 0, stream,
-                       static_cast<const uint16_t*>(x), cols, codes, scale);
-  else
-    hipLaunchKernelGGL(quantize_rows_kernel<float>, grid, block, 0, stream,
-                       static_cast<const float*>(x), cols, codes, scale);
+  if (dtype == CO_DTYPE_BF16) launch_quantize_t(static_cast<const uint16_t*>(x), rows, cols, codes, scale, stream);
+  else launch_quantize_t(static_cast<const float*>(x), rows, cols, codes, scale, stream);
   return hipGetLastError();
 }
 
@@ -526,17 +726,35 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
   p.splits = 1;
   p.k_per_split = K;
   const int64_t force = tuning(CO_TUNE_MATMUL_I8);
-  if (force < 0 ? M <= kFewRows : force == kFew && M <= kFewRows) {
-    p.variant = kFew;
-    // columns of a workgroup: as many (the rows' codes are read once for them) as leave
-    // two workgroups to a compute unit
-    p.cols = N >= 128 * num_cus ? 4 : (N >= 64 * num_cus ? 2 : 1);
-    p.workgroups = (N + 16 * p.cols - 1) / (16 * p.cols);
-    // wavefronts: enough of them on the chip, each with a unit of K or more
-    p.waves = 4;
-    while (p.waves < 16 && p.workgroups * p.waves < 16ll * num_cus && K / kUnit > p.waves) p.waves *= 2;
-    if (p.cols * (M > 16 ? 2 : 1) > 2 && p.waves == 16) p.waves = 8;
-    return p;
+  if (M <= 64 && (force < 0 || force >= kFew)) {
+    const int64_t tiles = (static_cast<int64_t>(N) + 63) / 64;
+    int split = 1;
+    while (tiles * split < 2 * num_cus && K / (split * 2) >= 2 * kUnit) split *= 2;
+    // us, few rows by register and by stream: 16 x 2048 x 4096 6.9, 9.6; 16 x 10240 x 4096
+    // 14.7, 15.2; 16 x 4096 x 20480 26.0, 22.6; 16 x 256 x 20480 20.6, 14.5; unsplit 17 x 128000
+    // x 4096 127, 104.  The stream against 64-row tiles: 64 x 128000 x 4096 130, 113; 64 x 4096 x
+    // 20480 25.6, 29.3.
+    const bool few = force < 0 ? split > 1 && K <= 8192 : force == kFew;
+    if (M <= kFewRows && few) {
+      p.variant = kFew;
+      // columns of a workgroup: as many (the rows' codes are read once for them) as leave
+      // two workgroups to a compute unit
+      p.cols = N >= 128 * num_cus ? 4 : (N >= 64 * num_cus ? 2 : 1);
+      p.workgroups = (N + 16 * p.cols - 1) / (16 * p.cols);
+      // wavefronts: enough of them on the chip, each with a unit of K or more
+      p.waves = 4;
+      while (p.waves < 16 && p.workgroups * p.waves < 16ll * num_cus && K / kUnit > p.waves) p.waves *= 2;
+      if (p.cols * (M > 16 ? 2 : 1) > 2 && p.waves == 16) p.waves = 8;
+      return p;
+    }
+    if (force < 0 ? M <= kFewRows || (split > 1 && K > 8192) : force == kStream) {
+      p.variant = kStream;
+      p.k_per_split = ((K + split - 1) / split + kUnit - 1) / kUnit * kUnit;
+      p.splits = (K + p.k_per_split - 1) / p.k_per_split;
+      p.workgroups = tiles * p.splits;
+      p.ws_bytes = p.splits > 1 ? (static_cast<size_t>(p.splits) * M * N * 4 + 255) / 256 * 256 : 0;
+      return p;
+    }
   }
   double best = 1e30;
   for (int v = 0; v < kVariants; ++v) {
@@ -566,59 +784,170 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
   return p;
 }
 
-hipError_t launch_matmul_i8(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
+// keep_parts: the stream's parts of K stay in the workspace, rows by rows.
+static hipError_t launch_product(const MatmulI8Args& g, const MatmulI8Plan& p, bool keep_parts,
+                                 hipStream_t stream) {
   if (g.M == 0 || g.N == 0) return hipSuccess;
+  if (p.variant == kStream)
+    return g.dtype == CO_DTYPE_BF16 ? launch_stream<uint16_t>(g, p, keep_parts, stream)
+                                    : launch_stream<float>(g, p, keep_parts, stream);
   if (p.variant == kFew)
     return g.dtype == CO_DTYPE_BF16 ? launch_few<uint16_t>(g, p, stream) : launch_few<float>(g, p, stream);
   return g.dtype == CO_DTYPE_BF16 ? launch_wide<uint16_t>(g, p, stream) : launch_wide<float>(g, p, stream);
 }
 
+hipError_t launch_matmul_i8(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
+  return launch_product(g, p, false, stream);
+}
+
 // -------------------------------------------- projection with 8-bit weights
+//
+// quantise, F's product, its rows finished and quantised, the K/V product, rows stored.  The
+// stream kernel's parts of K are added up by the kernel that reads them.
 
 namespace {
 
-// A row of z: F(E) on carried rows, the optional RMS norm, then its codes.
-__global__ __launch_bounds__(256) void z_codes_kernel(float* z, int d, const float* fe,
-                                                      const float* gain, const int32_t* row_dst,
-                                                      int8_t* codes, float* scale) {
+// A product's results: fp32, or parts of its sums with the scales (splits > 0).
+struct Product {
+  const float* y;          // [M][N]
+  const int* part;         // [splits][M][N]
+  const float* a_scale;    // [M]
+  const float* w_scale;    // [N]
+  int M, N, splits;
+  __device__ __forceinline__ f32x4 four(int64_t row, int col) const {
 #pragma clang fp contract(off)
-  __shared__ float red[4];
-  __shared__ uint32_t redu[4];
-  const int64_t row = blockIdx.x;
-  const int tid = threadIdx.x;
-  float* zr = z + row * d;
-  const int32_t dst = row_dst[row];
-  const bool carry = fe && dst < 0 && dst != kSkip;
-  float ss = 0.f;
-  for (int c = tid; c < d; c += 256) {
-    const float v = carry ? zr[c] + fe[c] : zr[c];
-    zr[c] = v;
-    ss += v * v;
-  }
-  float r = 1.f;
-  if (gain) {
+    const int64_t at = row * N + col;
+    if (splits == 0) return *reinterpret_cast<const f32x4*>(y + at);
+    i32x4 sum = *reinterpret_cast<const i32x4*>(part + at);
+    for (int s = 1; s < splits; ++s)
+      sum += *reinterpret_cast<const i32x4*>(part + s * static_cast<int64_t>(M) * N + at);
+    const float sa = a_scale[row];
+    const f32x4u sw = *reinterpret_cast<const f32x4u*>(w_scale + col);   // (aligned to an element)
+    f32x4 v;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
-    if ((tid & 63) == 0) red[tid >> 6] = ss;
-    __syncthreads();
-    r = rsqrtf(((red[0] + red[1]) + (red[2] + red[3])) / static_cast<float>(d) + 1e-6f);
+    for (int i = 0; i < 4; ++i) v[i] = scaled(sum[i], sa, sw[i]);
+    return v;
   }
-  uint32_t top = 0;
-  for (int c = tid; c < d; c += 256) {
-    float v = zr[c];
-    if (gain) zr[c] = v = v * r * gain[c];
-    top = max(top, __float_as_uint(v) & 0x7FFFFFFFu);
-  }
+};
+
+template <int NT>
+__device__ __forceinline__ float block_sum(float v, float* red) {
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off)));
-  if ((tid & 63) == 0) redu[tid >> 6] = top;
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  top = max(max(redu[0], redu[1]), max(redu[2], redu[3]));
-  const bool fine = top < 0x7F800000u;
-  const float a = fmaxf(__uint_as_float(top), kLeast), q = 127.f / a;
+  v = 0.f;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) v += red[w];
+  return v;
+}
+
+// A row of z from F's product: F E on a carry row, the optional RMS norm, its codes.  Q
+// times eight entries of it stay in a thread's registers; Q = 0: rows of any length by way
+// of `spill` [M][d] (which may be the product's own fp32 results).
+template <int NT, int Q>
+__global__ __launch_bounds__(NT) void z_codes_kernel(Product p, float* spill, const float* fe,
+                                                     const float* gain, const int32_t* row_dst,
+                                                     int8_t* codes, float* scale) {
+#pragma clang fp contract(off)
+  __shared__ float red[NT / 64];
+  __shared__ uint32_t redu[NT / 64];
+  const int64_t row = blockIdx.x;
+  const int d = p.N;
+  const bool carry = fe && is_carry_row(row_dst[row]);
   int8_t* cr = codes + row * d;
-  for (int c = tid; c < d; c += 256) cr[c] = fine ? static_cast<int8_t>(code_of(zr[c], a, q)) : 0;
-  if (tid == 0) scale[row] = fine ? a / 127.f : NAN;
+  float* sr = spill + row * d;
+  constexpr int QN = Q > 0 ? Q : 1;
+  float v[QN][8];
+  auto read = [&](int c, float (&x)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x4 z = p.four(row, c + 4 * h);
+      if (carry) z += *reinterpret_cast<const f32x4*>(fe + c + 4 * h);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * h + i] = z[i];
+    }
+  };
+  float ss = 0.f, r = 1.f;
+  uint32_t top = 0;
+  auto squares = [&](const float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
+  };
+  auto normed = [&](int c, float (&x)[8]) {
+    if (gain) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = x[e] * r * gain[c + e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, magnitude(x[e]));
+  };
+  if constexpr (Q > 0) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int c = (q * NT + threadIdx.x) * 8;
+      if (c < d) {
+        read(c, v[q]);
+        squares(v[q]);
+      }
+    }
+    if (gain) r = rsqrtf(block_sum<NT>(ss, red) / static_cast<float>(d) + kRmsEps);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int c = (q * NT + threadIdx.x) * 8;
+      if (c < d) normed(c, v[q]);
+    }
+    const RowScale s(block_max<NT>(top, redu));
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int c = (q * NT + threadIdx.x) * 8;
+      if (c < d) s.codes(v[q], cr + c);
+    }
+    if (threadIdx.x == 0) scale[row] = s.scale;
+  } else {
+    for (int c = threadIdx.x * 8; c < d; c += NT * 8) {
+      read(c, v[0]);
+      squares(v[0]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sr[c + e] = v[0][e];
+    }
+    if (gain) r = rsqrtf(block_sum<NT>(ss, red) / static_cast<float>(d) + kRmsEps);
+    for (int c = threadIdx.x * 8; c < d; c += NT * 8) {   // (a thread reads what it wrote)
+      eight(sr + c, v[0]);
+      normed(c, v[0]);
+    }
+    const RowScale s(block_max<NT>(top, redu));
+    for (int c = threadIdx.x * 8; c < d; c += NT * 8) {
+      eight(sr + c, v[0]);
+      normed(c, v[0]);
+      s.codes(v[0], cr + c);
+    }
+    if (threadIdx.x == 0) scale[row] = s.scale;
+  }
+}
+
+// Rows of the K/V product to their destinations, four rotation pairs a thread.
+__global__ __launch_bounds__(256) void store_rows_i8_kernel(Product p, KvDest e) {
+  __shared__ double inv_tab[64];
+  const int half = e.hd / 2;
+  if (threadIdx.x < half) inv_tab[threadIdx.x] = rope_table<uint16_t>(e, threadIdx.x);
+  __syncthreads();
+  const int per_row = p.N / 8, lanes = half / 4;   // lanes of a head segment
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= static_cast<int64_t>(p.M) * per_row) return;   // (whole rows of lanes at a time)
+  const int row = static_cast<int>(i / per_row), rem = static_cast<int>(i % per_row);
+  const int32_t dst = e.row_dst[row];
+  if (dst == kSkip) return;                               // all lanes of the row
+  const int seg = rem / lanes, i0 = rem % lanes * 4;
+  const f32x4 a = p.four(row, seg * e.hd + i0), b = p.four(row, seg * e.hd + half + i0);
+  float lo[4], hi[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    lo[q] = a[q];
+    hi[q] = b[q];
+  }
+  k_norm<4>(e, seg, i0, lanes, lo, hi);
+  kv_store<uint16_t, 4>(e, row, dst, e.row_pos[row], seg, i0, lo, hi, inv_tab);
 }
 
 size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
@@ -636,34 +965,46 @@ size_t project_i8_ws_bytes(int M, int Dcat, int d, int n_kv, int num_cus) {
 hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t stream) {
   if (a.M == 0) return hipSuccess;
   const int n_kv = 2 * a.dst.L * a.dst.Hkv * a.dst.hd;
-  const int wide = a.Dcat > a.d ? a.Dcat : a.d;
+  const int wide = a.Dcat > a.d ? a.Dcat : a.d, out = a.d > n_kv ? a.d : n_kv;
   char* ws = static_cast<char*>(a.ws);
   int8_t* codes = reinterpret_cast<int8_t*>(ws);
   float* scale = reinterpret_cast<float*>(ws + pad256(static_cast<size_t>(a.M) * wide));
   float* y = reinterpret_cast<float*>(reinterpret_cast<char*>(scale) + pad256(static_cast<size_t>(a.M) * 4));
-  const int out = a.d > n_kv ? a.d : n_kv;
-  hipError_t err = launch_quantize_i8(a.hidden, a.M, a.Dcat, CO_DTYPE_BF16, codes, scale, stream);
-  if (err != hipSuccess) return err;
   MatmulI8Args g{};
   g.M = a.M;
-  g.N = a.d;
-  g.K = a.Dcat;
   g.dtype = CO_DTYPE_F32;
   g.A = codes;
   g.a_scale = scale;
-  g.W = a.wf;
-  g.w_scale = a.wf_scale;
   g.out = y;
   g.ws = reinterpret_cast<char*>(y) + pad256(static_cast<size_t>(a.M) * out * 4);
-  if ((err = launch_matmul_i8(g, plan_matmul_i8(g.M, g.N, g.K, num_cus), stream)) != hipSuccess) return err;
-  hipLaunchKernelGGL(z_codes_kernel, dim3(a.M), dim3(256), 0, stream, y, a.d, a.fe, a.znorm,
-                     a.dst.row_dst, codes, scale);
-  g.N = n_kv;
-  g.K = a.d;
-  g.W = a.wkv;
-  g.w_scale = a.wkv_scale;
-  if ((err = launch_matmul_i8(g, plan_matmul_i8(g.M, g.N, g.K, num_cus), stream)) != hipSuccess) return err;
-  return launch_store_products(y, 1, a.M, n_kv, a.dst, stream);
+  auto product = [&](int N, int K, const int8_t* w, const float* w_scale, Product* p) {
+    g.N = N;
+    g.K = K;
+    g.W = w;
+    g.w_scale = w_scale;
+    const MatmulI8Plan plan = plan_matmul_i8(g.M, N, K, num_cus);
+    const bool parts = plan.variant == kStream && plan.splits > 1;
+    *p = Product{y, static_cast<const int*>(g.ws), scale, w_scale, g.M, N, parts ? plan.splits : 0};
+    return launch_product(g, plan, parts, stream);
+  };
+  hipError_t err = launch_quantize_i8(a.hidden, a.M, a.Dcat, CO_DTYPE_BF16, codes, scale, stream);
+  if (err != hipSuccess) return err;
+  Product p;
+  if ((err = product(a.d, a.Dcat, a.wf, a.wf_scale, &p)) != hipSuccess) return err;
+  const dim3 rows(a.M);
+  if (a.d <= 2048)
+    hipLaunchKernelGGL((z_codes_kernel<256, 1>), rows, dim3(256), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
+  else if (a.d <= 4096)
+    hipLaunchKernelGGL((z_codes_kernel<512, 1>), rows, dim3(512), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
+  else if (a.d <= 16384)
+    hipLaunchKernelGGL((z_codes_kernel<1024, 2>), rows, dim3(1024), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
+  else
+    hipLaunchKernelGGL((z_codes_kernel<1024, 0>), rows, dim3(1024), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
+  if ((err = product(n_kv, a.d, a.wkv, a.wkv_scale, &p)) != hipSuccess) return err;
+  const int64_t items = static_cast<int64_t>(a.M) * (n_kv / 8);
+  hipLaunchKernelGGL(store_rows_i8_kernel, dim3(static_cast<unsigned>((items + 255) / 256)), dim3(256), 0,
+                     stream, p, a.dst);
+  return hipGetLastError();
 }
 
 }  // namespace co

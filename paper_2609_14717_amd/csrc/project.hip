@@ -1514,14 +1514,6 @@ hipError_t launch_project(const ProjectArgs& a, const ProjectPlan& p, hipStream_
   return hipGetLastError();
 }
 
-hipError_t launch_store_products(const float* y, int splits, int M, int n_kv, const KvDest& dst,
-                                 hipStream_t stream) {
-  const int64_t items = static_cast<int64_t>(M) * (n_kv / 2);
-  hipLaunchKernelGGL(epi_kv_kernel<uint16_t>, dim3(static_cast<unsigned>((items + 255) / 256)),
-                     dim3(256), 0, stream, y, splits, M, n_kv, dst);
-  return hipGetLastError();
-}
-
 // ------------------------------------------------------------- F(E) fold
 
 // One wavefront per output: f_e[row] = sum_k wf[row][k] * e[k] in fp32, lanes
