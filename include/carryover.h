@@ -213,7 +213,7 @@ typedef struct co_weights_i8 {
  * What the requests of a batch ask of their logits (carryover_logit_rules,
  * carryover_probabilities); every part is optional.  Let c be how often token v
  * was generated before a row: the count of its history word, and in row j of a
- * window the proposals before j that are v.  In this order, each operation
+ * window the proposals before j that are v (up to 32767 in all).  In this order, each operation
  * rounded to fp32:
  *   x = x > 0 ? x / repetition : x * repetition   where v is in the prompt or c > 0
  *   x = x - frequency * c;  x = x - presence       where c > 0

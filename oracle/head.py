@@ -109,7 +109,7 @@ def rules_row(x, word=None, window=(), repetition=1.0, presence=0.0, frequency=0
             c = (word & 0x7FFF).astype(np.float64)
             for t in window:
                 if 0 <= t < V:
-                    c[t] += 1
+                    c[t] = min(c[t] + 1, MOST_COUNT)
             known = np.flatnonzero(((word & 0x8000) != 0) | (c > 0))
             r = float(repetition)
             put(known, np.where(x[known] > 0, x[known] / r, x[known] * r), 0.0)

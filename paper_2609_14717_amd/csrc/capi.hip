@@ -229,7 +229,8 @@ co_status check_logits(const co_dims* d, int32_t vocab, int32_t rows, int32_t dt
   if (vocab < 1 || d->block > 1024 || !dtype_ok(dtype) ||
       static_cast<int64_t>(d->num_seqs) * rows > (int64_t{1} << 40) / vocab)
     return CO_ERR_UNSUPPORTED;
-  return plan_logits(d->num_seqs, rows, vocab, num_cus()).workgroups < kMaxGrid
+  return plan_logits(d->num_seqs, rows, vocab, num_cus(), true).workgroups < kMaxGrid &&
+                 plan_logits(d->num_seqs, rows, vocab, num_cus(), false).workgroups < kMaxGrid
              ? CO_OK
              : CO_ERR_UNSUPPORTED;
 }
@@ -253,8 +254,9 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 }
 
 LogitArgs logit_args(const co_dims* d, int32_t vocab, int32_t rows, const void* logits,
-                     const int32_t* draft_tok, const co_logit_rules* r, int32_t* status) {
-  const LogitPlan p = plan_logits(d->num_seqs, rows, vocab, num_cus());
+                     const int32_t* draft_tok, const co_logit_rules* r, int32_t* status,
+                     bool rules_call) {
+  const LogitPlan p = plan_logits(d->num_seqs, rows, vocab, num_cus(), rules_call);
   LogitArgs a{};
   a.S = d->num_seqs;
   a.B = d->block;
@@ -279,7 +281,6 @@ LogitArgs logit_args(const co_dims* d, int32_t vocab, int32_t rows, const void* 
   a.groups = p.groups;
   a.rows_per = p.rows_per;
   a.tiles = p.tiles;
-  a.chunks = p.chunks;
   return a;
 }
 
@@ -1099,7 +1100,7 @@ co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows
       !aligned(out, es) || !aligned(draft_tok, 4) || !aligned(status, 4) ||
       (out != logits && overlap(logits, bytes, out, bytes)))
     return CO_ERR_INVALID_ARG;
-  LogitArgs a = logit_args(dims, vocab, rows, logits, draft_tok, rules, status);
+  LogitArgs a = logit_args(dims, vocab, rows, logits, draft_tok, rules, status, true);
   a.out = out;
   clear_stale_error();
   return hip_status(launch_logit_rules(a, dtype, stream));
@@ -1107,7 +1108,7 @@ co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows
 
 size_t carryover_probabilities_workspace_bytes(const co_dims* dims, int32_t vocab, int32_t rows) {
   if (check_dims(dims) != CO_OK || check_logits(dims, vocab, rows, CO_DTYPE_F32) != CO_OK) return 0;
-  return plan_logits(dims->num_seqs, rows, vocab, num_cus()).ws_bytes;
+  return plan_logits(dims->num_seqs, rows, vocab, num_cus(), false).ws_bytes;
 }
 
 co_status carryover_probabilities(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,
@@ -1125,9 +1126,9 @@ co_status carryover_probabilities(const co_dims* dims, int32_t vocab, int32_t ro
       !aligned(top_tok, 4) || !aligned(status, 4) || overlap(logits, n * es, probs, n * 4))
     return CO_ERR_INVALID_ARG;
   if (!ws || !aligned(ws, 256)) return CO_ERR_INVALID_ARG;
-  if (ws_bytes < plan_logits(dims->num_seqs, rows, vocab, num_cus()).ws_bytes)
+  if (ws_bytes < plan_logits(dims->num_seqs, rows, vocab, num_cus(), false).ws_bytes)
     return CO_ERR_WORKSPACE;
-  LogitArgs a = logit_args(dims, vocab, rows, logits, draft_tok, rules, status);
+  LogitArgs a = logit_args(dims, vocab, rows, logits, draft_tok, rules, status, false);
   a.temperature = temperature;
   a.probs = probs;
   a.top = top_tok;

@@ -329,17 +329,18 @@ struct LogitArgs {
   int32_t* top;                           // [S][R] or null
   float4* ws;                             // [S][R][tiles]
   int32_t* status;
-  int groups, rows_per, tiles, chunks;    // of the plan
+  int groups, rows_per, tiles;            // of the plan
 };
 
 struct LogitPlan {
   int groups, rows_per;      // row groups of a sequence, rows of each
-  int tiles, chunks;         // tiles of a row, chunks of each
+  int tiles;                 // of a row
   int64_t workgroups;
   size_t ws_bytes;
 };
 
-LogitPlan plan_logits(int S, int R, int V, int num_cus);
+// rules: for the rules' call, which takes every row in tiles
+LogitPlan plan_logits(int S, int R, int V, int num_cus, bool rules);
 hipError_t launch_logit_rules(const LogitArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_probabilities(const LogitArgs& a, int dtype, hipStream_t stream);
 

@@ -12,7 +12,14 @@
 // each operation rounded to fp32 on its own, so that equal logits stay equal.  Probabilities
 // are exp((x - max) / T) / sum, in fp32.
 //
-// All of it is bound by memory: a logit is read and a logit or a probability written.
+// All of it is bound by memory: a logit is read and a logit or a probability written.  What
+// is done for every token is therefore kept to a few operations: its mask bit, the largest
+// value, an exponential.  The tokens that have a history, a proposal or a bias are special;
+// there are hundreds of them among a hundred thousand, but several in every run that a
+// wavefront takes, so that testing for them in place would run their code (a division among
+// it) almost everywhere.  They are masked out of the run, listed once for a workgroup's tile
+// and taken one each by its threads, as are the up to seven tokens behind the last whole
+// vector of a row.
 #include "co_kernels.h"
 
 namespace co {
@@ -20,80 +27,44 @@ namespace co {
 namespace {
 
 constexpr int kVec = 8;                     // tokens of a thread: one byte of a mask
-constexpr int kChunk = 256 * kVec;          // of a workgroup at a time
-constexpr int kRowsMax = 8;                 // rows of a sequence that a workgroup takes together
+constexpr int kVecs = 4;                    // such vectors of a thread
+constexpr int kRowsMax = 8;                 // rows of a sequence that a workgroup takes
 
-typedef uint16_t u16x8u __attribute__((ext_vector_type(8), aligned(2)));
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
-
-enum { kRules = 0, kStats = 1, kProbs = 2 };
+enum { kRules = 0, kStats = 1, kProbs = 2, kWhole = 3 };
 
 constexpr float kNone = -INFINITY;
 
-// Eight elements v .. v + 7 of a row that starts anywhere, `pad` from V on.
-template <typename T> struct Vec;
-template <> struct Vec<uint16_t> {
-  u16x8u x;
-  __device__ __forceinline__ float get(int e) const { return bf2f(x[e]); }
+__device__ __forceinline__ float widen(uint16_t v) { return bf2f(v); }
+__device__ __forceinline__ float widen(float v) { return v; }
+
+// Eight elements next to each other, at any address of an element.
+template <typename T>
+struct Vec {
+  typedef T vec __attribute__((ext_vector_type(kVec), aligned(sizeof(T))));
+  vec x;
+  __device__ __forceinline__ void load(const T* p) { x = *reinterpret_cast<const vec*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<vec*>(p) = x; }
 };
-template <> struct Vec<float> {
-  f32x4u lo, hi;
-  __device__ __forceinline__ float get(int e) const { return e < 4 ? lo[e & 3] : hi[e & 3]; }
-};
 
-__device__ __forceinline__ void load8(const uint16_t* p, int v, int V, Vec<uint16_t>* o,
-                                      uint16_t pad) {
-  if (v + kVec <= V) {
-    o->x = *reinterpret_cast<const u16x8u*>(p + v);
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < kVec; ++e) o->x[e] = v + e < V ? p[v + e] : pad;
+__device__ __forceinline__ void store8(float* p, const float (&x)[kVec]) {
+  typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+  *reinterpret_cast<vec*>(p) = vec{x[0], x[1], x[2], x[3]};
+  *reinterpret_cast<vec*>(p + 4) = vec{x[4], x[5], x[6], x[7]};
 }
 
-__device__ __forceinline__ void load8(const float* p, int v, int V, Vec<float>* o, float pad) {
-  if (v + kVec <= V) {
-    o->lo = *reinterpret_cast<const f32x4u*>(p + v);
-    o->hi = *reinterpret_cast<const f32x4u*>(p + v + 4);
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    o->lo[e] = v + e < V ? p[v + e] : pad;
-    o->hi[e] = v + e + 4 < V ? p[v + e + 4] : pad;
-  }
-}
+__device__ __forceinline__ void store1(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store1(uint16_t* p, float x) { *p = static_cast<uint16_t>(cvt_pk_bf16(x, x)); }
 
-template <typename T> __device__ __forceinline__ T lowest();
-template <> __device__ __forceinline__ uint16_t lowest<uint16_t>() { return 0xFF80u; }
-template <> __device__ __forceinline__ float lowest<float>() { return kNone; }
+template <typename T> constexpr T kLowest = T(-INFINITY);
+template <> constexpr uint16_t kLowest<uint16_t> = 0xFF80u;
 
-__device__ __forceinline__ void store8(float* p, int v, int V, const float (&x)[kVec]) {
-  if (v + kVec <= V) {
-    *reinterpret_cast<f32x4u*>(p + v) = f32x4u{x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<f32x4u*>(p + v + 4) = f32x4u{x[4], x[5], x[6], x[7]};
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < kVec; ++e)
-    if (v + e < V) p[v + e] = x[e];
-}
-
-__device__ __forceinline__ void store8(uint16_t* p, int v, int V, const float (&x)[kVec]) {
-  u16x8u o;
-#pragma unroll
-  for (int e = 0; e < kVec; e += 2) {
-    const uint32_t w = cvt_pk_bf16(x[e], x[e + 1]);
-    o[e] = static_cast<uint16_t>(w);
-    o[e + 1] = static_cast<uint16_t>(w >> 16);
-  }
-  if (v + kVec <= V) {
-    *reinterpret_cast<u16x8u*>(p + v) = o;
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < kVec; ++e)
-    if (v + e < V) p[v + e] = o[e];
+// y where bit e of `allowed` is set, minus infinity elsewhere: a bit field extract and an
+// insert (written out, the compiler makes five operations of the latter).
+__device__ __forceinline__ float masked(float y, uint32_t allowed, int e) {
+  const int m = __builtin_amdgcn_sbfe(static_cast<int>(allowed), e, 1);
+  float r;
+  asm("v_bfi_b32 %0, %1, %2, %3" : "=v"(r) : "v"(m), "v"(y), "v"(kNone));
+  return r;
 }
 
 // The penalties on one logit that was seen; c: how often generated.
@@ -108,253 +79,522 @@ __device__ __forceinline__ float penalise(float x, int c, float rep, float freq,
   return x;
 }
 
-// exp2 of non-positive arguments; 0 at -inf
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// log2(e) / T, kept finite and above 0; 0 for a greedy sequence (T <= 0 or NaN).
-__device__ __forceinline__ float row_slope(const float* temperature, int s) {
+// log2(e) / T, kept finite and above 0; greedy sequences (T <= 0 or NaN) have any.
+__device__ __forceinline__ float row_slope(const float* temperature, int s, bool* greedy) {
   const float t = temperature ? temperature[s] : 1.f;
-  if (!(t > 0.f)) return 0.f;
-  return fminf(fmaxf(1.44269504088896341f / t, 0x1p-126f), 0x1.fffffep+127f);
+  *greedy = !(t > 0.f);
+  return *greedy ? 1.f : fminf(fmaxf(1.44269504088896341f / t, 0x1p-126f), 0x1.fffffep+127f);
 }
 
-// What a part of a row holds: its largest logit, where it first is, and the sum of
-// exp2((x - m) k).
+// What a part of a row holds: its largest logit, the sum of exp2((x - m) k), and where the
+// largest is: the first vector of eight that has it, and the first special token that is it
+// (INT32_MAX: none).
 struct Part {
   float m, l;
-  int at;
+  int vec, one;
 };
 
-__device__ __forceinline__ Part join(const Part& a, const Part& b, float k) {
+constexpr int kNowhere = INT32_MAX;
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, false));
+}
+
+__device__ __forceinline__ float wave_max_f(float v) {
+  v = fmaxf(v, dpp<0x128>(v));   // rotations within 16 lanes: by 8, 4, 2, 1
+  v = fmaxf(v, dpp<0x124>(v));
+  v = fmaxf(v, dpp<0x122>(v));
+  v = fmaxf(v, dpp<0x121>(v));
+  return max_across_rows(v);
+}
+
+__device__ __forceinline__ float wave_sum_f(float v) {
+  v += dpp<0x128>(v);
+  v += dpp<0x124>(v);
+  v += dpp<0x122>(v);
+  v += dpp<0x121>(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+__device__ __forceinline__ int wave_min(int v) { return INT32_MAX - wave_max(INT32_MAX - v); }
+
+// The wavefront's parts joined, in every lane.
+__device__ __forceinline__ Part wave_join(const Part& p, float k) {
   Part r;
-  const bool other = b.m > a.m || (b.m == a.m && b.at < a.at);
-  r.m = other ? b.m : a.m;
-  r.at = other ? b.at : a.at;
+  r.m = wave_max_f(p.m);
   // (equal largest values, infinite ones among them, keep their sums as they are)
-  const float la = a.m == r.m ? a.l : a.l * exp2_fast((a.m - r.m) * k);
-  const float lb = b.m == r.m ? b.l : b.l * exp2_fast((b.m - r.m) * k);
-  r.l = la + lb;
+  r.l = wave_sum_f(p.m == r.m ? p.l : p.l * exp2_fast((p.m - r.m) * k));
+  r.vec = wave_min(p.m == r.m ? p.vec : kNowhere);
+  r.one = wave_min(p.m == r.m ? p.one : kNowhere);
   return r;
 }
 
-__device__ __forceinline__ Part shfl_part(const Part& p, int mask) {
-  return Part{__shfl_xor(p.m, mask), __shfl_xor(p.l, mask), __shfl_xor(p.at, mask)};
+// One more special token.  A NaN is left out, as if it were masked.
+__device__ __forceinline__ void take(Part& p, float y, int v, float k) {
+  if (y > p.m) {
+    p.l = p.m > kNone ? p.l * exp2_fast((p.m - y) * k) : 0.f;
+    p.m = y;
+    p.one = v;
+  } else if (y == p.m) {
+    p.one = min(p.one, v);
+  }
+  if (y > kNone) p.l += y == p.m ? 1.f : exp2_fast((y - p.m) * k);
 }
 
-// One workgroup: chunks of tokens of one sequence, up to kRowsMax of its rows together, so
-// that the history words and biases of a token are read once for them and every thread has
-// as many loads in flight as there are rows.
-template <typename T, int KIND>
-__global__ __launch_bounds__(256) void rows_kernel(LogitArgs a) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// A row's largest logit, one over its sum (0: nothing left) and its lowest largest token.
+struct Whole {
+  float m, inv;
+  int at;
+};
+
+template <int N>
+__device__ __forceinline__ void shares(const Whole& p, float (&y)[N], int v, float k, bool greedy) {
+  if (greedy || p.m == INFINITY || p.inv == 0.f) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      y[e] = p.inv == 0.f ? 0.f : (greedy ? (v + e == p.at ? 1.f : 0.f) : (y[e] == p.m ? p.inv : 0.f));
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < N; ++e) y[e] = fmaxf(exp2_fast((y[e] - p.m) * k) * p.inv, 0.f);   // (NaN: 0)
+}
+
+// A special token of a tile.
+struct Entry {
+  int v;                 // token
+  uint32_t word;         // its history
+  float bias;
+  bool biased;
+  uint32_t proposed[2];  // bit i: the window's proposal i is this token (of the first 64)
+};
+
+constexpr int kBiasHeld = 512;   // biases of a tile that are held in LDS
+
+// One workgroup: a tile of tokens of one sequence, C vectors of eight a thread, in rows one
+// after the other, the next row's logits in flight.
+//   kRules: rules on logits.  kStats: each tile's largest logit and sum; kProbs: the tiles'
+//   parts joined, and the probabilities.  kWhole: both, where a row is one tile.
+template <typename T, int KIND, int NT, int C>
+__global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
+  constexpr int kTokens = NT * kVec * C, kWaves = NT / 64;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int b = blockIdx.x;
   const int grp = b % a.groups;
   b /= a.groups;
   const int tile = b % a.tiles, s = b / a.tiles;
   const int j0 = grp * a.rows_per, nr = min(a.rows_per, a.R - j0);
-  const int V = a.V;
+  const int V = a.V, base = tile * kTokens;
   const int64_t row0 = static_cast<int64_t>(s) * a.R + j0;
   const T* logits = static_cast<const T*>(a.logits) + row0 * V;
-  const bool first = tile == 0 && grp == 0 && tid == 0;   // reports what concerns a sequence
+  const bool reports = KIND != kProbs && tile == 0 && grp == 0;   // what concerns a sequence
 
-  const bool penalties = a.seen != nullptr;
-  const float rep = a.repetition ? a.repetition[s] : 1.f;
-  const float freq = a.frequency ? a.frequency[s] : 0.f;
-  const float pres = a.presence ? a.presence[s] : 0.f;
-  const int32_t* draft = a.draft && penalties ? a.draft + static_cast<int64_t>(s) * a.B : nullptr;
-  if (KIND != kProbs && draft && tile == 0 && grp == 0)
-    for (int i = tid; i < a.R - 1; i += 256)
-      if (static_cast<uint32_t>(draft[i]) >= static_cast<uint32_t>(V))
-        set_status(a.status, CO_ERR_TOKEN);
+  __shared__ uint32_t special[kTokens / 32], with_bias[kTokens / 32];   // a bit a token
+  __shared__ uint16_t list[kTokens];
+  __shared__ uint16_t held_tok[kBiasHeld];
+  __shared__ int held_order[kBiasHeld];
+  __shared__ float held_val[kBiasHeld];
+  __shared__ int num_held, listed[kWaves];
+  constexpr int kParts = KIND == kStats || KIND == kWhole ? kRowsMax * kWaves : 1;
+  __shared__ Part parts[kParts], ones[kParts];   // of the wavefronts; of their special tokens
+  __shared__ Whole whole[kRowsMax];
+  __shared__ float own_special[KIND == kRules || KIND == kProbs ? kRowsMax * NT : 1];
+  bool greedy = false;
+  const float k = KIND == kRules ? 0.f : row_slope(a.temperature, s, &greedy);
+
+  // Vector c of this thread: whole where full(c); others are loaded from the row's last whole
+  // one, so that no load is behind a branch, and masked.
+  auto vec = [&](int c) { return base + (c * NT + tid) * kVec; };
+  auto full = [&](int c) { return vec(c) + kVec <= V; };
+  auto at_vec = [&](int c) { return min(vec(c), V - kVec); };
+  const bool vectors = V >= kVec;
+  const int64_t mask_bytes = static_cast<int64_t>((V + 31) / 32) * 4;
+  // What hangs on nothing but the indices is loaded first, all at once.
+  int mask_held = a.mask_row && lane < nr ? a.mask_row[row0 + lane] : -1;
+  const uint16_t* seen = a.seen ? a.seen + static_cast<int64_t>(s) * V : nullptr;
+  const int32_t* draft = a.draft && a.seen ? a.draft + static_cast<int64_t>(s) * a.B : nullptr;
+  const int before = draft ? j0 + nr - 1 : 0;              // proposals that some row has behind it
+  const int held = lane < before ? draft[lane] : -1;       // lane i holds number i, later ones are read
   int b0 = 0, b1 = 0;
   if (a.bias_start) {
     b0 = a.bias_start[s];
     b1 = a.bias_start[s + 1];
-    if (b0 < 0 || b1 < b0 || b1 > a.num_bias) {
-      if (first) set_status(a.status, CO_ERR_LENGTH);
-      b0 = b1 = 0;
+  }
+  Vec<uint16_t> w[C];
+  if (seen && vectors) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) w[c].load(seen + at_vec(c));
+  }
+  struct Row {
+    Vec<T> x[C];
+    uint32_t allowed[C];   // (words: bytes would be packed, and waited for, as they arrive)
+  };
+  auto load = [&](int r, Row& o) {
+    if (!vectors) return;
+    const T* p = logits + static_cast<int64_t>(r) * V;
+#pragma unroll
+    for (int c = 0; c < C; ++c) o.x[c].load(p + at_vec(c));
+  };
+  Row cur, next;
+  load(0, cur);
+  const float rep = a.repetition ? a.repetition[s] : 1.f;
+  const float freq = a.frequency ? a.frequency[s] : 0.f;
+  const float pres = a.presence ? a.presence[s] : 0.f;
+
+  // lane r holds the mask of row r: >= 0, or -1: none, -2: no such mask, nothing is allowed
+  mask_held = max(-1, mask_held);
+  if (mask_held >= a.num_masks) {
+    mask_held = -2;
+    if (KIND != kProbs) set_status(a.status, CO_ERR_MASK);
+  }
+  auto mask_of = [&](int r) { return __builtin_amdgcn_readlane(mask_held, r); };
+  auto bits_of = [&](int m) { return reinterpret_cast<const uint8_t*>(a.mask_bits) + m * mask_bytes; };
+  auto load_mask = [&](int r, Row& o) {
+    const int m = mask_of(r);
+    if (m >= 0 && vectors) {
+      const uint8_t* bits = bits_of(m);
+#pragma unroll
+      for (int c = 0; c < C; ++c) o.allowed[c] = bits[at_vec(c) / kVec];
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c) o.allowed[c] = m == -1 ? 0xFF : 0;
+    }
+  };
+  load_mask(0, cur);
+
+  // ---- the tile's special tokens
+  auto proposal = [&](int i) { return i < 64 ? __builtin_amdgcn_readlane(held, i) : draft[i]; };
+  const bool right = b0 >= 0 && b1 >= b0 && b1 <= a.num_bias;
+  if (!right && reports && tid == 0) set_status(a.status, CO_ERR_LENGTH);
+  const int n_bias = right ? b1 - b0 : 0;
+  const int own_tok = tid < n_bias ? a.bias_tok[b0 + tid] : -1;
+  const float own_val = tid < n_bias ? a.bias_val[b0 + tid] : 0.f;
+  uint8_t* special8 = reinterpret_cast<uint8_t*>(special);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    uint32_t m = 0;
+    if (full(c)) {
+      if (seen) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) m |= (w[c].x[e] != 0 ? 1u : 0u) << e;
+      }
+    } else if (vec(c) < V) {
+      m = (1u << (V - vec(c))) - 1;
+    }
+    special8[c * NT + tid] = static_cast<uint8_t>(m);
+    reinterpret_cast<uint8_t*>(with_bias)[c * NT + tid] = 0;
+  }
+  if (tid == 0) num_held = 0;
+  if (n_bias > 0 || draft) {
+    __syncthreads();
+    for (int i = tid; i < (reports && draft ? a.R - 1 : before); i += NT) {
+      const int d = i == lane && i < before ? held : draft[i], t = d - base;
+      if (static_cast<uint32_t>(d) >= static_cast<uint32_t>(V)) {
+        if (reports) set_status(a.status, CO_ERR_TOKEN);
+      } else if (i < before && t >= 0 && t < kTokens) {
+        atomicOr(&special[t >> 5], 1u << (t & 31));
+      }
+    }
+    for (int i = tid; i < n_bias; i += NT) {
+      const int d = i == tid ? own_tok : a.bias_tok[b0 + i], t = d - base;
+      if (static_cast<uint32_t>(d) >= static_cast<uint32_t>(V)) {
+        if (reports) set_status(a.status, CO_ERR_TOKEN);
+      } else if (t >= 0 && t < kTokens) {
+        atomicOr(&special[t >> 5], 1u << (t & 31));
+        atomicOr(&with_bias[t >> 5], 1u << (t & 31));
+        const int at = atomicAdd(&num_held, 1);
+        if (at < kBiasHeld) {
+          held_tok[at] = static_cast<uint16_t>(t);
+          held_order[at] = i;
+          held_val[at] = i == tid ? own_val : a.bias_val[b0 + i];
+        }
+      }
     }
   }
-  int mask[kRowsMax];   // >= 0: the row's mask, -1: none, -2: no such mask, nothing allowed
+  __syncthreads();
+  uint32_t plain[C];          // tokens of a vector that are not special
+  int own = 0;
 #pragma unroll
-  for (int r = 0; r < kRowsMax; ++r) {
-    mask[r] = a.mask_row && r < nr ? max(-1, a.mask_row[row0 + r]) : -1;
-    if (mask[r] >= a.num_masks) {
-      mask[r] = -2;
-      if (tid == 0) set_status(a.status, CO_ERR_MASK);
+  for (int c = 0; c < C; ++c) {
+    const uint32_t m = special8[c * NT + tid];
+    plain[c] = full(c) ? m ^ 0xFF : 0;
+    own += __builtin_popcount(m);
+  }
+  const int upto = wave_scan(own);
+  if (lane == 63) listed[wave] = upto;
+  __syncthreads();
+  int at = upto - own, n = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    at += w < wave ? listed[w] : 0;
+    n += listed[w];
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    for (uint32_t m = special8[c * NT + tid]; m != 0; m &= m - 1)
+      list[at++] = static_cast<uint16_t>((c * NT + tid) * kVec + __builtin_ctz(m));
+  __syncthreads();
+
+  // number i of the list; the last entry of a token in the list of biases counts
+  auto entry = [&](int i) {
+    Entry e{};
+    const int t = list[i];
+    e.v = base + t;
+    e.word = seen ? seen[e.v] : 0;
+    e.biased = with_bias[t >> 5] >> (t & 31) & 1;
+    if (e.biased) {
+      int order = -1;
+      if (num_held <= kBiasHeld) {
+        for (int j = 0; j < num_held; ++j)
+          if (held_tok[j] == t && held_order[j] > order) {
+            order = held_order[j];
+            e.bias = held_val[j];
+          }
+      } else {
+        for (int j = 0; j < n_bias; ++j)
+          if (a.bias_tok[b0 + j] == e.v) order = j;
+        e.bias = a.bias_val[b0 + order];
+      }
     }
-  }
-  const int64_t mask_bytes = static_cast<int64_t>((V + 31) / 32) * 4;
-
-  __shared__ int last[kChunk];
-  __shared__ Part parts[4][kRowsMax];
-  __shared__ Part whole[kRowsMax];
-  const float k = KIND == kRules ? 0.f : row_slope(a.temperature, s);
-
-  Part acc[kRowsMax];
-  if constexpr (KIND == kStats) {
 #pragma unroll
-    for (int r = 0; r < kRowsMax; ++r) acc[r] = Part{kNone, 0.f, INT32_MAX};
-  }
+    for (int h = 0; h < 2; ++h)
+      for (int j = 32 * h; j < min(before, 32 * h + 32); ++j)
+        e.proposed[h] |= __builtin_amdgcn_readlane(held, j) == e.v ? 1u << (j & 31) : 0;
+    return e;
+  };
+  // its logit x after the rules, in row r; `allowed`: its byte of the row's mask
+  auto ruled = [&](const Entry& e, int r, float x, uint32_t allowed) {
+    const int j = j0 + r;       // proposals behind the row
+    uint32_t count = e.word & 0x7FFFu;
+    count += __builtin_popcount(e.proposed[0] & (j < 32 ? (1u << j) - 1 : ~0u));
+    if (j > 32) count += __builtin_popcount(e.proposed[1] & (j < 64 ? (1u << (j - 32)) - 1 : ~0u));
+    for (int i = 64; i < (draft ? j : 0); ++i) count += draft[i] == e.v ? 1 : 0;
+    if (e.word != 0 || count != 0) x = penalise(x, static_cast<int>(min(count, 0x7FFFu)), rep, freq, pres);
+    if (e.biased) x = x + e.bias;
+    return allowed >> (e.v % 8) & 1 ? x : kNone;
+  };
+  // Every special token of this wavefront's share (one a lane, the rest idle) in every row:
+  // f(r, token, whether there is one, its logit after the rules).  Its logits and mask bytes
+  // of all rows are loaded together.
+  auto each_special = [&](int from, int to, auto&& f) {
+    for (int i0 = from + wave * 64; i0 < to; i0 += NT) {
+      const bool on = i0 + lane < n;
+      Entry e{base};
+      if (on) e = entry(i0 + lane);
+      T x[kRowsMax];
+      uint32_t allowed[kRowsMax];
+#pragma unroll
+      for (int q = 0; q < kRowsMax; ++q) x[q] = logits[static_cast<int64_t>(min(q, nr - 1)) * V + e.v];
+#pragma unroll
+      for (int q = 0; q < kRowsMax; ++q) {
+        const int m = mask_of(min(q, nr - 1));
+        if (m >= 0) allowed[q] = bits_of(m)[e.v / 8];
+        else allowed[q] = m == -1 ? 0xFF : 0;
+      }
+#pragma unroll 1
+      for (int r = 0; r < nr; ++r) {
+        T xr = x[0];
+        uint32_t ar = allowed[0];
+#pragma unroll
+        for (int q = 1; q < kRowsMax; ++q) {
+          xr = q == r ? x[q] : xr;
+          ar = q == r ? allowed[q] : ar;
+        }
+        f(r, e.v, on, ruled(e, r, widen(xr), ar));
+      }
+    }
+  };
+
+  // Which token a part's largest is, by the lanes of a wavefront: the first of its vector's
+  // eight that is neither masked nor special, or a special one before it.
+  auto place = [&](const Part& p, int r) {
+    if (p.vec == kNowhere) return p.one;
+    const int v = p.vec + (lane & 7), t = v - base, m = mask_of(r);
+    const uint32_t allowed = m >= 0 ? bits_of(m)[v / 8] >> (v % 8) & 1 : (m == -1 ? 1 : 0);
+    const bool is = allowed && !(special[t >> 5] >> (t & 31) & 1) &&
+                    widen(logits[static_cast<int64_t>(r) * V + v]) == p.m;
+    const unsigned long long found = __ballot(is) & 0xFF;
+    return min(p.one, p.vec + __ffsll(static_cast<long long>(found)) - 1);
+  };
+  const Part nothing{kNone, 0.f, kNowhere, kNowhere};
   if constexpr (KIND == kProbs) {
-    // the row's parts joined: its largest logit and one over its sum
-    for (int r = wave; r < nr; r += 4) {
-      Part p{kNone, 0.f, INT32_MAX};
+    // the rows' parts joined
+    for (int r = wave; r < nr; r += kWaves) {
+      Part p = nothing;
       for (int t = lane; t < a.tiles; t += 64) {
         const float4 w = a.ws[(row0 + r) * a.tiles + t];
-        p = join(p, Part{w.x, w.y, __float_as_int(w.z)}, k);
+        const int at = __float_as_int(w.z);
+        if (w.x > p.m) {
+          p.l = p.m > kNone ? p.l * exp2_fast((p.m - w.x) * k) : 0.f;
+          p.m = w.x;
+          p.one = at;
+        } else if (w.x == p.m) {
+          p.one = min(p.one, at);
+        }
+        if (w.x > kNone) p.l += w.x == p.m ? w.y : w.y * exp2_fast((w.x - p.m) * k);
       }
-#pragma unroll
-      for (int x = 32; x >= 1; x >>= 1) p = join(p, shfl_part(p, x), k);
+      p = wave_join(p, k);
       if (lane == 0) {
-        p.l = p.l > 0.f ? 1.f / p.l : 0.f;
-        whole[r] = p;
-        if (tile == 0 && a.top) a.top[row0 + r] = p.m > kNone ? p.at : -1;
+        whole[r] = Whole{p.m, p.m > kNone ? 1.f / p.l : 0.f, p.one};
+        if (tile == 0 && a.top) a.top[row0 + r] = p.m > kNone ? p.one : -1;
       }
     }
     __syncthreads();
   }
 
-  for (int c = 0; c < a.chunks; ++c) {
-    const int base = (tile * a.chunks + c) * kChunk;
-    if (base >= V) break;
-    const int v = base + tid * kVec;
-    // the last entry of each token of the chunk in the sequence's list of biases
-    if (b1 > b0) {
-      __syncthreads();
-      for (int i = tid; i < kChunk; i += 256) last[i] = 0;
-      __syncthreads();
-      for (int i = b0 + tid; i < b1; i += 256) {
-        const int t = a.bias_tok[i];
-        if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(V)) set_status(a.status, CO_ERR_TOKEN);
-        else if (t >= base && t - base < kChunk) atomicMax(&last[t - base], i + 1 - b0);
-      }
-      __syncthreads();
-    }
-    if (v >= V) continue;
-
-    Vec<T> x[kRowsMax];
-#pragma unroll
-    for (int r = 0; r < kRowsMax; ++r)
-      if (r < nr) load8(logits + static_cast<int64_t>(r) * V, v, V, &x[r], lowest<T>());
-    uint8_t allowed[kRowsMax];
-#pragma unroll
-    for (int r = 0; r < kRowsMax; ++r) {
-      allowed[r] = mask[r] == -2 ? 0 : 0xFF;
-      if (mask[r] >= 0)
-        allowed[r] = reinterpret_cast<const uint8_t*>(a.mask_bits)[mask[r] * mask_bytes + v / 8];
-    }
-    int cnt[kVec];
-    uint32_t known = 0;        // bit e: token v + e was seen
-    if (penalties) {
-      Vec<uint16_t> w;
-      load8(a.seen + static_cast<int64_t>(s) * V, v, V, &w, 0);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        cnt[e] = w.x[e] & 0x7FFF;
-        known |= (w.x[e] != 0 ? 1u : 0u) << e;
-      }
-    }
-    auto add = [&](int t) {    // one more proposal
-      const uint32_t e0 = static_cast<uint32_t>(t - v);
-      if (e0 >= kVec) return;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) cnt[e] += static_cast<int>(e0) == e ? 1 : 0;
-      known |= 1u << e0;
-    };
-    if (draft)
-      for (int i = 0; i < j0; ++i) add(draft[i]);
-    float bias[kVec];
-    uint32_t biased = 0;
-    if (b1 > b0) {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const int i = last[tid * kVec + e];
-        bias[e] = 0.f;
-        if (i > 0) {
-          bias[e] = a.bias_val[b0 + i - 1];
-          biased |= 1u << e;
-        }
-      }
-    }
-
-#pragma unroll
-    for (int r = 0; r < kRowsMax; ++r) {
-      if (r >= nr) continue;
-      if (draft && r > 0) add(draft[j0 + r - 1]);
-      float y[kVec];
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) y[e] = x[r].get(e);
-      if (known) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e)
-          if (known >> e & 1) y[e] = penalise(y[e], cnt[e], rep, freq, pres);
-      }
-      if (biased) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e)
-          if (biased >> e & 1) y[e] = y[e] + bias[e];
-      }
-      if (allowed[r] != 0xFF) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e)
-          if (!(allowed[r] >> e & 1)) y[e] = kNone;
-      }
-      if constexpr (KIND == kRules) {
-        store8(static_cast<T*>(a.out) + (row0 + r) * V, v, V, y);
-        continue;
-      }
-      // a NaN is left out, as if its token were masked
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) y[e] = y[e] == y[e] ? y[e] : kNone;
-      if constexpr (KIND == kStats) {
-        float top = y[0];
-#pragma unroll
-        for (int e = 1; e < kVec; ++e) top = fmaxf(top, y[e]);
-        Part& p = acc[r];
-        if (top > p.m) {
-          int at = 0;
-#pragma unroll
-          for (int e = kVec - 1; e >= 0; --e) at = y[e] == top ? e : at;
-          p.l = p.m > kNone ? p.l * exp2_fast((p.m - top) * k) : 0.f;
-          p.m = top;
-          p.at = v + at;
-        }
-        if (p.m > kNone) {
-#pragma unroll
-          for (int e = 0; e < kVec; ++e)
-            p.l += y[e] == p.m ? 1.f : exp2_fast((y[e] - p.m) * k);
-        }
+  if constexpr (KIND == kStats || KIND == kWhole) {
+    if (lane < nr) ones[lane * kWaves + wave] = nothing;
+    each_special(0, n, [&](int r, int v, bool on, float y) {
+      Part p = nothing;
+      if (on) take(p, y, v, k);
+      p = wave_join(p, k);
+      const Part q = ones[r * kWaves + wave];
+      if (q.m > p.m) {
+        p.l = q.l + (p.m > kNone ? p.l * exp2_fast((p.m - q.m) * k) : 0.f);
+        p.one = q.one;
+        p.m = q.m;
+      } else if (q.m == p.m) {
+        p.l += q.l;
+        p.one = min(p.one, q.one);
       } else {
-        const Part p = whole[r];
-        if (k > 0.f && p.m > kNone) {
+        p.l += q.m > kNone ? q.l * exp2_fast((q.m - p.m) * k) : 0.f;
+      }
+      if (lane == 0) ones[r * kWaves + wave] = p;
+    });
+  }
+  // What becomes of the first NT special tokens, kept where their thread stores it from,
+  // behind the vectors of its row (later, the lines that it lies in would be in memory
+  // already, and be fetched to be changed).
+  auto result = [&](int r, int v, float x) {
+    if constexpr (KIND == kRules) return x;
+    float y[1] = {x};
+    shares(whole[r], y, v, k, greedy);
+    return y[0];
+  };
+  if constexpr (KIND == kRules || KIND == kProbs) {
+    each_special(0, min(n, NT), [&](int r, int v, bool on, float x) {
+      if (on) own_special[r * NT + tid] = result(r, v, x);
+    });
+  }
+  const int own_v = (KIND == kRules || KIND == kProbs) && tid < n ? base + list[tid] : 0;
+  auto store_special = [&](int r) {
+    __syncthreads();
+    if (tid >= n) return;
+    const float y = own_special[r * NT + tid];
+    if constexpr (KIND == kRules) store1(static_cast<T*>(a.out) + (row0 + r) * V + own_v, y);
+    else a.probs[(row0 + r) * V + own_v] = y;
+  };
+
+#pragma unroll 1
+  for (int r = 0; r < nr; ++r) {
+    if (r + 1 < nr) {
+      load(r + 1, next);
+      load_mask(r + 1, next);
+    }
+    T* out = static_cast<T*>(a.out) + (row0 + r) * V;
+    float* probs = a.probs + (row0 + r) * V;
+    if constexpr (KIND == kRules) {
+      // what is not special is forbidden or stays as it is (where it is, in place)
 #pragma unroll
-          for (int e = 0; e < kVec; ++e)
-            y[e] = (y[e] == p.m ? 1.f : exp2_fast((y[e] - p.m) * k)) * p.l;
-        } else {   // greedy, or nothing left
+      for (int c = 0; c < C; ++c) {
+        if (!full(c)) continue;
+        const uint32_t allowed = (cur.allowed[c] | ~plain[c]) & 0xFF;
+        if (allowed == 0xFF && out == logits + static_cast<int64_t>(r) * V) continue;
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) y[e] = p.m > kNone && v + e == p.at ? 1.f : 0.f;
+        for (int e = 0; e < kVec; ++e) cur.x[c].x[e] = allowed >> e & 1 ? cur.x[c].x[e] : kLowest<T>;
+        cur.x[c].store(out + vec(c));
+      }
+    } else {
+      float y[C][kVec], top = kNone;
+      int where = kNowhere;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const uint32_t allowed = vectors ? cur.allowed[c] & plain[c] : 0;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) y[c][e] = widen(cur.x[c].x[e]);
+        if (__any(allowed != 0xFF)) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) y[c][e] = masked(y[c][e], allowed, e);
         }
-        store8(a.probs + (row0 + r) * V, v, V, y);
+        if constexpr (KIND == kProbs) {
+          shares(whole[r], y[c], vec(c), k, greedy);
+          if (full(c)) store8(probs + vec(c), y[c]);
+        } else {
+          float most = y[c][0];
+#pragma unroll
+          for (int e = 1; e < kVec; ++e) most = fmaxf(most, y[c][e]);
+          where = most > top ? vec(c) : where;
+          top = fmaxf(top, most);
+        }
+      }
+      if constexpr (KIND != kProbs) {
+        const Part p = ones[r * kWaves + wave];
+        Part w;   // the wavefront's
+        w.m = fmaxf(wave_max_f(top), p.m);
+        w.l = 0.f;
+        if (__builtin_amdgcn_readfirstlane(w.m > kNone)) {
+          float sum = 0.f;
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) sum += exp2_fast((y[c][e] - w.m) * k);
+          if (sum != sum) {   // a NaN, or infinities, which count 1 each
+            sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+              for (int e = 0; e < kVec; ++e)
+                if (y[c][e] == y[c][e]) sum += y[c][e] == w.m ? 1.f : exp2_fast((y[c][e] - w.m) * k);
+          }
+          w.l = wave_sum_f(sum);
+          if (p.m > kNone) w.l += p.m == w.m ? p.l : p.l * exp2_fast((p.m - w.m) * k);
+        }
+        w.vec = wave_min(top == w.m ? where : kNowhere);
+        w.one = p.m == w.m ? p.one : kNowhere;
+        if (lane == 0) parts[r * kWaves + wave] = w;
+        if constexpr (KIND == kWhole) {
+          __syncthreads();
+          const Part q = wave_join(lane < kWaves ? parts[r * kWaves + lane] : nothing, k);
+          const int at = q.m > kNone ? place(q, r) : -1;
+          const Whole all{q.m, q.m > kNone ? 1.f / q.l : 0.f, at};
+          if (tid == 0) {
+            whole[r] = all;
+            if (a.top) a.top[row0 + r] = at;
+          }
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            if (!full(c)) continue;
+            shares(all, y[c], vec(c), k, greedy);
+            store8(probs + vec(c), y[c]);
+          }
+        }
       }
     }
+    if constexpr (KIND == kRules || KIND == kProbs) store_special(r);
+    cur = next;
   }
 
+  __syncthreads();
   if constexpr (KIND == kStats) {
-#pragma unroll
-    for (int r = 0; r < kRowsMax; ++r) {
-      if (r >= nr) continue;
-      Part p = acc[r];
-#pragma unroll
-      for (int x = 32; x >= 1; x >>= 1) p = join(p, shfl_part(p, x), k);
-      if (lane == 0) parts[wave][r] = p;
+    for (int r = wave; r < nr; r += kWaves) {
+      const Part p = wave_join(lane < kWaves ? parts[r * kWaves + lane] : nothing, k);
+      const int at = p.m > kNone ? place(p, r) : kNowhere;
+      if (lane == 0) a.ws[(row0 + r) * a.tiles + tile] = float4{p.m, p.l, __int_as_float(at), 0.f};
     }
-    __syncthreads();
-    if (tid < nr) {
-      Part p = parts[0][tid];
-      for (int w = 1; w < 4; ++w) p = join(p, parts[w][tid], k);
-      a.ws[(row0 + tid) * a.tiles + tile] = float4{p.m, p.l, __int_as_float(p.at), 0.f};
-    }
+  } else {
+    // the special tokens that are left, behind the vectors that hold them
+    each_special(KIND == kWhole ? 0 : NT, n, [&](int r, int v, bool on, float x) {
+      if (!on) return;
+      const float y = result(r, v, x);
+      if constexpr (KIND == kRules) store1(static_cast<T*>(a.out) + (row0 + r) * V + v, y);
+      else a.probs[(row0 + r) * V + v] = y;
+    });
   }
 }
 
@@ -431,30 +671,33 @@ __global__ __launch_bounds__(256) void count_few_kernel(CountArgs a) {
 }
 
 template <typename T>
-hipError_t launch_rows(const LogitArgs& a, int kind, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.S) * a.tiles * a.groups)), block(256);
-  if (kind == kRules) {
-    hipLaunchKernelGGL((rows_kernel<T, kRules>), grid, block, 0, stream, a);
+hipError_t launch_rows(const LogitArgs& a, bool rules, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.S) * a.tiles * a.groups));
+  if (rules) {
+    hipLaunchKernelGGL((rows_kernel<T, kRules, 256, kVecs>), grid, dim3(256), 0, stream, a);
+  } else if (a.tiles == 1 && a.V <= 256 * kVec) {
+    hipLaunchKernelGGL((rows_kernel<T, kWhole, 256, 1>), grid, dim3(256), 0, stream, a);
+  } else if (a.tiles == 1) {
+    hipLaunchKernelGGL((rows_kernel<T, kWhole, 1024, 2>), grid, dim3(1024), 0, stream, a);
   } else {
-    hipLaunchKernelGGL((rows_kernel<T, kStats>), grid, block, 0, stream, a);
-    hipLaunchKernelGGL((rows_kernel<T, kProbs>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((rows_kernel<T, kStats, 256, kVecs>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((rows_kernel<T, kProbs, 256, kVecs>), grid, dim3(256), 0, stream, a);
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-LogitPlan plan_logits(int S, int R, int V, int num_cus) {
+LogitPlan plan_logits(int S, int R, int V, int num_cus, bool rules) {
   LogitPlan p{};
-  p.groups = (R + kRowsMax - 1) / kRowsMax;
+  const int tile = rules || V > 1024 * kVec * 2 ? 256 * kVec * kVecs : V;
+  p.tiles = static_cast<int>((static_cast<int64_t>(V) + tile - 1) / tile);
+  // rows together as long as four workgroups are left to every compute unit
+  int64_t per = static_cast<int64_t>(p.tiles) * S * R / (4 * num_cus);
+  per = per < 1 ? 1 : (per > kRowsMax ? kRowsMax : per);
+  p.groups = (R + static_cast<int>(per) - 1) / static_cast<int>(per);
   p.rows_per = (R + p.groups - 1) / p.groups;
   p.groups = (R + p.rows_per - 1) / p.rows_per;
-  const int64_t all = (static_cast<int64_t>(V) + kChunk - 1) / kChunk;
-  // as many chunks to a workgroup as leave eight workgroups to every compute unit
-  int64_t chunks = all * S * p.groups / (8 * num_cus);
-  chunks = chunks < 1 ? 1 : (chunks > 8 ? 8 : chunks);
-  p.chunks = static_cast<int>(chunks);
-  p.tiles = static_cast<int>((all + chunks - 1) / chunks);
   p.workgroups = static_cast<int64_t>(S) * p.groups * p.tiles;
   p.ws_bytes = (static_cast<size_t>(S) * R * p.tiles * sizeof(float4) + 255) / 256 * 256;
   return p;
@@ -462,14 +705,12 @@ LogitPlan plan_logits(int S, int R, int V, int num_cus) {
 
 hipError_t launch_logit_rules(const LogitArgs& a, int dtype, hipStream_t stream) {
   if (a.S == 0) return hipSuccess;
-  return dtype == CO_DTYPE_BF16 ? launch_rows<uint16_t>(a, kRules, stream)
-                                : launch_rows<float>(a, kRules, stream);
+  return dtype == CO_DTYPE_BF16 ? launch_rows<uint16_t>(a, true, stream) : launch_rows<float>(a, true, stream);
 }
 
 hipError_t launch_probabilities(const LogitArgs& a, int dtype, hipStream_t stream) {
   if (a.S == 0) return hipSuccess;
-  return dtype == CO_DTYPE_BF16 ? launch_rows<uint16_t>(a, kProbs, stream)
-                                : launch_rows<float>(a, kProbs, stream);
+  return dtype == CO_DTYPE_BF16 ? launch_rows<uint16_t>(a, false, stream) : launch_rows<float>(a, false, stream);
 }
 
 int64_t count_workgroups(int S, int V) {
