@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kVec = 8;                     // tokens of a thread: one byte of a mask
 constexpr int kVecs = 4;                    // such vectors of a thread
-constexpr int kRowsMax = 8;                 // rows of a sequence that a workgroup takes
+constexpr int kRowsMax = 6;                 // rows of a sequence that a workgroup takes
 
 enum { kRules = 0, kStats = 1, kProbs = 2, kWhole = 3 };
 
@@ -65,6 +65,16 @@ __device__ __forceinline__ float masked(float y, uint32_t allowed, int e) {
   float r;
   asm("v_bfi_b32 %0, %1, %2, %3" : "=v"(r) : "v"(m), "v"(y), "v"(kNone));
   return r;
+}
+
+// The same for 16-bit logits two at a time; m: all ones where a token is allowed.
+__device__ __forceinline__ uint32_t masked2(uint32_t x, uint32_t m) {
+  uint32_t r;
+  asm("v_bfi_b32 %0, %1, %2, %3" : "=v"(r) : "v"(m), "v"(x), "v"(0xFF80FF80u));
+  return r;
+}
+__device__ __forceinline__ uint32_t pair_mask(uint32_t allowed, int pair) {
+  return (allowed >> (2 * pair) & 1 ? 0xFFFFu : 0u) | (allowed >> (2 * pair + 1) & 1 ? 0xFFFF0000u : 0u);
 }
 
 // The penalties on one logit that was seen; c: how often generated.
@@ -174,7 +184,7 @@ struct Entry {
   uint32_t proposed[2];  // bit i: the window's proposal i is this token (of the first 64)
 };
 
-constexpr int kBiasHeld = 512;   // biases of a tile that are held in LDS
+constexpr int kBiasHeld = 256;   // biases of a tile that are held in LDS
 
 // One workgroup: a tile of tokens of one sequence, C vectors of eight a thread, in rows one
 // after the other, the next row's logits in flight.
@@ -182,7 +192,7 @@ constexpr int kBiasHeld = 512;   // biases of a tile that are held in LDS
 //   parts joined, and the probabilities.  kWhole: both, where a row is one tile.
 template <typename T, int KIND, int NT, int C>
 __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
-  constexpr int kTokens = NT * kVec * C, kWaves = NT / 64;
+  constexpr int kTokens = NT * kVec * C, kWaves = NT / 64, kBlock = 64 * kVec;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int b = blockIdx.x;
@@ -190,7 +200,7 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   b /= a.groups;
   const int tile = b % a.tiles, s = b / a.tiles;
   const int j0 = grp * a.rows_per, nr = min(a.rows_per, a.R - j0);
-  const int V = a.V, base = tile * kTokens;
+  const int V = a.V;
   const int64_t row0 = static_cast<int64_t>(s) * a.R + j0;
   const T* logits = static_cast<const T*>(a.logits) + row0 * V;
   const bool reports = KIND != kProbs && tile == 0 && grp == 0;   // what concerns a sequence
@@ -210,7 +220,14 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
 
   // Vector c of this thread: whole where full(c); others are loaded from the row's last whole
   // one, so that no load is behind a branch, and masked.
-  auto vec = [&](int c) { return base + (c * NT + tid) * kVec; };
+  // Tiles interleave in blocks of a wavefront's 512 tokens: frequent tokens have low numbers,
+  // and a tile of them alone would have most of the special ones.
+  auto vec = [&](int c) { return ((c * kWaves + wave) * a.tiles + tile) * kBlock + lane * kVec; };
+  auto token_of = [&](int t) { return ((t / kBlock) * a.tiles + tile) * kBlock + t % kBlock; };
+  auto in_tile = [&](int v) {   // the inverse; -1: another tile's
+    const int b = v / kBlock;
+    return b % a.tiles == tile ? b / a.tiles * kBlock + v % kBlock : -1;
+  };
   auto full = [&](int c) { return vec(c) + kVec <= V; };
   auto at_vec = [&](int c) { return min(vec(c), V - kVec); };
   const bool vectors = V >= kVec;
@@ -294,18 +311,19 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   if (n_bias > 0 || draft) {
     __syncthreads();
     for (int i = tid; i < (reports && draft ? a.R - 1 : before); i += NT) {
-      const int d = i == lane && i < before ? held : draft[i], t = d - base;
+      const int d = i == lane && i < before ? held : draft[i];
       if (static_cast<uint32_t>(d) >= static_cast<uint32_t>(V)) {
         if (reports) set_status(a.status, CO_ERR_TOKEN);
-      } else if (i < before && t >= 0 && t < kTokens) {
-        atomicOr(&special[t >> 5], 1u << (t & 31));
+      } else if (i < before) {
+        const int t = in_tile(d);
+        if (t >= 0) atomicOr(&special[t >> 5], 1u << (t & 31));
       }
     }
     for (int i = tid; i < n_bias; i += NT) {
-      const int d = i == tid ? own_tok : a.bias_tok[b0 + i], t = d - base;
+      const int d = i == tid ? own_tok : a.bias_tok[b0 + i];
       if (static_cast<uint32_t>(d) >= static_cast<uint32_t>(V)) {
         if (reports) set_status(a.status, CO_ERR_TOKEN);
-      } else if (t >= 0 && t < kTokens) {
+      } else if (const int t = in_tile(d); t >= 0) {
         atomicOr(&special[t >> 5], 1u << (t & 31));
         atomicOr(&with_bias[t >> 5], 1u << (t & 31));
         const int at = atomicAdd(&num_held, 1);
@@ -326,6 +344,13 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
     plain[c] = full(c) ? m ^ 0xFF : 0;
     own += __builtin_popcount(m);
   }
+  uint32_t pairs[sizeof(T) == 2 ? C : 1][4];   // 16-bit logits: the masks of `plain`
+  if constexpr (sizeof(T) == 2 && KIND != kRules) {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) pairs[c][q] = pair_mask(vectors ? plain[c] : 0, q);
+  }
   const int upto = wave_scan(own);
   if (lane == 63) listed[wave] = upto;
   __syncthreads();
@@ -345,7 +370,7 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   auto entry = [&](int i) {
     Entry e{};
     const int t = list[i];
-    e.v = base + t;
+    e.v = token_of(t);
     e.word = seen ? seen[e.v] : 0;
     e.biased = with_bias[t >> 5] >> (t & 31) & 1;
     if (e.biased) {
@@ -385,17 +410,17 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   auto each_special = [&](int from, int to, auto&& f) {
     for (int i0 = from + wave * 64; i0 < to; i0 += NT) {
       const bool on = i0 + lane < n;
-      Entry e{base};
+      Entry e{};
       if (on) e = entry(i0 + lane);
       T x[kRowsMax];
       uint32_t allowed[kRowsMax];
 #pragma unroll
       for (int q = 0; q < kRowsMax; ++q) x[q] = logits[static_cast<int64_t>(min(q, nr - 1)) * V + e.v];
 #pragma unroll
-      for (int q = 0; q < kRowsMax; ++q) {
-        const int m = mask_of(min(q, nr - 1));
-        if (m >= 0) allowed[q] = bits_of(m)[e.v / 8];
-        else allowed[q] = m == -1 ? 0xFF : 0;
+      for (int q = 0; q < kRowsMax; ++q) allowed[q] = 0xFF;
+      if (a.mask_row && a.num_masks > 0) {   // (rows without a mask read the first one's)
+#pragma unroll
+        for (int q = 0; q < kRowsMax; ++q) allowed[q] = bits_of(max(0, mask_of(min(q, nr - 1))))[e.v / 8];
       }
 #pragma unroll 1
       for (int r = 0; r < nr; ++r) {
@@ -406,7 +431,8 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
           xr = q == r ? x[q] : xr;
           ar = q == r ? allowed[q] : ar;
         }
-        f(r, e.v, on, ruled(e, r, widen(xr), ar));
+        const int m = mask_of(r);
+        f(r, e.v, on, ruled(e, r, widen(xr), m >= 0 ? ar : (m == -1 ? 0xFF : 0)));
       }
     }
   };
@@ -415,7 +441,7 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   // eight that is neither masked nor special, or a special one before it.
   auto place = [&](const Part& p, int r) {
     if (p.vec == kNowhere) return p.one;
-    const int v = p.vec + (lane & 7), t = v - base, m = mask_of(r);
+    const int v = p.vec + (lane & 7), t = in_tile(v), m = mask_of(r);
     const uint32_t allowed = m >= 0 ? bits_of(m)[v / 8] >> (v % 8) & 1 : (m == -1 ? 1 : 0);
     const bool is = allowed && !(special[t >> 5] >> (t & 31) & 1) &&
                     widen(logits[static_cast<int64_t>(r) * V + v]) == p.m;
@@ -477,12 +503,7 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
     shares(whole[r], y, v, k, greedy);
     return y[0];
   };
-  if constexpr (KIND == kRules || KIND == kProbs) {
-    each_special(0, min(n, NT), [&](int r, int v, bool on, float x) {
-      if (on) own_special[r * NT + tid] = result(r, v, x);
-    });
-  }
-  const int own_v = (KIND == kRules || KIND == kProbs) && tid < n ? base + list[tid] : 0;
+  const int own_v = (KIND == kRules || KIND == kProbs) && tid < n ? token_of(list[tid]) : 0;
   auto store_special = [&](int r) {
     __syncthreads();
     if (tid >= n) return;
@@ -491,6 +512,22 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
     else a.probs[(row0 + r) * V + own_v] = y;
   };
 
+  // kRules, kProbs: the first NT special tokens before the rows, the others behind them
+#pragma unroll 1
+  for (int phase = 0; phase < (KIND == kStats ? 1 : 2); ++phase) {
+    if constexpr (KIND != kStats) {
+      if (KIND != kWhole || phase == 1) {
+        each_special(KIND == kWhole || phase == 0 ? 0 : NT, KIND != kWhole && phase == 0 ? min(n, NT) : n,
+                     [&](int r, int v, bool on, float x) {
+          if (!on) return;
+          const float y = result(r, v, x);
+          if (KIND != kWhole && phase == 0) own_special[r * NT + tid] = y;
+          else if constexpr (KIND == kRules) store1(static_cast<T*>(a.out) + (row0 + r) * V + v, y);
+          else a.probs[(row0 + r) * V + v] = y;
+        });
+      }
+      if (phase == 1) break;
+    }
 #pragma unroll 1
   for (int r = 0; r < nr; ++r) {
     if (r + 1 < nr) {
@@ -515,12 +552,28 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
       int where = kNowhere;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const uint32_t allowed = vectors ? cur.allowed[c] & plain[c] : 0;
+        if constexpr (sizeof(T) == 2) {
+          typedef uint16_t plain8 __attribute__((ext_vector_type(8)));
+          typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+          const u32x4 x = __builtin_bit_cast(u32x4, static_cast<plain8>(cur.x[c].x));
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) y[c][e] = widen(cur.x[c].x[e]);
-        if (__any(allowed != 0xFF)) {
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t z = masked2(x[q], pairs[c][q]);
+            y[c][2 * q] = __uint_as_float(z << 16);
+            y[c][2 * q + 1] = __uint_as_float(z & 0xFFFF0000u);
+          }
+          if (mask_of(r) != -1) {
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) y[c][e] = masked(y[c][e], allowed, e);
+            for (int e = 0; e < kVec; ++e) y[c][e] = masked(y[c][e], cur.allowed[c], e);
+          }
+        } else {
+          const uint32_t allowed = vectors ? cur.allowed[c] & plain[c] : 0;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) y[c][e] = widen(cur.x[c].x[e]);
+          if (__any(allowed != 0xFF)) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) y[c][e] = masked(y[c][e], allowed, e);
+          }
         }
         if constexpr (KIND == kProbs) {
           shares(whole[r], y[c], vec(c), k, greedy);
@@ -579,22 +632,16 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
     if constexpr (KIND == kRules || KIND == kProbs) store_special(r);
     cur = next;
   }
-
   __syncthreads();
+  if ((KIND == kRules || KIND == kProbs) && n <= NT) break;
+  }
+
   if constexpr (KIND == kStats) {
     for (int r = wave; r < nr; r += kWaves) {
       const Part p = wave_join(lane < kWaves ? parts[r * kWaves + lane] : nothing, k);
       const int at = p.m > kNone ? place(p, r) : kNowhere;
       if (lane == 0) a.ws[(row0 + r) * a.tiles + tile] = float4{p.m, p.l, __int_as_float(at), 0.f};
     }
-  } else {
-    // the special tokens that are left, behind the vectors that hold them
-    each_special(KIND == kWhole ? 0 : NT, n, [&](int r, int v, bool on, float x) {
-      if (!on) return;
-      const float y = result(r, v, x);
-      if constexpr (KIND == kRules) store1(static_cast<T*>(a.out) + (row0 + r) * V + v, y);
-      else a.probs[(row0 + r) * V + v] = y;
-    });
   }
 }
 
