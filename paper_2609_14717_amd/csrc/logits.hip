@@ -27,7 +27,7 @@ namespace co {
 namespace {
 
 constexpr int kVec = 8;                     // tokens of a thread: one byte of a mask
-constexpr int kVecs = 4;                    // such vectors of a thread
+constexpr int kVecs = 2;                    // such vectors of a thread
 constexpr int kRowsMax = 6;                 // rows of a sequence that a workgroup takes
 
 enum { kRules = 0, kStats = 1, kProbs = 2, kWhole = 3 };
