@@ -1084,7 +1084,7 @@ co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t wid
   a.seen = seen;
   a.status = status;
   clear_stale_error();
-  return hip_status(launch_count_tokens(a, stream));
+  return hip_status(launch_count_tokens(a, num_cus(), stream));
 }
 
 co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,

@@ -355,7 +355,7 @@ struct CountArgs {
 };
 
 int64_t count_workgroups(int S, int V);
-hipError_t launch_count_tokens(CountArgs a, hipStream_t stream);
+hipError_t launch_count_tokens(CountArgs a, int num_cus, hipStream_t stream);
 
 // Launch-shape override in force (-1: automatic); see carryover_set_tuning.
 int64_t tuning(int knob);

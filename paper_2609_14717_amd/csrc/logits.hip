@@ -661,9 +661,28 @@ __device__ __forceinline__ uint16_t counted(uint16_t word, uint32_t n, uint32_t 
   return static_cast<uint16_t>((word & 0x8000u) | c);
 }
 
-// A tile of one sequence's words: the tokens that fall into it are counted in LDS, then
-// the tile is written whole (a row that starts afresh), or its touched words are.  Every
-// word has one writer.
+// Every token of a sequence, four to a load where they are aligned: f(token).
+template <int NT, typename F>
+__device__ __forceinline__ void each_token(const int32_t* tok, int n, F&& f) {
+  const int tid = threadIdx.x;
+  int done = 0;
+  if ((reinterpret_cast<uintptr_t>(tok) & 15) == 0) {
+    const int4* four = reinterpret_cast<const int4*>(tok);
+    for (int i = tid; i < n / 4; i += NT) {
+      const int4 t = four[i];
+      f(t.x);
+      f(t.y);
+      f(t.z);
+      f(t.w);
+    }
+    done = n & ~3;
+  }
+  for (int i = done + tid; i < n; i += NT) f(tok[i]);
+}
+
+// A tile of one sequence's words: the tokens that fall into it are counted in LDS, then the
+// tile is written whole (a row that starts afresh), or its touched words are.  Every word
+// has one writer.
 __global__ __launch_bounds__(256) void count_tile_kernel(CountArgs a) {
   __shared__ uint32_t cnt[kTile];
   const int tid = threadIdx.x;
@@ -674,19 +693,52 @@ __global__ __launch_bounds__(256) void count_tile_kernel(CountArgs a) {
   const int base = tile * kTile, here = min(kTile, a.V - base);
   for (int i = tid; i < here; i += 256) cnt[i] = 0;
   __syncthreads();
-  const int32_t* tok = a.tokens + static_cast<int64_t>(s) * a.width;
-  for (int i = tid; i < n; i += 256) {
-    const int t = tok[i];
+  each_token<256>(a.tokens + static_cast<int64_t>(s) * a.width, n, [&](int t) {
     if (t >= a.V) set_status(a.status, CO_ERR_TOKEN);
     else if (t >= base && t - base < here) atomicAdd(&cnt[t - base], 1u);
-  }
+  });
   __syncthreads();
   uint16_t* row = a.seen + static_cast<int64_t>(s) * a.V + base;
+  for (int i = tid; i < here; i += 256) {
+    const uint16_t old = a.flags & CO_COUNT_FRESH || !cnt[i] ? 0 : row[i];
+    if (cnt[i]) row[i] = counted(old, cnt[i], 0);
+    else if (a.flags & CO_COUNT_FRESH) row[i] = 0;
+  }
+}
+
+// The same for prompts, of which a bit a token is all there is to know: tiles of up to
+// 65536 tokens, so that the tokens are read few times over.
+constexpr int kPromptTile = 65536;
+
+__global__ __launch_bounds__(512) void mark_tile_kernel(CountArgs a, int size) {
+  __shared__ uint32_t bits[kPromptTile / 32];
+  const int tid = threadIdx.x;
+  const int tile = blockIdx.x % a.tiles, s = blockIdx.x / a.tiles;
+  const int n = token_count(a, s);
+  if (n < 0 && tile == 0 && tid == 0) set_status(a.status, CO_ERR_LENGTH);
+  if (n <= 0) return;
+  const int base = tile * size, here = min(size, a.V - base);
+  for (int i = tid; i < size / 32; i += 512) bits[i] = 0;
+  __syncthreads();
+  each_token<512>(a.tokens + static_cast<int64_t>(s) * a.width, n, [&](int t) {
+    if (t >= a.V) set_status(a.status, CO_ERR_TOKEN);
+    else if (t >= base && t - base < here) atomicOr(&bits[(t - base) >> 5], 1u << (t & 31));
+  });
+  __syncthreads();
+  uint16_t* row = a.seen + static_cast<int64_t>(s) * a.V + base;
+  const uint8_t* byte = reinterpret_cast<const uint8_t*>(bits);
   if (a.flags & CO_COUNT_FRESH) {
-    for (int i = tid; i < here; i += 256) row[i] = cnt[i] ? counted(0, cnt[i], a.flags) : 0;
+    for (int i = tid; i < here / kVec; i += 512) {
+      Vec<uint16_t> w;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) w.x[e] = static_cast<uint16_t>((byte[i] >> e & 1) << 15);
+      w.store(row + i * kVec);
+    }
+    for (int i = (here & ~(kVec - 1)) + tid; i < here; i += 512)
+      row[i] = static_cast<uint16_t>((bits[i >> 5] >> (i & 31) & 1) << 15);
   } else {
-    for (int i = tid; i < here; i += 256)
-      if (cnt[i]) row[i] = counted(row[i], cnt[i], a.flags);
+    for (int i = tid; i < (here + 31) / 32; i += 512)
+      for (uint32_t m = bits[i]; m != 0; m &= m - 1) row[32 * i + __builtin_ctz(m)] |= 0x8000u;
   }
 }
 
@@ -764,10 +816,17 @@ int64_t count_workgroups(int S, int V) {
   return static_cast<int64_t>(S) * ((static_cast<int64_t>(V) + kTile - 1) / kTile);
 }
 
-hipError_t launch_count_tokens(CountArgs a, hipStream_t stream) {
+hipError_t launch_count_tokens(CountArgs a, int num_cus, hipStream_t stream) {
   if (a.S == 0 || a.width == 0) return hipSuccess;
   if (a.width <= 64 && !(a.flags & CO_COUNT_FRESH)) {
     hipLaunchKernelGGL(count_few_kernel, dim3((a.S + 3) / 4), dim3(256), 0, stream, a);
+  } else if (a.flags & CO_COUNT_PROMPT) {
+    // tiles as large as leave a workgroup to every compute unit, from kTile on
+    int size = kPromptTile;
+    while (size > kTile && static_cast<int64_t>(a.S) * ((a.V + int64_t{size} - 1) / size) < num_cus) size /= 2;
+    a.tiles = static_cast<int>((static_cast<int64_t>(a.V) + size - 1) / size);
+    hipLaunchKernelGGL(mark_tile_kernel, dim3(static_cast<unsigned>(a.S) * a.tiles), dim3(512), 0, stream, a,
+                       size);
   } else {
     a.tiles = static_cast<int>((static_cast<int64_t>(a.V) + kTile - 1) / kTile);
     hipLaunchKernelGGL(count_tile_kernel, dim3(static_cast<unsigned>(count_workgroups(a.S, a.V))),

@@ -319,7 +319,8 @@ def u16(x):
 
 @pytest.mark.parametrize("S,V,width,flags", [
     (1, 1, 1, 0), (1, 50, 40, 3), (3, 1000, 16, 0), (5, 1000, 64, 1), (4, 1000, 65, 0), (2, 8192, 300, 2),
-    (3, 8193, 5000, 3), (7, 32001, 700, 1), (2, 40000, 64, 3), (600, 77, 8, 0)])
+    (3, 8193, 5000, 3), (7, 32001, 700, 1), (2, 40000, 64, 3), (600, 77, 8, 0), (2, 131077, 3001, 3),
+    (300, 70003, 90, 3), (3, 65537, 2000, 2), (150, 70001, 100, 1)])
 @pytest.mark.parametrize("lens", [True, False])
 def test_history(S, V, width, flags, lens):
     print(f"[history] S={S} V={V} width={width} flags={flags}", flush=True)
