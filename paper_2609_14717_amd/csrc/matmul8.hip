@@ -19,17 +19,11 @@ constexpr float kLeast = 0x1.fcp-120f;   // 127 * 2^-126: smallest magnitude tha
 
 // -------------------------------------------------------------- quantisation
 
-// One code: 127 x / a to the nearest integer, ties to even, exactly: where the fp32
-// product with r = 127 / a (off by up to 2^-16) is too close to the middle of two
-// integers, the quotient in fp64 decides (its rounding cannot reach a middle that the
-// exact quotient, of two 24-bit numbers, does not lie on).
-__device__ __forceinline__ int code_of(float x, float a, float r) {
-#pragma clang fp contract(off)
-  const float t = x * r;
-  const float n = rintf(t);
-  if (fabsf(fabsf(t - n) - 0.5f) < 0x1p-14f)
-    return static_cast<int>(rint(static_cast<double>(x) * 127.0 / static_cast<double>(a)));
-  return static_cast<int>(n);
+// One code: 127 x / a to the nearest integer, ties to even (the fp64 quotient's rounding
+// cannot reach a middle of two integers that the exact quotient, of two 24-bit numbers, does
+// not lie on).
+__device__ __forceinline__ int code_of(float x, float a) {
+  return static_cast<int>(rint(static_cast<double>(x) * 127.0 / static_cast<double>(a)));
 }
 
 // Largest of the workgroup's values, in every thread.
@@ -71,11 +65,30 @@ struct RowScale {
     r = 127.f / a;
     scale = bad ? NAN : a / 127.f;
   }
+  // x r, r = 127 / a, is off from the quotient by up to 2^-16 (127 times two roundings): added
+  // to 1.5 * 2^23 it leaves the nearest integer in the sum's low bits.  Where one of the eight
+  // comes within 2^-14 of a middle, the quotients decide.
   __device__ __forceinline__ void codes(const float (&x)[8], int8_t* out) const {
-    uint32_t w[2] = {0, 0};
+    constexpr float kMagic = 12582912.f;
+    uint32_t w[2], n[8];
+    float far = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      w[e >> 2] |= (bad ? 0u : static_cast<uint32_t>(code_of(x[e], a, r)) & 0xFFu) << (8 * (e & 3));
+    for (int e = 0; e < 8; ++e) {
+      const float t = fmaf(x[e], r, kMagic);
+      far = fmaxf(far, fabsf(fmaf(x[e], r, kMagic - t)));
+      n[e] = __float_as_uint(t);
+    }
+    if (far > 0.5f - 0x1p-14f) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) n[e] = static_cast<uint32_t>(code_of(x[e], a));
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // the low bytes of four words: pairs, then both pairs
+      const uint32_t lo = __builtin_amdgcn_perm(n[4 * h + 1], n[4 * h], 0x0C0C0400u);
+      const uint32_t hi = __builtin_amdgcn_perm(n[4 * h + 3], n[4 * h + 2], 0x0C0C0400u);
+      w[h] = bad ? 0u : (lo | hi << 16);
+    }
     *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
   }
 };
@@ -818,9 +831,14 @@ struct Product {
 #pragma clang fp contract(off)
     const int64_t at = row * N + col;
     if (splits == 0) return *reinterpret_cast<const f32x4*>(y + at);
-    i32x4 sum = *reinterpret_cast<const i32x4*>(part + at);
-    for (int s = 1; s < splits; ++s)
-      sum += *reinterpret_cast<const i32x4*>(part + s * static_cast<int64_t>(M) * N + at);
+    i32x4 sum = {};
+    int s = 0;
+    for (; s + 4 <= splits; s += 4) {   // four loads in flight
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        sum += *reinterpret_cast<const i32x4*>(part + (s + q) * static_cast<int64_t>(M) * N + at);
+    }
+    for (; s < splits; ++s) sum += *reinterpret_cast<const i32x4*>(part + s * static_cast<int64_t>(M) * N + at);
     const float sa = a_scale[row];
     const f32x4u sw = *reinterpret_cast<const f32x4u*>(w_scale + col);   // (aligned to an element)
     f32x4 v;
@@ -926,19 +944,24 @@ __global__ __launch_bounds__(NT) void z_codes_kernel(Product p, float* spill, co
   }
 }
 
-// Rows of the K/V product to their destinations, four rotation pairs a thread.
+// Rows of the K/V product to their destinations: one head segment of some rows a workgroup,
+// four rotation pairs a thread.  Keys: the lanes of a row side by side (its dims lie next to
+// each other).  Values: rows side by side, for their pages have a dim's sixteen tokens next
+// to each other (two bytes a token; dims side by side 23 us, rows 12 us for 512 rows of five
+// layers).
 __global__ __launch_bounds__(256) void store_rows_i8_kernel(Product p, KvDest e) {
   __shared__ double inv_tab[64];
-  const int half = e.hd / 2;
+  const int half = e.hd / 2, lanes = half / 4, rows = 256 / lanes;   // 16 or 8 lanes a row
   if (threadIdx.x < half) inv_tab[threadIdx.x] = rope_table<uint16_t>(e, threadIdx.x);
   __syncthreads();
-  const int per_row = p.N / 8, lanes = half / 4;   // lanes of a head segment
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= static_cast<int64_t>(p.M) * per_row) return;   // (whole rows of lanes at a time)
-  const int row = static_cast<int>(i / per_row), rem = static_cast<int>(i % per_row);
+  const int segs = p.N / e.hd, seg = blockIdx.x % segs;
+  const bool value = (seg / e.Hkv & 1) != 0;
+  const int tid = threadIdx.x;
+  const int row = static_cast<int>(blockIdx.x / segs) * rows + (value ? tid % rows : tid / lanes);
+  const int i0 = (value ? tid / rows : tid % lanes) * 4;
+  if (row >= p.M) return;                  // (a key's lanes of a row leave together)
   const int32_t dst = e.row_dst[row];
-  if (dst == kSkip) return;                               // all lanes of the row
-  const int seg = rem / lanes, i0 = rem % lanes * 4;
+  if (dst == kSkip) return;
   const f32x4 a = p.four(row, seg * e.hd + i0), b = p.four(row, seg * e.hd + half + i0);
   float lo[4], hi[4];
 #pragma unroll
@@ -1001,8 +1024,9 @@ hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t st
   else
     hipLaunchKernelGGL((z_codes_kernel<1024, 0>), rows, dim3(1024), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
   if ((err = product(n_kv, a.d, a.wkv, a.wkv_scale, &p)) != hipSuccess) return err;
-  const int64_t items = static_cast<int64_t>(a.M) * (n_kv / 8);
-  hipLaunchKernelGGL(store_rows_i8_kernel, dim3(static_cast<unsigned>((items + 255) / 256)), dim3(256), 0,
+  const int per = 1024 / (a.dst.hd / 2);   // rows of a workgroup
+  hipLaunchKernelGGL(store_rows_i8_kernel,
+                     dim3(static_cast<unsigned>((a.M + per - 1) / per) * (n_kv / a.dst.hd)), dim3(256), 0,
                      stream, p, a.dst);
   return hipGetLastError();
 }
