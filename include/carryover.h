@@ -655,8 +655,8 @@ co_status carryover_round_kv8(const co_dims* dims, const co_weights* w, const vo
  * (exactly), from -127 to 127.  A row with an infinity or a NaN gets scale NaN and
  * codes 0, so that every product with it is NaN.  x [num_rows][num_cols] of
  * `dtype` (CO_DTYPE_F32 or CO_DTYPE_BF16) and codes of the same shape, 16-byte
- * aligned; scale fp32 [num_rows].  num_cols: a multiple of 64; num_rows * num_cols
- * any, num_rows below 2^24 (CO_ERR_UNSUPPORTED otherwise).
+ * aligned; scale fp32 [num_rows].  num_cols: a multiple of 64; num_rows below
+ * 2^22 (CO_ERR_UNSUPPORTED otherwise).
  */
 co_status carryover_quantize_i8(int32_t num_rows, int32_t num_cols, int32_t dtype, const void* x,
                                 int8_t* codes, float* scale, hipStream_t stream);
@@ -670,7 +670,7 @@ co_status carryover_quantize_i8(int32_t num_rows, int32_t num_cols, int32_t dtyp
  * `dtype` (CO_DTYPE_F32 or CO_DTYPE_BF16), 16-byte aligned.  m and n from 0 to 2^24 - 1,
  * k a multiple of 64 from 64 to 131008 (CO_ERR_UNSUPPORTED otherwise).  `ws`:
  * carryover_matmul_i8_workspace_bytes(m, n, k) bytes of scratch, 256-byte
- * aligned (any contents; NULL where that is 0).
+ * aligned (any contents, for one call at a time; NULL where that is 0).
  */
 co_status carryover_matmul_i8(int32_t m, int32_t n, int32_t k, const int8_t* a,
                               const float* a_scale, const int8_t* w, const float* w_scale,
@@ -685,7 +685,8 @@ size_t carryover_matmul_i8_workspace_bytes(int32_t m, int32_t n, int32_t k);
  * and those of z = F x, are quantised as carryover_quantize_i8 does (z from its
  * fp32 sums, after F E and the norm), both products are carryover_matmul_i8's in
  * fp32, keys are normalised and rotated and rows stored as ever, in bf16.  No
- * separate carry projector.  Supported: bf16, feat_dim and model_dim up to 131008.
+ * separate carry projector.  Supported: bf16, feat_dim and model_dim up to 131008,
+ * num_seqs * block below 2^22, and times the wider of model_dim and NKV below 2^32.
  * `ws`: carryover_workspace_bytes(dims, CO_WS_PROJECT_I8) bytes, 256-byte aligned.
  * Other arguments and errors as carryover_project_kv.
  */
@@ -704,7 +705,8 @@ co_status carryover_project_kv_i8(const co_dims* dims, const co_weights_i8* w, c
  * dims is used (the rest must still be valid).  Device errors, written to *status:
  * CO_ERR_LENGTH (len outside [0, width]; the sequence stays as it is), CO_ERR_TOKEN
  * (a token >= vocab; it is left out).  Calls on one history must not overlap.
- * Host: vocab >= 1, num_seqs * ceil(vocab / 8192) below 2^23 (CO_ERR_UNSUPPORTED).
+ * Host: vocab from 1 to 2^30, num_seqs * ceil(vocab / 8192) below 2^23
+ * (CO_ERR_UNSUPPORTED).
  */
 enum { CO_COUNT_PROMPT = 1, CO_COUNT_FRESH = 2 };
 co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t width,
@@ -717,13 +719,13 @@ co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t wid
  * and must not overlap it otherwise.  rows from 1 to block + 1: a verified window
  * has block + 1, single tokens 1.  draft_tok int32 [num_seqs][block]: the window's
  * proposals, of which row j has the first j behind it (NULL: rows do not follow each
- * other).  Only num_seqs and block of dims are used (the rest must still be valid).
+ * other); they count with rules->seen.  Only num_seqs and block of dims are used (the rest must still be valid).
  * Device errors, written to *status: CO_ERR_TOKEN (a proposal or a bias's token outside
  * [0, vocab); it is left out), CO_ERR_LENGTH (bias_start that decreases or lies outside
  * [0, num_bias]; the sequence has no biases), CO_ERR_MASK (mask_row >= num_masks; the row
  * allows no token).
- * Host: vocab >= 1, block <= 1024, num_seqs * rows * vocab <= 2^40, and a grid of
- * workgroups below 2^24 (CO_ERR_UNSUPPORTED).
+ * Host: vocab from 1 to 2^30, block <= 1024, num_seqs * rows * vocab <= 2^40, fewer than
+ * 2^23 workgroups of up to 6 rows and 4096 tokens (CO_ERR_UNSUPPORTED).
  */
 co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,
                                 const void* logits, const int32_t* draft_tok,
@@ -740,8 +742,8 @@ co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows
  * of carryover_route).  A NaN among the logits is left out, as if masked; infinite ones
  * share the row.  A row with nothing left has probabilities 0 and top_tok -1.  The
  * logits are not changed; probs must not overlap them.  `ws`:
- * carryover_probabilities_workspace_bytes(dims, vocab, rows) bytes of scratch,
- * 256-byte aligned.  Other arguments and errors as carryover_logit_rules.
+ * carryover_probabilities_workspace_bytes(dims, vocab, rows) bytes of scratch (any
+ * contents, for one call at a time), 256-byte aligned.  Other arguments and errors as carryover_logit_rules.
  */
 co_status carryover_probabilities(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,
                                   const void* logits, const int32_t* draft_tok,

@@ -205,7 +205,7 @@ co_status check_project_i8_dims(const co_dims* d) {
     return CO_ERR_UNSUPPORTED;
   const int64_t n_kv = 2ll * d->num_layers * d->num_kv_heads * d->head_dim;
   const int64_t rows = static_cast<int64_t>(d->num_seqs) * d->block;
-  if (rows > kMaxSideI8 || n_kv > kMaxSideI8 || rows * n_kv >= int64_t{1} << 32 ||
+  if (rows > kMaxRowsI8 || n_kv > kMaxSideI8 || rows * n_kv >= int64_t{1} << 32 ||
       rows * d->model_dim >= int64_t{1} << 32)
     return CO_ERR_UNSUPPORTED;
   return CO_OK;
@@ -226,7 +226,7 @@ co_status check_matmul_i8(int32_t m, int32_t n, int32_t k) {
 // Sizes of the logits' calls: dims are already checked.
 co_status check_logits(const co_dims* d, int32_t vocab, int32_t rows, int32_t dtype) {
   if (rows < 1 || rows > static_cast<int64_t>(d->block) + 1) return CO_ERR_INVALID_ARG;
-  if (vocab < 1 || d->block > 1024 || !dtype_ok(dtype) ||
+  if (vocab < 1 || vocab > kMaxVocab || d->block > 1024 || !dtype_ok(dtype) ||
       static_cast<int64_t>(d->num_seqs) * rows > (int64_t{1} << 40) / vocab)
     return CO_ERR_UNSUPPORTED;
   return plan_logits(d->num_seqs, rows, vocab, num_cus(), true).workgroups < kMaxGrid &&
@@ -991,7 +991,7 @@ co_status carryover_round_kv8(const co_dims* dims, const co_weights* w, const vo
 co_status carryover_quantize_i8(int32_t num_rows, int32_t num_cols, int32_t dtype, const void* x,
                                 int8_t* codes, float* scale, hipStream_t stream) {
   if (num_rows < 0 || num_cols < 1) return CO_ERR_INVALID_ARG;
-  if (num_rows > kMaxSideI8 || num_cols % 64 || !dtype_ok(dtype)) return CO_ERR_UNSUPPORTED;
+  if (num_rows > kMaxRowsI8 || num_cols % 64 || !dtype_ok(dtype)) return CO_ERR_UNSUPPORTED;
   if (!x || !codes || !scale || !aligned(x, 16) || !aligned(codes, 16) || !aligned(scale, 4))
     return CO_ERR_INVALID_ARG;
   clear_stale_error();
@@ -1070,7 +1070,8 @@ co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t wid
                                  uint16_t* seen, int32_t* status, hipStream_t stream) {
   co_status s = check_dims(dims);
   if (s != CO_OK) return s;
-  if (vocab < 1 || count_workgroups(dims->num_seqs, vocab) >= kMaxGrid) return CO_ERR_UNSUPPORTED;
+  if (vocab < 1 || vocab > kMaxVocab || count_workgroups(dims->num_seqs, vocab) >= kMaxGrid)
+    return CO_ERR_UNSUPPORTED;
   if (width < 0 || !tokens || !seen || !status || !aligned(tokens, 4) || !aligned(len, 4) ||
       !aligned(seen, 2) || !aligned(status, 4) || (flags & ~(CO_COUNT_PROMPT | CO_COUNT_FRESH)))
     return CO_ERR_INVALID_ARG;

@@ -265,7 +265,9 @@ struct StoreArgs {
 // Products of 8-bit integers with a scale for each row of both operands.
 constexpr int kMaxSumI8 = 131008;         // of codes from -128 on: the sum fits 32 bits
 constexpr int kMaxSideI8 = (1 << 24) - 1; // rows of an operand
-constexpr int64_t kMaxGrid = 1 << 23;     // workgroups of up to 511 threads in one launch
+constexpr int kMaxRowsI8 = (1 << 22) - 1; // rows to quantise, up to 1024 threads each
+constexpr int64_t kMaxGrid = 1 << 23;     // fewer workgroups of up to 512 threads in one launch
+constexpr int kMaxVocab = 1 << 30;        // tokens (tiles of them are counted in 32 bits)
 
 struct MatmulI8Args {
   int M, N, K, dtype;                     // dtype of out

@@ -410,8 +410,7 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   auto each_special = [&](int from, int to, auto&& f) {
     for (int i0 = from + wave * 64; i0 < to; i0 += NT) {
       const bool on = i0 + lane < n;
-      Entry e{};
-      if (on) e = entry(i0 + lane);
+      const Entry e = entry(min(i0 + lane, n - 1));   // (by all lanes: it reads across them)
       T x[kRowsMax];
       uint32_t allowed[kRowsMax];
 #pragma unroll
@@ -529,111 +528,111 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
       if (phase == 1) break;
     }
 #pragma unroll 1
-  for (int r = 0; r < nr; ++r) {
-    if (r + 1 < nr) {
-      load(r + 1, next);
-      load_mask(r + 1, next);
-    }
-    T* out = static_cast<T*>(a.out) + (row0 + r) * V;
-    float* probs = a.probs + (row0 + r) * V;
-    if constexpr (KIND == kRules) {
-      // what is not special is forbidden or stays as it is (where it is, in place)
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        if (!full(c)) continue;
-        const uint32_t allowed = (cur.allowed[c] | ~plain[c]) & 0xFF;
-        if (allowed == 0xFF && out == logits + static_cast<int64_t>(r) * V) continue;
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) cur.x[c].x[e] = allowed >> e & 1 ? cur.x[c].x[e] : kLowest<T>;
-        cur.x[c].store(out + vec(c));
+    for (int r = 0; r < nr; ++r) {
+      if (r + 1 < nr) {
+        load(r + 1, next);
+        load_mask(r + 1, next);
       }
-    } else {
-      float y[C][kVec], top = kNone;
-      int where = kNowhere;
+      T* out = static_cast<T*>(a.out) + (row0 + r) * V;
+      float* probs = a.probs + (row0 + r) * V;
+      if constexpr (KIND == kRules) {
+        // what is not special is forbidden or stays as it is (where it is, in place)
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        if constexpr (sizeof(T) == 2) {
-          typedef uint16_t plain8 __attribute__((ext_vector_type(8)));
-          typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-          const u32x4 x = __builtin_bit_cast(u32x4, static_cast<plain8>(cur.x[c].x));
+        for (int c = 0; c < C; ++c) {
+          if (!full(c)) continue;
+          const uint32_t allowed = (cur.allowed[c] | ~plain[c]) & 0xFF;
+          if (allowed == 0xFF && out == logits + static_cast<int64_t>(r) * V) continue;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const uint32_t z = masked2(x[q], pairs[c][q]);
-            y[c][2 * q] = __uint_as_float(z << 16);
-            y[c][2 * q + 1] = __uint_as_float(z & 0xFFFF0000u);
+          for (int e = 0; e < kVec; ++e) cur.x[c].x[e] = allowed >> e & 1 ? cur.x[c].x[e] : kLowest<T>;
+          cur.x[c].store(out + vec(c));
+        }
+      } else {
+        float y[C][kVec], top = kNone;
+        int where = kNowhere;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          if constexpr (sizeof(T) == 2) {
+            typedef uint16_t plain8 __attribute__((ext_vector_type(8)));
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+            const u32x4 x = __builtin_bit_cast(u32x4, static_cast<plain8>(cur.x[c].x));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const uint32_t z = masked2(x[q], pairs[c][q]);
+              y[c][2 * q] = __uint_as_float(z << 16);
+              y[c][2 * q + 1] = __uint_as_float(z & 0xFFFF0000u);
+            }
+            if (mask_of(r) != -1) {
+#pragma unroll
+              for (int e = 0; e < kVec; ++e) y[c][e] = masked(y[c][e], cur.allowed[c], e);
+            }
+          } else {
+            const uint32_t allowed = vectors ? cur.allowed[c] & plain[c] : 0;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) y[c][e] = widen(cur.x[c].x[e]);
+            if (__any(allowed != 0xFF)) {
+#pragma unroll
+              for (int e = 0; e < kVec; ++e) y[c][e] = masked(y[c][e], allowed, e);
+            }
           }
-          if (mask_of(r) != -1) {
+          if constexpr (KIND == kProbs) {
+            shares(whole[r], y[c], vec(c), k, greedy);
+            if (full(c)) store8(probs + vec(c), y[c]);
+          } else {
+            float most = y[c][0];
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) y[c][e] = masked(y[c][e], cur.allowed[c], e);
-          }
-        } else {
-          const uint32_t allowed = vectors ? cur.allowed[c] & plain[c] : 0;
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) y[c][e] = widen(cur.x[c].x[e]);
-          if (__any(allowed != 0xFF)) {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) y[c][e] = masked(y[c][e], allowed, e);
+            for (int e = 1; e < kVec; ++e) most = fmaxf(most, y[c][e]);
+            where = most > top ? vec(c) : where;
+            top = fmaxf(top, most);
           }
         }
-        if constexpr (KIND == kProbs) {
-          shares(whole[r], y[c], vec(c), k, greedy);
-          if (full(c)) store8(probs + vec(c), y[c]);
-        } else {
-          float most = y[c][0];
-#pragma unroll
-          for (int e = 1; e < kVec; ++e) most = fmaxf(most, y[c][e]);
-          where = most > top ? vec(c) : where;
-          top = fmaxf(top, most);
-        }
-      }
-      if constexpr (KIND != kProbs) {
-        const Part p = ones[r * kWaves + wave];
-        Part w;   // the wavefront's
-        w.m = fmaxf(wave_max_f(top), p.m);
-        w.l = 0.f;
-        if (__builtin_amdgcn_readfirstlane(w.m > kNone)) {
-          float sum = 0.f;
-#pragma unroll
-          for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) sum += exp2_fast((y[c][e] - w.m) * k);
-          if (sum != sum) {   // a NaN, or infinities, which count 1 each
-            sum = 0.f;
+        if constexpr (KIND != kProbs) {
+          const Part p = ones[r * kWaves + wave];
+          Part w;   // the wavefront's
+          w.m = fmaxf(wave_max_f(top), p.m);
+          w.l = 0.f;
+          if (__builtin_amdgcn_readfirstlane(w.m > kNone)) {
+            float sum = 0.f;
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
-              for (int e = 0; e < kVec; ++e)
-                if (y[c][e] == y[c][e]) sum += y[c][e] == w.m ? 1.f : exp2_fast((y[c][e] - w.m) * k);
-          }
-          w.l = wave_sum_f(sum);
-          if (p.m > kNone) w.l += p.m == w.m ? p.l : p.l * exp2_fast((p.m - w.m) * k);
-        }
-        w.vec = wave_min(top == w.m ? where : kNowhere);
-        w.one = p.m == w.m ? p.one : kNowhere;
-        if (lane == 0) parts[r * kWaves + wave] = w;
-        if constexpr (KIND == kWhole) {
-          __syncthreads();
-          const Part q = wave_join(lane < kWaves ? parts[r * kWaves + lane] : nothing, k);
-          const int at = q.m > kNone ? place(q, r) : -1;
-          const Whole all{q.m, q.m > kNone ? 1.f / q.l : 0.f, at};
-          if (tid == 0) {
-            whole[r] = all;
-            if (a.top) a.top[row0 + r] = at;
-          }
+              for (int e = 0; e < kVec; ++e) sum += exp2_fast((y[c][e] - w.m) * k);
+            if (sum != sum) {   // a NaN, or infinities, which count 1 each
+              sum = 0.f;
 #pragma unroll
-          for (int c = 0; c < C; ++c) {
-            if (!full(c)) continue;
-            shares(all, y[c], vec(c), k, greedy);
-            store8(probs + vec(c), y[c]);
+              for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e)
+                  if (y[c][e] == y[c][e]) sum += y[c][e] == w.m ? 1.f : exp2_fast((y[c][e] - w.m) * k);
+            }
+            w.l = wave_sum_f(sum);
+            if (p.m > kNone) w.l += p.m == w.m ? p.l : p.l * exp2_fast((p.m - w.m) * k);
+          }
+          w.vec = wave_min(top == w.m ? where : kNowhere);
+          w.one = p.m == w.m ? p.one : kNowhere;
+          if (lane == 0) parts[r * kWaves + wave] = w;
+          if constexpr (KIND == kWhole) {
+            __syncthreads();
+            const Part q = wave_join(lane < kWaves ? parts[r * kWaves + lane] : nothing, k);
+            const int at = q.m > kNone ? place(q, r) : -1;
+            const Whole all{q.m, q.m > kNone ? 1.f / q.l : 0.f, at};
+            if (tid == 0) {
+              whole[r] = all;
+              if (a.top) a.top[row0 + r] = at;
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+              if (!full(c)) continue;
+              shares(all, y[c], vec(c), k, greedy);
+              store8(probs + vec(c), y[c]);
+            }
           }
         }
       }
+      if constexpr (KIND == kRules || KIND == kProbs) store_special(r);
+      cur = next;
     }
-    if constexpr (KIND == kRules || KIND == kProbs) store_special(r);
-    cur = next;
-  }
-  __syncthreads();
-  if ((KIND == kRules || KIND == kProbs) && n <= NT) break;
+    __syncthreads();
+    if ((KIND == kRules || KIND == kProbs) && n <= NT) break;
   }
 
   if constexpr (KIND == kStats) {

@@ -743,11 +743,13 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
     const int64_t tiles = (static_cast<int64_t>(N) + 63) / 64;
     int split = 1;
     while (tiles * split < 2 * num_cus && K / (split * 2) >= 2 * kUnit) split *= 2;
-    // us, few rows by register and by stream: 16 x 2048 x 4096 6.9, 9.6; 16 x 10240 x 4096
-    // 14.7, 15.2; 16 x 4096 x 20480 26.0, 22.6; 16 x 256 x 20480 20.6, 14.5; unsplit 17 x 128000
-    // x 4096 127, 104.  The stream against 64-row tiles: 64 x 128000 x 4096 130, 113; 64 x 4096 x
-    // 20480 25.6, 29.3.
-    const bool few = force < 0 ? split > 1 && K <= 8192 : force == kFew;
+    // A split stream's parts are added up by a second launch; the registers' kernel has none,
+    // but reads the rows' codes once for 16 columns.  us, by registers and by stream:
+    // 16 x 2048 x 4096 6.9, 9.6; 16 x 10240 x 4096 14.7, 15.2; 12 x 4339 x 7680 16.2, 13.3;
+    // 16 x 4096 x 20480 26.0, 22.6; 4 x 1218 x 16448 11.5, 15.0; 1 x 20 x 11584 7.7, 8.2;
+    // 1 x 155 x 704 3.7, 4.8; unsplit 17 x 128000 x 4096 127, 104.  The stream against 64-row tiles: unsplit
+    // 64 x 128000 x 4096 130, 113; split 64 x 4096 x 20480 25.6, 29.3; 39 x 468 x 3136 8.6, 10.2.
+    const bool few = force < 0 ? tiles < num_cus && static_cast<int64_t>(K) * M <= 81920 : force == kFew;
     if (M <= kFewRows && few) {
       p.variant = kFew;
       // columns of a workgroup: as many (the rows' codes are read once for them) as leave
@@ -760,7 +762,7 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
       if (p.cols * (M > 16 ? 2 : 1) > 2 && p.waves == 16) p.waves = 8;
       return p;
     }
-    if (force < 0 ? M <= kFewRows || (split > 1 && K > 8192) : force == kStream) {
+    if (force < 0 ? M <= kFewRows || split > 1 : force == kStream) {
       p.variant = kStream;
       p.k_per_split = ((K + split - 1) / split + kUnit - 1) / kUnit * kUnit;
       p.splits = (K + p.k_per_split - 1) / p.k_per_split;
@@ -779,7 +781,7 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
       if (s > 1 && (kps < 512 || (K + kps - 1) / kps != s || static_cast<int64_t>(M) * N * s > (1ll << 28)))
         continue;
       const int64_t wgs = tiles * s, waves = (wgs + num_cus - 1) / num_cus;
-      constexpr double kEff[kVariants] = {1.0, 0.8, 0.85, 0.95, 0.7, 0.6, 0.45};
+      constexpr double kEff[kVariants] = {1.0, 0.8, 0.85, 0.95, 0.7, 0.6, 0.55};
       const double t_mfma = static_cast<double>(waves) * kBM[v] * kBN[v] * (kps + 256.0) * 2.0 / (8.0e12 * kEff[v]);
       const double t_mem = static_cast<double>(tm) * N * K / 8.0e12 + static_cast<double>(N) * K / 8e12;
       const double t_part = s > 1 ? static_cast<double>(s) * M * N * 8.0 / 4.0e12 + 3e-6 : 0.0;

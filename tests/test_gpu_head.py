@@ -493,6 +493,11 @@ CASES = [
     (2, 3, 4, 32001, "bf16", True, True, 50, 0.5),
     (9, 4, 5, 9001, "f32", True, True, 50, 0.5),
     (1, 40, 41, 130, "bf16", True, True, 4, 0.2),
+    (1, 100, 101, 40, "f32", True, True, 4, 0.2),          # more proposals than lanes
+    (2, 100, 101, 17000, "bf16", True, True, 0, 0.0),
+    (2, 3, 4, 600, "f32", True, True, 1500, 0.3),          # more biases of a tile than are held
+    (1, 1, 2, 20000, "bf16", False, True, 9000, 0.0),
+    (3, 2, 3, 7, "f32", True, True, 3, 0.5),               # less than a vector
     (1, 2, 3, 131072, "bf16", True, True, 100, 0.3),
     (300, 2, 3, 33, "f32", True, True, 3, 0.3),
     (200, 3, 4, 8195, "bf16", True, True, 3, 0.3),
@@ -530,6 +535,27 @@ def test_probabilities_without_rules_or_temperature():
     a.check_probs(p, top, rules=False, temperature=False)
     q, none = a.probs(rules=False, temperature=False, top=False)
     assert none is None and torch.equal(p, q)
+
+
+def test_results_repeat_bit_for_bit():
+    a = Logits(5, 7, 8, 20011, "bf16", 77, bias=40, masked=0.5)
+    p, top = a.probs()
+    out = a.apply()
+    for _ in range(3):
+        q, t = a.probs()
+        assert torch.equal(p, q) and torch.equal(top, t) and torch.equal(out, a.apply())
+
+
+def test_counts_stop_at_their_largest():
+    """A word that is full stays full in a window, and its prompt bit stays clear."""
+    a = Logits(1, 4, 5, 64, "f32", 3, penalties=True)
+    a.seen[:] = 0
+    a.seen[0, 5], a.seen[0, 6] = 32767, 0x8000 | 32766
+    a.draft[:] = [[5, 6, 6, 5]]
+    a.pen = [np.array([1.5]), np.array([0.25]), np.array([2.0 ** -10])]
+    out = a.apply()
+    a.check(out)
+    assert float(out[0, 4, 5]) == float(np.float32(a.row(0, 4)[0][5]))
 
 
 def test_equal_logits_have_equal_probabilities_and_the_lowest_token_wins():

@@ -128,7 +128,7 @@ def dims(S=2, B=16, **kw):
     (-1, 64, "bf16", {}, co.CO_ERR_INVALID_ARG),
     (1, 0, "bf16", {}, co.CO_ERR_INVALID_ARG),
     (1, 65, "bf16", {}, co.CO_ERR_UNSUPPORTED),
-    (1 << 24, 64, "bf16", {}, co.CO_ERR_UNSUPPORTED),
+    (1 << 22, 64, "bf16", {}, co.CO_ERR_UNSUPPORTED),
     (1, 64, 7, {}, co.CO_ERR_UNSUPPORTED),
     (1, 64, "f32", dict(x=0), co.CO_ERR_INVALID_ARG),
     (1, 64, "f32", dict(x=FAKE + 4), co.CO_ERR_INVALID_ARG),
@@ -197,7 +197,8 @@ def _weights_i8(**kw):
     (dict(Dcat=131072), {}, co.CO_ERR_UNSUPPORTED),
     (dict(d=131072), {}, co.CO_ERR_UNSUPPORTED),
     (dict(d=16448), dict(z_norm=FAKE), co.CO_ERR_UNSUPPORTED),
-    (dict(S=1 << 20), {}, co.CO_ERR_UNSUPPORTED),
+    (dict(S=1 << 18), {}, co.CO_ERR_UNSUPPORTED),
+    (dict(S=1 << 16, d=4096), {}, co.CO_ERR_UNSUPPORTED),
     ({}, dict(w_f=0), co.CO_ERR_INVALID_ARG),
     ({}, dict(w_f_scale=0), co.CO_ERR_INVALID_ARG),
     ({}, dict(w_kv=FAKE + 8), co.CO_ERR_INVALID_ARG),
@@ -242,6 +243,7 @@ def test_project_workspace_is_checked():
     (dict(status=0), co.CO_ERR_INVALID_ARG),
     (dict(dims=dims(B=0)), co.CO_ERR_INVALID_ARG),
     (dict(dims=dims(S=1 << 20), vocab=1 << 20), co.CO_ERR_UNSUPPORTED),
+    (dict(dims=dims(S=1), vocab=(1 << 30) + 1), co.CO_ERR_UNSUPPORTED),
 ])
 def test_count_refusals(kw, code):
     p = dict(dims=dims(), vocab=1000, width=16, tokens=FAKE, lens=None, flags=0, seen=FAKE, status=FAKE)
@@ -285,6 +287,7 @@ def _raw_rules(**kw):
     (dict(status=0), co.CO_ERR_INVALID_ARG),
     (dict(dims=dims(B=1025)), co.CO_ERR_UNSUPPORTED),
     (dict(dims=dims(S=1 << 20), vocab=1 << 20), co.CO_ERR_UNSUPPORTED),
+    (dict(dims=dims(S=1), vocab=(1 << 30) + 1), co.CO_ERR_UNSUPPORTED),
 ] + [(dict(rules=_raw_rules(**r)), c) for r, c in RULE_CASES] + [
     (dict(rules=_raw_rules(num_bias=-1)), co.CO_ERR_INVALID_ARG),
     (dict(rules=_raw_rules(num_masks=-1)), co.CO_ERR_INVALID_ARG),
