@@ -781,8 +781,9 @@ co_status carryover_read_status(const co_state* state, int32_t* host_out, hipStr
  *                                   attention kernel
  *   CO_TUNE_ATTN_GROUP_SPLIT_TILES  committed tiles per share, grouped-prefix
  *                                   attention
- *   CO_TUNE_MATMUL_I8               8-bit product: tile variant 0..6 at any size, or 7: the
- *                                   kernel for up to 32 rows, 8: the one for up to 64, where they apply
+ *   CO_TUNE_MATMUL_I8               8-bit product: tile variant 0..7 at any size; 8: the
+ *                                   kernel for up to 32 rows, 9: the one for up to 64,
+ *                                   where they apply
  * Returns CO_ERR_INVALID_ARG for an unknown knob.  Workspace sizes follow the
  * overrides in force when carryover_workspace_bytes is called.
  */

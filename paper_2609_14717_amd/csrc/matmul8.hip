@@ -653,9 +653,9 @@ __global__ __launch_bounds__(512) void sum_parts_i8_kernel(MatmulI8Args g, int t
 }
 
 // Tile variants of the wide kernel; kFew: the kernel for few rows.
-constexpr int kVariants = 7, kFew = kVariants, kStream = kVariants + 1;
-constexpr int kBM[kVariants] = {256, 256, 128, 192, 128, 64, 64};
-constexpr int kBN[kVariants] = {256, 128, 256, 256, 128, 256, 128};
+constexpr int kVariants = 8, kFew = kVariants, kStream = kVariants + 1;
+constexpr int kBM[kVariants] = {256, 256, 128, 192, 128, 64, 64, 192};
+constexpr int kBN[kVariants] = {256, 128, 256, 256, 128, 256, 128, 128};
 
 template <int TMW, int TNW, int NS, typename T>
 void launch_wide_t(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
@@ -676,7 +676,8 @@ hipError_t launch_wide(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t
     case 3: launch_wide_t<3, 2, 2, T>(g, p, stream); break;
     case 4: launch_wide_t<2, 1, 4, T>(g, p, stream); break;
     case 5: launch_wide_t<1, 2, 3, T>(g, p, stream); break;
-    default: launch_wide_t<1, 1, 4, T>(g, p, stream); break;
+    case 6: launch_wide_t<1, 1, 4, T>(g, p, stream); break;
+    default: launch_wide_t<3, 1, 3, T>(g, p, stream); break;
   }
   return hipGetLastError();
 }
@@ -781,7 +782,7 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
       if (s > 1 && (kps < 512 || (K + kps - 1) / kps != s || static_cast<int64_t>(M) * N * s > (1ll << 28)))
         continue;
       const int64_t wgs = tiles * s, waves = (wgs + num_cus - 1) / num_cus;
-      constexpr double kEff[kVariants] = {1.0, 0.8, 0.85, 0.95, 0.7, 0.6, 0.55};
+      constexpr double kEff[kVariants] = {1.0, 0.8, 0.85, 0.95, 0.7, 0.6, 0.55, 0.78};
       const double t_mfma = static_cast<double>(waves) * kBM[v] * kBN[v] * (kps + 256.0) * 2.0 / (8.0e12 * kEff[v]);
       const double t_mem = static_cast<double>(tm) * N * K / 8.0e12 + static_cast<double>(N) * K / 8e12;
       const double t_part = s > 1 ? static_cast<double>(s) * M * N * 8.0 / 4.0e12 + 3e-6 : 0.0;

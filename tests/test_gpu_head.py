@@ -142,7 +142,7 @@ def test_product(m, n, k, dtype, bias):
     check_product(*ops, dtype, product(*ops, dtype), f"{m} x {n} x {k}")
 
 
-@pytest.mark.parametrize("variant", range(9))
+@pytest.mark.parametrize("variant", range(10))
 def test_product_variants(variant, tune):
     """Every tile at sizes that end inside it, with one stage of K, few and many, with and
     without a split of K."""
