@@ -468,15 +468,52 @@ __device__ __forceinline__ void tile_of(int r, int tiles_m, int tiles_n, int* m0
   *n0 = rg / gsz * BN;
 }
 
-template <int TMW, int TNW, int NS, typename T>
-__global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, int tiles_m,
+// Where a tile's results go: plain rows, or (X = KvDest) the K/V rows of the projection, each
+// 32 columns of a tile then being 16 rotation pairs of a head: their low halves, then their
+// high ones, so that a lane holds both of a pair in registers q and q + 2.
+struct PlainRows {};
+
+template <typename X>
+__device__ __forceinline__ int column(const X& x, int n0, int c) {
+  if constexpr (sizeof(X) > 1) {
+    const int t = c & ~31, j = c & 31;
+    return n0 + t / x.hd * x.hd + t % x.hd / 2 + (j & 15) + (j >> 4) * (x.hd / 2);
+  }
+  return n0 + c;
+}
+
+// A wavefront's 32 x 32 results of the K/V product: scaled, rotated and stored.
+__device__ __forceinline__ void put_pairs(const MatmulI8Args& g, const KvDest& e, const i32x16& acc, int row,
+                                          float sa, int n0, int cb, int lane, const float* col_scale,
+                                          const double* inv_tab) {
+  const int seg = n0 / e.hd + cb / e.hd;
+  if (row >= g.M || seg * e.hd >= g.N) return;
+  const int32_t dst = e.row_dst[row];
+  if (dst == kSkip) return;
+  const int pos = e.row_pos[row];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int c = 8 * q + 4 * (lane >> 5);
+    float lo[4], hi[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lo[i] = scaled(acc[4 * q + i], sa, col_scale[c + i]);
+      hi[i] = scaled(acc[4 * q + 8 + i], sa, col_scale[c + 16 + i]);
+    }
+    kv_store<uint16_t, 4>(e, row, dst, pos, seg, cb % e.hd / 2 + c, lo, hi, inv_tab);
+  }
+}
+
+template <int TMW, int TNW, int NS, typename T, typename X>
+__global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, X x, int tiles_m,
                                                                 int tiles_n, int k_per_split) {
   constexpr int BM = 64 * TMW, BN = 128 * TNW, ROWS = BM + BN, STAGE = ROWS * kStageK;
   constexpr int LPW = ROWS / 64;                         // 1 KiB loads of a wavefront, a stage
   static_assert(LPW * (NS - 1) < 64 && NS >= 2 && NS <= 4, "vmcnt");
-  static_assert(NS * STAGE + 8 * BN <= 160 * 1024, "LDS");
+  static_assert(NS * STAGE + 8 * BN + 512 <= 160 * 1024, "LDS");
   __shared__ __align__(16) unsigned char smem[NS * STAGE];
   __shared__ __align__(16) float col_scale[BN], col_bias[BN];
+  __shared__ double inv_tab[sizeof(X) > 1 ? 64 : 1];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -498,7 +535,7 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
     const int row = (LPW * wave + j) * 8 + lane / 8;
     const int chunk = (lane & 7) ^ ((row >> 1) & 7);
     const int8_t* base = row < BM ? g.A + static_cast<int64_t>(min(m0 + row, g.M - 1)) * g.K
-                                  : g.W + static_cast<int64_t>(min(n0 + row - BM, g.N - 1)) * g.K;
+                                  : g.W + static_cast<int64_t>(min(column(x, n0, row - BM), g.N - 1)) * g.K;
     src[j] = base + kbeg + chunk * 16;
   }
   // chunks past a half stage are not read: they take the half before
@@ -555,10 +592,12 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
   };
 
   for (int c = tid; c < BN; c += 512) {   // (read behind the main loop's barriers)
-    const int col = min(n0 + c, g.N - 1);
+    const int col = min(column(x, n0, c), g.N - 1);
     col_scale[c] = g.w_scale[col];
     col_bias[c] = g.bias ? g.bias[col] : 0.f;
   }
+  if constexpr (sizeof(X) > 1)
+    if (tid < x.hd / 2) inv_tab[tid] = rope_table<uint16_t>(x, tid);
 #pragma unroll
   for (int s = 0; s < NS; ++s)
     if (s < nk) issue(s);
@@ -613,27 +652,33 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
 #pragma unroll
     for (int b = 0; b < TNW; ++b) {
       const int cb = (wn * TNW + b) * 32;
-      put_tile<T>(g, acc[a][b], row, sa, n0 + cb, lane, col_scale + cb, col_bias + cb);
+      if constexpr (sizeof(X) > 1)
+        put_pairs(g, x, acc[a][b], row, sa, n0, cb, lane, col_scale + cb, inv_tab);
+      else
+        put_tile<T>(g, acc[a][b], row, sa, n0 + cb, lane, col_scale + cb, col_bias + cb);
     }
   }
 }
 
 // The parts of K of one 32 x 32 tile for each wavefront, added up, scaled and stored.
-template <int TMW, int TNW, typename T>
-__global__ __launch_bounds__(512) void sum_parts_i8_kernel(MatmulI8Args g, int tiles_m, int tiles_n,
-                                                           int splits) {
+template <int TMW, int TNW, typename T, typename X>
+__global__ __launch_bounds__(512) void sum_parts_i8_kernel(MatmulI8Args g, X x, int tiles_m,
+                                                           int tiles_n, int splits) {
   constexpr int BM = 64 * TMW, BN = 128 * TNW;
   __shared__ __align__(16) float col_scale[BN], col_bias[BN];
+  __shared__ double inv_tab[sizeof(X) > 1 ? 64 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 2, wn = wave & 3;
   const int frag = blockIdx.x % (TMW * TNW), r0 = blockIdx.x / (TMW * TNW);
   int m0, n0;
   tile_of<BM, BN>(r0, tiles_m, tiles_n, &m0, &n0);
   for (int c = tid; c < BN; c += 512) {
-    const int col = min(n0 + c, g.N - 1);
+    const int col = min(column(x, n0, c), g.N - 1);
     col_scale[c] = g.w_scale[col];
     col_bias[c] = g.bias ? g.bias[col] : 0.f;
   }
+  if constexpr (sizeof(X) > 1)
+    if (tid < x.hd / 2) inv_tab[tid] = rope_table<uint16_t>(x, tid);
   const int64_t step = static_cast<int64_t>(tiles_m) * tiles_n * (BM * BN / 4);
   const i32x4* part = reinterpret_cast<const i32x4*>(g.ws) + static_cast<int64_t>(r0) * (BM * BN / 4) +
                       frag * 4 * 512 + tid;
@@ -649,7 +694,9 @@ __global__ __launch_bounds__(512) void sum_parts_i8_kernel(MatmulI8Args g, int t
   const int a = frag / TNW, b = frag % TNW;
   const int row = m0 + (wm * TMW + a) * 32 + (lane & 31);
   const int cb = (wn * TNW + b) * 32;
-  put_tile<T>(g, acc, row, row < g.M ? g.a_scale[row] : 0.f, n0 + cb, lane, col_scale + cb, col_bias + cb);
+  const float sa = row < g.M ? g.a_scale[row] : 0.f;
+  if constexpr (sizeof(X) > 1) put_pairs(g, x, acc, row, sa, n0, cb, lane, col_scale + cb, inv_tab);
+  else put_tile<T>(g, acc, row, sa, n0 + cb, lane, col_scale + cb, col_bias + cb);
 }
 
 // Tile variants of the wide kernel; kFew: the kernel for few rows.
@@ -657,27 +704,27 @@ constexpr int kVariants = 8, kFew = kVariants, kStream = kVariants + 1;
 constexpr int kBM[kVariants] = {256, 256, 128, 192, 128, 64, 64, 192};
 constexpr int kBN[kVariants] = {256, 128, 256, 256, 128, 256, 128, 128};
 
-template <int TMW, int TNW, int NS, typename T>
-void launch_wide_t(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
+template <int TMW, int TNW, int NS, typename T, typename X>
+void launch_wide_t(const MatmulI8Args& g, const X& x, const MatmulI8Plan& p, hipStream_t stream) {
   const int tm = (g.M + 64 * TMW - 1) / (64 * TMW), tn = (g.N + 128 * TNW - 1) / (128 * TNW);
-  hipLaunchKernelGGL((matmul_i8_wide_kernel<TMW, TNW, NS, T>), dim3(static_cast<unsigned>(p.workgroups)),
-                     dim3(512), 0, stream, g, tm, tn, p.k_per_split);
+  hipLaunchKernelGGL((matmul_i8_wide_kernel<TMW, TNW, NS, T, X>), dim3(static_cast<unsigned>(p.workgroups)),
+                     dim3(512), 0, stream, g, x, tm, tn, p.k_per_split);
   if (p.splits > 1)
-    hipLaunchKernelGGL((sum_parts_i8_kernel<TMW, TNW, T>), dim3(static_cast<unsigned>(tm) * tn * TMW * TNW),
-                       dim3(512), 0, stream, g, tm, tn, p.splits);
+    hipLaunchKernelGGL((sum_parts_i8_kernel<TMW, TNW, T, X>), dim3(static_cast<unsigned>(tm) * tn * TMW * TNW),
+                       dim3(512), 0, stream, g, x, tm, tn, p.splits);
 }
 
-template <typename T>
-hipError_t launch_wide(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
+template <typename T, typename X>
+hipError_t launch_wide(const MatmulI8Args& g, const X& x, const MatmulI8Plan& p, hipStream_t stream) {
   switch (p.variant) {
-    case 0: launch_wide_t<4, 2, 2, T>(g, p, stream); break;
-    case 1: launch_wide_t<4, 1, 3, T>(g, p, stream); break;
-    case 2: launch_wide_t<2, 2, 3, T>(g, p, stream); break;
-    case 3: launch_wide_t<3, 2, 2, T>(g, p, stream); break;
-    case 4: launch_wide_t<2, 1, 4, T>(g, p, stream); break;
-    case 5: launch_wide_t<1, 2, 3, T>(g, p, stream); break;
-    case 6: launch_wide_t<1, 1, 4, T>(g, p, stream); break;
-    default: launch_wide_t<3, 1, 3, T>(g, p, stream); break;
+    case 0: launch_wide_t<4, 2, 2, T>(g, x, p, stream); break;
+    case 1: launch_wide_t<4, 1, 3, T>(g, x, p, stream); break;
+    case 2: launch_wide_t<2, 2, 3, T>(g, x, p, stream); break;
+    case 3: launch_wide_t<3, 2, 2, T>(g, x, p, stream); break;
+    case 4: launch_wide_t<2, 1, 4, T>(g, x, p, stream); break;
+    case 5: launch_wide_t<1, 2, 3, T>(g, x, p, stream); break;
+    case 6: launch_wide_t<1, 1, 4, T>(g, x, p, stream); break;
+    default: launch_wide_t<3, 1, 3, T>(g, x, p, stream); break;
   }
   return hipGetLastError();
 }
@@ -749,8 +796,10 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
     // 16 x 2048 x 4096 6.9, 9.6; 16 x 10240 x 4096 14.7, 15.2; 12 x 4339 x 7680 16.2, 13.3;
     // 16 x 4096 x 20480 26.0, 22.6; 4 x 1218 x 16448 11.5, 15.0; 1 x 20 x 11584 7.7, 8.2;
     // 1 x 155 x 704 3.7, 4.8; unsplit 17 x 128000 x 4096 127, 104.  The stream against 64-row tiles: unsplit
-    // 64 x 128000 x 4096 130, 113; split 64 x 4096 x 20480 25.6, 29.3; 39 x 468 x 3136 8.6, 10.2.
-    const bool few = force < 0 ? tiles < num_cus && static_cast<int64_t>(K) * M <= 81920 : force == kFew;
+    // 64 x 128000 x 4096 130, 113; split 64 x 4096 x 20480 25.6, 29.3; 39 x 468 x 3136 8.6, 10.2;
+    // 60 x 20911 x 11264 70, 56.
+    const bool few = force < 0 ? (split > 1 || tiles < num_cus) && static_cast<int64_t>(K) * M <= 81920
+                               : force == kFew;
     if (M <= kFewRows && few) {
       p.variant = kFew;
       // columns of a workgroup: as many (the rows' codes are read once for them) as leave
@@ -763,7 +812,7 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
       if (p.cols * (M > 16 ? 2 : 1) > 2 && p.waves == 16) p.waves = 8;
       return p;
     }
-    if (force < 0 ? M <= kFewRows || split > 1 : force == kStream) {
+    if (force < 0 ? M <= kFewRows || (split > 1 && tiles * 4 <= num_cus) : force == kStream) {
       p.variant = kStream;
       p.k_per_split = ((K + split - 1) / split + kUnit - 1) / kUnit * kUnit;
       p.splits = (K + p.k_per_split - 1) / p.k_per_split;
@@ -809,7 +858,8 @@ static hipError_t launch_product(const MatmulI8Args& g, const MatmulI8Plan& p, b
                                     : launch_stream<float>(g, p, keep_parts, stream);
   if (p.variant == kFew)
     return g.dtype == CO_DTYPE_BF16 ? launch_few<uint16_t>(g, p, stream) : launch_few<float>(g, p, stream);
-  return g.dtype == CO_DTYPE_BF16 ? launch_wide<uint16_t>(g, p, stream) : launch_wide<float>(g, p, stream);
+  return g.dtype == CO_DTYPE_BF16 ? launch_wide<uint16_t>(g, PlainRows{}, p, stream)
+                                  : launch_wide<float>(g, PlainRows{}, p, stream);
 }
 
 hipError_t launch_matmul_i8(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
@@ -1026,6 +1076,14 @@ hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t st
     hipLaunchKernelGGL((z_codes_kernel<1024, 2>), rows, dim3(1024), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
   else
     hipLaunchKernelGGL((z_codes_kernel<1024, 0>), rows, dim3(1024), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
+  const MatmulI8Plan kv = plan_matmul_i8(a.M, n_kv, a.d, num_cus);
+  if (kv.variant < kFew && a.dst.knorm == nullptr) {   // tiles rotate and store their rows
+    g.N = n_kv;
+    g.K = a.d;
+    g.W = a.wkv;
+    g.w_scale = a.wkv_scale;
+    return launch_wide<float>(g, a.dst, kv, stream);
+  }
   if ((err = product(n_kv, a.d, a.wkv, a.wkv_scale, &p)) != hipSuccess) return err;
   const int per = 1024 / (a.dst.hd / 2);   // rows of a workgroup
   hipLaunchKernelGGL(store_rows_i8_kernel,

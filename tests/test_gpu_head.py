@@ -289,6 +289,18 @@ def test_project(S, B, Dcat, d, L, Hkv, hd, theta, norms):
     check_project(c)
 
 
+@pytest.mark.parametrize("variant", range(10))
+@pytest.mark.parametrize("S,B,Dcat,d,L,Hkv,hd", [(5, 16, 192, 128, 1, 1, 64), (9, 15, 320, 1088, 2, 3, 128),
+                                                  (3, 100, 64, 64, 1, 5, 64), (2, 13, 256, 2112, 1, 1, 128)])
+def test_project_variants(variant, S, B, Dcat, d, L, Hkv, hd, tune):
+    """Every tile of both products, whose last one stores the rows itself, split and unsplit."""
+    print(f"[project i8] variant {variant} S={S} B={B} {Dcat}->{d} L={L} {Hkv}x{hd}", flush=True)
+    tune("matmul_i8", variant)
+    c = project_case(S, B, Dcat, d, L, Hkv, hd, 1e4, variant + d, False)
+    run_project(c)
+    check_project(c)
+
+
 def test_project_without_an_embedding():
     c = project_case(2, 8, 256, 256, 1, 2, 64, 1e4, 9, False, embed=False)
     run_project(c)
