@@ -354,12 +354,13 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   const int upto = wave_scan(own);
   if (lane == 63) listed[wave] = upto;
   __syncthreads();
-  int at = upto - own, n = 0;
+  int start = upto - own, n = 0;   // of this thread's tokens in the list
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    at += w < wave ? listed[w] : 0;
+    start += w < wave ? listed[w] : 0;
     n += listed[w];
   }
+  int at = start;
 #pragma unroll
   for (int c = 0; c < C; ++c)
     for (uint32_t m = special8[c * NT + tid]; m != 0; m &= m - 1)
@@ -493,22 +494,23 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
       if (lane == 0) ones[r * kWaves + wave] = p;
     });
   }
-  // What becomes of the first NT special tokens, kept where their thread stores it from,
-  // behind the vectors of its row (later, the lines that it lies in would be in memory
-  // already, and be fetched to be changed).
   auto result = [&](int r, int v, float x) {
     if constexpr (KIND == kRules) return x;
     float y[1] = {x};
     shares(whole[r], y, v, k, greedy);
     return y[0];
   };
-  const int own_v = (KIND == kRules || KIND == kProbs) && tid < n ? token_of(list[tid]) : 0;
+  // What becomes of the first NT special tokens waits in LDS for the thread that stores the
+  // vectors that hold them, which writes them behind its own stores, row by row (later, the
+  // lines that they lie in would be in memory already, and be fetched to be changed).
+  const int stop = min(start + own, NT);
   auto store_special = [&](int r) {
-    __syncthreads();
-    if (tid >= n) return;
-    const float y = own_special[r * NT + tid];
-    if constexpr (KIND == kRules) store1(static_cast<T*>(a.out) + (row0 + r) * V + own_v, y);
-    else a.probs[(row0 + r) * V + own_v] = y;
+    for (int i = start; i < stop; ++i) {
+      const int v = token_of(list[i]);
+      const float y = own_special[r * NT + i];
+      if constexpr (KIND == kRules) store1(static_cast<T*>(a.out) + (row0 + r) * V + v, y);
+      else a.probs[(row0 + r) * V + v] = y;
+    }
   };
 
   // kRules, kProbs: the first NT special tokens before the rows, the others behind them
@@ -526,6 +528,7 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
         });
       }
       if (phase == 1) break;
+      if (KIND != kWhole) __syncthreads();
     }
 #pragma unroll 1
     for (int r = 0; r < nr; ++r) {
