@@ -747,7 +747,7 @@ hipError_t launch_stream(const MatmulI8Args& g, const MatmulI8Plan& p, bool keep
 template <int MT, int TN, typename T>
 hipError_t launch_few_nw(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(p.workgroups));
-  if constexpr (MT * TN <= 2) {   // (more tiles need more than the 128 registers of sixteen wavefronts)
+  if constexpr (TN == 1) {   // (32 columns: the plan has eight at most)
     if (p.waves == 16) {
       hipLaunchKernelGGL((matmul_i8_few_kernel<MT, TN, 16, T>), grid, dim3(1024), 0, stream, g);
       return hipGetLastError();
@@ -760,14 +760,9 @@ hipError_t launch_few_nw(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream
 
 template <typename T>
 hipError_t launch_few(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
-  if (g.M <= 16) {
-    if (p.cols == 4) return launch_few_nw<1, 4, T>(g, p, stream);
-    if (p.cols == 2) return launch_few_nw<1, 2, T>(g, p, stream);
-    return launch_few_nw<1, 1, T>(g, p, stream);
-  }
-  if (p.cols == 4) return launch_few_nw<2, 4, T>(g, p, stream);
-  if (p.cols == 2) return launch_few_nw<2, 2, T>(g, p, stream);
-  return launch_few_nw<2, 1, T>(g, p, stream);
+  if (g.M <= 16)
+    return p.cols == 2 ? launch_few_nw<1, 2, T>(g, p, stream) : launch_few_nw<1, 1, T>(g, p, stream);
+  return p.cols == 2 ? launch_few_nw<2, 2, T>(g, p, stream) : launch_few_nw<2, 1, T>(g, p, stream);
 }
 
 }  // namespace
@@ -802,14 +797,14 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
                                : force == kFew;
     if (M <= kFewRows && few) {
       p.variant = kFew;
-      // columns of a workgroup: as many (the rows' codes are read once for them) as leave
-      // two workgroups to a compute unit
-      p.cols = N >= 128 * num_cus ? 4 : (N >= 64 * num_cus ? 2 : 1);
+      // columns of a workgroup / 16: two (the rows' codes are read once for both) where that
+      // leaves two workgroups to a compute unit
+      p.cols = N >= 64 * num_cus ? 2 : 1;
       p.workgroups = (N + 16 * p.cols - 1) / (16 * p.cols);
-      // wavefronts: enough of them on the chip, each with a unit of K or more
+      // wavefronts: enough of them on the chip, each with a unit of K or more (32 columns are
+      // two workgroups to a compute unit or more, so eight)
       p.waves = 4;
       while (p.waves < 16 && p.workgroups * p.waves < 16ll * num_cus && K / kUnit > p.waves) p.waves *= 2;
-      if (p.cols * (M > 16 ? 2 : 1) > 2 && p.waves == 16) p.waves = 8;
       return p;
     }
     if (force < 0 ? M <= kFewRows || (split > 1 && tiles * 4 <= num_cus) : force == kStream) {
