@@ -237,7 +237,7 @@ typedef struct co_logit_rules {
                                  both of these are given or NULL                      */
   const uint32_t* mask_bits;  /* [num_masks][ceil(vocab / 32)]: bit v % 32 of word v / 32 set
                                  allows token v; bits past the vocabulary are ignored */
-  int32_t num_bias;
+  int32_t num_bias;           /* 0 to 2^30                                            */
   int32_t num_masks;
 } co_logit_rules;
 
@@ -656,7 +656,7 @@ co_status carryover_round_kv8(const co_dims* dims, const co_weights* w, const vo
  * codes 0, so that every product with it is NaN.  x [num_rows][num_cols] of
  * `dtype` (CO_DTYPE_F32 or CO_DTYPE_BF16) and codes of the same shape, 16-byte
  * aligned; scale fp32 [num_rows].  num_cols: a multiple of 64; num_rows below
- * 2^22 (CO_ERR_UNSUPPORTED otherwise).
+ * 2^22 (CO_ERR_UNSUPPORTED otherwise), 0 does nothing (pointers may be NULL).
  */
 co_status carryover_quantize_i8(int32_t num_rows, int32_t num_cols, int32_t dtype, const void* x,
                                 int8_t* codes, float* scale, hipStream_t stream);
@@ -668,7 +668,8 @@ co_status carryover_quantize_i8(int32_t num_rows, int32_t num_cols, int32_t dtyp
  * result to `dtype`.  a [m][k] and w [n][k] int8 (any codes, -128 too), 16-byte
  * aligned; a_scale fp32 [m], w_scale fp32 [n]; bias fp32 [n] or NULL; out [m][n] of
  * `dtype` (CO_DTYPE_F32 or CO_DTYPE_BF16), 16-byte aligned.  m and n from 0 to 2^24 - 1,
- * k a multiple of 64 from 64 to 131008 (CO_ERR_UNSUPPORTED otherwise).  `ws`:
+ * k a multiple of 64 from 64 to 131008 (CO_ERR_UNSUPPORTED otherwise); pointers
+ * may be NULL where m or n is 0.  `ws`:
  * carryover_matmul_i8_workspace_bytes(m, n, k) bytes of scratch, 256-byte
  * aligned (any contents, for one call at a time; NULL where that is 0).
  */
@@ -705,8 +706,8 @@ co_status carryover_project_kv_i8(const co_dims* dims, const co_weights_i8* w, c
  * dims is used (the rest must still be valid).  Device errors, written to *status:
  * CO_ERR_LENGTH (len outside [0, width]; the sequence stays as it is), CO_ERR_TOKEN
  * (a token >= vocab; it is left out).  Calls on one history must not overlap.
- * Host: vocab from 1 to 2^30, num_seqs * ceil(vocab / 8192) below 2^23
- * (CO_ERR_UNSUPPORTED).
+ * Host: vocab from 1 to 2^30, width from 0 (tokens may then be NULL) to 2^30,
+ * num_seqs * ceil(vocab / 8192) below 2^23 (CO_ERR_UNSUPPORTED).
  */
 enum { CO_COUNT_PROMPT = 1, CO_COUNT_FRESH = 2 };
 co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t width,

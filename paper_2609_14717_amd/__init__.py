@@ -278,20 +278,28 @@ def page_pool(t):
 
 def weights_i8(w_f, w_f_scale, w_kv, w_kv_scale, f_e=None, z_norm=None, k_norm=None):
     """co_weights_i8 over device tensors: codes and scales of ``carryover_quantize_i8``; f_e
-    from ``carryover_fold_e``, z_norm and k_norm as in ``weights``."""
-    return co_weights_i8(*(_dense(x, n) for x, n in (
+    from ``carryover_fold_e``, z_norm and k_norm as in ``weights``.  It keeps the tensors."""
+    w = co_weights_i8(*(_dense(x, n) for x, n in (
         (w_f, "w_f"), (w_f_scale, "w_f_scale"), (w_kv, "w_kv"), (w_kv_scale, "w_kv_scale"),
         (f_e, "f_e"), (z_norm, "z_norm"), (k_norm, "k_norm"))))
+    w.tensors = (w_f, w_f_scale, w_kv, w_kv_scale, f_e, z_norm, k_norm)
+    return w
 
 
 def logit_rules(seen=None, repetition=None, presence=None, frequency=None, bias_start=None,
                 bias_tok=None, bias_val=None, mask_row=None, mask_bits=None):
     """co_logit_rules over device tensors; num_bias and num_masks are their lengths.  Masks
-    are ``mask_bits`` [masks][ceil(vocab / 32)] of 32-bit words.  The tensors must outlive it."""
+    are ``mask_bits`` [masks][ceil(vocab / 32)] of 32-bit words.  It keeps the tensors."""
     r = co_logit_rules(*(_dense(x, n) for x, n in (
         (seen, "seen"), (repetition, "repetition"), (presence, "presence"),
         (frequency, "frequency"), (bias_start, "bias_start"), (bias_tok, "bias_tok"),
         (bias_val, "bias_val"), (mask_row, "mask_row"), (mask_bits, "mask_bits"))))
+    r.tensors = (seen, repetition, presence, frequency, bias_start, bias_tok, bias_val, mask_row, mask_bits)
+    # an empty tensor has no address, and nothing of it is read: any will do
+    if bias_tok is not None and bias_val is not None and r.bias_start and len(bias_tok) == 0:
+        r.bias_tok = r.bias_val = r.bias_start
+    if mask_bits is not None and r.mask_row and len(mask_bits) == 0:
+        r.mask_bits = r.mask_row
     r.num_bias = 0 if bias_tok is None else len(bias_tok)
     r.num_masks = 0 if mask_bits is None else len(mask_bits)
     return r

@@ -245,7 +245,7 @@ bool rules_ok(const co_logit_rules* r) {
       (r->bias_start == nullptr) != (r->bias_val == nullptr) ||
       (r->mask_row == nullptr) != (r->mask_bits == nullptr))
     return false;
-  return r->num_bias >= 0 && r->num_masks >= 0;
+  return r->num_bias >= 0 && r->num_bias <= kMaxVocab && r->num_masks >= 0;
 }
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
@@ -992,6 +992,7 @@ co_status carryover_quantize_i8(int32_t num_rows, int32_t num_cols, int32_t dtyp
                                 int8_t* codes, float* scale, hipStream_t stream) {
   if (num_rows < 0 || num_cols < 1) return CO_ERR_INVALID_ARG;
   if (num_rows > kMaxRowsI8 || num_cols % 64 || !dtype_ok(dtype)) return CO_ERR_UNSUPPORTED;
+  if (num_rows == 0) return CO_OK;   // (an empty tensor has no address)
   if (!x || !codes || !scale || !aligned(x, 16) || !aligned(codes, 16) || !aligned(scale, 4))
     return CO_ERR_INVALID_ARG;
   clear_stale_error();
@@ -1009,6 +1010,7 @@ co_status carryover_matmul_i8(int32_t m, int32_t n, int32_t k, const int8_t* a,
   co_status s = check_matmul_i8(m, n, k);
   if (s != CO_OK) return s;
   if (!dtype_ok(dtype)) return CO_ERR_UNSUPPORTED;
+  if (m == 0 || n == 0) return CO_OK;   // (an empty tensor has no address)
   if (!a || !a_scale || !w || !w_scale || !out || !aligned(a, 16) || !aligned(w, 16) ||
       !aligned(out, 16) || !aligned(a_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4))
     return CO_ERR_INVALID_ARG;
@@ -1072,7 +1074,8 @@ co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t wid
   if (s != CO_OK) return s;
   if (vocab < 1 || vocab > kMaxVocab || count_workgroups(dims->num_seqs, vocab) >= kMaxGrid)
     return CO_ERR_UNSUPPORTED;
-  if (width < 0 || !tokens || !seen || !status || !aligned(tokens, 4) || !aligned(len, 4) ||
+  if (width > kMaxVocab) return CO_ERR_UNSUPPORTED;
+  if (width < 0 || (width > 0 && !tokens) || !seen || !status || !aligned(tokens, 4) || !aligned(len, 4) ||
       !aligned(seen, 2) || !aligned(status, 4) || (flags & ~(CO_COUNT_PROMPT | CO_COUNT_FRESH)))
     return CO_ERR_INVALID_ARG;
   CountArgs a{};

@@ -185,6 +185,15 @@ def test_product_without_rows(m, n):
     assert (out == 2).all()
 
 
+@pytest.mark.parametrize("m", [3, 16, 19, 32])
+def test_product_of_few_rows_with_many_columns(m):
+    """Two column tiles a workgroup, the second of the last one partly and wholly outside."""
+    for n, k in ((16389, 1088), (17010, 1024)):
+        print(f"[product] {m} x {n} x {k}", flush=True)
+        ops = operands(m, n, k, m + n, False)
+        check_product(*ops, "bf16", product(*ops, "bf16"), f"{m} x {n} x {k}")
+
+
 def test_product_repeats_bit_for_bit_on_another_stream():
     ops = operands(45, 3001, 4160, 5, True)
     first = product(*ops, "f32")
@@ -378,6 +387,22 @@ def test_history_of_nothing():
 
 
 # --------------------------------------------------------- rules, probabilities
+
+@pytest.mark.parametrize("mask", [-1, 0])
+def test_rules_of_empty_lists(mask):
+    """A batch in which no request has a bias and there are no masks; a mask named all the
+    same allows nothing."""
+    S, V = 2, 300
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    r = co.logit_rules(bias_start=i32([0, 0, 0]), bias_tok=i32([]), bias_val=torch.empty(0, device=DEV),
+                       mask_row=i32([[mask], [-1]]), mask_bits=torch.empty(0, 10, dtype=torch.int32, device=DEV))
+    x, st = torch.randn(S, 1, V, device=DEV), zero()
+    out = torch.empty_like(x)
+    co.carryover_logit_rules(history_dims(S), V, 1, "f32", x, None, r, out, st)
+    assert torch.equal(out[1], x[1])
+    assert torch.isneginf(out[0]).all() if mask == 0 else torch.equal(out[0], x[0])
+    assert int(st) == (co.CO_ERR_MASK if mask == 0 else 0)
+
 
 class Logits:
     """Logits of a batch with rules, beside the oracle."""

@@ -331,6 +331,49 @@ def test_rules_call_needs_rules():
                                           0) == co.CO_ERR_INVALID_ARG
 
 
+@needs_lib
+def test_calls_of_nothing_take_empty_tensors():
+    """An empty tensor has no address."""
+    i8, f = torch.empty(0, 64, dtype=torch.int8), torch.empty(0)
+    w = torch.zeros(4, 64, dtype=torch.int8)
+    co.carryover_quantize_i8(0, 64, "f32", torch.empty(0, 64), i8, f, stream=0)
+    co.carryover_matmul_i8(0, 4, 64, i8, f, w, torch.zeros(4), None, "bf16", f, None, stream=0)
+    co.carryover_matmul_i8(4, 0, 64, w, torch.zeros(4), i8, f, None, "bf16", f, None, stream=0)
+    co.carryover_count_tokens(dims(S=2), 10, 0, torch.empty(2, 0, dtype=torch.int32), None, 0, FAKE, FAKE,
+                              stream=0)
+    with pytest.raises(co.CarryoverError):
+        co.carryover_matmul_i8(0, 4, 65, i8, f, w, torch.zeros(4), None, "bf16", f, None, stream=0)
+
+
+@needs_lib
+def test_lists_too_long_to_walk_in_32_bits_are_refused():
+    assert _rc(lambda: co.carryover_count_tokens(dims(), 1000, (1 << 30) + 1, FAKE, None, 0, FAKE, FAKE,
+                                                 stream=0)) == co.CO_ERR_UNSUPPORTED
+    r = _raw_rules(bias_start=FAKE, bias_tok=FAKE, bias_val=FAKE, num_bias=(1 << 30) + 1)
+    assert _rc(lambda: co.carryover_logit_rules(dims(), 1000, 17, "f32", FAKE, None, r, 1 << 30, FAKE,
+                                                stream=0)) == co.CO_ERR_INVALID_ARG
+
+
+def test_empty_lists_of_rules_have_addresses():
+    e = torch.empty(0)
+    r = co.logit_rules(bias_start=torch.zeros(3), bias_tok=e, bias_val=e, mask_row=torch.zeros(2),
+                       mask_bits=torch.empty(0, 4))
+    assert r.bias_tok and r.bias_val and r.mask_bits and r.num_bias == r.num_masks == 0
+
+
+def test_rules_and_weights_keep_their_tensors():
+    import weakref
+    t = torch.zeros(4)
+    alive = weakref.ref(t)
+    r, w = co.logit_rules(repetition=t), co.weights_i8(t, t, t, t)
+    del t
+    assert alive() is not None
+    del r
+    assert alive() is not None
+    del w
+    assert alive() is None
+
+
 def test_strided_tensors_are_refused():
     x = torch.zeros(4, 128)[:, ::2]
     with pytest.raises(ValueError, match="x is not contiguous"):
