@@ -191,6 +191,20 @@ __device__ __forceinline__ int xcd_run(int t, int total) {
   return x * q + min(x, r) + (t >> 3);
 }
 
+// Where results go: plain rows, or (X = KvDest) the K/V rows of the projection.  Each C
+// columns of a tile are then C / 2 rotation pairs of a head: their low halves, then their high
+// ones, so that whoever has a tile's row has both of a pair.
+struct PlainRows {};
+
+template <int C, typename X>
+__device__ __forceinline__ int column(const X& x, int n0, int c) {
+  if constexpr (sizeof(X) > 1) {
+    const int t = c & -C, j = c & (C - 1);
+    return n0 + t / x.hd * x.hd + t % x.hd / 2 + j % (C / 2) + j / (C / 2) * (x.hd / 2);
+  }
+  return n0 + c;
+}
+
 // Few rows (16 MT of them): bound by reading the weights once.  A workgroup's NW
 // wavefronts share 16 TN columns and split K: a wavefront takes every NW-th unit of 256
 // bytes of K, straight into the operand registers of v_mfma_i32_16x16x64_i8 (lane l holds
@@ -199,9 +213,10 @@ __device__ __forceinline__ int xcd_run(int t, int total) {
 // tiles are added in LDS: whole numbers, so the order does not matter.
 constexpr int kUnit = 256;
 
-template <int MT, int TN, int NW, typename T>
-__global__ __launch_bounds__(64 * NW) void matmul_i8_few_kernel(MatmulI8Args g) {
-  __shared__ int red[NW][MT * TN * 256];
+template <int MT, int TN, int NW, typename T, typename X>
+__global__ __launch_bounds__(64 * NW) void matmul_i8_few_kernel(MatmulI8Args g, X x) {
+  __shared__ __align__(16) int red[NW][MT * TN * 256];
+  __shared__ double inv_tab[sizeof(X) > 1 ? 64 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n0 = static_cast<int>(blockIdx.x) * 16 * TN;
   const int quad = (lane >> 4) * 16;
@@ -212,7 +227,9 @@ __global__ __launch_bounds__(64 * NW) void matmul_i8_few_kernel(MatmulI8Args g) 
     pa[i] = g.A + static_cast<int64_t>(min(16 * i + (lane & 15), g.M - 1)) * g.K + quad;
 #pragma unroll
   for (int j = 0; j < TN; ++j)
-    pw[j] = g.W + static_cast<int64_t>(min(n0 + 16 * j + (lane & 15), g.N - 1)) * g.K + quad;
+    pw[j] = g.W + static_cast<int64_t>(min(column<16>(x, 0, n0 + 16 * j + (lane & 15)), g.N - 1)) * g.K + quad;
+  if constexpr (sizeof(X) > 1)
+    if (tid < x.hd / 2) inv_tab[tid] = rope_table<uint16_t>(x, tid);
   i32x4 acc[MT][TN] = {};
   struct Unit {
     i32x4 a[4][MT], w[4][TN];
@@ -270,6 +287,30 @@ __global__ __launch_bounds__(64 * NW) void matmul_i8_few_kernel(MatmulI8Args g) 
       for (int r = 0; r < 4; ++r)
         red[wave][(16 * i + 4 * (lane >> 4) + r) * (16 * TN) + 16 * j + (lane & 15)] = acc[i][j][r];
   __syncthreads();
+  if constexpr (sizeof(X) > 1) {
+    // four pairs a thread, rows side by side (a value page has a dim's tokens next to each other)
+    for (int o = tid; o < MT * TN * 32; o += 64 * NW) {
+      const int row = o % (16 * MT), h = o / (16 * MT) % 2, j = o / (32 * MT);
+      const int32_t dst = row < g.M && n0 + 16 * j < g.N ? x.row_dst[row] : kSkip;
+      if (dst == kSkip) continue;
+      const int at = row * (16 * TN) + 16 * j + 4 * h, col = column<16>(x, 0, n0 + 16 * j + 4 * h);
+      i32x4 a = {}, b = {};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        a += *reinterpret_cast<const i32x4*>(&red[w][at]);
+        b += *reinterpret_cast<const i32x4*>(&red[w][at + 8]);
+      }
+      const float sa = g.a_scale[row];
+      float lo[4], hi[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        lo[i] = scaled(a[i], sa, g.w_scale[col + i]);
+        hi[i] = scaled(b[i], sa, g.w_scale[col + x.hd / 2 + i]);
+      }
+      kv_store<uint16_t, 4>(x, row, dst, x.row_pos[row], col / x.hd, col % x.hd, lo, hi, inv_tab);
+    }
+    return;
+  }
   for (int o = tid; o < MT * TN * 256; o += 64 * NW) {
     const int row = o / (16 * TN), col = n0 + o % (16 * TN);
     if (row >= g.M || col >= g.N) continue;
@@ -468,20 +509,6 @@ __device__ __forceinline__ void tile_of(int r, int tiles_m, int tiles_n, int* m0
   *n0 = rg / gsz * BN;
 }
 
-// Where a tile's results go: plain rows, or (X = KvDest) the K/V rows of the projection, each
-// 32 columns of a tile then being 16 rotation pairs of a head: their low halves, then their
-// high ones, so that a lane holds both of a pair in registers q and q + 2.
-struct PlainRows {};
-
-template <typename X>
-__device__ __forceinline__ int column(const X& x, int n0, int c) {
-  if constexpr (sizeof(X) > 1) {
-    const int t = c & ~31, j = c & 31;
-    return n0 + t / x.hd * x.hd + t % x.hd / 2 + (j & 15) + (j >> 4) * (x.hd / 2);
-  }
-  return n0 + c;
-}
-
 // A wavefront's 32 x 32 results of the K/V product: scaled, rotated and stored.
 __device__ __forceinline__ void put_pairs(const MatmulI8Args& g, const KvDest& e, const i32x16& acc, int row,
                                           float sa, int n0, int cb, int lane, const float* col_scale,
@@ -535,7 +562,7 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
     const int row = (LPW * wave + j) * 8 + lane / 8;
     const int chunk = (lane & 7) ^ ((row >> 1) & 7);
     const int8_t* base = row < BM ? g.A + static_cast<int64_t>(min(m0 + row, g.M - 1)) * g.K
-                                  : g.W + static_cast<int64_t>(min(column(x, n0, row - BM), g.N - 1)) * g.K;
+                                  : g.W + static_cast<int64_t>(min(column<32>(x, n0, row - BM), g.N - 1)) * g.K;
     src[j] = base + kbeg + chunk * 16;
   }
   // chunks past a half stage are not read: they take the half before
@@ -592,7 +619,7 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
   };
 
   for (int c = tid; c < BN; c += 512) {   // (read behind the main loop's barriers)
-    const int col = min(column(x, n0, c), g.N - 1);
+    const int col = min(column<32>(x, n0, c), g.N - 1);
     col_scale[c] = g.w_scale[col];
     col_bias[c] = g.bias ? g.bias[col] : 0.f;
   }
@@ -673,7 +700,7 @@ __global__ __launch_bounds__(512) void sum_parts_i8_kernel(MatmulI8Args g, X x, 
   int m0, n0;
   tile_of<BM, BN>(r0, tiles_m, tiles_n, &m0, &n0);
   for (int c = tid; c < BN; c += 512) {
-    const int col = min(column(x, n0, c), g.N - 1);
+    const int col = min(column<32>(x, n0, c), g.N - 1);
     col_scale[c] = g.w_scale[col];
     col_bias[c] = g.bias ? g.bias[col] : 0.f;
   }
@@ -744,25 +771,25 @@ hipError_t launch_stream(const MatmulI8Args& g, const MatmulI8Plan& p, bool keep
   return hipGetLastError();
 }
 
-template <int MT, int TN, typename T>
-hipError_t launch_few_nw(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
+template <int MT, int TN, typename T, typename X>
+hipError_t launch_few_nw(const MatmulI8Args& g, const X& x, const MatmulI8Plan& p, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(p.workgroups));
   if constexpr (TN == 1) {   // (32 columns: the plan has eight at most)
     if (p.waves == 16) {
-      hipLaunchKernelGGL((matmul_i8_few_kernel<MT, TN, 16, T>), grid, dim3(1024), 0, stream, g);
+      hipLaunchKernelGGL((matmul_i8_few_kernel<MT, TN, 16, T, X>), grid, dim3(1024), 0, stream, g, x);
       return hipGetLastError();
     }
   }
-  if (p.waves == 8) hipLaunchKernelGGL((matmul_i8_few_kernel<MT, TN, 8, T>), grid, dim3(512), 0, stream, g);
-  else hipLaunchKernelGGL((matmul_i8_few_kernel<MT, TN, 4, T>), grid, dim3(256), 0, stream, g);
+  if (p.waves == 8) hipLaunchKernelGGL((matmul_i8_few_kernel<MT, TN, 8, T, X>), grid, dim3(512), 0, stream, g, x);
+  else hipLaunchKernelGGL((matmul_i8_few_kernel<MT, TN, 4, T, X>), grid, dim3(256), 0, stream, g, x);
   return hipGetLastError();
 }
 
-template <typename T>
-hipError_t launch_few(const MatmulI8Args& g, const MatmulI8Plan& p, hipStream_t stream) {
+template <typename T, typename X>
+hipError_t launch_few(const MatmulI8Args& g, const X& x, const MatmulI8Plan& p, hipStream_t stream) {
   if (g.M <= 16)
-    return p.cols == 2 ? launch_few_nw<1, 2, T>(g, p, stream) : launch_few_nw<1, 1, T>(g, p, stream);
-  return p.cols == 2 ? launch_few_nw<2, 2, T>(g, p, stream) : launch_few_nw<2, 1, T>(g, p, stream);
+    return p.cols == 2 ? launch_few_nw<1, 2, T>(g, x, p, stream) : launch_few_nw<1, 1, T>(g, x, p, stream);
+  return p.cols == 2 ? launch_few_nw<2, 2, T>(g, x, p, stream) : launch_few_nw<2, 1, T>(g, x, p, stream);
 }
 
 }  // namespace
@@ -852,7 +879,8 @@ static hipError_t launch_product(const MatmulI8Args& g, const MatmulI8Plan& p, b
     return g.dtype == CO_DTYPE_BF16 ? launch_stream<uint16_t>(g, p, keep_parts, stream)
                                     : launch_stream<float>(g, p, keep_parts, stream);
   if (p.variant == kFew)
-    return g.dtype == CO_DTYPE_BF16 ? launch_few<uint16_t>(g, p, stream) : launch_few<float>(g, p, stream);
+    return g.dtype == CO_DTYPE_BF16 ? launch_few<uint16_t>(g, PlainRows{}, p, stream)
+                                    : launch_few<float>(g, PlainRows{}, p, stream);
   return g.dtype == CO_DTYPE_BF16 ? launch_wide<uint16_t>(g, PlainRows{}, p, stream)
                                   : launch_wide<float>(g, PlainRows{}, p, stream);
 }
@@ -1072,12 +1100,12 @@ hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t st
   else
     hipLaunchKernelGGL((z_codes_kernel<1024, 0>), rows, dim3(1024), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
   const MatmulI8Plan kv = plan_matmul_i8(a.M, n_kv, a.d, num_cus);
-  if (kv.variant < kFew && a.dst.knorm == nullptr) {   // tiles rotate and store their rows
+  if (kv.variant != kStream && a.dst.knorm == nullptr) {   // tiles rotate and store their rows
     g.N = n_kv;
     g.K = a.d;
     g.W = a.wkv;
     g.w_scale = a.wkv_scale;
-    return launch_wide<float>(g, a.dst, kv, stream);
+    return kv.variant == kFew ? launch_few<float>(g, a.dst, kv, stream) : launch_wide<float>(g, a.dst, kv, stream);
   }
   if ((err = product(n_kv, a.d, a.wkv, a.wkv_scale, &p)) != hipSuccess) return err;
   const int per = 1024 / (a.dst.hd / 2);   // rows of a workgroup

@@ -310,6 +310,14 @@ def test_project_variants(variant, S, B, Dcat, d, L, Hkv, hd, tune):
     check_project(c)
 
 
+@pytest.mark.parametrize("S,B,hd", [(1, 4, 128), (3, 7, 64), (1, 32, 128)])
+def test_project_of_few_rows_into_many_heads(S, B, hd):
+    """Two column tiles a workgroup, which are rotation pairs of a head."""
+    c = project_case(S, B, 128, 1088, 5, 2048 // hd, hd, 1e4, S * B, False)
+    run_project(c)
+    check_project(c)
+
+
 def test_project_without_an_embedding():
     c = project_case(2, 8, 256, 256, 1, 2, 64, 1e4, 9, False, embed=False)
     run_project(c)
