@@ -212,7 +212,10 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   __shared__ float held_val[kBiasHeld];
   __shared__ int num_held, listed[kWaves];
   constexpr int kParts = KIND == kStats || KIND == kWhole ? kRowsMax * kWaves : 1;
-  __shared__ Part parts[kParts], ones[kParts];   // of the wavefronts; of their special tokens
+  __shared__ Part parts[kParts];                 // of the wavefronts
+  constexpr int kLanes = KIND == kStats || KIND == kWhole ? kRowsMax * NT : 1;
+  __shared__ float one_m[kLanes], one_l[kLanes]; // of each thread's special tokens
+  __shared__ int one_at[kLanes];
   __shared__ Whole whole[kRowsMax];
   __shared__ float own_special[KIND == kRules || KIND == kProbs ? kRowsMax * NT : 1];
   bool greedy = false;
@@ -406,8 +409,8 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
     return allowed >> (e.v % 8) & 1 ? x : kNone;
   };
   // Every special token of this wavefront's share (one a lane, the rest idle) in every row:
-  // f(r, token, whether there is one, its logit after the rules).  Its logits and mask bytes
-  // of all rows are loaded together.
+  // f(r, number in the list, token, its logit after the rules).  Its logits and mask bytes of
+  // all rows are loaded together.
   auto each_special = [&](int from, int to, auto&& f) {
     for (int i0 = from + wave * 64; i0 < to; i0 += NT) {
       const bool on = i0 + lane < n;
@@ -432,7 +435,8 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
           ar = q == r ? allowed[q] : ar;
         }
         const int m = mask_of(r);
-        f(r, e.v, on, ruled(e, r, widen(xr), m >= 0 ? ar : (m == -1 ? 0xFF : 0)));
+        const float y = ruled(e, r, widen(xr), m >= 0 ? ar : (m == -1 ? 0xFF : 0));
+        if (on) f(r, i0 + lane, e.v, y);
       }
     }
   };
@@ -475,23 +479,15 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   }
 
   if constexpr (KIND == kStats || KIND == kWhole) {
-    if (lane < nr) ones[lane * kWaves + wave] = nothing;
-    each_special(0, n, [&](int r, int v, bool on, float y) {
+    // (a thread has every NT-th of the list, and joins them by itself)
+    each_special(0, n, [&](int r, int i, int v, float y) {
+      const int o = r * NT + tid;
       Part p = nothing;
-      if (on) take(p, y, v, k);
-      p = wave_join(p, k);
-      const Part q = ones[r * kWaves + wave];
-      if (q.m > p.m) {
-        p.l = q.l + (p.m > kNone ? p.l * exp2_fast((p.m - q.m) * k) : 0.f);
-        p.one = q.one;
-        p.m = q.m;
-      } else if (q.m == p.m) {
-        p.l += q.l;
-        p.one = min(p.one, q.one);
-      } else {
-        p.l += q.m > kNone ? q.l * exp2_fast((q.m - p.m) * k) : 0.f;
-      }
-      if (lane == 0) ones[r * kWaves + wave] = p;
+      if (i >= NT) p = Part{one_m[o], one_l[o], kNowhere, one_at[o]};
+      take(p, y, v, k);
+      one_m[o] = p.m;
+      one_l[o] = p.l;
+      one_at[o] = p.one;
     });
   }
   auto result = [&](int r, int v, float x) {
@@ -519,10 +515,9 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
     if constexpr (KIND != kStats) {
       if (KIND != kWhole || phase == 1) {
         each_special(KIND == kWhole || phase == 0 ? 0 : NT, KIND != kWhole && phase == 0 ? min(n, NT) : n,
-                     [&](int r, int v, bool on, float x) {
-          if (!on) return;
+                     [&](int r, int i, int v, float x) {
           const float y = result(r, v, x);
-          if (KIND != kWhole && phase == 0) own_special[r * NT + tid] = y;
+          if (KIND != kWhole && phase == 0) own_special[r * NT + i] = y;
           else if constexpr (KIND == kRules) store1(static_cast<T*>(a.out) + (row0 + r) * V + v, y);
           else a.probs[(row0 + r) * V + v] = y;
         });
@@ -589,9 +584,10 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
           }
         }
         if constexpr (KIND != kProbs) {
-          const Part p = ones[r * kWaves + wave];
+          Part p = nothing;   // of this thread's special tokens
+          if (tid < n) p = Part{one_m[r * NT + tid], one_l[r * NT + tid], kNowhere, one_at[r * NT + tid]};
           Part w;   // the wavefront's
-          w.m = fmaxf(wave_max_f(top), p.m);
+          w.m = wave_max_f(fmaxf(top, p.m));
           w.l = 0.f;
           if (__builtin_amdgcn_readfirstlane(w.m > kNone)) {
             float sum = 0.f;
@@ -607,11 +603,11 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
                 for (int e = 0; e < kVec; ++e)
                   if (y[c][e] == y[c][e]) sum += y[c][e] == w.m ? 1.f : exp2_fast((y[c][e] - w.m) * k);
             }
+            if (p.m > kNone) sum += p.m == w.m ? p.l : p.l * exp2_fast((p.m - w.m) * k);
             w.l = wave_sum_f(sum);
-            if (p.m > kNone) w.l += p.m == w.m ? p.l : p.l * exp2_fast((p.m - w.m) * k);
           }
           w.vec = wave_min(top == w.m ? where : kNowhere);
-          w.one = p.m == w.m ? p.one : kNowhere;
+          w.one = wave_min(p.m == w.m ? p.one : kNowhere);
           if (lane == 0) parts[r * kWaves + wave] = w;
           if constexpr (KIND == kWhole) {
             __syncthreads();
