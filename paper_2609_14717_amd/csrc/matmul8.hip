@@ -95,7 +95,9 @@ struct RowScale {
 
 // One workgroup per row, which it holds in registers (Q times eight entries a thread) from
 // the search for its largest magnitude to its codes; Q = 0: rows of any length, read twice.
-// Magnitudes compare as their bits, infinities and NaNs as the largest.
+// Magnitudes compare as their bits, infinities and NaNs as the largest.  Memory traffic bounds
+// it in the limit; at the sizes of a round its three steps one behind the other do: 512 bf16
+// rows of 20480 12.2 us (2.6 TB/s), 544 of 4096 4.9, one of 768 2.4.
 template <typename T, int NT, int Q>
 __global__ __launch_bounds__(NT) void quantize_rows_kernel(const T* x, int cols, int8_t* codes,
                                                            float* scale) {
@@ -210,7 +212,9 @@ __device__ __forceinline__ int column(const X& x, int n0, int c) {
 // bytes of K, straight into the operand registers of v_mfma_i32_16x16x64_i8 (lane l holds
 // row or column l % 16, 16 k from 16 (l / 16) on; result register r is row 4 (l / 16) + r,
 // column l % 16), the next unit's loads in flight while one is multiplied.  The NW partial
-// tiles are added in LDS: whole numbers, so the order does not matter.
+// tiles are added in LDS: whole numbers, so the order does not matter.  One launch, so the
+// kernel of the smallest products: 1 x 256 x 768 2.8 us, 16 x 2048 x 4096 6.9 (its K/V rows
+// rotated and stored 7.8).
 constexpr int kUnit = 256;
 
 template <int MT, int TN, int NW, typename T, typename X>
@@ -339,7 +343,10 @@ __device__ __forceinline__ void put_cols(E* row, int col, int N, const V& v) {
 // Few rows through LDS: a workgroup's four wavefronts take 16 columns each and share 16 MT
 // rows; K advances in stages of 256 bytes a row (long runs of memory) through a ring of NS,
 // and is split over workgroups until the chip is full.  The weights are the first operand: a
-// lane ends with row l % 16 and four columns from 4 (l / 16) on.
+// lane ends with row l % 16 and four columns from 4 (l / 16) on.  17 x 128000 x 4096 104-107 us:
+// 5.0 TB/s of weights, a large copy's rate (reads alone reach 5.7-5.9); the same by registers,
+// each wavefront reading 256-byte pieces of 16 rows, 127.  16 x 4096 x 20480, parts left to the
+// reader, 14.9 us.
 template <int MT, int NS, typename T>
 __global__ __launch_bounds__(256) void matmul_i8_stream_kernel(MatmulI8Args g, int tiles_n, int k_per_split) {
   constexpr int ROWS = 64 + 16 * MT, STAGE = ROWS * kUnit;
@@ -458,6 +465,12 @@ __global__ __launch_bounds__(256) void sum_rows_i8_kernel(MatmulI8Args g, int sp
 // 16-byte chunks of a staged row are permuted by row / 2, so that 16 lanes reading a
 // fragment hit 16 bank groups.  Fragments of a step of 32 k are read while the step before
 // multiplies.
+// Bound by the matrix instructions and the LDS reads that feed them.  8192^3 530 us, 2073 TOP/s
+// (the library's 541); 544 x 128000 x 4096, bf16 results, 333 us, 1.71 POP/s (its int32 results
+// 408): three row tiles of 192 hold 544 (6 %), and the 139 MB of results leave no time of their
+// own, for one workgroup fills a compute unit; 512 x 4096 x 20480 in four parts 52 + 9;
+// 512 x 10240 x 4096 34, with rotation and stores of K/V rows 39.
+// Stages of 64 bytes 469 us for the second, results by way of LDS 421.
 constexpr int kStageK = 128;
 
 // A wavefront's 32 x 32 results: scaled, the bias added, stored.
@@ -687,7 +700,8 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
   }
 }
 
-// The parts of K of one 32 x 32 tile for each wavefront, added up, scaled and stored.
+// The parts of K of one 32 x 32 tile for each wavefront, added up, scaled and stored: memory
+// traffic and a launch, 9 us for 512 x 4096 (with the product 60; parts by rows of the result 65).
 template <int TMW, int TNW, typename T, typename X>
 __global__ __launch_bounds__(512) void sum_parts_i8_kernel(MatmulI8Args g, X x, int tiles_m,
                                                            int tiles_n, int splits) {
@@ -843,6 +857,12 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
       return p;
     }
   }
+  // The tile and split of K with the least time by a model: rounds of workgroups over the compute
+  // units at the rate that each tile reached on a large product (256 x 256: 2.07e15 a second on
+  // 256 units), 256 k more for a workgroup's start and end, or the operands' bytes if they take
+  // longer; parts written and read, and a launch.  Over a sweep of sizes (every variant timed) its
+  // choice takes 1.03 to 1.05 times the best variant's time on average; small tiles win where
+  // large ones leave units idle (us: 512 x 10240 x 4096 with 192 x 128 34, 256 x 128 38).
   double best = 1e30;
   for (int v = 0; v < kVariants; ++v) {
     if (force >= 0 && force < kFew && force != v) continue;
@@ -938,7 +958,8 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
 
 // A row of z from F's product: F E on a carry row, the optional RMS norm, its codes.  Q
 // times eight entries of it stay in a thread's registers; Q = 0: rows of any length by way
-// of `spill` [M][d] (which may be the product's own fp32 results).
+// of `spill` [M][d] (which may be the product's own fp32 results).  A chain of a row's loads,
+// one or two sums over the workgroup, and its stores: 5.0 us for 16 rows of 4096, 5.5 for 512.
 template <int NT, int Q>
 __global__ __launch_bounds__(NT) void z_codes_kernel(Product p, float* spill, const float* fe,
                                                      const float* gain, const int32_t* row_dst,
