@@ -282,7 +282,7 @@ struct MatmulI8Args {
 
 struct MatmulI8Plan {
   int variant;               // tile of the wide kernel, or the kernel for few rows
-  int splits, k_per_split;   // wide: parts of K
+  int splits, k_per_split;   // parts of K (not: few rows)
   int cols, waves;           // few rows: columns of a workgroup / 16, wavefronts
   int64_t workgroups;
   size_t ws_bytes;

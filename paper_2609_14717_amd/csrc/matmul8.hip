@@ -862,7 +862,7 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
   // 256 units), 256 k more for a workgroup's start and end, or the operands' bytes if they take
   // longer; parts written and read, and a launch.  Over a sweep of sizes (every variant timed) its
   // choice takes 1.03 to 1.05 times the best variant's time on average; small tiles win where
-  // large ones leave units idle (us: 512 x 10240 x 4096 with 192 x 128 34, 256 x 128 38).
+  // large ones leave units idle (us: 512 x 10240 x 4096 with 192 x 128 34, the best of the others 38).
   double best = 1e30;
   for (int v = 0; v < kVariants; ++v) {
     if (force >= 0 && force < kFew && force != v) continue;
