@@ -1130,13 +1130,15 @@ co_status carryover_probabilities(const co_dims* dims, int32_t vocab, int32_t ro
       !aligned(top_tok, 4) || !aligned(status, 4) || overlap(logits, n * es, probs, n * 4))
     return CO_ERR_INVALID_ARG;
   if (!ws || !aligned(ws, 256)) return CO_ERR_INVALID_ARG;
-  if (ws_bytes < plan_logits(dims->num_seqs, rows, vocab, num_cus(), false).ws_bytes)
-    return CO_ERR_WORKSPACE;
+  const LogitPlan p = plan_logits(dims->num_seqs, rows, vocab, num_cus(), false);
+  if (ws_bytes < p.ws_bytes) return CO_ERR_WORKSPACE;
   LogitArgs a = logit_args(dims, vocab, rows, logits, draft_tok, rules, status, false);
   a.temperature = temperature;
   a.probs = probs;
   a.top = top_tok;
   a.ws = static_cast<float4*>(ws);
+  a.marks = static_cast<uint8_t*>(ws) + p.marks_at;
+  a.ruled = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.ruled_at);
   clear_stale_error();
   return hip_status(launch_probabilities(a, dtype, stream));
 }

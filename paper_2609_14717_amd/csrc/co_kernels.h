@@ -330,6 +330,8 @@ struct LogitArgs {
   float* probs;                           // [S][R][V]
   int32_t* top;                           // [S][R] or null
   float4* ws;                             // [S][R][tiles]
+  uint8_t* marks;                         // [workgroups][tokens of a tile / 8]: special ones
+  float* ruled;                           // [S][R][tiles][256]: the first of them after the rules
   int32_t* status;
   int groups, rows_per, tiles;            // of the plan
 };
@@ -338,6 +340,7 @@ struct LogitPlan {
   int groups, rows_per;      // row groups of a sequence, rows of each
   int tiles;                 // of a row
   int64_t workgroups;
+  size_t marks_at, ruled_at; // in the workspace
   size_t ws_bytes;
 };
 

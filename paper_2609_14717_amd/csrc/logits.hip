@@ -263,10 +263,22 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
     b1 = a.bias_start[s + 1];
   }
   Vec<uint16_t> w[C];
-  if (seen && vectors) {
+  auto load_history = [&]() {
+    if (seen && vectors) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) w[c].load(seen + at_vec(c));
+      for (int c = 0; c < C; ++c) w[c].load(seen + at_vec(c));
+    }
+  };
+  // kProbs: the marks of special tokens are those of the pass before (where there is nothing to
+  // mark but the tokens behind the last vector, they are made again: no load to wait for)
+  const bool kept = a.seen || a.bias_start;
+  uint8_t* marks = a.marks + static_cast<int64_t>(blockIdx.x) * (kTokens / 8) + tid;
+  uint32_t mine[C];           // of this thread's vectors
+  if (KIND == kProbs && kept) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) mine[c] = marks[c * NT];
   }
+  if constexpr (KIND != kProbs) load_history();
   struct Row {
     Vec<T> x[C];
     uint32_t allowed[C];   // (words: bytes would be packed, and waited for, as they arrive)
@@ -292,76 +304,87 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   auto mask_of = [&](int r) { return __builtin_amdgcn_readlane(mask_held, r); };
   auto bits_of = [&](int m) { return reinterpret_cast<const uint8_t*>(a.mask_bits) + m * mask_bytes; };
   auto load_mask = [&](int r, Row& o) {
+    // (what is so without a mask first: behind a branch it would wait for every load in flight)
     const int m = mask_of(r);
+    uint32_t without = m == -1 ? 0xFF : 0;
+    asm volatile("" : "+v"(without));
+#pragma unroll
+    for (int c = 0; c < C; ++c) o.allowed[c] = without;
     if (m >= 0 && vectors) {
       const uint8_t* bits = bits_of(m);
 #pragma unroll
       for (int c = 0; c < C; ++c) o.allowed[c] = bits[at_vec(c) / kVec];
-    } else {
-#pragma unroll
-      for (int c = 0; c < C; ++c) o.allowed[c] = m == -1 ? 0xFF : 0;
     }
   };
   load_mask(0, cur);
 
   // ---- the tile's special tokens
-  auto proposal = [&](int i) { return i < 64 ? __builtin_amdgcn_readlane(held, i) : draft[i]; };
+  auto proposal_held = [&](int i) { return i == lane && i < before ? held : draft[i]; };
   const bool right = b0 >= 0 && b1 >= b0 && b1 <= a.num_bias;
   if (!right && reports && tid == 0) set_status(a.status, CO_ERR_LENGTH);
   const int n_bias = right ? b1 - b0 : 0;
-  const int own_tok = tid < n_bias ? a.bias_tok[b0 + tid] : -1;
-  const float own_val = tid < n_bias ? a.bias_val[b0 + tid] : 0.f;
   uint8_t* special8 = reinterpret_cast<uint8_t*>(special);
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    uint32_t m = 0;
-    if (full(c)) {
-      if (seen) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) m |= (w[c].x[e] != 0 ? 1u : 0u) << e;
-      }
-    } else if (vec(c) < V) {
-      m = (1u << (V - vec(c))) - 1;
-    }
-    special8[c * NT + tid] = static_cast<uint8_t>(m);
-    reinterpret_cast<uint8_t*>(with_bias)[c * NT + tid] = 0;
+  int own_tok = -1;           // bias number tid
+  float own_val = 0.f;
+  if (KIND != kProbs && tid < n_bias) {
+    own_tok = a.bias_tok[b0 + tid];
+    own_val = a.bias_val[b0 + tid];
   }
-  if (tid == 0) num_held = 0;
-  if (n_bias > 0 || draft) {
-    __syncthreads();
-    for (int i = tid; i < (reports && draft ? a.R - 1 : before); i += NT) {
-      const int d = i == lane && i < before ? held : draft[i];
-      if (static_cast<uint32_t>(d) >= static_cast<uint32_t>(V)) {
-        if (reports) set_status(a.status, CO_ERR_TOKEN);
-      } else if (i < before) {
-        const int t = in_tile(d);
-        if (t >= 0) atomicOr(&special[t >> 5], 1u << (t & 31));
+  // Marks them, with those that have a bias.
+  auto mark = [&]() {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      uint32_t m = 0;
+      if (full(c)) {
+        if (seen) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) m |= (w[c].x[e] != 0 ? 1u : 0u) << e;
+        }
+      } else if (vec(c) < V) {
+        m = (1u << (V - vec(c))) - 1;
       }
+      special8[c * NT + tid] = static_cast<uint8_t>(m);
+      reinterpret_cast<uint8_t*>(with_bias)[c * NT + tid] = 0;
     }
-    for (int i = tid; i < n_bias; i += NT) {
-      const int d = i == tid ? own_tok : a.bias_tok[b0 + i];
-      if (static_cast<uint32_t>(d) >= static_cast<uint32_t>(V)) {
-        if (reports) set_status(a.status, CO_ERR_TOKEN);
-      } else if (const int t = in_tile(d); t >= 0) {
-        atomicOr(&special[t >> 5], 1u << (t & 31));
-        atomicOr(&with_bias[t >> 5], 1u << (t & 31));
-        const int at = atomicAdd(&num_held, 1);
-        if (at < kBiasHeld) {
-          held_tok[at] = static_cast<uint16_t>(t);
-          held_order[at] = i;
-          held_val[at] = i == tid ? own_val : a.bias_val[b0 + i];
+    if (tid == 0) num_held = 0;
+    if (n_bias > 0 || draft) {
+      __syncthreads();
+      for (int i = tid; i < (reports && draft ? a.R - 1 : before); i += NT) {
+        const int d = proposal_held(i);
+        if (static_cast<uint32_t>(d) >= static_cast<uint32_t>(V)) {
+          if (reports) set_status(a.status, CO_ERR_TOKEN);
+        } else if (i < before) {
+          const int t = in_tile(d);
+          if (t >= 0) atomicOr(&special[t >> 5], 1u << (t & 31));
+        }
+      }
+      for (int i = tid; i < n_bias; i += NT) {
+        const int d = KIND != kProbs && i == tid ? own_tok : a.bias_tok[b0 + i];
+        if (static_cast<uint32_t>(d) >= static_cast<uint32_t>(V)) {
+          if (reports) set_status(a.status, CO_ERR_TOKEN);
+        } else if (const int t = in_tile(d); t >= 0) {
+          atomicOr(&special[t >> 5], 1u << (t & 31));
+          atomicOr(&with_bias[t >> 5], 1u << (t & 31));
+          const int at = atomicAdd(&num_held, 1);
+          if (at < kBiasHeld) {
+            held_tok[at] = static_cast<uint16_t>(t);
+            held_order[at] = i;
+            held_val[at] = KIND != kProbs && i == tid ? own_val : a.bias_val[b0 + i];
+          }
         }
       }
     }
-  }
-  __syncthreads();
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < C; ++c) mine[c] = special8[c * NT + tid];
+  };
+  if (KIND != kProbs || !kept) mark();
   uint32_t plain[C];          // tokens of a vector that are not special
   int own = 0;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const uint32_t m = special8[c * NT + tid];
-    plain[c] = full(c) ? m ^ 0xFF : 0;
-    own += __builtin_popcount(m);
+    plain[c] = full(c) ? mine[c] ^ 0xFF : 0;
+    own += __builtin_popcount(mine[c]);
   }
   uint32_t pairs[sizeof(T) == 2 ? C : 1][4];   // 16-bit logits: the masks of `plain`
   if constexpr (sizeof(T) == 2 && KIND != kRules) {
@@ -379,12 +402,18 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
     start += w < wave ? listed[w] : 0;
     n += listed[w];
   }
-  int at = start;
+  if (KIND != kProbs || n > NT) {
+    if constexpr (KIND == kProbs) {   // (the list is walked again behind the rows)
+      load_history();
+      mark();
+    }
+    int at = start;
 #pragma unroll
-  for (int c = 0; c < C; ++c)
-    for (uint32_t m = special8[c * NT + tid]; m != 0; m &= m - 1)
-      list[at++] = static_cast<uint16_t>((c * NT + tid) * kVec + __builtin_ctz(m));
-  __syncthreads();
+    for (int c = 0; c < C; ++c)
+      for (uint32_t m = mine[c]; m != 0; m &= m - 1)
+        list[at++] = static_cast<uint16_t>((c * NT + tid) * kVec + __builtin_ctz(m));
+    __syncthreads();
+  }
 
   // number i of the list; the last entry of a token in the list of biases counts
   auto entry = [&](int i) {
@@ -512,34 +541,46 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
     shares(whole[r], y, v, k, greedy);
     return y[0];
   };
-  // What becomes of the first NT special tokens waits in LDS for the thread that stores the
-  // vectors that hold them, which writes them behind its own stores, row by row (later, the
-  // lines that they lie in would be in memory already, and be fetched to be changed).
-  const int stop = min(start + own, NT);
-  auto store_special = [&](int r) {
-    for (int i = start; i < stop; ++i) {
-      const int v = token_of(list[i]);
-      const float y = own_special[r * NT + i];
-      if constexpr (KIND == kRules) store1(static_cast<T*>(a.out) + (row0 + r) * V + v, y);
-      else a.probs[(row0 + r) * V + v] = y;
-    }
+  // The first NT special tokens after the rules wait in LDS, row by row, for the thread that
+  // stores the vectors that hold them.  It stores rules behind its own vector (later, the lines
+  // that they lie in would be in memory already, and be fetched to be changed); probabilities it
+  // puts into the vector before.  (Either is slower the other way: rules on 64 x 128000 bf16
+  // 17.3 us, 16.0; probabilities of 32 x 17 x 128000 164, 160.)
+  auto each_own = [&](int r, int c, auto&& f) {   // f(place in vector c, logit)
+    int i = start;
+#pragma unroll
+    for (int b = 0; b < C; ++b) i += b < c ? __builtin_popcount(mine[b]) : 0;
+    for (uint32_t m = mine[c]; m != 0 && i < NT; m &= m - 1, ++i) f(__builtin_ctz(m), own_special[r * NT + i]);
   };
+  if constexpr (KIND == kProbs) {   // the first pass left them
+    float y[kRowsMax];
+    if (n > NT) {
+      each_special(0, NT, [&](int r, int i, int, float x) { own_special[r * NT + i] = x; });
+    } else if (tid < n) {
+#pragma unroll
+      for (int q = 0; q < kRowsMax; ++q) y[q] = a.ruled[((row0 + min(q, nr - 1)) * a.tiles + tile) * NT + tid];
+#pragma unroll
+      for (int q = 0; q < kRowsMax; ++q) own_special[q * NT + tid] = y[q];
+    }
+    __syncthreads();
+  }
 
   // kRules, kProbs: the first NT special tokens before the rows, the others behind them
 #pragma unroll 1
   for (int phase = 0; phase < (KIND == kStats ? 1 : 2); ++phase) {
-    if constexpr (KIND != kStats) {
-      if (KIND != kWhole || phase == 1) {
-        each_special(KIND == kWhole || phase == 0 ? 0 : NT, KIND != kWhole && phase == 0 ? min(n, NT) : n,
-                     [&](int r, int i, int v, float x) {
-          const float y = result(r, v, x);
-          if (KIND != kWhole && phase == 0) own_special[r * NT + i] = y;
-          else if constexpr (KIND == kRules) store1(static_cast<T*>(a.out) + (row0 + r) * V + v, y);
-          else a.probs[(row0 + r) * V + v] = y;
-        });
+    if constexpr (KIND == kRules) {
+      if (phase == 0) {
+        each_special(0, min(n, NT), [&](int r, int i, int, float x) { own_special[r * NT + i] = x; });
+        __syncthreads();
       }
-      if (phase == 1) break;
-      if (KIND != kWhole) __syncthreads();
+    }
+    if (KIND != kStats && phase == 1) {
+      each_special(KIND == kWhole ? 0 : NT, n, [&](int r, int, int v, float x) {
+        const float y = result(r, v, x);
+        if constexpr (KIND == kRules) store1(static_cast<T*>(a.out) + (row0 + r) * V + v, y);
+        else a.probs[(row0 + r) * V + v] = y;
+      });
+      break;
     }
 #pragma unroll 1
     for (int r = 0; r < nr; ++r) {
@@ -589,8 +630,16 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
             }
           }
           if constexpr (KIND == kProbs) {
-            shares(whole[r], y[c], vec(c), k, greedy);
-            if (full(c)) store8(probs + vec(c), y[c]);
+            if (full(c)) {
+              each_own(r, c, [&](int at, float x) {
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) y[c][e] = e == at ? x : y[c][e];
+              });
+              shares(whole[r], y[c], vec(c), k, greedy);
+              store8(probs + vec(c), y[c]);
+            } else {
+              each_own(r, c, [&](int e, float x) { probs[vec(c) + e] = result(r, vec(c) + e, x); });
+            }
           } else {
             float most = y[c][0];
 #pragma unroll
@@ -643,7 +692,10 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
           }
         }
       }
-      if constexpr (KIND == kRules || KIND == kProbs) store_special(r);
+      if constexpr (KIND == kRules) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) each_own(r, c, [&](int e, float x) { store1(out + vec(c) + e, x); });
+      }
       cur = next;
     }
     __syncthreads();
@@ -651,6 +703,12 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   }
 
   if constexpr (KIND == kStats) {
+    if (kept) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) marks[c * NT] = special8[c * NT + tid];
+    }
+    if (n <= NT && tid < n)
+      for (int r = 0; r < nr; ++r) a.ruled[((row0 + r) * a.tiles + tile) * NT + tid] = one_m[r * NT + tid];
     for (int r = wave; r < nr; r += kWaves) {
       const Part p = wave_join(lane < kWaves ? parts[r * kWaves + lane] : nothing, k);
       const int at = p.m > kNone ? place(p, r) : kNowhere;
@@ -823,7 +881,11 @@ LogitPlan plan_logits(int S, int R, int V, int num_cus, bool rules) {
   p.rows_per = (R + p.groups - 1) / p.groups;
   p.groups = (R + p.rows_per - 1) / p.rows_per;
   p.workgroups = static_cast<int64_t>(S) * p.groups * p.tiles;
-  p.ws_bytes = (static_cast<size_t>(S) * R * p.tiles * sizeof(float4) + 255) / 256 * 256;
+  // parts of the rows; where there are several, also marks and values of special tokens
+  const size_t parts = static_cast<size_t>(S) * R * p.tiles;
+  p.marks_at = (parts * sizeof(float4) + 255) / 256 * 256;
+  p.ruled_at = p.marks_at + (whole ? 0 : static_cast<size_t>(p.workgroups) * (tile / 8));
+  p.ws_bytes = p.ruled_at + (whole ? 0 : parts * 256 * sizeof(float));
   return p;
 }
 
