@@ -25,9 +25,9 @@
 // is more than a compute unit holds.  Measured: rules on 64 rows of 128000 fp32 logits, about
 // 1800 special tokens each, 22 us, 3.7 TB/s; on 8 rows of 32001 bf16 logits of 11 sequences
 // 11 us, a chain of loads from the history to the first row.  Probabilities of 17 rows of
-// 128000 bf16 logits for 32 sequences 164 us: first pass 62, second 98; without any rule 128,
-// which is 4.3 TB/s over both passes.  The special tokens (1800 a sequence) are the rest: they
-// are listed in both passes for every six rows.
+// 128000 bf16 logits for 32 sequences 148 us: first pass 62, second 85; without any rule 124,
+// which is 4.5 TB/s over both passes.  The special tokens (1800 a sequence) are the rest: the
+// first pass lists them for every six rows and leaves their marks and logits for the second.
 #include "co_kernels.h"
 
 namespace co {
@@ -58,7 +58,7 @@ struct Vec {
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<vec*>(p) = x; }
 };
 
-// (Stores that bypass the caches are slower: the second pass above 109 us, these 98.)
+// (Stores that bypass the caches are slower: a second pass of 98 us took 109.)
 __device__ __forceinline__ void store8(float* p, const float (&x)[kVec]) {
   typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
   *reinterpret_cast<vec*>(p) = vec{x[0], x[1], x[2], x[3]};
@@ -202,7 +202,9 @@ constexpr int kBiasHeld = 256;   // biases of a tile that are held in LDS
 // One workgroup: a tile of tokens of one sequence, C vectors of eight a thread, in rows one
 // after the other, the next row's logits in flight.
 // Special tokens of all rows come first, so that the rows' loop has nothing to wait for but
-// its own loads.
+// its own loads.  kProbs finds up to NT of them in the workspace (when it listed them again the
+// call above took 160 us, now 148; one sequence of 17 rows 19.0, now 16.8); it lists those of a
+// tile that has more.
 //   kRules: rules on logits.  kStats: each tile's largest logit and sum; kProbs: the tiles'
 //   parts joined, and the probabilities.  kWhole: both, where a row is one tile.
 template <typename T, int KIND, int NT, int C>
@@ -304,7 +306,8 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   auto mask_of = [&](int r) { return __builtin_amdgcn_readlane(mask_held, r); };
   auto bits_of = [&](int m) { return reinterpret_cast<const uint8_t*>(a.mask_bits) + m * mask_bytes; };
   auto load_mask = [&](int r, Row& o) {
-    // (what is so without a mask first: behind a branch it would wait for every load in flight)
+    // (what is so without a mask first: written behind a branch, it would wait for every load in
+    // flight; the call above 153 us, now 148)
     const int m = mask_of(r);
     uint32_t without = m == -1 ? 0xFF : 0;
     asm volatile("" : "+v"(without));
