@@ -726,7 +726,7 @@ co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t wid
  * [0, num_bias]; the sequence has no biases), CO_ERR_MASK (mask_row >= num_masks; the row
  * allows no token).
  * Host: vocab from 1 to 2^30, block <= 1024, num_seqs * rows * vocab <= 2^40, fewer than
- * 2^23 workgroups of up to 6 rows and 4096 tokens (CO_ERR_UNSUPPORTED).
+ * 2^23 workgroups of up to 4 rows and 4096 tokens (CO_ERR_UNSUPPORTED).
  */
 co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,
                                 const void* logits, const int32_t* draft_tok,

@@ -25,9 +25,9 @@
 // is more than a compute unit holds.  Measured: rules on 64 rows of 128000 fp32 logits, about
 // 1800 special tokens each, 22 us, 3.7 TB/s; on 8 rows of 32001 bf16 logits of 11 sequences
 // 11 us, a chain of loads from the history to the first row.  Probabilities of 17 rows of
-// 128000 bf16 logits for 32 sequences 148 us: first pass 62, second 85; without any rule 124,
-// which is 4.5 TB/s over both passes.  The special tokens (1800 a sequence) are the rest: the
-// first pass lists them for every six rows and leaves their marks and logits for the second.
+// 128000 bf16 logits for 32 sequences 142 us: first pass 62, second 79; without any rule 120,
+// which is 4.6 TB/s over both passes.  The special tokens (1800 a sequence) are the rest: the
+// first pass lists them for every four rows and leaves their marks and logits for the second.
 #include "co_kernels.h"
 
 namespace co {
@@ -39,8 +39,10 @@ constexpr int kVec = 8;                     // tokens of a thread: one byte of a
 // three workgroups share a compute unit (rules on 64 x 128000 25.8 us, with two 21.6).
 constexpr int kVecs = 2;
 // Rows of a sequence that a workgroup takes: its special tokens' logits of all of them are in
-// registers (32 x 17 x 128000, probabilities: with 9 183 us, with 6 174).
-constexpr int kRowsMax = 6;
+// registers, and more workgroups share a compute unit the fewer they are, while each lists them
+// once more (32 x 17 x 128000, probabilities, with 2 to 6 and 9 rows: 151, 144, 142, 160, 147,
+// 169 us; 100 x 17 x 12000 with 2 to 5: 88, 86, 77, 88).
+constexpr int kRowsMax = 4;
 
 enum { kRules = 0, kStats = 1, kProbs = 2, kWhole = 3 };
 
@@ -197,13 +199,22 @@ struct Entry {
   uint32_t proposed[2];  // bit i: the window's proposal i is this token (of the first 64)
 };
 
-constexpr int kBiasHeld = 256;   // biases of a tile that are held in LDS
+// The biased tokens of a tile are found again by a table in LDS: place of a token, then the next
+// ones.  Lists of more tokens than such steps find are walked (us for 16 rows of 4886 tokens and
+// up to 300 biases, two sequences: walked 104, by the table 15; 17
+// rows of 2919 with every rule, 113 sequences: 217, 72).
+constexpr int kSteps = 32;
+template <int SLOTS>
+__device__ __forceinline__ int slot_of(int t) {
+  return static_cast<int>(static_cast<uint32_t>(t) * 2654435769u >> 20) & (SLOTS - 1);
+}
 
 // One workgroup: a tile of tokens of one sequence, C vectors of eight a thread, in rows one
 // after the other, the next row's logits in flight.
 // Special tokens of all rows come first, so that the rows' loop has nothing to wait for but
-// its own loads.  kProbs finds up to NT of them in the workspace (when it listed them again the
-// call above took 160 us, now 148; one sequence of 17 rows 19.0, now 16.8); it lists those of a
+// its own loads.  kProbs finds up to NT of them in the workspace (at six rows a workgroup
+// the call above takes 147 us; 160 when it listed them again, and one sequence of 17 rows 19.0 in
+// place of 16.8); it lists those of a
 // tile that has more.
 //   kRules: rules on logits.  kStats: each tile's largest logit and sum; kProbs: the tiles'
 //   parts joined, and the probabilities.  kWhole: both, where a row is one tile.
@@ -224,10 +235,9 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
 
   __shared__ uint32_t special[kTokens / 32], with_bias[kTokens / 32];   // a bit a token
   __shared__ uint16_t list[kTokens];
-  __shared__ uint16_t held_tok[kBiasHeld];
-  __shared__ int held_order[kBiasHeld];
-  __shared__ float held_val[kBiasHeld];
-  __shared__ int num_held, listed[kWaves];
+  constexpr int kSlots = NT == 1024 ? 4096 : 512;
+  __shared__ int bias_key[kSlots], bias_order[kSlots];   // token of the tile, its last entry
+  __shared__ int walked, listed[kWaves];                 // walked: not all found a place
   constexpr int kParts = KIND == kStats || KIND == kWhole ? kRowsMax * kWaves : 1;
   __shared__ Part parts[kParts];                 // of the wavefronts
   constexpr int kLanes = KIND == kStats || KIND == kWhole ? kRowsMax * NT : 1;
@@ -307,7 +317,7 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   auto bits_of = [&](int m) { return reinterpret_cast<const uint8_t*>(a.mask_bits) + m * mask_bytes; };
   auto load_mask = [&](int r, Row& o) {
     // (what is so without a mask first: written behind a branch, it would wait for every load in
-    // flight; the call above 153 us, now 148)
+    // flight: at six rows a workgroup 153 us for the call above, 147 so)
     const int m = mask_of(r);
     uint32_t without = m == -1 ? 0xFF : 0;
     asm volatile("" : "+v"(without));
@@ -327,12 +337,8 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
   if (!right && reports && tid == 0) set_status(a.status, CO_ERR_LENGTH);
   const int n_bias = right ? b1 - b0 : 0;
   uint8_t* special8 = reinterpret_cast<uint8_t*>(special);
-  int own_tok = -1;           // bias number tid
-  float own_val = 0.f;
-  if (KIND != kProbs && tid < n_bias) {
-    own_tok = a.bias_tok[b0 + tid];
-    own_val = a.bias_val[b0 + tid];
-  }
+  int own_tok = -1;           // of bias number tid
+  if (KIND != kProbs && tid < n_bias) own_tok = a.bias_tok[b0 + tid];
   // Marks them, with those that have a bias.
   auto mark = [&]() {
 #pragma unroll
@@ -349,7 +355,10 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
       special8[c * NT + tid] = static_cast<uint8_t>(m);
       reinterpret_cast<uint8_t*>(with_bias)[c * NT + tid] = 0;
     }
-    if (tid == 0) num_held = 0;
+    if (tid == 0) walked = 0;
+    if (n_bias > 0) {
+      for (int i = tid; i < kSlots; i += NT) bias_key[i] = bias_order[i] = -1;
+    }
     if (n_bias > 0 || draft) {
       __syncthreads();
       for (int i = tid; i < (reports && draft ? a.R - 1 : before); i += NT) {
@@ -368,12 +377,14 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
         } else if (const int t = in_tile(d); t >= 0) {
           atomicOr(&special[t >> 5], 1u << (t & 31));
           atomicOr(&with_bias[t >> 5], 1u << (t & 31));
-          const int at = atomicAdd(&num_held, 1);
-          if (at < kBiasHeld) {
-            held_tok[at] = static_cast<uint16_t>(t);
-            held_order[at] = i;
-            held_val[at] = KIND != kProbs && i == tid ? own_val : a.bias_val[b0 + i];
+          int h = slot_of<kSlots>(t), step = 0;
+          for (; step < kSteps; ++step) {
+            const int was = atomicCAS(&bias_key[h], -1, t);
+            if (was == -1 || was == t) break;
+            h = (h + 1) & (kSlots - 1);
           }
+          if (step < kSteps) atomicMax(&bias_order[h], i);
+          else walked = 1;
         }
       }
     }
@@ -427,17 +438,15 @@ __global__ __launch_bounds__(NT) void rows_kernel(LogitArgs a) {
     e.biased = with_bias[t >> 5] >> (t & 31) & 1;
     if (e.biased) {
       int order = -1;
-      if (num_held <= kBiasHeld) {
-        for (int j = 0; j < num_held; ++j)
-          if (held_tok[j] == t && held_order[j] > order) {
-            order = held_order[j];
-            e.bias = held_val[j];
-          }
+      if (walked == 0) {
+        int h = slot_of<kSlots>(t);
+        for (int step = 0; step < kSteps && bias_key[h] != t; ++step) h = (h + 1) & (kSlots - 1);
+        order = bias_order[h];
       } else {
-        for (int j = 0; j < n_bias; ++j)
-          if (a.bias_tok[b0 + j] == e.v) order = j;
-        e.bias = a.bias_val[b0 + order];
+#pragma unroll 8
+        for (int j = 0; j < n_bias; ++j) order = a.bias_tok[b0 + j] == e.v ? j : order;
       }
+      e.bias = a.bias_val[b0 + order];
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)

@@ -574,6 +574,17 @@ def test_probabilities(c):
     a.check_probs(p, top)
 
 
+@pytest.mark.parametrize("S,R,V,bias", [(2, 3, 300, 3000), (2, 5, 4099, 9000), (1, 3, 9000, 9000), (2, 2, 16001, 60000),
+                                        (1, 6, 20011, 50000)])
+def test_long_lists_of_biases(S, R, V, bias):
+    """Tokens many times over, more distinct ones in a tile than it can look up, and lists of
+    which a tile holds few."""
+    print(f"[biases] {S} x {R} x {V}, up to {bias}", flush=True)
+    a = Logits(S, 7, R, V, "f32", V, bias=bias, masked=0.3)
+    a.check(a.apply())
+    a.check_probs(*a.probs())
+
+
 def test_probabilities_without_rules_or_temperature():
     a = Logits(3, 4, 5, 3001, "bf16", 11, window=False, penalties=False)
     p, top = a.probs(rules=False, temperature=False)
