@@ -144,10 +144,14 @@ __global__ __launch_bounds__(NT) void quantize_rows_kernel(const T* x, int cols,
 template <typename T>
 void launch_quantize_t(const T* x, int64_t rows, int cols, int8_t* codes, float* scale, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(rows));
-  if (cols <= 2048) hipLaunchKernelGGL((quantize_rows_kernel<T, 256, 1>), grid, dim3(256), 0, stream, x, cols, codes, scale);
-  else if (cols <= 8192) hipLaunchKernelGGL((quantize_rows_kernel<T, 512, 2>), grid, dim3(512), 0, stream, x, cols, codes, scale);
-  else if (cols <= 32768) hipLaunchKernelGGL((quantize_rows_kernel<T, 1024, 4>), grid, dim3(1024), 0, stream, x, cols, codes, scale);
-  else hipLaunchKernelGGL((quantize_rows_kernel<T, 1024, 0>), grid, dim3(1024), 0, stream, x, cols, codes, scale);
+  auto launch = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, x, cols, codes, scale);
+  };
+  // as many threads as hold a row
+  if (cols <= 2048) launch(quantize_rows_kernel<T, 256, 1>, 256);
+  else if (cols <= 8192) launch(quantize_rows_kernel<T, 512, 2>, 512);
+  else if (cols <= 32768) launch(quantize_rows_kernel<T, 1024, 4>, 1024);
+  else launch(quantize_rows_kernel<T, 1024, 0>, 1024);
 }
 
 // ------------------------------------------------------------------- product
@@ -1111,15 +1115,13 @@ hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t st
   if (err != hipSuccess) return err;
   Product p;
   if ((err = product(a.d, a.Dcat, a.wf, a.wf_scale, &p)) != hipSuccess) return err;
-  const dim3 rows(a.M);
-  if (a.d <= 2048)
-    hipLaunchKernelGGL((z_codes_kernel<256, 1>), rows, dim3(256), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
-  else if (a.d <= 4096)
-    hipLaunchKernelGGL((z_codes_kernel<512, 1>), rows, dim3(512), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
-  else if (a.d <= 16384)
-    hipLaunchKernelGGL((z_codes_kernel<1024, 2>), rows, dim3(1024), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
-  else
-    hipLaunchKernelGGL((z_codes_kernel<1024, 0>), rows, dim3(1024), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
+  auto finish = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, dim3(a.M), dim3(threads), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
+  };
+  if (a.d <= 2048) finish(z_codes_kernel<256, 1>, 256);
+  else if (a.d <= 4096) finish(z_codes_kernel<512, 1>, 512);
+  else if (a.d <= 16384) finish(z_codes_kernel<1024, 2>, 1024);
+  else finish(z_codes_kernel<1024, 0>, 1024);
   const MatmulI8Plan kv = plan_matmul_i8(a.M, n_kv, a.d, num_cus);
   if (kv.variant != kStream && a.dst.knorm == nullptr) {   // tiles rotate and store their rows
     g.N = n_kv;
