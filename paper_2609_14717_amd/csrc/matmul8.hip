@@ -94,7 +94,8 @@ struct RowScale {
 };
 
 // One workgroup per row, which it holds in registers (Q times eight entries a thread) from
-// the search for its largest magnitude to its codes; Q = 0: rows of any length, read twice.
+// the search for its largest magnitude to its codes; Q = 0: rows of any length, read twice
+// (their columns are counted without a sign: the step behind the last may pass 2^31).
 // Magnitudes compare as their bits, infinities and NaNs as the largest.  Memory traffic bounds
 // it in the limit; at the sizes of a round its three steps one behind the other do: 512 bf16
 // rows of 20480 12.2 us (2.6 TB/s), 544 of 4096 4.9, one of 768 2.4.
@@ -126,14 +127,15 @@ __global__ __launch_bounds__(NT) void quantize_rows_kernel(const T* x, int cols,
     }
     if (threadIdx.x == 0) scale[row] = s.scale;
   } else {
+    const uint32_t end = cols;
     float v[8];
-    for (int c = threadIdx.x * 8; c < cols; c += NT * 8) {
+    for (uint32_t c = threadIdx.x * 8; c < end; c += NT * 8) {
       eight(xr + c, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
     }
     const RowScale s(block_max<NT>(top, red));
-    for (int c = threadIdx.x * 8; c < cols; c += NT * 8) {
+    for (uint32_t c = threadIdx.x * 8; c < end; c += NT * 8) {
       eight(xr + c, v);
       s.codes(v, cr + c);
     }

@@ -89,6 +89,28 @@ def test_codes_of_special_rows(dtype):
     within(np.nan_to_num(np_(scale), nan=-7), np.nan_to_num(s, nan=-7), F32 * np.nan_to_num(s), "scale")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_codes_of_the_longest_row(dtype):
+    """2^31 - 64 columns: the column behind a thread's last one passes 31 bits.  A few entries in
+    all of it, the largest at the end; what lies behind the row stays as it was."""
+    cols, guard = 2 ** 31 - 64, 1 << 20
+    print(f"[quantize] 1 x {cols} {dtype}", flush=True)
+    x = torch.zeros(cols + guard, dtype=typed(dtype), device=DEV)
+    x[cols:] = 1000.0                                   # (a row that reads on has another scale)
+    at = [0, 7, 8191, 8192, 10 ** 9 + 1, cols - 8193, cols - 8192, cols - 9, cols - 1]
+    value = [1.0, -2.0, 3.0, -4.0, 5.0, -6.0, 7.0, -8.0, 127.0]
+    for i, v in zip(at, value):
+        x[i] = v
+    codes = torch.full((cols + guard,), 99, dtype=torch.int8, device=DEV)
+    scale = torch.full((2,), -1.0, device=DEV)
+    co.carryover_quantize_i8(1, cols, dtype, x, codes, scale)
+    assert scale.tolist() == [1.0, -1.0]
+    assert [int(codes[i]) for i in at] == value
+    assert (codes[cols:] == 99).all()
+    parts = [codes[a:min(a + (1 << 28), cols)] for a in range(0, cols, 1 << 28)]
+    assert sum(int(p.count_nonzero()) for p in parts) == len(at)
+
+
 def test_quantize_of_no_rows_touches_nothing():
     s = torch.full((4,), 5.0, device=DEV)
     c = torch.full((4, 64), 7, dtype=torch.int8, device=DEV)
