@@ -744,7 +744,9 @@ co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows
  * share the row.  A row with nothing left has probabilities 0 and top_tok -1.  The
  * logits are not changed; probs must not overlap them.  `ws`:
  * carryover_probabilities_workspace_bytes(dims, vocab, rows) bytes of scratch (any
- * contents, for one call at a time), 256-byte aligned.  Other arguments and errors as carryover_logit_rules.
+ * contents, for one call at a time), 256-byte aligned.  Other arguments and errors as
+ * carryover_logit_rules; from 2049 to 4096 tokens fewer than 2^22 workgroups of up to 4 rows
+ * (CO_ERR_UNSUPPORTED).
  */
 co_status carryover_probabilities(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,
                                   const void* logits, const int32_t* draft_tok,

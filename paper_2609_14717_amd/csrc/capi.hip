@@ -235,6 +235,14 @@ co_status check_logits(const co_dims* d, int32_t vocab, int32_t rows, int32_t dt
              : CO_ERR_UNSUPPORTED;
 }
 
+// And of the probabilities' call, whose whole rows have workgroups of up to 1024 threads.
+co_status check_probabilities(const co_dims* d, int32_t vocab, int32_t rows, int32_t dtype) {
+  const co_status s = check_logits(d, vocab, rows, dtype);
+  if (s != CO_OK) return s;
+  const LogitPlan p = plan_logits(d->num_seqs, rows, vocab, num_cus(), false);
+  return p.workgroups * p.threads < int64_t{1} << 32 ? CO_OK : CO_ERR_UNSUPPORTED;
+}
+
 bool rules_ok(const co_logit_rules* r) {
   if (!r->seen && (r->repetition || r->presence || r->frequency)) return false;
   if (!aligned(r->seen, 2) || !aligned(r->repetition, 4) || !aligned(r->presence, 4) ||
@@ -1111,7 +1119,7 @@ co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows
 }
 
 size_t carryover_probabilities_workspace_bytes(const co_dims* dims, int32_t vocab, int32_t rows) {
-  if (check_dims(dims) != CO_OK || check_logits(dims, vocab, rows, CO_DTYPE_F32) != CO_OK) return 0;
+  if (check_dims(dims) != CO_OK || check_probabilities(dims, vocab, rows, CO_DTYPE_F32) != CO_OK) return 0;
   return plan_logits(dims->num_seqs, rows, vocab, num_cus(), false).ws_bytes;
 }
 
@@ -1122,7 +1130,7 @@ co_status carryover_probabilities(const co_dims* dims, int32_t vocab, int32_t ro
                                   size_t ws_bytes, hipStream_t stream) {
   co_status s = check_dims(dims);
   if (s != CO_OK) return s;
-  if ((s = check_logits(dims, vocab, rows, dtype)) != CO_OK) return s;
+  if ((s = check_probabilities(dims, vocab, rows, dtype)) != CO_OK) return s;
   const size_t es = dtype == CO_DTYPE_BF16 ? 2 : 4;
   const size_t n = static_cast<size_t>(dims->num_seqs) * rows * vocab;
   if (!logits || !probs || !status || (rules && !rules_ok(rules)) || !aligned(logits, es) ||

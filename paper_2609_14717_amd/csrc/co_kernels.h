@@ -266,7 +266,8 @@ struct StoreArgs {
 constexpr int kMaxSumI8 = 131008;         // of codes from -128 on: the sum fits 32 bits
 constexpr int kMaxSideI8 = (1 << 24) - 1; // rows of an operand
 constexpr int kMaxRowsI8 = (1 << 22) - 1; // rows to quantise, up to 1024 threads each
-constexpr int64_t kMaxGrid = 1 << 23;     // fewer workgroups of up to 512 threads in one launch
+constexpr int64_t kMaxGrid = 1 << 23;     // fewer workgroups of up to 512 threads in one launch,
+                                          // whose threads are counted in 32 bits
 constexpr int kMaxVocab = 1 << 30;        // tokens (tiles of them are counted in 32 bits)
 
 struct MatmulI8Args {
@@ -339,6 +340,7 @@ struct LogitArgs {
 struct LogitPlan {
   int groups, rows_per;      // row groups of a sequence, rows of each
   int tiles;                 // of a row
+  int threads;               // of a workgroup
   int64_t workgroups;
   size_t marks_at, ruled_at; // in the workspace
   size_t ws_bytes;

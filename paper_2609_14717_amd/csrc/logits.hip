@@ -880,13 +880,14 @@ LogitPlan plan_logits(int S, int R, int V, int num_cus, bool rules) {
   // 1 x 17 x 16000 22.2, 21.1; 32 x 17 x 16000 61.2, 52.8; 32 x 17 x 4000 42.3, 40.6)
   const bool whole = !rules && V <= 1024 * kVec * 2;
   const int tile = whole ? V : 256 * kVec * kVecs;
+  p.threads = whole && V > 256 * kVec ? 1024 : 256;
   p.tiles = static_cast<int>((static_cast<int64_t>(V) + tile - 1) / tile);
   // Rows together (what is special is listed once for them) as long as so many workgroups are
   // left to every compute unit: tiles 4 (us at 1, 4, 16, bf16 rows by tokens with 2000 tokens of
   // history: 4 x 17 x 128000 41.9, 36.0, 40.4; 8 x 17 x 32000 39.4, 31.2, 31.1), rows whole 1 of
   // 1024 threads (at 1, 2, 4: 32 x 17 x 4000 40.4, 46.9, 46.9; 100 x 17 x 12000 96.4, 91.9, 126.5)
   // or 2 of 256 (100 x 17 x 1000 35.2, 28.3, 31.7).
-  const int left = !whole ? 4 : (V > 256 * kVec ? 1 : 2);
+  const int left = !whole ? 4 : (p.threads == 1024 ? 1 : 2);
   int64_t per = static_cast<int64_t>(p.tiles) * S * R / (left * num_cus);
   per = per < 1 ? 1 : (per > kRowsMax ? kRowsMax : per);
   p.groups = (R + static_cast<int>(per) - 1) / static_cast<int>(per);

@@ -324,6 +324,20 @@ def test_probabilities_workspace_temperature_and_top():
 
 
 @needs_lib
+@pytest.mark.parametrize("vocab,rows,S,ok", [
+    (2049, 1, 1 << 22, False), (2049, 4, (1 << 23) - 1, False), (4096, 5, 1 << 21, False),
+    (4096, 4, (1 << 22) - 1, True), (2048, 4, 1 << 22, True), (4097, 4, (1 << 22) - 1, True)])
+def test_probabilities_of_more_threads_than_a_launch_has_are_refused(vocab, rows, S, ok):
+    """Whole rows of more than 2048 tokens have a workgroup of 1024 threads for up to four rows:
+    2^22 workgroups are 2^32 threads.  The rules' call has 256 threads at any size."""
+    d = dims(S=S, B=rows)
+    assert (co.probabilities_workspace_bytes(d, vocab, rows) > 0) == ok
+    if not ok:
+        assert _rc(lambda: co.carryover_probabilities(d, vocab, rows, "bf16", FAKE, None, None, None, 1 << 45, None,
+                                                      FAKE, FAKE, stream=0, ws_bytes=1 << 60)) == co.CO_ERR_UNSUPPORTED
+
+
+@needs_lib
 def test_rules_call_needs_rules():
     import ctypes
     d = dims()
