@@ -689,7 +689,8 @@ size_t carryover_matmul_i8_workspace_bytes(int32_t m, int32_t n, int32_t k);
  * separate carry projector.  Supported: bf16, feat_dim and model_dim up to 131008,
  * num_seqs * block below 2^22, and times the wider of model_dim and NKV below 2^32.
  * `ws`: carryover_workspace_bytes(dims, CO_WS_PROJECT_I8) bytes, 256-byte aligned.
- * Other arguments and errors as carryover_project_kv.
+ * num_seqs 0 does nothing (what the batch would hold, and ws, may be NULL).  Other
+ * arguments and errors as carryover_project_kv.
  */
 co_status carryover_project_kv_i8(const co_dims* dims, const co_weights_i8* w, const void* hidden,
                                   const co_route* route, const co_state* state, void* ws,
@@ -707,7 +708,8 @@ co_status carryover_project_kv_i8(const co_dims* dims, const co_weights_i8* w, c
  * CO_ERR_LENGTH (len outside [0, width]; the sequence stays as it is), CO_ERR_TOKEN
  * (a token >= vocab; it is left out).  Calls on one history must not overlap.
  * Host: vocab from 1 to 2^30, width from 0 (tokens may then be NULL) to 2^30,
- * num_seqs * ceil(vocab / 8192) below 2^23 (CO_ERR_UNSUPPORTED).
+ * num_seqs * ceil(vocab / 8192) below 2^23 (CO_ERR_UNSUPPORTED); num_seqs 0 does nothing
+ * (pointers may be NULL).
  */
 enum { CO_COUNT_PROMPT = 1, CO_COUNT_FRESH = 2 };
 co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t width,
@@ -726,7 +728,8 @@ co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t wid
  * [0, num_bias]; the sequence has no biases), CO_ERR_MASK (mask_row >= num_masks; the row
  * allows no token).
  * Host: vocab from 1 to 2^30, block <= 1024, num_seqs * rows * vocab <= 2^40, fewer than
- * 2^23 workgroups of up to 4 rows and 4096 tokens (CO_ERR_UNSUPPORTED).
+ * 2^23 workgroups of up to 4 rows and 4096 tokens (CO_ERR_UNSUPPORTED); num_seqs 0 does
+ * nothing (pointers but rules may be NULL).
  */
 co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows, int32_t dtype,
                                 const void* logits, const int32_t* draft_tok,

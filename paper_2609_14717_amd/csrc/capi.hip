@@ -1047,14 +1047,14 @@ co_status carryover_project_kv_i8(const co_dims* dims, const co_weights_i8* w, c
   co_status s = check_dims(dims);
   if (s != CO_OK) return s;
   if ((s = check_project_i8_dims(dims)) != CO_OK) return s;
-  if (!w || !w->w_f || !w->w_f_scale || !w->w_kv || !w->w_kv_scale || !hidden ||
-      !route_ok(route) || !state_ok(state))
-    return CO_ERR_INVALID_ARG;
-  if (!aligned(hidden, 16) || !aligned(w->w_f, 16) || !aligned(w->w_kv, 16) ||
-      !aligned(w->w_f_scale, 4) || !aligned(w->w_kv_scale, 4) || !aligned(w->f_e, 16) ||
-      !aligned(w->z_norm, 4) || !aligned(w->k_norm, 4))
+  if (!w || !w->w_f || !w->w_f_scale || !w->w_kv || !w->w_kv_scale || !aligned(w->w_f, 16) ||
+      !aligned(w->w_kv, 16) || !aligned(w->w_f_scale, 4) || !aligned(w->w_kv_scale, 4) ||
+      !aligned(w->f_e, 16) || !aligned(w->z_norm, 4) || !aligned(w->k_norm, 4))
     return CO_ERR_INVALID_ARG;
   if (w->z_norm && dims->model_dim > kNormMaxCols) return CO_ERR_UNSUPPORTED;
+  if (dims->num_seqs == 0) return CO_OK;   // (an empty tensor has no address)
+  if (!hidden || !aligned(hidden, 16) || !route_ok(route) || !state_ok(state))
+    return CO_ERR_INVALID_ARG;
   if (!ws || !aligned(ws, 256)) return CO_ERR_INVALID_ARG;
   if (ws_bytes < project_i8_bytes(dims)) return CO_ERR_WORKSPACE;
   ProjectI8Args a{};
@@ -1083,8 +1083,10 @@ co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t wid
   if (vocab < 1 || vocab > kMaxVocab || count_workgroups(dims->num_seqs, vocab) >= kMaxGrid)
     return CO_ERR_UNSUPPORTED;
   if (width > kMaxVocab) return CO_ERR_UNSUPPORTED;
-  if (width < 0 || (width > 0 && !tokens) || !seen || !status || !aligned(tokens, 4) || !aligned(len, 4) ||
-      !aligned(seen, 2) || !aligned(status, 4) || (flags & ~(CO_COUNT_PROMPT | CO_COUNT_FRESH)))
+  if (width < 0 || (flags & ~(CO_COUNT_PROMPT | CO_COUNT_FRESH))) return CO_ERR_INVALID_ARG;
+  if (dims->num_seqs == 0) return CO_OK;   // (an empty tensor has no address)
+  if ((width > 0 && !tokens) || !seen || !status || !aligned(tokens, 4) || !aligned(len, 4) ||
+      !aligned(seen, 2) || !aligned(status, 4))
     return CO_ERR_INVALID_ARG;
   CountArgs a{};
   a.S = dims->num_seqs;
@@ -1106,9 +1108,11 @@ co_status carryover_logit_rules(const co_dims* dims, int32_t vocab, int32_t rows
   co_status s = check_dims(dims);
   if (s != CO_OK) return s;
   if ((s = check_logits(dims, vocab, rows, dtype)) != CO_OK) return s;
+  if (!rules) return CO_ERR_INVALID_ARG;
+  if (dims->num_seqs == 0) return CO_OK;   // (an empty tensor has no address)
   const size_t es = dtype == CO_DTYPE_BF16 ? 2 : 4;
   const size_t bytes = static_cast<size_t>(dims->num_seqs) * rows * vocab * es;
-  if (!logits || !rules || !out || !status || !rules_ok(rules) || !aligned(logits, es) ||
+  if (!logits || !out || !status || !rules_ok(rules) || !aligned(logits, es) ||
       !aligned(out, es) || !aligned(draft_tok, 4) || !aligned(status, 4) ||
       (out != logits && overlap(logits, bytes, out, bytes)))
     return CO_ERR_INVALID_ARG;
@@ -1131,6 +1135,7 @@ co_status carryover_probabilities(const co_dims* dims, int32_t vocab, int32_t ro
   co_status s = check_dims(dims);
   if (s != CO_OK) return s;
   if ((s = check_probabilities(dims, vocab, rows, dtype)) != CO_OK) return s;
+  if (dims->num_seqs == 0) return CO_OK;   // (an empty tensor has no address)
   const size_t es = dtype == CO_DTYPE_BF16 ? 2 : 4;
   const size_t n = static_cast<size_t>(dims->num_seqs) * rows * vocab;
   if (!logits || !probs || !status || (rules && !rules_ok(rules)) || !aligned(logits, es) ||

@@ -360,6 +360,36 @@ def test_calls_of_nothing_take_empty_tensors():
 
 
 @needs_lib
+def test_empty_batches_take_empty_tensors():
+    """num_seqs 0: sizes, weights and rules are checked, then there is nothing to do."""
+    d, i32 = dims(S=0), lambda *s: torch.empty(s, dtype=torch.int32)  # noqa: E731
+    e = lambda *s, t=torch.float32: torch.empty(s, dtype=t)  # noqa: E731
+    seen, status = e(0, 1000, t=torch.int16), torch.zeros(1, dtype=torch.int32)
+    co.carryover_count_tokens(d, 1000, 16, i32(0, 16), i32(0), co.CO_COUNT_PROMPT, seen, status, stream=0)
+    r = co.logit_rules(seen, e(0), e(0), e(0), torch.zeros(1, dtype=torch.int32), i32(0), e(0), i32(0, 17),
+                       torch.zeros(3, 32, dtype=torch.int32))
+    x = e(0, 17, 1000)
+    co.carryover_logit_rules(d, 1000, 17, "f32", x, i32(0, 16), r, x, status, stream=0)
+    assert co.probabilities_workspace_bytes(d, 1000, 17) == 0
+    ws = e(0, t=torch.uint8)
+    for rules in (r, None):
+        co.carryover_probabilities(d, 1000, 17, "f32", x, i32(0, 16), rules, e(0), e(0, 17, 1000), i32(0, 17), status, ws,
+                                   stream=0)
+    st = dict(ctx_len=i32(0), carry_len=i32(0), page_table=i32(0, 8), k_cache=e(1, 16, 2, 16, 64), v_cache=e(1, 16, 2, 64, 16),
+              k_carry=e(1, 0, 1, 2, 16, 64), v_carry=e(1, 0, 1, 2, 64, 16), status=status)
+    rt = dict(accept_len=i32(0), row_pos=i32(0, 16), row_dst=i32(0, 16))
+    project = lambda **w: _rc(lambda: co.carryover_project_kv_i8(  # noqa: E731
+        d, _weights_i8(**w), e(0, 768, t=torch.bfloat16), rt, st, ws, stream=0))
+    assert project() == co.CO_OK
+    # what does not hang on the batch is refused as ever
+    assert project(w_f=FAKE + 8) == co.CO_ERR_INVALID_ARG
+    assert _rc(lambda: co.carryover_count_tokens(d, 1000, 16, 0, 0, 4, 0, 0, stream=0)) == co.CO_ERR_INVALID_ARG
+    assert _rc(lambda: co.carryover_count_tokens(d, 0, 16, 0, 0, 0, 0, 0, stream=0)) == co.CO_ERR_UNSUPPORTED
+    assert _rc(lambda: co.carryover_logit_rules(d, 1000, 18, "f32", x, None, r, x, status,
+                                                stream=0)) == co.CO_ERR_INVALID_ARG
+
+
+@needs_lib
 def test_lists_too_long_to_walk_in_32_bits_are_refused():
     assert _rc(lambda: co.carryover_count_tokens(dims(), 1000, (1 << 30) + 1, FAKE, None, 0, FAKE, FAKE,
                                                  stream=0)) == co.CO_ERR_UNSUPPORTED
