@@ -964,7 +964,8 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
 
 // A row of z from F's product: F E on a carry row, the optional RMS norm, its codes.  Q
 // times eight entries of it stay in a thread's registers; Q = 0: rows of any length by way
-// of `spill` [M][d] (which may be the product's own fp32 results).  A chain of a row's loads,
+// of `spill` [M][d] (which may be the product's own fp32 results), without a norm: rows of more
+// than kNormMaxCols have none.  A chain of a row's loads,
 // one or two sums over the workgroup, and its stores: 5.0 us for 16 rows of 4096, 5.5 for 512.
 template <int NT, int Q>
 __global__ __launch_bounds__(NT) void z_codes_kernel(Product p, float* spill, const float* fe,
@@ -1028,19 +1029,15 @@ __global__ __launch_bounds__(NT) void z_codes_kernel(Product p, float* spill, co
   } else {
     for (int c = threadIdx.x * 8; c < d; c += NT * 8) {
       read(c, v[0]);
-      squares(v[0]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sr[c + e] = v[0][e];
-    }
-    if (gain) r = rsqrtf(block_sum<NT>(ss, red) / static_cast<float>(d) + kRmsEps);
-    for (int c = threadIdx.x * 8; c < d; c += NT * 8) {   // (a thread reads what it wrote)
-      eight(sr + c, v[0]);
-      normed(c, v[0]);
+      for (int e = 0; e < 8; ++e) {
+        sr[c + e] = v[0][e];
+        top = max(top, magnitude(v[0][e]));
+      }
     }
     const RowScale s(block_max<NT>(top, redu));
-    for (int c = threadIdx.x * 8; c < d; c += NT * 8) {
+    for (int c = threadIdx.x * 8; c < d; c += NT * 8) {   // (a thread reads what it wrote)
       eight(sr + c, v[0]);
-      normed(c, v[0]);
       s.codes(v[0], cr + c);
     }
     if (threadIdx.x == 0) scale[row] = s.scale;
@@ -1120,6 +1117,7 @@ hipError_t launch_project_i8(const ProjectI8Args& a, int num_cus, hipStream_t st
   auto finish = [&](auto kernel, int threads) {
     hipLaunchKernelGGL(kernel, dim3(a.M), dim3(threads), 0, stream, p, y, a.fe, a.znorm, a.dst.row_dst, codes, scale);
   };
+  static_assert(kNormMaxCols <= 16384, "a norm's rows are in registers");
   if (a.d <= 2048) finish(z_codes_kernel<256, 1>, 256);
   else if (a.d <= 4096) finish(z_codes_kernel<512, 1>, 512);
   else if (a.d <= 16384) finish(z_codes_kernel<1024, 2>, 1024);

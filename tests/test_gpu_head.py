@@ -340,6 +340,37 @@ def test_project_of_few_rows_into_many_heads(S, B, hd):
     check_project(c)
 
 
+@pytest.mark.parametrize("S,B,Dcat,d,norms,force", [
+    (1, 5, 64, 4160, True, None),              # F's results in fp32, z's rows in registers
+    (5, 16, 128, 4160, False, None),
+    (1, 16, 6400, 4160, True, None),           # F's parts added up by the reader
+    (2, 3, 64, 16384, True, None),
+    (1, 3, 1088, 16384, True, 9),
+    (1, 5, 64, 16448, False, None),            # z's rows by way of memory, over F's results
+    (5, 16, 64, 16448, False, None),
+    (2, 7, 1088, 16448, False, 9),             # or beside its parts
+    (1, 2, 64, 20480, False, None),
+])
+def test_project_of_wide_models(S, B, Dcat, d, norms, force, tune):
+    print(f"[project i8] S={S} B={B} {Dcat}->{d} norms={norms} force={force}", flush=True)
+    if force is not None:
+        tune("matmul_i8", force)
+    c = project_case(S, B, Dcat, d, 1, 1, 64, 1e4, S * B + d, norms)
+    run_project(c)
+    check_project(c)
+
+
+@pytest.mark.parametrize("S,B,Dcat,d,L,Hkv,hd,norms", [
+    (3, 16, 4160, 1088, 1, 2, 128, False), (3, 16, 4160, 1088, 1, 2, 128, True), (11, 3, 2112, 1088, 1, 1, 64, True),
+    (4, 16, 8256, 2048, 2, 1, 64, False)])
+def test_project_of_up_to_64_rows(S, B, Dcat, d, L, Hkv, hd, norms):
+    """33 to 64 rows whose products are both split over K: z and the stores add the parts up."""
+    print(f"[project i8] S={S} B={B} {Dcat}->{d} L={L} {Hkv}x{hd} norms={norms}", flush=True)
+    c = project_case(S, B, Dcat, d, L, Hkv, hd, 1e6, S * B + d, norms)
+    run_project(c)
+    check_project(c)
+
+
 def test_project_without_an_embedding():
     c = project_case(2, 8, 256, 256, 1, 2, 64, 1e4, 9, False, embed=False)
     run_project(c)
