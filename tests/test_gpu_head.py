@@ -216,6 +216,23 @@ def test_product_of_few_rows_with_many_columns(m):
         check_product(*ops, "bf16", product(*ops, "bf16"), f"{m} x {n} x {k}")
 
 
+@pytest.mark.parametrize("dtype,bias", [("bf16", False), ("bf16", True), ("f32", True)])
+@pytest.mark.parametrize("m,n,k,forced", [
+    (33, 70, 8256, False), (45, 3001, 4160, False), (47, 255, 1088, False), (64, 130, 8256, False),   # split over K
+    (33, 70, 64, True), (48, 65, 448, True), (64, 300, 960, True),                                    # in one part
+    (16, 33000, 5184, False), (1, 70, 64, True), (5, 300, 448, True), (16, 64, 960, True),
+    (17, 33, 448, True), (32, 300, 960, True), (16, 4096, 20480, False)])
+def test_product_of_streamed_weights(m, n, k, forced, dtype, bias, tune):
+    """The kernel for up to 64 rows with one, two and four row tiles, K whole and in parts."""
+    print(f"[product] {m} x {n} x {k} {dtype} bias={bias} forced={forced}", flush=True)
+    if forced:
+        tune("matmul_i8", 9)
+    parts = co.matmul_i8_workspace_bytes(m, n, k) > 0
+    assert parts == (k >= 1024 and n != 33000)
+    ops = operands(m, n, k, m + n + k, bias)
+    check_product(*ops, dtype, product(*ops, dtype), f"{m} x {n} x {k}")
+
+
 def test_product_repeats_bit_for_bit_on_another_stream():
     ops = operands(45, 3001, 4160, 5, True)
     first = product(*ops, "f32")
