@@ -185,6 +185,21 @@ def test_matmul_workspace_is_checked(m, n, k):
         assert call(0, need) == co.CO_ERR_INVALID_ARG
 
 
+@needs_lib
+@pytest.mark.parametrize("m,n,k,parts", [(1, 256, 768, 0), (17, 128000, 4096, 0), (45, 3001, 4160, 6),
+                                         (16, 4096, 20480, 8), (64, 130, 8256, 11)])
+def test_products_in_parts_need_their_workspace(m, n, k, parts):
+    """int32 results for every part of K, to whole lines of 256 bytes."""
+    need = co.matmul_i8_workspace_bytes(m, n, k)
+    assert need == -(-parts * m * n * 4 // 256) * 256
+    call = lambda ws, nb: _rc(lambda: co.carryover_matmul_i8(  # noqa: E731
+        m, n, k, FAKE, FAKE, FAKE, FAKE, None, "bf16", FAKE, ws, stream=0, ws_bytes=nb))
+    if parts:
+        assert call(FAKE, need - 1) == co.CO_ERR_WORKSPACE
+        assert call(FAKE + 16, need) == co.CO_ERR_INVALID_ARG
+        assert call(0, need) == co.CO_ERR_INVALID_ARG
+
+
 def _weights_i8(**kw):
     p = dict(w_f=FAKE, w_f_scale=FAKE, w_kv=FAKE, w_kv_scale=FAKE)
     p.update(kw)
