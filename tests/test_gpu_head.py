@@ -655,6 +655,30 @@ def test_long_lists_of_biases(S, R, V, bias):
     a.check_probs(*a.probs())
 
 
+@pytest.mark.parametrize("S,B,R,V,dtype,window,bias,masked,crowded", [
+    (2, 8, 9, 32001, "bf16", True, 30, 0.5, False), (2, 8, 9, 32001, "f32", True, 30, 0.5, False),
+    (3, 16, 17, 20011, "bf16", True, 0, 0.0, False), (1, 16, 17, 128000, "bf16", True, 100, 0.25, False),
+    (1, 4, 3, 128000, "f32", False, 0, 0.0, False), (40, 2, 3, 16385, "f32", True, 5, 0.3, False),
+    (2, 8, 9, 32001, "bf16", True, 30, 0.5, True), (5, 1, 1, 50003, "f32", False, 20, 1.0, True)])
+def test_sparse_histories_of_large_vocabularies(S, B, R, V, dtype, window, bias, masked, crowded):
+    """Few special tokens in most tiles, as a text of hundreds of tokens leaves them: the second
+    pass finds their marks and logits in the workspace.  crowded: every token of one block of 512
+    was seen, so that its tile has more than the workspace holds, beside tiles that have few."""
+    print(f"[sparse] {S} x {R} x {V} {dtype} crowded={crowded}", flush=True)
+    a = Logits(S, B, R, V, dtype, S * V + R, window, True, bias, masked)
+    rng = a.rng
+    a.seen = np.where(rng.random((S, V)) < 0.01, rng.integers(1, 4, (S, V)), 0) + 0x8000 * (rng.random((S, V)) < 0.01)
+    a.seen[:, V - 1] = 0x8001                           # behind the last whole vector, or its last
+    if crowded:
+        a.seen[0, 512:1024] = 0x8000
+    a.x[0, 0, 3:5] = float("nan")
+    a.x[0, -1, V - 1] = 40.0                            # the largest is special
+    p, top = a.probs()
+    assert int(a.status) == 0
+    a.check_probs(p, top)
+    a.check(a.apply())
+
+
 def test_probabilities_without_rules_or_temperature():
     a = Logits(3, 4, 5, 3001, "bf16", 11, window=False, penalties=False)
     p, top = a.probs(rules=False, temperature=False)
