@@ -230,7 +230,10 @@ typedef struct co_logit_rules {
   const float* frequency;     /* [num_seqs] (0: none)                                 */
   const int32_t* bias_start;  /* [num_seqs + 1]: sequence s has entries bias_start[s] ..
                                  bias_start[s + 1] - 1; a token's last entry counts.
-                                 These three are all given or all NULL                */
+                                 These three are all given or all NULL.  Meant for some
+                                 thousands of entries a sequence: where more than about
+                                 500 tokens among 4096 have one, the time grows with
+                                 tokens times entries                                 */
   const int32_t* bias_tok;    /* [num_bias]                                           */
   const float* bias_val;      /* [num_bias]                                           */
   const int32_t* mask_row;    /* [num_seqs][rows]: the mask of each row, negative: none;
@@ -722,7 +725,8 @@ co_status carryover_count_tokens(const co_dims* dims, int32_t vocab, int32_t wid
  * and must not overlap it otherwise.  rows from 1 to block + 1: a verified window
  * has block + 1, single tokens 1.  draft_tok int32 [num_seqs][block]: the window's
  * proposals, of which row j has the first j behind it (NULL: rows do not follow each
- * other); they count with rules->seen.  Only num_seqs and block of dims are used (the rest must still be valid).
+ * other); they count with rules->seen, and are read where that is given, those before the
+ * last row.  Only num_seqs and block of dims are used (the rest must still be valid).
  * Device errors, written to *status: CO_ERR_TOKEN (a proposal or a bias's token outside
  * [0, vocab); it is left out), CO_ERR_LENGTH (bias_start that decreases or lies outside
  * [0, num_bias]; the sequence has no biases), CO_ERR_MASK (mask_row >= num_masks; the row

@@ -21,12 +21,14 @@
 // and taken one each by its threads, as are the up to seven tokens behind the last whole
 // vector of a row.
 //
-// Probabilities read a row twice (largest logit and sum first), since a row of 128000 logits
-// is more than a compute unit holds.  Measured: rules on 64 rows of 128000 fp32 logits, about
-// 1800 special tokens each, 22 us, 3.7 TB/s; on 8 rows of 32001 bf16 logits of 11 sequences
-// 11 us, a chain of loads from the history to the first row.  Probabilities of 17 rows of
-// 128000 bf16 logits for 32 sequences 142 us: first pass 62, second 79; without any rule 120,
-// which is 4.6 TB/s over both passes.  The special tokens (1800 a sequence) are the rest: the
+// Probabilities read a row of more than 16384 logits twice (largest logit and sum first).  One
+// of 128000 fp32 logits takes all of a compute unit's registers; one of bf16 logits would fit
+// (63 of the 128 that 1024 threads have each), which has not been measured.  Measured (kernels:
+// averages under the profiler): rules on 64 rows of 128000 fp32 logits, about 1800 special
+// tokens each, 20 us, 4.1 TB/s; on 8 rows of 32001 bf16 logits of 11 sequences 9.6 us, a chain
+// of loads from the history to the first row.  Probabilities of 17 rows of 128000 bf16 logits
+// for 32 sequences 142 us: first pass 62, second 81; without any rule 120, which is 4.6 TB/s
+// over both passes.  The special tokens (1800 a sequence) are the rest: the
 // first pass lists them for every four rows and leaves their marks and logits for the second.
 #include "co_kernels.h"
 
@@ -202,7 +204,10 @@ struct Entry {
 // The biased tokens of a tile are found again by a table in LDS: place of a token, then the next
 // ones.  Lists of more tokens than such steps find are walked (us for 16 rows of 4886 tokens and
 // up to 300 biases, two sequences: walked 104, by the table 15; 17
-// rows of 2919 with every rule, 113 sequences: 217, 72).
+// rows of 2919 with every rule, 113 sequences: 217, 72).  Every biased token of a tile walks the
+// whole list there, so that its time is tokens times entries (one row of 128000 tokens with 300,
+// 8000, 16000, 32000 and 128000 different biased tokens: rules 6, 21, 890, 3000, 36000 us,
+// probabilities twice that).
 constexpr int kSteps = 32;
 template <int SLOTS>
 __device__ __forceinline__ int slot_of(int t) {

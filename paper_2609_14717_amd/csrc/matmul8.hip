@@ -98,7 +98,8 @@ struct RowScale {
 // (their columns are counted without a sign: the step behind the last may pass 2^31).
 // Magnitudes compare as their bits, infinities and NaNs as the largest.  Memory traffic bounds
 // it in the limit; at the sizes of a round its three steps one behind the other do: 512 bf16
-// rows of 20480 12.2 us (2.6 TB/s), 544 of 4096 4.9, one of 768 2.4.
+// rows of 20480 13.6 us (2.3 TB/s), 544 of 4096 5.4, one of 768 2.4 (here and at the other
+// kernels: averages under the profiler, where no other kind is named).
 template <typename T, int NT, int Q>
 __global__ __launch_bounds__(NT) void quantize_rows_kernel(const T* x, int cols, int8_t* codes,
                                                            float* scale) {
@@ -219,8 +220,9 @@ __device__ __forceinline__ int column(const X& x, int n0, int c) {
 // row or column l % 16, 16 k from 16 (l / 16) on; result register r is row 4 (l / 16) + r,
 // column l % 16), the next unit's loads in flight while one is multiplied.  The NW partial
 // tiles are added in LDS: whole numbers, so the order does not matter.  One launch, so the
-// kernel of the smallest products: 1 x 256 x 768 2.8 us, 16 x 2048 x 4096 6.9 (its K/V rows
-// rotated and stored 7.8).
+// kernel of the smallest products: 1 x 256 x 768 2.8 us, 16 x 2048 x 4096 6.2 (its K/V rows
+// rotated and stored 7.8: with 16 wavefronts, which have 128 registers a lane, that form keeps
+// 100 bytes a lane in scratch).
 constexpr int kUnit = 256;
 
 template <int MT, int TN, int NW, typename T, typename X>
@@ -352,7 +354,7 @@ __device__ __forceinline__ void put_cols(E* row, int col, int N, const V& v) {
 // lane ends with row l % 16 and four columns from 4 (l / 16) on.  17 x 128000 x 4096 104-107 us:
 // 5.0 TB/s of weights, a large copy's rate (reads alone reach 5.7-5.9); the same by registers,
 // each wavefront reading 256-byte pieces of 16 rows, 127.  16 x 4096 x 20480, parts left to the
-// reader, 14.9 us.
+// reader, 14.7 us.
 template <int MT, int NS, typename T>
 __global__ __launch_bounds__(256) void matmul_i8_stream_kernel(MatmulI8Args g, int tiles_n, int k_per_split) {
   constexpr int ROWS = 64 + 16 * MT, STAGE = ROWS * kUnit;
@@ -471,12 +473,13 @@ __global__ __launch_bounds__(256) void sum_rows_i8_kernel(MatmulI8Args g, int sp
 // 16-byte chunks of a staged row are permuted by row / 2, so that 16 lanes reading a
 // fragment hit 16 bank groups.  Fragments of a step of 32 k are read while the step before
 // multiplies.
-// Bound by the matrix instructions and the LDS reads that feed them.  8192^3 530 us, 2073 TOP/s
-// (the library's 541); 544 x 128000 x 4096, bf16 results, 333 us, 1.71 POP/s (its int32 results
-// 408): three row tiles of 192 hold 544 (6 %), and the 139 MB of results leave no time of their
-// own, for one workgroup fills a compute unit; 512 x 4096 x 20480 in four parts 52 + 9;
-// 512 x 10240 x 4096 34, with rotation and stores of K/V rows 39.
-// Stages of 64 bytes 469 us for the second, results by way of LDS 421.
+// Bound by the matrix instructions and the LDS reads that feed them.  8192^3 486 us, 2.26 POP/s;
+// 544 x 128000 x 4096, bf16 results, 337 us, 1.69 POP/s: three row tiles of 192 hold 544 (6 %),
+// and the 139 MB of results leave no time of their own, for one workgroup fills a compute unit;
+// 512 x 4096 x 20480 in four parts 56 + 9; 512 x 10240 x 4096 34, with rotation and stores of
+// K/V rows 42.  The first by calls one behind the other, as the following: the library's 440 with
+// int32 results, this kernel's with fp32 results 512; the second 332, with fp32 results 360, the
+// library's 388; stages of 64 bytes 469, results by way of LDS 421.
 constexpr int kStageK = 128;
 
 // A wavefront's 32 x 32 results: scaled, the bias added, stored.
@@ -707,7 +710,8 @@ __global__ __launch_bounds__(512, 1) void matmul_i8_wide_kernel(MatmulI8Args g, 
 }
 
 // The parts of K of one 32 x 32 tile for each wavefront, added up, scaled and stored: memory
-// traffic and a launch, 9 us for 512 x 4096 (with the product 60; parts by rows of the result 65).
+// traffic and a launch, 9 us for 512 x 4096 (the call with the product 60; parts by rows of the
+// result 65).
 template <int TMW, int TNW, typename T, typename X>
 __global__ __launch_bounds__(512) void sum_parts_i8_kernel(MatmulI8Args g, X x, int tiles_m,
                                                            int tiles_n, int splits) {
@@ -864,11 +868,13 @@ MatmulI8Plan plan_matmul_i8(int M, int N, int K, int num_cus) {
     }
   }
   // The tile and split of K with the least time by a model: rounds of workgroups over the compute
-  // units at the rate that each tile reached on a large product (256 x 256: 2.07e15 a second on
-  // 256 units), 256 k more for a workgroup's start and end, or the operands' bytes if they take
-  // longer; parts written and read, and a launch.  Over a sweep of sizes (every variant timed) its
-  // choice takes 1.03 to 1.05 times the best variant's time on average; small tiles win where
-  // large ones leave units idle (us: 512 x 10240 x 4096 with 192 x 128 34, the best of the others 38).
+  // units at the rate that each tile reached on a large product (256 x 256 taken as 2.05e15 a
+  // second on 256 units, the others as shares of it), 256 k more for a workgroup's start and end,
+  // or the weights' bytes, once from memory and once for every row tile, if they take longer; parts
+  // written and read, and a launch.  (The rows' bytes are in neither term.)  Over a sweep of sizes,
+  // 1 to 4096 rows and 16 to 131072 columns, every variant timed, its choice takes 1.03 to 1.05
+  // times the best variant's time on average; small tiles win where large ones leave units idle
+  // (us: 512 x 10240 x 4096 with 192 x 128 34, the best of the others 38).
   double best = 1e30;
   for (int v = 0; v < kVariants; ++v) {
     if (force >= 0 && force < kFew && force != v) continue;
@@ -966,7 +972,7 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
 // times eight entries of it stay in a thread's registers; Q = 0: rows of any length by way
 // of `spill` [M][d] (which may be the product's own fp32 results), without a norm: rows of more
 // than kNormMaxCols have none.  A chain of a row's loads,
-// one or two sums over the workgroup, and its stores: 5.0 us for 16 rows of 4096, 5.5 for 512.
+// one or two sums over the workgroup, and its stores: 5.9 us for 16 rows of 4096, 6.3 for 512.
 template <int NT, int Q>
 __global__ __launch_bounds__(NT) void z_codes_kernel(Product p, float* spill, const float* fe,
                                                      const float* gain, const int32_t* row_dst,
